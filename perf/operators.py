@@ -293,7 +293,8 @@ def _prepare_logprob(c, seed):
         if c["entropy"]:
             s["out"]["entropy"] = torch.zeros(R, device="cuda")
         return s
-    # what the forward pass left: the rows' maxima and sums, and entropies
+    # what the forward pass left: the rows' largest logits, their sums of
+    # exponentials relative to it, and entropies
     T = c["temperature"]
     parts = [_forward_of(part, t, T) for part, t in zip(z.split(512), target.split(512))]
     m, sums, entropy = (torch.cat(v) for v in zip(*parts))
@@ -317,11 +318,11 @@ def _scale(c):
 
 
 def _forward_of(z, target, T):
-    x = z.float() / T
-    m = x.amax(1, keepdim=True)
-    e = torch.exp(x - m)
+    m = z.amax(1, keepdim=True).float()
+    y = (z.float() - m) / T
+    e = torch.exp(y)
     s = e.sum(1)
-    h = torch.where(e > 0, e * (x - m), torch.zeros_like(e)).sum(1)
+    h = torch.where(e > 0, e * y, torch.zeros_like(e)).sum(1)
     return m[:, 0], s, torch.log(s) - h / s
 
 
@@ -457,7 +458,7 @@ def _plain_logprob(s):
             out["entropy"] = torch.where(live, h, torch.zeros_like(h))
         return out
     m, sums = s["stats"][:, :1], s["stats"][:, 1:]
-    y = z / T - m
+    y = (z - m) / T
     p = torch.exp(y) / sums
     grad = _plain_logits_grad(p, s["target"], s["dlogp"], T)
     if c["entropy"]:
@@ -631,9 +632,9 @@ def work(case):
 # --- exact: the same from the definitions, in 64 bits ---------------------------------
 def _exact_rows(z, target, live, T):
     """(logp, entropy, m, S) of some rows."""
-    x = z.double() / T
+    x = z.double()
     m = x.max(1).values
-    y = x - m[:, None]
+    y = (x - m[:, None]) / T
     S = y.exp().sum(1)
     h = S.log() - torch.nan_to_num(y, neginf=0.0).mul(y.exp()).sum(1) / S
     logp = y.gather(1, target.long()[:, None])[:, 0] - S.log()
@@ -642,7 +643,7 @@ def _exact_rows(z, target, live, T):
 
 def _exact_logits_grad(z, target, live, T, m, lnS, dlogp, h=None, dh=None):
     """dz = (g (1[j = t] - p) - dh p (ln p + h)) / T, row by row, in z's type."""
-    logq = z.double() / T - m[:, None] - lnS[:, None]
+    logq = (z.double() - m[:, None]) / T - lnS[:, None]
     p = logq.exp()
     grad = -dlogp[:, None] * p
     if h is not None:
