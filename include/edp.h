@@ -13,6 +13,8 @@
  *   delivery   -> edp_sample            (uniform, prioritized, shuffle)
  *                 edp_deliver           (gather + transform + collate)
  *   callback   -> edp_update_priorities / edp_update_priorities_td
+ *   learner    -> edp_token_logprob*, edp_policy_loss*, edp_preference_loss,
+ *                 edp_balance_loss (the losses of an LLM learner on its batch)
  *   sharding   -> edp_tree_total, edp_route_prioritized, edp_sample_targets,
  *                 edp_batch_qmin, edp_is_weights, edp_gae_stats,
  *                 edp_gae_normalize (a buffer split across GPUs, Sec. 5.1)
@@ -30,8 +32,8 @@
  *   when NULL) and released by edp_destroy.  libedp never frees caller memory.
  *   Scratch is allocated at a call's first use and grown (after a device
  *   synchronisation) when a later call needs more: the PERMUTE sampling
- *   mode, edp_gae with normalisation and edp_pack_deliver (20 bytes per
- *   batch entry).  Before
+ *   mode, edp_gae with normalisation, edp_pack_deliver (20 bytes per
+ *   batch entry) and the losses (a few bytes per token or sequence).  Before
  *   capturing calls into a CUDA graph, make each of them once at its
  *   largest size, outside the capture: a call that would have to grow its
  *   scratch while its stream is being captured returns EDP_ERR_STATE and
@@ -512,6 +514,218 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
                                          int32_t *out_tokens, uint64_t *out_off,
                                          float *out_value, uint64_t out_cap,
                                          edp_stream stream);
+
+/* ---------------------------------------------------------------------------
+ * The learner's losses over a packed batch (Appendix A, Table "Verl map": the
+ * update that the delivered batch feeds).  A packed batch is what
+ * edp_pack_deliver writes: tokens, offsets (sequence s is
+ * [off[s], off[s+1])) and a value on every token (its advantage).  Row t of
+ * the logits predicts target[t]; a program that predicts each token from the
+ * ones before it gives the tokens shifted by one, and masks each sequence's
+ * last row.  Any context of the GPU serves; its ring is not used.
+ *
+ * All arrays are device memory.  mask (uint8 per token, or NULL: all ones)
+ * leaves out the tokens where it is 0: their log-probabilities, advantages and
+ * logits may hold anything, their outputs and gradients are 0.  Arithmetic is fp32, sums over tokens fp32 pairs or
+ * fp64, each output rounded once to its type; no result depends on the order
+ * in which threads run.  edp_policy_loss*, edp_preference_loss and
+ * edp_balance_loss use the scratch that edp_gae and edp_pack_deliver use and
+ * must be ordered with them and each other; edp_token_logprob* use none.
+ * ------------------------------------------------------------------------- */
+
+/* Element type of logits and of their gradient. */
+typedef enum { EDP_F32 = 0, EDP_BF16 = 1, EDP_F16 = 2 } edp_dtype;
+
+/* Log-probabilities of given tokens.  Logits [rows][vocab] of type dtype,
+ * `stride` elements from row to row (any alignment of the element type).  For
+ * row t, with m = max_j z_j and S = sum_j exp((z_j - m) / temperature):
+ *   logp[t]    = (z_target - m) / temperature - ln S
+ *   entropy[t] = ln S - (1/S) sum_j exp((z_j - m)/temperature) (z_j - m)/temperature
+ *   stats[t]   = (m, S), for edp_token_logprob_grad
+ * entropy (float [rows]) and stats (float [rows][2]) may be NULL.  A logit of
+ * -infinity is a token of probability 0.  A row with a negative target is left
+ * out like a masked one.  A target >= vocab, and a row whose logits are all
+ * -infinity, are written as 0 (S as 0) and reported by edp_sync
+ * (EDP_ERR_INVALID).  NaN or +infinity in a row makes its outputs NaN.
+ * Errors: EDP_ERR_INVALID for an unknown dtype, vocab == 0, stride < vocab,
+ * rows or vocab >= 2^31, temperature not finite or not > 0, a NULL logits,
+ * target or logp, arrays outside device memory, or logits not aligned to their
+ * type.  rows == 0 does nothing. */
+EDP_API edp_status edp_token_logprob(edp_ctx *ctx, const void *logits, uint32_t dtype,
+                                     uint64_t rows, uint32_t vocab, uint64_t stride,
+                                     const int32_t *target, const uint8_t *mask,
+                                     double temperature, float *logp, float *entropy,
+                                     float *stats, edp_stream stream);
+
+/* The gradient of the logits: with p_j = exp((z_j - m)/temperature) / S,
+ * g = dlogp[t], h = dentropy[t] and H = entropy[t],
+ *   dlogits[t][j] = (1/temperature) (g ([j = target] - p_j) - h p_j (ln p_j + H))
+ * of the type of the logits, dstride elements from row to row.  stats and
+ * entropy are those of edp_token_logprob; entropy and dentropy go together and
+ * may be NULL.  dlogits may be the logits' own array (with dstride == stride),
+ * which it then replaces.  Rows left out, and rows with S == 0, get 0.
+ * Errors as edp_token_logprob, and EDP_ERR_INVALID for entropy without
+ * dentropy or the reverse, dstride < vocab, or the logits' array with another
+ * stride. */
+EDP_API edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint32_t dtype,
+                                          uint64_t rows, uint32_t vocab, uint64_t stride,
+                                          const int32_t *target, const uint8_t *mask,
+                                          double temperature, const float *stats,
+                                          const float *entropy, const float *dlogp,
+                                          const float *dentropy, void *dlogits,
+                                          uint64_t dstride, edp_stream stream);
+
+/* How token losses become one number. */
+typedef enum {
+  EDP_REDUCE_TOKEN_MEAN = 0, /* sum over the batch's tokens / their number */
+  EDP_REDUCE_SEQ_MEAN = 1,   /* mean over sequences of each one's mean */
+  EDP_REDUCE_SEQ_SUM = 2     /* sum over the batch's tokens / number of sequences */
+} edp_reduce;
+
+/* Estimators of the divergence from the reference policy, by its log ratio
+ * q = ref_logp - logp. */
+typedef enum {
+  EDP_KL_K1 = 0, /* -q */
+  EDP_KL_K2 = 1, /* q^2 / 2 */
+  EDP_KL_K3 = 2  /* e^q - 1 - q */
+} edp_kl;
+
+typedef struct {
+  double clip_low, clip_high; /* the ratio's interval [1 - clip_low, 1 + clip_high];
+                                 0 <= clip_low < 1, clip_high >= 0 */
+  double dual_clip;    /* limit of the ratio where the advantage is negative,
+                          > 1, or 0: none */
+  double kl_coef;      /* >= 0 */
+  double entropy_coef; /* >= 0 */
+  double norm;         /* > 0: divides in the place of the batch's number of tokens
+                          (TOKEN_MEAN) or of sequences, for a micro-batch of a larger
+                          batch; 0: the batch's own */
+  double grad_scale;   /* factor of every gradient */
+  uint32_t kl;         /* edp_kl */
+  uint32_t reduce;     /* edp_reduce */
+  uint32_t reserved[2];/* must be 0 */
+} edp_policy_config;
+
+/* The clipped policy loss (PPO, Schulman et al. 2017) with a KL and an entropy
+ * term.  For token t with advantage A, d = logp - old_logp and r = e^d,
+ *   pg = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),
+ *        and with dual_clip = c, where A < 0: min(pg, -c A)
+ *   l  = pg + kl_coef kl(ref_logp - logp) - entropy_coef entropy
+ *   L  = sum_t w_t l_t,  w_t = 1/tokens, 1/(n_seq tokens of its sequence) or
+ *        1/n_seq by `reduce` (norm in the place of tokens or n_seq)
+ *   dlogp = grad_scale dL/dlogp,  dentropy = grad_scale dL/dentropy
+ * A token is clipped, with no gradient of pg, where A > 0 and d >
+ * ln(1 + clip_high), or A < 0 and d < ln(1 - clip_low) or d > ln c.
+ * loss (float [8]) = L; the sums of w pg, w kl, w entropy; the means over the
+ * tokens of: clipped above (A > 0), clipped with A < 0, r, and e^d - 1 - d (an
+ * estimate of the divergence from the old policy).  kl is 0 without ref_logp,
+ * entropy 0 without entropy.  Without tokens all are 0, and a sequence without
+ * tokens adds 0.
+ * adv: float per token.  off (uint64 [n_seq + 1], non-decreasing) is needed for
+ * SEQ_MEAN and SEQ_SUM; given, tokens outside [off[0], off[n_seq]) are left
+ * out, so n_tokens may be the arrays' room.  ref_logp, entropy, mask, dlogp and
+ * dentropy may be NULL.
+ * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, NULL
+ * logp, old_logp, adv or loss, n_tokens == 0 or >= 2^40, n_seq >= 2^31, a missing
+ * off, off without n_seq, kl_coef > 0 without ref_logp, entropy_coef > 0 without
+ * entropy, or arrays outside device memory; EDP_ERR_OOM when the scratch cannot
+ * be allocated. */
+EDP_API edp_status edp_policy_loss(edp_ctx *ctx, const edp_policy_config *cfg,
+                                   const float *logp, const float *old_logp,
+                                   const float *ref_logp, const float *adv,
+                                   const float *entropy, const uint8_t *mask,
+                                   const uint64_t *off, uint64_t n_seq, uint64_t n_tokens,
+                                   float *loss, float *dlogp, float *dentropy,
+                                   edp_stream stream);
+
+/* edp_token_logprob, edp_policy_loss and edp_token_logprob_grad in one pass
+ * over the logits: loss (float [8]), logp (float [rows]), entropy (float [rows]
+ * or NULL) and dlogits, as the three calls give them (a row that the first
+ * reports has log-probability and entropy 0 in the loss, and no gradient).
+ * Rows with a negative target, or one >= vocab, are left out of the loss too.
+ * entropy_coef > 0 needs no entropy array.  dlogits may be the logits' own
+ * array (with dstride == stride).  Errors as of the three calls; rows == 0 is
+ * EDP_ERR_INVALID. */
+EDP_API edp_status edp_policy_loss_logits(edp_ctx *ctx, const edp_policy_config *cfg,
+                                          const void *logits, uint32_t dtype, uint64_t rows,
+                                          uint32_t vocab, uint64_t stride,
+                                          const int32_t *target, double temperature,
+                                          const float *old_logp, const float *ref_logp,
+                                          const float *adv, const uint8_t *mask,
+                                          const uint64_t *off, uint64_t n_seq, float *loss,
+                                          float *logp, float *entropy, void *dlogits,
+                                          uint64_t dstride, edp_stream stream);
+
+/* Losses of a pair of sequences by their log ratios. */
+typedef enum {
+  EDP_PREF_LOGISTIC = 0, /* -(1 - e) ln s(D) - e ln s(-D), s the logistic function,
+                            e = label_smoothing (DPO, Rafailov et al. 2023) */
+  EDP_PREF_SQUARE = 1,   /* (u_c - u_r - 1/(2 beta))^2 (IPO, Azar et al. 2023) */
+  EDP_PREF_HINGE = 2     /* max(0, 1 - D) */
+} edp_pref_kind;
+
+typedef struct {
+  double beta;            /* > 0 */
+  double label_smoothing; /* LOGISTIC: 0 <= e < 1/2; else 0 */
+  double margin;          /* LOGISTIC and HINGE: D = beta (u_c - u_r) - margin;
+                             SQUARE: 0 */
+  double norm;            /* > 0: divides in the place of n_pair; 0: n_pair */
+  double grad_scale;      /* factor of the gradient */
+  uint32_t kind;          /* edp_pref_kind */
+  uint32_t average;       /* 1: u is a mean over the sequence's tokens, 0: a sum */
+  uint32_t reserved[2];   /* must be 0 */
+} edp_preference_config;
+
+/* Preference loss over pairs of sequences of a packed batch.  With
+ * x_t = logp - ref_logp (logp without ref_logp), u_s = sum or mean of x over the
+ * tokens of sequence s (0 for one without tokens), and pair i = (chosen c,
+ * rejected r):
+ *   L = (1/norm) sum_i loss(u_c, u_r),  dlogp[t] = grad_scale dL/dlogp[t]
+ * A sequence may be in any number of pairs; its gradients add up (exactly, to
+ * 2^-62 of |dloss/du| before norm and grad_scale, so in no order; beyond 2^22
+ * they become NaN).  loss (float [4]) = L, and the means over the pairs of:
+ * u_c > u_r, beta u_c, beta u_r.  seq_ratio (float [n_seq]) = u, pair_loss
+ * (float [n_pair]) and dlogp (float [n_tokens]) may be NULL.  off and the tokens
+ * outside it as for edp_policy_loss.  pair: int64 [n_pair][2]; a pair with an
+ * index outside [0, n_seq) has loss 0 and adds nothing, and edp_sync reports it
+ * (EDP_ERR_INVALID).
+ * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, a NULL
+ * logp, off, pair or loss, n_seq == 0 or >= 2^31, n_tokens == 0 or >= 2^40,
+ * n_pair == 0 or > 2^20, or arrays outside device memory; EDP_ERR_OOM when the
+ * scratch cannot be allocated. */
+EDP_API edp_status edp_preference_loss(edp_ctx *ctx, const edp_preference_config *cfg,
+                                       const float *logp, const float *ref_logp,
+                                       const uint8_t *mask, const uint64_t *off,
+                                       uint64_t n_seq, uint64_t n_tokens, const int64_t *pair,
+                                       uint32_t n_pair, float *loss, float *seq_ratio,
+                                       float *pair_loss, float *dlogp, edp_stream stream);
+
+/* The balance loss of a mixture-of-experts policy's router over the batch's
+ * tokens, and the experts' loads (Fedus et al. 2021, for `top` experts a token).
+ * Router logits [rows][experts] of type dtype, stride elements from row to row;
+ * sel (int32 [rows][top]) the experts that the router chose (negative: none).
+ * With N the tokens not masked and p = softmax(logits):
+ *   counts[e] = how often a token chose e            (int64 [experts])
+ *   prob[e]   = (1/N) sum_t p_te                     (float [experts] or NULL)
+ *   f_e       = experts counts[e] / (top N)
+ *   loss[0]   = coef sum_e f_e prob[e]               (float [1])
+ *   dlogits   = grad_scale coef / N p_te (f_e - sum_j f_j p_tj), of the type
+ *               of the logits (or NULL); 0 for a masked token
+ * No token: all 0.  An expert >= experts is not counted and reported by
+ * edp_sync (EDP_ERR_INVALID).  A row whose logits are all -infinity has p = 0
+ * and is reported the same way; NaN or +infinity makes loss, prob and the row's
+ * gradient NaN.  dlogits may be the logits' own array (with dstride == stride).
+ * Errors: EDP_ERR_INVALID for an unknown dtype, rows == 0 or >= 2^31, experts
+ * outside [1, 1024], top outside [1, 64], stride or dstride < experts, coef or
+ * grad_scale not finite, a NULL logits, sel, loss or counts, or arrays outside
+ * device memory or not aligned to their type; EDP_ERR_OOM when the scratch
+ * cannot be allocated. */
+EDP_API edp_status edp_balance_loss(edp_ctx *ctx, const void *logits, uint32_t dtype,
+                                    uint64_t rows, uint32_t experts, uint64_t stride,
+                                    const int32_t *sel, uint32_t top, const uint8_t *mask,
+                                    double coef, double grad_scale, float *loss,
+                                    int64_t *counts, float *prob, void *dlogits,
+                                    uint64_t dstride, edp_stream stream);
 
 /* Wait for `stream`, then report (and clear) asynchronous CUDA errors and
  * device-side flags recorded since the previous edp_sync. */

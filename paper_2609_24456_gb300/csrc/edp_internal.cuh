@@ -22,6 +22,7 @@ enum : uint32_t {
   DEVERR_TIMEOUT = 4u,  // a bounded device-side wait expired (packed delivery)
   DEVERR_TREE = 8u,     // a tree descent found no child holding its target
   DEVERR_OVERFLOW = 16u,  // packed output larger than its buffer (clipped)
+  DEVERR_ROW = 32u,       // a row of logits that are all -infinity
 };
 
 // Small device-resident control block (one per context).
@@ -35,6 +36,9 @@ struct Ctrl {
   uint32_t pad[2];
   unsigned long long bad_index;  // first offending index (diagnostics)
   unsigned long long host_bytes;  // two-tier deliveries: bytes read from the host tier
+  // losses (calls are ordered), each 0 between calls: tokens counted, CTAs done
+  unsigned long long loss_tokens;
+  uint32_t loss_ticket, pad2;
 };
 
 constexpr int kFanout = 32;
@@ -536,6 +540,51 @@ cudaError_t launch_gae(edp_ctx *ctx, const float *r, const float *v,
                        cudaStream_t s);
 cudaError_t launch_probe_read(const void *src, uint64_t bytes, uint64_t *fold,
                               cudaStream_t s);
+
+// Losses of a packed batch (k_logits.cu, k_loss.cu).
+// Logits of `rows` tokens: element (t, j) at z + t * stride + j.
+struct Logits {
+  const void *z;
+  uint32_t dtype;  // edp_dtype
+  uint32_t vocab;
+  uint64_t rows, stride;
+  const int32_t *target;
+  const uint8_t *mask;
+  double temperature;
+};
+// Which tokens of a batch count, and for how much (edp_policy_config::reduce).
+struct TokenSet {
+  const uint8_t *mask;
+  const uint64_t *off;    // nullptr: one run of n tokens
+  const int32_t *target;  // of the form from logits: 0 <= target < vocab
+  uint32_t vocab;
+  uint32_t reduce;
+  uint64_t n_seq, n;
+  double norm;
+};
+struct PolicyTokens {
+  const float *logp, *old_logp, *ref_logp, *adv, *entropy;
+};
+cudaError_t launch_token_logprob(edp_ctx *ctx, const Logits &z, float *logp, float *entropy,
+                                 float *stats, cudaStream_t s);
+cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float *stats,
+                                      const float *entropy, const float *dlogp,
+                                      const float *dentropy, void *dz, uint64_t dstride,
+                                      cudaStream_t s);
+cudaError_t launch_policy_loss(edp_ctx *ctx, const edp_policy_config &cfg, const TokenSet &set,
+                               const PolicyTokens &p, float *loss, float *dlogp,
+                               float *dentropy, cudaStream_t s);
+cudaError_t launch_policy_loss_logits(edp_ctx *ctx, const edp_policy_config &cfg,
+                                      const TokenSet &set, const PolicyTokens &p,
+                                      const Logits &z, float *loss, float *logp, float *entropy,
+                                      void *dz, uint64_t dstride, cudaStream_t s);
+cudaError_t launch_preference_loss(edp_ctx *ctx, const edp_preference_config &cfg,
+                                   const TokenSet &set, const float *logp, const float *ref,
+                                   const int64_t *pair, uint32_t n_pair, float *loss,
+                                   float *ratio, float *pair_loss, float *dlogp, cudaStream_t s);
+cudaError_t launch_balance_loss(edp_ctx *ctx, const Logits &z, const int32_t *sel, uint32_t top,
+                                double coef, double grad_scale, float *loss, int64_t *counts,
+                                float *prob, void *dz, uint64_t dstride, cudaStream_t s);
 
 // Scratch owned by the context, grown on demand.  Growing allocates, and
 // first waits for the device (the old block may still be in use); neither

@@ -83,6 +83,26 @@ class edp_sched_choice(C.Structure):
                 ("t_iter", C.c_double)]
 
 
+EDP_F32, EDP_BF16, EDP_F16 = range(3)
+EDP_REDUCE_TOKEN_MEAN, EDP_REDUCE_SEQ_MEAN, EDP_REDUCE_SEQ_SUM = range(3)
+EDP_KL_K1, EDP_KL_K2, EDP_KL_K3 = range(3)
+EDP_PREF_LOGISTIC, EDP_PREF_SQUARE, EDP_PREF_HINGE = range(3)
+
+
+class edp_policy_config(C.Structure):
+    _fields_ = [("clip_low", C.c_double), ("clip_high", C.c_double),
+                ("dual_clip", C.c_double), ("kl_coef", C.c_double),
+                ("entropy_coef", C.c_double), ("norm", C.c_double),
+                ("grad_scale", C.c_double), ("kl", C.c_uint32), ("reduce", C.c_uint32),
+                ("reserved", C.c_uint32 * 2)]
+
+
+class edp_preference_config(C.Structure):
+    _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double),
+                ("margin", C.c_double), ("norm", C.c_double), ("grad_scale", C.c_double),
+                ("kind", C.c_uint32), ("average", C.c_uint32), ("reserved", C.c_uint32 * 2)]
+
+
 EDP_PLACE_HOST_PAGEABLE, EDP_PLACE_HOST_PINNED, EDP_PLACE_GPU, EDP_PLACE_GPU_HOST = range(4)
 
 
@@ -144,6 +164,19 @@ SIGNATURES = {
     "edp_grpo_advantage": (C.c_int, [_VP, _VP, _VP, _U32, C.c_float, _VP, _VP]),
     "edp_pack_deliver": (C.c_int, [_VP, _VP, _VP, _U64, _VP, _U32, _VP, _VP, _VP, _VP,
                                    _U64, _VP]),
+    "edp_token_logprob": (C.c_int, [_VP, _VP, _U32, _U64, _U32, _U64, _VP, _VP, _D, _VP, _VP,
+                                    _VP, _VP]),
+    "edp_token_logprob_grad": (C.c_int, [_VP, _VP, _U32, _U64, _U32, _U64, _VP, _VP, _D, _VP,
+                                         _VP, _VP, _VP, _VP, _U64, _VP]),
+    "edp_policy_loss": (C.c_int, [_VP, C.POINTER(edp_policy_config)] + [_VP] * 7 +
+                        [_U64, _U64, _VP, _VP, _VP, _VP]),
+    "edp_policy_loss_logits": (C.c_int, [_VP, C.POINTER(edp_policy_config), _VP, _U32, _U64, _U32,
+                                         _U64, _VP, _D, _VP, _VP, _VP, _VP, _VP, _U64, _VP, _VP,
+                                         _VP, _VP, _U64, _VP]),
+    "edp_preference_loss": (C.c_int, [_VP, C.POINTER(edp_preference_config), _VP, _VP, _VP, _VP,
+                                      _U64, _U64, _VP, _U32, _VP, _VP, _VP, _VP, _VP]),
+    "edp_balance_loss": (C.c_int, [_VP, _VP, _U32, _U64, _U32, _U64, _VP, _U32, _VP, _D, _D, _VP,
+                                   _VP, _VP, _VP, _U64, _VP]),
     "edp_grpo_pack_deliver": (C.c_int, [_VP, _VP, _VP, _U32, C.c_float, _VP, _VP, _VP, _U64,
                                         _VP, _U32, _VP, _VP, _VP, _U64, _VP]),
 }
@@ -584,6 +617,110 @@ def edp_grpo_pack_deliver(ctx, r, group_off, n_groups, eps, adv, tokens, seq_off
         ctx, ptr(r), ptr(group_off), n_groups, eps, ptr(adv), ptr(tokens), ptr(seq_off),
         n_seq, ptr(idx), batch, ptr(out_tokens), ptr(out_off), ptr(out_value), out_cap,
         stream_handle(stream)), "edp_grpo_pack_deliver")
+
+
+# --- the learner's losses (include/edp.h, "The learner's losses") ----------------
+def make_policy_config(clip_low=0.2, clip_high=0.2, dual_clip=0.0, kl_coef=0.0, kl=EDP_KL_K3,
+                       entropy_coef=0.0, reduce=EDP_REDUCE_TOKEN_MEAN, norm=0.0,
+                       grad_scale=1.0):
+    return edp_policy_config(clip_low, clip_high, dual_clip, kl_coef, entropy_coef, norm,
+                             grad_scale, kl, reduce)
+
+
+def make_preference_config(beta, kind=EDP_PREF_LOGISTIC, label_smoothing=0.0, margin=0.0,
+                           average=False, norm=0.0, grad_scale=1.0):
+    return edp_preference_config(beta, label_smoothing, margin, norm, grad_scale, kind,
+                                 int(bool(average)))
+
+
+def _dtype(t):
+    name = str(t.dtype)
+    if name not in ("torch.float32", "torch.bfloat16", "torch.float16"):
+        raise TypeError("logits of %s: float32, bfloat16 or float16" % name)
+    return {"torch.float32": EDP_F32, "torch.bfloat16": EDP_BF16, "torch.float16": EDP_F16}[name]
+
+
+def _rows(t):
+    """(address, dtype, rows, columns, stride) of a 2-D tensor whose rows are
+    contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("logits: a 2-D tensor with contiguous rows")
+    rows, cols = t.shape
+    return t.data_ptr(), _dtype(t), rows, cols, t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _grad_rows(t, z):
+    """(address, stride) of the gradient of the logits z."""
+    if t is None:
+        return None, 0
+    p, _, _, _, stride = _rows(t)
+    if t.shape != z.shape or t.dtype != z.dtype:
+        raise ValueError("dlogits: the shape and type of the logits")
+    return p, stride
+
+
+def edp_token_logprob(ctx, logits, target, logp, mask=None, temperature=1.0, entropy=None,
+                      stats=None, stream=None):
+    """Log-probabilities (and entropies) of target[t] under logits[t]."""
+    p, dt, rows, vocab, stride = _rows(logits)
+    return _check(ctx, lib().edp_token_logprob(
+        ctx, p, dt, rows, vocab, stride, ptr(target), ptr(mask), temperature, ptr(logp),
+        ptr(entropy), ptr(stats), stream_handle(stream)), "edp_token_logprob")
+
+
+def edp_token_logprob_grad(ctx, logits, target, stats, dlogp, dlogits, mask=None,
+                           temperature=1.0, entropy=None, dentropy=None, stream=None):
+    """Gradient of the logits; dlogits may be the logits."""
+    p, dt, rows, vocab, stride = _rows(logits)
+    d, dstride = _grad_rows(dlogits, logits)
+    return _check(ctx, lib().edp_token_logprob_grad(
+        ctx, p, dt, rows, vocab, stride, ptr(target), ptr(mask), temperature, ptr(stats),
+        ptr(entropy), ptr(dlogp), ptr(dentropy), d, dstride, stream_handle(stream)),
+        "edp_token_logprob_grad")
+
+
+def edp_policy_loss(ctx, cfg: edp_policy_config, logp, old_logp, adv, n_tokens, loss,
+                    ref_logp=None, mask=None, off=None, n_seq=0, entropy=None, dlogp=None,
+                    dentropy=None, stream=None):
+    return _check(ctx, lib().edp_policy_loss(
+        ctx, C.byref(cfg), ptr(logp), ptr(old_logp), ptr(ref_logp), ptr(adv), ptr(entropy),
+        ptr(mask), ptr(off), n_seq, n_tokens, ptr(loss), ptr(dlogp), ptr(dentropy),
+        stream_handle(stream)), "edp_policy_loss")
+
+
+def edp_policy_loss_logits(ctx, cfg: edp_policy_config, logits, target, old_logp, adv, loss,
+                           logp, dlogits, ref_logp=None, mask=None, off=None, n_seq=0,
+                           temperature=1.0, entropy=None, stream=None):
+    """edp_token_logprob, edp_policy_loss and edp_token_logprob_grad in one."""
+    p, dt, rows, vocab, stride = _rows(logits)
+    d, dstride = _grad_rows(dlogits, logits)
+    return _check(ctx, lib().edp_policy_loss_logits(
+        ctx, C.byref(cfg), p, dt, rows, vocab, stride, ptr(target), temperature, ptr(old_logp),
+        ptr(ref_logp), ptr(adv), ptr(mask), ptr(off), n_seq, ptr(loss), ptr(logp), ptr(entropy),
+        d, dstride, stream_handle(stream)), "edp_policy_loss_logits")
+
+
+def edp_preference_loss(ctx, cfg: edp_preference_config, logp, off, n_seq, n_tokens, pair,
+                        n_pair, loss, ref_logp=None, mask=None, seq_ratio=None, pair_loss=None,
+                        dlogp=None, stream=None):
+    return _check(ctx, lib().edp_preference_loss(
+        ctx, C.byref(cfg), ptr(logp), ptr(ref_logp), ptr(mask), ptr(off), n_seq, n_tokens,
+        ptr(pair), n_pair, ptr(loss), ptr(seq_ratio), ptr(pair_loss), ptr(dlogp),
+        stream_handle(stream)), "edp_preference_loss")
+
+
+def edp_balance_loss(ctx, logits, sel, coef, loss, counts, mask=None, prob=None, dlogits=None,
+                     grad_scale=1.0, stream=None):
+    """Loads and balance loss of a router: logits [rows][experts], sel
+    [rows][top]."""
+    p, dt, rows, experts, stride = _rows(logits)
+    if sel.dim() != 2 or not sel.is_contiguous():
+        raise ValueError("sel: a contiguous 2-D tensor")
+    d, dstride = _grad_rows(dlogits, logits)
+    return _check(ctx, lib().edp_balance_loss(
+        ctx, p, dt, rows, experts, stride, ptr(sel), sel.shape[1], ptr(mask), coef, grad_scale,
+        ptr(loss), ptr(counts), ptr(prob), d, dstride, stream_handle(stream)),
+        "edp_balance_loss")
 
 
 def edp_save(ctx, path, stream=None):
