@@ -57,6 +57,8 @@ void free_all(edp_ctx *c) {
   if (c->ctrl) fr(c->cfg.alloc_user, c->ctrl);
   if (c->scratch) fr(c->cfg.alloc_user, c->scratch);
   if (c->perm_scratch) fr(c->cfg.alloc_user, c->perm_scratch);
+  if (c->zeroed) fr(c->cfg.alloc_user, c->zeroed);
+  c->zeroed = nullptr;
   c->perm_scratch = nullptr;
   c->tree_mem = nullptr;
   c->ctrl = nullptr;
@@ -280,6 +282,12 @@ cudaError_t edp::ctx_perm_scratch(edp_ctx *ctx, size_t bytes, cudaStream_t s, vo
   const cudaError_t e =
       grow(ctx, &ctx->perm_scratch, &ctx->perm_bytes, bytes, perm_zeroed_bytes(), s);
   *out = ctx->perm_scratch;
+  return e;
+}
+
+cudaError_t edp::ctx_zeroed_scratch(edp_ctx *ctx, size_t bytes, cudaStream_t s, void **out) {
+  const cudaError_t e = grow(ctx, &ctx->zeroed, &ctx->zeroed_bytes, bytes, bytes, s);
+  *out = ctx->zeroed;
   return e;
 }
 

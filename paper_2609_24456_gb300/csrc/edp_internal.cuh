@@ -66,6 +66,8 @@ struct edp_ctx {
   size_t scratch_bytes = 0;
   void *perm_scratch = nullptr;
   size_t perm_bytes = 0;
+  void *zeroed = nullptr;  // sums of the balance loss, 0 between calls
+  size_t zeroed_bytes = 0;
   // byte -> fl32(b/255) constants: x*R1 + x*R2 with one rounding
   float r1 = 0.f, r2 = 0.f;
   // per-channel normalisation: t = x - mean; y = t*S1 + t*S2 (one rounding)
@@ -541,7 +543,7 @@ cudaError_t launch_gae(edp_ctx *ctx, const float *r, const float *v,
 cudaError_t launch_probe_read(const void *src, uint64_t bytes, uint64_t *fold,
                               cudaStream_t s);
 
-// Losses of a packed batch (k_logits.cu, k_loss.cu).
+// Losses of a packed batch (k_logits.cu, k_policy.cu, k_pref.cu, k_balance.cu).
 // Logits of `rows` tokens: element (t, j) at z + t * stride + j.
 struct Logits {
   const void *z;
@@ -596,6 +598,8 @@ cudaError_t ctx_scratch(edp_ctx *ctx, size_t bytes, cudaStream_t s, void **out);
 // shuffle scratch: its first perm_zeroed_bytes() start zeroed and are left
 // zeroed by every shuffle
 cudaError_t ctx_perm_scratch(edp_ctx *ctx, size_t bytes, cudaStream_t s, void **out);
+// sums that start zeroed and that every call leaves zeroed
+cudaError_t ctx_zeroed_scratch(edp_ctx *ctx, size_t bytes, cudaStream_t s, void **out);
 size_t perm_scratch_bytes(uint32_t n);
 size_t perm_zeroed_bytes();
 

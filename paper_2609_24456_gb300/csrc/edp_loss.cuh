@@ -1,5 +1,6 @@
 // edp_loss.cuh -- what the kernels of the losses share: element types, the
-// policy loss of one token, sums that keep the bits of more than fp32.
+// policy loss of one token, sums that keep the bits of more than fp32, and the
+// walk over a packed batch's tokens.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -118,5 +119,169 @@ __device__ __forceinline__ PolicyToken policy_token(const PolicyRule &c, float l
   return o;
 }
 
+
+// ---------------------------------------------------------------------------
+// Sums in pairs of fp32 numbers: hi is the running sum, lo the sum of its
+// rounding errors (Ogita, Rump and Oishi 2005, "Sum2").  About 46 bits, for 7
+// operations a term; fp64 runs at a sixty-fourth of the fp32 rate here.  hi
+// alone carries infinities and NaN.
+// ---------------------------------------------------------------------------
+struct Pair {
+  float hi, lo;
+};
+__device__ __forceinline__ void pair_add(Pair &a, float x) {
+  const df s = two_sum(a.hi, x);
+  a.hi = s.hi;
+  a.lo = __fadd_rn(a.lo, s.lo);
+}
+__device__ __forceinline__ Pair pair_join(Pair a, Pair b) {
+  const df s = two_sum(a.hi, b.hi);
+  return {s.hi, __fadd_rn(__fadd_rn(a.lo, b.lo), s.lo)};
+}
+__device__ __forceinline__ double pair_value(Pair a) {
+  return isfinite(a.hi) ? (double)a.hi + (double)a.lo : (double)a.hi;
+}
+__device__ __forceinline__ Pair pair_shfl_xor(Pair a, int o) {
+  return {__shfl_xor_sync(kAllLanes, a.hi, o), __shfl_xor_sync(kAllLanes, a.lo, o)};
+}
+__device__ __forceinline__ Pair warp_join(Pair a) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) a = pair_join(a, pair_shfl_xor(a, o));
+  return a;
+}
+
+// K sums over the grid: the pairs of every thread of every CTA joined in a fixed
+// order.  True in the last CTA to arrive, where total[] (shared) then holds them.
+// part: [K][gridDim.x]; ticket: 0 before and after.
+template <int NT, int K>
+__device__ __forceinline__ bool grid_join(const Pair (&mine)[K], Pair *total, Pair *part,
+                                          uint32_t *ticket) {
+  static_assert(K <= NT / 32, "a warp per sum");
+  __shared__ Pair red[K][NT / 32];
+  __shared__ bool last;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const Pair v = warp_join(mine[k]);
+    if (lane == 0) red[k][wid] = v;
+  }
+  __syncthreads();
+  Pair v{0.f, 0.f};
+  if (wid < K) {
+    if (lane < NT / 32) v = red[wid][lane];
+    v = warp_join(v);
+  }
+  if (gridDim.x == 1) {
+    if (wid < K && lane == 0) total[wid] = v;
+    __syncthreads();
+    return true;
+  }
+  if (wid < K && lane == 0) {
+    __stcg(reinterpret_cast<float2 *>(part) + (uint64_t)wid * gridDim.x + blockIdx.x,
+           make_float2(v.hi, v.lo));
+    __threadfence();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!last) return false;
+  __threadfence();
+  if (wid < K) {
+    v = Pair{0.f, 0.f};
+    for (uint32_t b = lane; b < gridDim.x; b += 32) {
+      const float2 x =
+          __ldcg(reinterpret_cast<const float2 *>(part) + (uint64_t)wid * gridDim.x + b);
+      v = pair_join(v, Pair{x.x, x.y});
+    }
+    v = warp_join(v);
+    if (lane == 0) total[wid] = v;
+  }
+  if (threadIdx.x == 0) *ticket = 0u;
+  __syncthreads();
+  return true;
+}
+
+// ---------------------------------------------------------------------------
+// Tokens in chunks: a CTA of NT threads takes 4 NT consecutive tokens, 4 per
+// thread, whatever the sequences' lengths.
+// ---------------------------------------------------------------------------
+
+// The sequence of token t among lo .. hi - 1: the last one that starts at t or
+// before (so an empty one holds none).
+__device__ __forceinline__ uint32_t sequence_of(const uint64_t *off, uint32_t lo, uint32_t hi,
+                                                uint64_t t) {
+  while (hi - lo > 1) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (off[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+// The same by a warp, 32 probes at a time: three rounds for 32,768 sequences.
+__device__ __forceinline__ uint32_t sequence_of_warp(const uint64_t *off, uint32_t n, uint64_t t) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const uint32_t step = (hi - lo + 31) / 32;  // probes lo + step, lo + 2 step, ...
+    const uint32_t at = min((uint64_t)lo + (uint64_t)(lane + 1) * step, (uint64_t)hi);
+    const bool le = at < hi && off[at] <= t;
+    const uint32_t k = __popc(__ballot_sync(kAllLanes, le));  // probes at or before t
+    const uint32_t top = (uint32_t)min((uint64_t)lo + (uint64_t)(k + 1) * step, (uint64_t)hi);
+    lo += k * step;
+    hi = top;
+  }
+  return lo;
+}
+
+// Which of the tokens t .. t + 3 count, as bits; t is a multiple of 4.  first,
+// end: the tokens that the sequences hold.
+template <bool VEC>
+__device__ __forceinline__ uint32_t token_bits(const TokenSet &s, uint64_t t, uint64_t first,
+                                               uint64_t end) {
+  if (t >= end) return 0;
+  uint32_t bits = t + 4 <= end ? 15u : (1u << (uint32_t)(end - t)) - 1u;
+  if (t < first) bits &= t + 4 <= first ? 0u : ~((1u << (uint32_t)(first - t)) - 1u);
+  if (s.mask) {
+    if (VEC && t + 4 <= s.n) {
+      const uint32_t m = *reinterpret_cast<const uint32_t *>(s.mask + t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!((m >> (8 * i)) & 0xffu)) bits &= ~(1u << i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((bits >> i & 1u) && !s.mask[t + i]) bits &= ~(1u << i);
+    }
+  }
+  if (s.target) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((bits >> i & 1u) && (uint32_t)s.target[t + i] >= s.vocab) bits &= ~(1u << i);
+  }
+  return bits;
+}
+
+// Elements t .. t + 3 of an array of n; NaN-safe: what is beyond n is 0.
+template <bool VEC>
+__device__ __forceinline__ float4 load4(const float *p, uint64_t t, uint64_t n) {
+  if (VEC && t + 4 <= n) return *reinterpret_cast<const float4 *>(p + t);
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (t < n) v.x = p[t];
+  if (t + 1 < n) v.y = p[t + 1];
+  if (t + 2 < n) v.z = p[t + 2];
+  if (t + 3 < n) v.w = p[t + 3];
+  return v;
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(float *p, uint64_t t, uint64_t n, float4 v) {
+  if (VEC && t + 4 <= n) {
+    *reinterpret_cast<float4 *>(p + t) = v;
+    return;
+  }
+  if (t < n) p[t] = v.x;
+  if (t + 1 < n) p[t + 1] = v.y;
+  if (t + 2 < n) p[t + 2] = v.z;
+  if (t + 3 < n) p[t + 3] = v.w;
+}
 
 }  // namespace edp

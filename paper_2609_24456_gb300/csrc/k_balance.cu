@@ -1,0 +1,318 @@
+// k_balance.cu -- the balance loss of a router over a batch's tokens: how often
+// each expert was chosen, the mean probability of each, their product's sum and
+// its gradient by the router's logits.
+//
+// The counts need the choices alone (4 bytes each), so they come first; the
+// gradient then takes one pass over the logits, read once and written once.  A
+// row is a group of lanes with a 16-byte vector each (or a warp, element by
+// element, where rows do not lie on 16-byte boundaries); the softmax stays in
+// registers.  Counts and probabilities add up over CTAs as whole numbers, in
+// any order to the same bits.  Up to kOneCta elements one CTA does both steps.
+#include "edp_loss.cuh"
+
+namespace edp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr uint32_t kMaxExperts = 1024;
+constexpr uint64_t kOneCta = 32768;
+constexpr uint32_t kCountRows = 256;  // rows a CTA counts at a time
+constexpr float kProbUnits = 1099511627776.f;  // 2^40
+
+}  // namespace
+
+// Sums over CTAs, all 0 between calls.
+struct BalanceSums {
+  unsigned long long tokens;
+  uint32_t nan, pad;
+  unsigned long long prob[kMaxExperts];  // in units of 2^-40
+  uint32_t count[kMaxExperts];
+};
+
+namespace {
+
+struct BalanceArgs {
+  const void *z;
+  uint64_t rows, stride;
+  uint32_t E, top;
+  const int32_t *sel;
+  const uint8_t *mask;
+  float coef, scale;  // coef, grad_scale coef
+  float *loss, *prob;
+  int64_t *counts;
+  void *dz;
+  uint64_t dstride;
+};
+
+// Rows r0, r0 + step, ... (each kCountRows) into hist; how many of them count.
+template <int NT>
+__device__ __forceinline__ uint32_t count_choices(const BalanceArgs &a, uint64_t r0, uint64_t step,
+                                                  uint32_t *hist, Ctrl *ctrl) {
+  uint32_t tokens = 0;
+  for (; r0 < a.rows; r0 += step) {
+    const uint32_t nr = (uint32_t)min((uint64_t)kCountRows, a.rows - r0);
+    for (uint32_t i = threadIdx.x; i < nr; i += NT) tokens += !a.mask || a.mask[r0 + i];
+    const int32_t *sel = a.sel + r0 * a.top;
+    for (uint32_t i = threadIdx.x; i < nr * a.top; i += NT) {
+      if (a.mask && !a.mask[r0 + i / a.top]) continue;
+      const int32_t e = sel[i];
+      if (e < 0) continue;
+      if ((uint32_t)e < a.E) atomicAdd(&hist[e], 1u);
+      else flag(ctrl, DEVERR_INDEX, (unsigned long long)e);
+    }
+  }
+  return tokens;
+}
+
+__global__ void __launch_bounds__(kThreads)
+k_expert_counts(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
+  __shared__ uint32_t hist[kMaxExperts];
+  pdl_wait();
+  pdl_launch();
+  for (uint32_t e = threadIdx.x; e < a.E; e += kThreads) hist[e] = 0;
+  __syncthreads();
+  uint32_t n = count_choices<kThreads>(a, (uint64_t)blockIdx.x * kCountRows,
+                                       (uint64_t)gridDim.x * kCountRows, hist, ctrl);
+  n = __reduce_add_sync(kAllLanes, n);
+  if ((threadIdx.x & 31) == 0 && n) atomicAdd(&sums->tokens, (unsigned long long)n);
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < a.E; e += kThreads)
+    if (hist[e]) atomicAdd(&sums->count[e], hist[e]);
+}
+
+// L lanes per row, V loads of VN elements per lane: element i of lane l is in
+// column ((i / VN) L + l) VN + i % VN.
+template <typename T, int VN>
+__device__ __forceinline__ void load_row(const T *p, float (&v)[VN]) {
+  if constexpr (VN == 1) {
+    v[0] = to_f32(*p);
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    const T *x = reinterpret_cast<const T *>(&w);
+#pragma unroll
+    for (int i = 0; i < VN; ++i) v[i] = to_f32(x[i]);
+  }
+}
+template <typename T, int VN>
+__device__ __forceinline__ void store_row(T *p, const float (&v)[VN]) {
+  if constexpr (VN == 1) {
+    *p = from_f32<T>(v[0]);
+  } else {
+    uint4 w;
+    T *x = reinterpret_cast<T *>(&w);
+#pragma unroll
+    for (int i = 0; i < VN; ++i) x[i] = from_f32<T>(v[i]);
+    *reinterpret_cast<uint4 *>(p) = w;
+  }
+}
+
+// ONE: a single CTA, which counts the choices itself.
+template <typename T, int L, int V, int VN, int NT, bool ONE>
+__global__ void __launch_bounds__(NT)
+k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
+  constexpr int N = V * VN, kGroups = NT / L, kWarps = NT / 32;
+  constexpr uint32_t kCols = (uint32_t)N * L;  // columns with room for all experts
+  __shared__ float col[kWarps][kCols <= kMaxExperts ? kCols : kMaxExperts];
+  __shared__ uint32_t hist[ONE ? kMaxExperts : 1];
+  __shared__ uint32_t one_tokens;
+  __shared__ bool last;
+  pdl_wait();
+  if (ONE) pdl_launch();
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int l = threadIdx.x % L;
+  unsigned long long tokens;
+  if (ONE) {
+    for (uint32_t e = threadIdx.x; e < a.E; e += NT) hist[e] = 0;
+    if (threadIdx.x == 0) one_tokens = 0;
+    __syncthreads();
+    uint32_t n = count_choices<NT>(a, 0, kCountRows, hist, ctrl);
+    n = __reduce_add_sync(kAllLanes, n);
+    if (lane == 0 && n) atomicAdd(&one_tokens, n);
+    __syncthreads();
+    tokens = one_tokens;
+  } else {
+    tokens = __ldcg(&sums->tokens);
+  }
+  const float inv_n = 1.f / (float)(tokens ? tokens : 1);
+  const float per = (float)a.E / (float)a.top * inv_n;  // f_e = counts[e] * per
+  const float scale = a.scale * inv_n;
+  float f[N], ps[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t e = ((uint32_t)(i / VN) * L + l) * VN + i % VN;
+    f[i] = e < a.E ? (float)(ONE ? hist[e] : __ldcg(&sums->count[e])) * per : 0.f;
+    ps[i] = 0.f;
+  }
+  bool nan = false;
+  const uint64_t step = (uint64_t)gridDim.x * kGroups;
+  // the warp's groups take neighbouring rows and leave together
+  for (uint64_t t0 = (uint64_t)blockIdx.x * kGroups + (threadIdx.x / 32) * (32 / L); t0 < a.rows;
+       t0 += step) {
+    const uint64_t t = t0 + lane / L;
+    const bool in = t < a.rows, use = in && (!a.mask || a.mask[t]);
+    float y[N], m = kNegInf;
+    const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const uint32_t e = ((uint32_t)k * L + l) * VN;
+      float v[VN];
+#pragma unroll
+      for (int i = 0; i < VN; ++i) v[i] = kNegInf;
+      if (use && e < a.E) load_row<T, VN>(row + e, v);
+#pragma unroll
+      for (int i = 0; i < VN; ++i) {
+        y[k * VN + i] = v[i];
+        m = fmaxf(m, v[i]);
+      }
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
+    if (m == kNegInf) m = 0.f;
+    float s = 0.f, fp = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      y[i] = ex2((y[i] - m) * (float)kLog2e);
+      s += y[i];
+      fp = fmaf(y[i], f[i], fp);
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) {
+      s += __shfl_xor_sync(kAllLanes, s, o);
+      fp += __shfl_xor_sync(kAllLanes, fp, o);
+    }
+    if (use && s == 0.f && l == 0) flag(ctrl, DEVERR_ROW, t);  // no distribution: p = 0
+    const float inv = s == 0.f ? 0.f : 1.f / s;
+    fp *= inv;
+    nan |= isnan(inv);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      y[i] *= inv;
+      ps[i] += y[i];
+    }
+    if (a.dz && in) {
+      T *d = reinterpret_cast<T *>(a.dz) + t * a.dstride;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const uint32_t e = ((uint32_t)k * L + l) * VN;
+        float v[VN];
+#pragma unroll
+        for (int i = 0; i < VN; ++i) v[i] = scale * y[k * VN + i] * (f[k * VN + i] - fp);
+        if (e < a.E) store_row<T, VN>(d + e, v);
+      }
+    }
+  }
+  if (!ONE) pdl_launch();
+  if (nan) atomicExch(&sums->nan, 1u);
+  // over the warp's groups, then its CTA's warps, in order
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+#pragma unroll
+    for (int o = L; o < 32; o <<= 1) ps[i] += __shfl_xor_sync(kAllLanes, ps[i], o);
+    const uint32_t e = ((uint32_t)(i / VN) * L + l) * VN + i % VN;
+    if (lane < L && e < a.E) col[wid][e] = ps[i];
+  }
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < a.E; e += NT) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) v += col[w][e];
+    if (ONE) col[0][e] = v;
+    else if (v > 0.f) atomicAdd(&sums->prob[e], (unsigned long long)__float2ull_rn(v * kProbUnits));
+  }
+  __threadfence();
+  __syncthreads();
+  if (!ONE) {
+    if (threadIdx.x == 0) last = atomicAdd(&ctrl->loss_ticket, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+  }
+  const bool bad = __ldcg(&sums->nan) != 0;
+  Pair v{0.f, 0.f};
+  for (uint32_t e = threadIdx.x; e < a.E; e += NT) {
+    const uint32_t n = ONE ? hist[e] : __ldcg(&sums->count[e]);
+    float p = ONE ? col[0][e]
+                  : (float)__ldcg(&sums->prob[e]) * (1.f / kProbUnits);
+    p = bad ? __int_as_float(0x7fc00000) : p * inv_n;
+    if (a.prob) a.prob[e] = p;
+    a.counts[e] = n;
+    pair_add(v, (float)n * per * p);
+    if (!ONE) {
+      sums->prob[e] = 0;
+      sums->count[e] = 0;
+    }
+  }
+  v = warp_join(v);
+  __shared__ Pair red[kWarps];
+  if (lane == 0) red[wid] = v;
+  __syncthreads();  // every thread has seen sums->nan
+  if (threadIdx.x) return;
+  for (int w = 1; w < kWarps; ++w) v = pair_join(v, red[w]);
+  a.loss[0] = a.coef * (float)pair_value(v);
+  sums->tokens = 0;
+  sums->nan = 0;
+  ctrl->loss_ticket = 0;
+}
+
+template <typename T, int L, int V, int VN>
+cudaError_t launch_shape(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cudaStream_t s) {
+  if (a.rows * a.E <= kOneCta) {
+    constexpr int NT = V * VN * L <= 256 ? 1024 : 256;  // columns of each warp in shared memory
+    return launch_pdl(k_balance<T, L, V, VN, NT, true>, dim3(1), dim3(NT), s, a, sums, c->ctrl);
+  }
+  const uint64_t sms = (uint64_t)c->coop_sms;
+  const uint64_t cb = (a.rows + kCountRows - 1) / kCountRows;
+  cudaError_t e = launch_pdl(k_expert_counts, dim3((unsigned)(cb < sms ? cb : sms)),
+                             dim3(kThreads), s, a, sums, c->ctrl);
+  if (e != cudaSuccess) return e;
+  const uint64_t b = (a.rows * L + kThreads - 1) / kThreads;
+  return launch_pdl(k_balance<T, L, V, VN, kThreads, false>,
+                    dim3((unsigned)(b < 4 * sms ? b : 4 * sms)), dim3(kThreads), s, a, sums,
+                    c->ctrl);
+}
+
+template <typename T>
+cudaError_t launch_type(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cudaStream_t s) {
+  constexpr int VN = 16 / sizeof(T);
+  const uint64_t bytes = sizeof(T);
+  const bool vec = ((uintptr_t)a.z | (uintptr_t)a.dz | a.E * bytes | a.stride * bytes |
+                    (a.dz ? a.dstride * bytes : 0)) % 16 == 0;
+  if (vec) {
+    const uint32_t n = a.E / VN;  // vectors of a row
+    if (n <= 1) return launch_shape<T, 1, 1, VN>(c, a, sums, s);
+    if (n <= 2) return launch_shape<T, 2, 1, VN>(c, a, sums, s);
+    if (n <= 4) return launch_shape<T, 4, 1, VN>(c, a, sums, s);
+    if (n <= 8) return launch_shape<T, 8, 1, VN>(c, a, sums, s);
+    if (n <= 16) return launch_shape<T, 16, 1, VN>(c, a, sums, s);
+    if (n <= 32) return launch_shape<T, 32, 1, VN>(c, a, sums, s);
+    if (n <= 64) return launch_shape<T, 32, 2, VN>(c, a, sums, s);
+    if (n <= 128) return launch_shape<T, 32, 4, VN>(c, a, sums, s);
+    if constexpr (VN == 4) return launch_shape<T, 32, 8, VN>(c, a, sums, s);
+  }
+  if (a.E <= 32) return launch_shape<T, 32, 1, 1>(c, a, sums, s);
+  if (a.E <= 64) return launch_shape<T, 32, 2, 1>(c, a, sums, s);
+  if (a.E <= 128) return launch_shape<T, 32, 4, 1>(c, a, sums, s);
+  if (a.E <= 256) return launch_shape<T, 32, 8, 1>(c, a, sums, s);
+  if (a.E <= 512) return launch_shape<T, 32, 16, 1>(c, a, sums, s);
+  return launch_shape<T, 32, 32, 1>(c, a, sums, s);
+}
+
+}  // namespace
+
+cudaError_t launch_balance_loss(edp_ctx *c, const Logits &z, const int32_t *sel, uint32_t top,
+                                double coef, double grad_scale, float *loss, int64_t *counts,
+                                float *prob, void *dz, uint64_t dstride, cudaStream_t s) {
+  void *blk = nullptr;
+  cudaError_t e = ctx_zeroed_scratch(c, sizeof(BalanceSums), s, &blk);
+  if (e != cudaSuccess) return e;
+  BalanceSums *sums = (BalanceSums *)blk;
+  const BalanceArgs a{z.z, z.rows, z.stride, z.vocab, top, sel, z.mask, (float)coef,
+                      (float)(grad_scale * coef), loss, prob, counts, dz, dstride};
+  switch (z.dtype) {
+    case EDP_BF16: return launch_type<__nv_bfloat16>(c, a, sums, s);
+    case EDP_F16: return launch_type<__half>(c, a, sums, s);
+    default: return launch_type<float>(c, a, sums, s);
+  }
+}
+
+}  // namespace edp

@@ -1,0 +1,428 @@
+// k_pref.cu -- the preference loss over pairs of sequences of a packed batch, with
+// the gradient of the tokens' log-probabilities.
+//
+// Three steps, since a token's gradient needs its pair's whole sequences: the
+// sums of logp - ref by sequence (9 bytes a token), the pairs, and the gradient
+// (1 byte read, 4 written).  The sums go by chunks of 4 tokens per thread: a
+// segmented scan gives every sequence's part of a chunk, and whoever wants a
+// sequence's sum adds its parts in order.  A sequence's gradients from its
+// pairs add up as whole numbers, in any order to the same bits.  A batch of one
+// chunk takes all three steps in one CTA.
+#include "edp_loss.cuh"
+
+namespace edp {
+namespace {
+
+constexpr int kThreads = 512;        // a chunk of 2,048 tokens
+constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
+constexpr int kPairThreads = 256;
+constexpr uint32_t kSmallPairs = 4096;
+
+// A sequence's part of a chunk.
+struct alignas(16) SeqPart {
+  float hi, lo;
+  uint32_t n, pad;
+};
+// Gradient by a sequence's u, before norm and grad_scale, in whole numbers of
+// 2^-20 and of 2^-62.
+struct SeqGrad {
+  unsigned long long hi, lo;
+};
+
+struct PrefScratch {
+  SeqPart *inner;  // [n_seq] the part in the chunk where the sequence starts
+  SeqPart *head;   // [chunks] the part of the sequence that comes in from the left
+  SeqGrad *grad;   // [n_seq]
+  uint32_t *bad;   // [n_seq] a gradient is not a finite number below 2^22
+  Pair *part;
+};
+
+struct PrefRule {
+  double beta, smooth, margin, norm;
+  uint32_t kind, average;
+};
+
+struct PrefIn {
+  TokenSet s;
+  const float *logp, *ref;
+  const int64_t *pair;
+  uint32_t n_pair;
+};
+struct PrefOut {
+  float *loss, *ratio, *pair_loss, *dlogp;
+};
+
+struct Run {
+  Pair v;
+  uint32_t n;
+};
+__device__ __forceinline__ Run run_join(Run a, Run b) { return {pair_join(a.v, b.v), a.n + b.n}; }
+__device__ __forceinline__ Run run_up(Run a, int o) {
+  return {{__shfl_up_sync(kAllLanes, a.v.hi, o), __shfl_up_sync(kAllLanes, a.v.lo, o)},
+          __shfl_up_sync(kAllLanes, a.n, o)};
+}
+
+template <int NT>
+struct PrefShared {
+  uint32_t lo, hi;
+  Run warp[NT / 32];
+  uint32_t cut[NT / 32];
+};
+
+// Parts of the sequences in the chunk at t0 (which is below the last one's end).
+template <int NT, bool VEC>
+__device__ __forceinline__ void chunk_parts(const PrefIn &in, const PrefScratch &x, uint64_t t0,
+                                            uint64_t first, uint64_t end, PrefShared<NT> &sh) {
+  const TokenSet &s = in.s;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  constexpr uint64_t C = 4ull * NT;
+  const uint64_t t = t0 + 4 * threadIdx.x, stop = min(t0 + C, end);
+  const float4 lp = load4<VEC>(in.logp, t, s.n);
+  float4 rf = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (in.ref) rf = load4<VEC>(in.ref, t, s.n);
+  const uint32_t bits = token_bits<VEC>(s, t, first, end);
+  __syncthreads();  // the chunk before is done with
+  if (wid < 2) {
+    const uint32_t q = sequence_of_warp(s.off, (uint32_t)s.n_seq, wid == 0 ? t0 : stop - 1);
+    if (lane == 0) (wid == 0 ? sh.lo : sh.hi) = q;
+  }
+  __syncthreads();
+  const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
+
+  // the runs of a thread's tokens: what its first run adds to the one before,
+  // whole runs in between, and the run that is open at its end
+  Run open{{0.f, 0.f}, 0}, closed = open;
+  uint32_t q = 0, closed_q = 0;
+  uint64_t qend = 0;
+  bool cut = false, pending = false;  // a run ended here; the first of them did, unwritten
+  auto emit = [&](uint32_t seq, const Run &r) {
+    const SeqPart p{r.v.hi, r.v.lo, r.n, 0};
+    if (s.off[seq] >= t0) {
+      x.inner[seq] = p;
+      x.grad[seq] = SeqGrad{0, 0};
+      x.bad[seq] = 0;
+    } else {
+      x.head[t0 / C] = p;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (t + i >= stop || t + i < first) continue;
+    if (t + i >= qend) {
+      q = sequence_of(s.off, qend ? q : sh.lo, sh.hi + 1, t + i);
+      qend = min(s.off[q + 1], end);
+    }
+    if (bits >> i & 1u) {
+      pair_add(open.v, l4[i]);
+      pair_add(open.v, -r4[i]);
+      ++open.n;
+    }
+    if (t + i + 1 == qend || t + i + 1 == stop) {  // the run ends with this token
+      if (!cut && s.off[q] < t) {  // it may have begun in another thread
+        closed = open;
+        closed_q = q;
+        pending = true;
+      } else {
+        emit(q, open);
+      }
+      cut = true;
+      open = Run{{0.f, 0.f}, 0};
+    }
+  }
+  // what comes into each thread from those before it in the chunk
+  Run incl = open;
+  bool c = cut;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const Run y = run_up(incl, o);
+    const bool yc = __shfl_up_sync(kAllLanes, c, o);
+    if (lane >= o && !c) {
+      incl = run_join(y, incl);
+      c = yc;
+    }
+  }
+  if (lane == 31) {
+    sh.warp[wid] = incl;
+    sh.cut[wid] = c;
+  }
+  Run into = run_up(incl, 1);
+  bool into_cut = __shfl_up_sync(kAllLanes, c, 1);
+  if (lane == 0) {
+    into = Run{{0.f, 0.f}, 0};
+    into_cut = false;
+  }
+  __syncthreads();
+  if (!pending) return;
+  if (!into_cut) {
+    Run w{{0.f, 0.f}, 0};
+    for (int k = wid - 1; k >= 0; --k) {
+      w = run_join(sh.warp[k], w);
+      if (sh.cut[k]) break;
+    }
+    into = run_join(w, into);
+  }
+  emit(closed_q, run_join(into, closed));
+}
+
+// A sequence's sum and its number of tokens.
+template <uint64_t C>
+__device__ __forceinline__ Run sequence_sum(const TokenSet &s, const PrefScratch &x, uint64_t seq) {
+  const uint64_t a = s.off[seq], b = min(s.off[seq + 1], s.n);
+  if (b <= a) return {{0.f, 0.f}, 0};
+  const float4 p = __ldcg(reinterpret_cast<const float4 *>(&x.inner[seq]));
+  Run r{{p.x, p.y}, __float_as_uint(p.z)};
+#pragma unroll 4
+  for (uint64_t c = a / C + 1; c <= (b - 1) / C; ++c) {
+    const float4 h = __ldcg(reinterpret_cast<const float4 *>(&x.head[c]));
+    r = run_join(r, Run{{h.x, h.y}, __float_as_uint(h.z)});
+  }
+  return r;
+}
+
+constexpr double kHiUnit = 1.0 / 1048576.0;              // 2^-20
+constexpr double kLoUnit = 1.0 / 4611686018427387904.0;  // 2^-62
+constexpr double kGradMost = 4194304.0;                  // 2^22
+
+__device__ __forceinline__ void grad_add(const PrefScratch &x, uint64_t seq, double v) {
+  if (!(fabs(v) < kGradMost)) {
+    x.bad[seq] = 1u;  // every writer writes the same
+    return;
+  }
+  const double h = rint(v * (1.0 / kHiUnit));
+  const double l = rint((v - h * kHiUnit) * (1.0 / kLoUnit));
+  if (h != 0.0) atomicAdd(&x.grad[seq].hi, (unsigned long long)(long long)h);
+  if (l != 0.0) atomicAdd(&x.grad[seq].lo, (unsigned long long)(long long)l);
+}
+
+// Pairs first, first + step, ...: their losses, gradients and sums.
+template <uint64_t C>
+__device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
+                                           const PrefScratch &x, const PrefOut &out,
+                                           uint32_t first, uint32_t step, Pair (&sum)[4],
+                                           Ctrl *ctrl) {
+  for (uint64_t i = first; i < in.n_pair; i += step) {
+    const int64_t c = in.pair[2 * i], j = in.pair[2 * i + 1];
+    float l = 0.f;
+    if ((uint64_t)c >= in.s.n_seq || (uint64_t)j >= in.s.n_seq) {
+      flag(ctrl, DEVERR_INDEX, (unsigned long long)((uint64_t)c >= in.s.n_seq ? c : j));
+    } else {
+      const Run rc = sequence_sum<C>(in.s, x, c), rj = sequence_sum<C>(in.s, x, j);
+      const double kc = r.average && rc.n ? 1.0 / (double)rc.n : 1.0;
+      const double kj = r.average && rj.n ? 1.0 / (double)rj.n : 1.0;
+      const double uc = pair_value(rc.v) * kc, uj = pair_value(rj.v) * kj;
+      const double h = uc - uj, d = r.beta * h - r.margin;
+      double g;  // by u of the chosen
+      if (r.kind == EDP_PREF_LOGISTIC) {
+        const float f = (float)d, e = expf(-fabsf(f));
+        const float tail = log1pf(e);  // -ln s(|d|)
+        const float up = tail + fmaxf(-f, 0.f), down = tail + fmaxf(f, 0.f);
+        const float m = (float)r.smooth;
+        l = m == 0.f ? up : fmaf(1.f - m, up, m * down);
+        // s(-d) (1 - e) - s(d) e = s(-d) - e
+        const float sd = f > 0.f ? e / (1.f + e) : 1.f / (1.f + e);
+        g = -r.beta * ((double)sd - r.smooth);
+      } else if (r.kind == EDP_PREF_HINGE) {
+        l = isnan(d) ? (float)d : (float)fmax(1.0 - d, 0.0);
+        g = d < 1.0 ? -r.beta : 0.0;
+      } else {
+        const double y = h - 0.5 / r.beta;
+        l = (float)(y * y);
+        g = 2.0 * y;
+      }
+      if (isnan(d)) g = d;
+      grad_add(x, c, g * kc);
+      grad_add(x, j, -g * kj);
+      pair_add(sum[0], l);
+      if (h > 0.0) pair_add(sum[1], 1.f);
+      const df bc = df_split(r.beta * uc), bj = df_split(r.beta * uj);
+      pair_add(sum[2], bc.hi);
+      pair_add(sum[2], bc.lo);
+      pair_add(sum[3], bj.hi);
+      pair_add(sum[3], bj.lo);
+    }
+    if (out.pair_loss) out.pair_loss[i] = l;
+  }
+}
+
+template <uint64_t C>
+__device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
+                                            const PrefScratch &x, const PrefOut &out,
+                                            uint64_t first, uint64_t step) {
+  if (!out.ratio) return;
+  for (uint64_t q = first; q < in.s.n_seq; q += step) {
+    const Run v = sequence_sum<C>(in.s, x, q);
+    out.ratio[q] = (float)(pair_value(v.v) * (r.average && v.n ? 1.0 / (double)v.n : 1.0));
+  }
+}
+
+__device__ __forceinline__ void write_loss(const PrefRule &r, uint32_t n_pair, const Pair *total,
+                                           float *loss) {
+  loss[0] = (float)(pair_value(total[0]) / r.norm);
+  for (int k = 1; k < 4; ++k) loss[k] = (float)(pair_value(total[k]) / (double)n_pair);
+}
+
+// The gradient of each token of a sequence, rounded once.
+__device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, df scale) {
+  if (__ldcg(&x.bad[seq])) return __int_as_float(0x7fc00000);
+  const ulonglong2 g = __ldcg(reinterpret_cast<const ulonglong2 *>(&x.grad[seq]));
+  // what is whole units of 2^-20 in lo goes to hi, so that neither cancels much
+  const long long up = ((long long)g.y + (1ll << 41)) >> 42;
+  const long long whole = (long long)g.x + up;
+  const float h = (float)whole, rest = (float)(whole - (long long)h);
+  const float vh = h * (float)kHiUnit;
+  const float vl = fmaf(rest, (float)kHiUnit, (float)((long long)g.y - (up << 42)) * (float)kLoUnit);
+  return fmaf(scale.hi, vh, fmaf(scale.hi, vl, scale.lo * vh));
+}
+
+template <int NT, bool VEC>
+__device__ __forceinline__ void chunk_grad(const PrefIn &in, const PrefScratch &x, df scale,
+                                           float *dlogp, uint64_t t0, uint64_t first,
+                                           uint64_t end, PrefShared<NT> &sh) {
+  const TokenSet &s = in.s;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const uint64_t t = t0 + 4 * threadIdx.x;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (t0 < end) {
+    const uint32_t bits = token_bits<VEC>(s, t, first, end);
+    __syncthreads();
+    if (wid < 2) {
+      const uint32_t q = sequence_of_warp(s.off, (uint32_t)s.n_seq,
+                                          wid == 0 ? t0 : min(t0 + (uint64_t)(4 * NT), end) - 1);
+      if (lane == 0) (wid == 0 ? sh.lo : sh.hi) = q;
+    }
+    __syncthreads();
+    uint32_t q = 0;
+    uint64_t qend = 0;
+    float g = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!(bits >> i & 1u)) continue;
+      if (t + i >= qend) {
+        q = sequence_of(s.off, qend ? q : sh.lo, sh.hi + 1, t + i);
+        qend = s.off[q + 1];
+        g = token_grad(x, q, scale);
+      }
+      v[i] = g;
+    }
+  }
+  store4<VEC>(dlogp, t, s.n, make_float4(v[0], v[1], v[2], v[3]));
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads)
+k_pref_parts(PrefIn in, PrefScratch x) {
+  __shared__ PrefShared<kThreads> sh;
+  pdl_wait();
+  pdl_launch();
+  const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
+  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * kThreads; t0 < end;
+       t0 += (uint64_t)gridDim.x * 4 * kThreads)
+    chunk_parts<kThreads, VEC>(in, x, t0, first, end, sh);
+}
+
+__global__ void __launch_bounds__(kPairThreads)
+k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, Ctrl *ctrl) {
+  __shared__ Pair total[4];
+  pdl_wait();
+  const uint32_t i = blockIdx.x * kPairThreads + threadIdx.x, step = gridDim.x * kPairThreads;
+  Pair sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
+  take_pairs<4ull * kThreads>(in, r, x, out, i, step, sum, ctrl);
+  take_ratios<4ull * kThreads>(in, r, x, out, i, step);
+  pdl_launch();
+  if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
+    write_loss(r, in.n_pair, total, out.loss);
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads)
+k_pref_grad(PrefIn in, PrefScratch x, df scale, float *dlogp) {
+  __shared__ PrefShared<kThreads> sh;
+  pdl_wait();
+  pdl_launch();
+  const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
+  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * kThreads; t0 < in.s.n;
+       t0 += (uint64_t)gridDim.x * 4 * kThreads)
+    chunk_grad<kThreads, VEC>(in, x, scale, dlogp, t0, first, end, sh);
+}
+
+// All three steps of a batch of one chunk.
+template <bool VEC>
+__global__ void __launch_bounds__(kSmallThreads)
+k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *ctrl) {
+  constexpr uint64_t C = 4ull * kSmallThreads;
+  __shared__ PrefShared<kSmallThreads> sh;
+  __shared__ Pair total[4];
+  pdl_wait();
+  pdl_launch();
+  const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
+  if (end) chunk_parts<kSmallThreads, VEC>(in, x, 0, first, end, sh);
+  __threadfence();  // the pairs read around the first-level cache
+  __syncthreads();
+  Pair sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
+  take_pairs<C>(in, r, x, out, threadIdx.x, kSmallThreads, sum, ctrl);
+  take_ratios<C>(in, r, x, out, threadIdx.x, kSmallThreads);
+  __threadfence();
+  if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
+    write_loss(r, in.n_pair, total, out.loss);
+  if (out.dlogp) chunk_grad<kSmallThreads, VEC>(in, x, scale, out.dlogp, 0, first, end, sh);
+}
+
+}  // namespace
+
+cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
+                                   const TokenSet &set, const float *logp, const float *ref,
+                                   const int64_t *pair, uint32_t n_pair, float *loss,
+                                   float *ratio, float *pair_loss, float *dlogp,
+                                   cudaStream_t s) {
+  const uint64_t sms = (uint64_t)c->coop_sms;
+  const bool small = set.n <= 4 * kSmallThreads && n_pair <= kSmallPairs;
+  const uint64_t chunks = (set.n + 4 * kThreads - 1) / (4 * kThreads);
+  const uint64_t want = ((n_pair > set.n_seq ? n_pair : set.n_seq) + kPairThreads - 1) / kPairThreads;
+  const uint64_t pair_grid = want < 4 * sms ? want : 4 * sms;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t a = at;
+    at += (bytes + 15) & ~(size_t)15;
+    return a;
+  };
+  const size_t inner = take(set.n_seq * sizeof(SeqPart)), grad = take(set.n_seq * sizeof(SeqGrad));
+  const size_t head = take(chunks * sizeof(SeqPart)), bad = take(set.n_seq * sizeof(uint32_t));
+  const size_t part = take(4 * pair_grid * sizeof(Pair));
+  void *blk = nullptr;
+  cudaError_t e = ctx_scratch(c, at, s, &blk);
+  if (e != cudaSuccess) return e;
+  uint8_t *b = (uint8_t *)blk;
+  const PrefScratch x{(SeqPart *)(b + inner), (SeqPart *)(b + head), (SeqGrad *)(b + grad),
+                      (uint32_t *)(b + bad), (Pair *)(b + part)};
+  PrefRule r;
+  r.beta = cfg.beta;
+  r.smooth = cfg.label_smoothing;
+  r.margin = cfg.margin;
+  r.norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
+  const double by = cfg.grad_scale / r.norm;
+  const df scale{(float)by, (float)(by - (double)(float)by)};
+  r.kind = cfg.kind;
+  r.average = cfg.average;
+  const PrefIn in{set, logp, ref, pair, n_pair};
+  const PrefOut out{loss, ratio, pair_loss, dlogp};
+  const bool vec = (((uintptr_t)logp | (uintptr_t)ref | (uintptr_t)dlogp) & 15) == 0 &&
+                   ((uintptr_t)set.mask & 3) == 0;
+  if (small)
+    return launch_pdl(vec ? k_pref_small<true> : k_pref_small<false>, dim3(1),
+                      dim3(kSmallThreads), s, in, r, x, out, scale, c->ctrl);
+  const unsigned grid = (unsigned)(chunks < 4 * sms ? chunks : 4 * sms);
+  e = launch_pdl(vec ? k_pref_parts<true> : k_pref_parts<false>, dim3(grid), dim3(kThreads), s, in,
+                 x);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(k_pref_pairs, dim3((unsigned)pair_grid), dim3(kPairThreads), s, in, r, x, out,
+                 c->ctrl);
+  if (e != cudaSuccess || !dlogp) return e;
+  return launch_pdl(vec ? k_pref_grad<true> : k_pref_grad<false>, dim3(grid), dim3(kThreads), s,
+                    in, x, scale, dlogp);
+}
+
+}  // namespace edp

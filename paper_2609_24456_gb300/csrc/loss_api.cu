@@ -1,5 +1,5 @@
 // loss_api.cu -- the C ABI of the losses over a packed batch: argument checks
-// and dispatch to k_logits.cu and k_loss.cu.
+// and dispatch to k_logits.cu, k_policy.cu, k_pref.cu and k_balance.cu.
 #include <cmath>
 #include <initializer_list>
 
