@@ -52,6 +52,15 @@ struct PolicyRule {
   uint32_t kl;
 };
 
+// What a row of logits weighs in the policy loss, by its token's place.
+struct RowWeights {
+  const uint64_t *off;
+  uint32_t n_seq;
+  const float *sequence;             // each sequence's weight,
+  const unsigned long long *tokens;  // or the divisor of all,
+  float fixed;                       // or the weight of all
+};
+
 // One token: its policy loss and divergence, the ratio, whether it is clipped,
 // and the loss's derivative by logp (entropy apart), before weight and scale.
 struct PolicyToken {
@@ -59,30 +68,21 @@ struct PolicyToken {
   bool above, below;
 };
 
-// e^q - 1 - q and e^q - 1: below 1 the Taylor series, without the difference
-// that would leave few bits of the first (relative error below 2^-23 for all q).
+// e^q - 1 - q and, in em1, e^q - 1; e = e^q.  Below 1/2 the Taylor series, whose
+// first term left out is 2^-24 of the sum; above, the difference loses at most
+// three bits.
 __device__ __forceinline__ float exp_less_line(float q, float e, float *em1) {
-  float k;
-  if (fabsf(q) < 1.f) {
-    float p = 1.f / 6227020800.f;  // 1/13!
-    p = fmaf(p, q, 1.f / 479001600.f);
-    p = fmaf(p, q, 1.f / 39916800.f);
-    p = fmaf(p, q, 1.f / 3628800.f);
-    p = fmaf(p, q, 1.f / 362880.f);
-    p = fmaf(p, q, 1.f / 40320.f);
-    p = fmaf(p, q, 1.f / 5040.f);
-    p = fmaf(p, q, 1.f / 720.f);
-    p = fmaf(p, q, 1.f / 120.f);
-    p = fmaf(p, q, 1.f / 24.f);
-    p = fmaf(p, q, 1.f / 6.f);
-    p = fmaf(p, q, 0.5f);
-    k = q * q * p;
-    *em1 = q + k;
-  } else {
-    *em1 = e - 1.f;
-    k = *em1 - q;
-  }
-  return k;
+  float p = 1.f / 40320.f;  // 1/8!
+  p = fmaf(p, q, 1.f / 5040.f);
+  p = fmaf(p, q, 1.f / 720.f);
+  p = fmaf(p, q, 1.f / 120.f);
+  p = fmaf(p, q, 1.f / 24.f);
+  p = fmaf(p, q, 1.f / 6.f);
+  p = fmaf(p, q, 0.5f);
+  const float near = q * q * p;
+  const bool far = !(fabsf(q) < 0.5f);
+  *em1 = far ? e - 1.f : q + near;
+  return far ? *em1 - q : near;
 }
 
 __device__ __forceinline__ PolicyToken policy_token(const PolicyRule &c, float logp, float old,
@@ -133,6 +133,10 @@ __device__ __forceinline__ void pair_add(Pair &a, float x) {
   const df s = two_sum(a.hi, x);
   a.hi = s.hi;
   a.lo = __fadd_rn(a.lo, s.lo);
+}
+__device__ __forceinline__ Pair pair_of(uint32_t n) {
+  const float hi = (float)n;
+  return {hi, (float)((long long)n - (long long)hi)};
 }
 __device__ __forceinline__ Pair pair_join(Pair a, Pair b) {
   const df s = two_sum(a.hi, b.hi);
@@ -202,9 +206,10 @@ __device__ __forceinline__ bool grid_join(const Pair (&mine)[K], Pair *total, Pa
 }
 
 // ---------------------------------------------------------------------------
-// Tokens in chunks: a CTA of NT threads takes 4 NT consecutive tokens, 4 per
-// thread, whatever the sequences' lengths.
+// A packed batch's tokens: a warp takes tiles of 128, 4 tokens per lane, and knows
+// the sequence that each tile starts in.
 // ---------------------------------------------------------------------------
+constexpr uint32_t kTile = 128;
 
 // The sequence of token t among lo .. hi - 1: the last one that starts at t or
 // before (so an empty one holds none).
@@ -218,20 +223,37 @@ __device__ __forceinline__ uint32_t sequence_of(const uint64_t *off, uint32_t lo
   return lo;
 }
 // The same by a warp, 32 probes at a time: three rounds for 32,768 sequences.
-__device__ __forceinline__ uint32_t sequence_of_warp(const uint64_t *off, uint32_t n, uint64_t t) {
+__device__ __forceinline__ uint32_t sequence_of_warp(const uint64_t *off, uint32_t lo, uint32_t hi,
+                                                     uint64_t t) {
   const uint32_t lane = threadIdx.x & 31;
-  uint32_t lo = 0, hi = n;
   while (hi - lo > 1) {
     const uint32_t step = (hi - lo + 31) / 32;  // probes lo + step, lo + 2 step, ...
-    const uint32_t at = min((uint64_t)lo + (uint64_t)(lane + 1) * step, (uint64_t)hi);
+    const uint32_t at = (uint32_t)min((uint64_t)lo + (uint64_t)(lane + 1) * step, (uint64_t)hi);
     const bool le = at < hi && off[at] <= t;
     const uint32_t k = __popc(__ballot_sync(kAllLanes, le));  // probes at or before t
-    const uint32_t top = (uint32_t)min((uint64_t)lo + (uint64_t)(k + 1) * step, (uint64_t)hi);
+    hi = (uint32_t)min((uint64_t)lo + (uint64_t)(k + 1) * step, (uint64_t)hi);
     lo += k * step;
-    hi = top;
   }
   return lo;
 }
+
+// A warp's place among the sequences, which only moves on.
+struct SeqWalk {
+  uint32_t q;     // the sequence
+  uint64_t next;  // and where the one after it starts
+  __device__ __forceinline__ void start(const uint64_t *off, uint32_t n, uint64_t t) {
+    q = sequence_of_warp(off, 0, n, t);
+    next = off[q + 1];
+  }
+  // to the sequence of token t: among the next 31 most often
+  __device__ __forceinline__ void to(const uint64_t *off, uint32_t n, uint64_t t) {
+    if (t < next) return;
+    const uint64_t at = (uint64_t)q + 1 + (threadIdx.x & 31);
+    const uint32_t k = __popc(__ballot_sync(kAllLanes, at < n && off[at] <= t));
+    q = k < 32 ? q + k : sequence_of_warp(off, q + 32, n, t);
+    next = off[q + 1];
+  }
+};
 
 // Which of the tokens t .. t + 3 count, as bits; t is a multiple of 4.  first,
 // end: the tokens that the sequences hold.

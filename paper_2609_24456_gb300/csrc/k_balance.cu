@@ -186,8 +186,8 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
     nan |= isnan(inv);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      y[i] *= inv;
-      ps[i] += y[i];
+      y[i] = __fmul_rn(y[i], inv);  // the same sums whether a gradient follows or not
+      ps[i] = __fadd_rn(ps[i], y[i]);
     }
     if (a.dz && in) {
       T *d = reinterpret_cast<T *>(a.dz) + t * a.dstride;

@@ -335,11 +335,18 @@ k_token_logprob_grad(RowArgs a, const float *stats, const float *entropy, const 
                     (uint32_t)a.target[t], g, a.c);
 }
 
+// What row t weighs in the policy loss, found by a warp; 0 outside the sequences.
+__device__ __forceinline__ float row_weight(const RowWeights &w, uint64_t t) {
+  if (w.off && (t < w.off[0] || t >= w.off[w.n_seq])) return 0.f;
+  if (w.sequence) return __ldcg(&w.sequence[sequence_of_warp(w.off, 0, w.n_seq, t)]);
+  return w.tokens ? 1.f / (float)__ldcg(w.tokens) : w.fixed;
+}
+
 // Log-probability, policy gradient and the logits' gradient of a row, by a
-// cluster of gridDim.y CTAs.  weight: the token's, 0 where it is left out.
+// cluster of gridDim.y CTAs.
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowThreads)
-k_policy_rows(RowArgs a, const float *weight, const float *old_logp, const float *ref_logp,
+k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
               const float *adv, PolicyRule rule, float *logp, float *entropy, void *dz,
               uint64_t dstride, Ctrl *ctrl) {
   __shared__ RowSum red[kRowWarps];
@@ -352,12 +359,13 @@ k_policy_rows(RowArgs a, const float *weight, const float *old_logp, const float
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   T *d = reinterpret_cast<T *>(dz) + t * dstride;
-  const float w = weight[t];
+  const Row kind = row_kind(a.target, a.mask, t, a.vocab);
+  const float w = kind == Row::kUse ? row_weight(weights, t) : 0.f;
   if (w == 0.f) {
     if (part == 0 && threadIdx.x == 0) {
       logp[t] = 0.f;
       if (entropy) entropy[t] = 0.f;
-      if (row_kind(a.target, a.mask, t, a.vocab) == Row::kBad)
+      if (kind == Row::kBad)
         flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)a.target[t]);
     }
     part_zero(d + first, n);
@@ -476,12 +484,12 @@ cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float
 }
 
 cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &rule,
-                               const float *weight, const PolicyTokens &p, float *logp,
+                               const RowWeights &w, const PolicyTokens &p, float *logp,
                                float *entropy, void *dz, uint64_t dstride, cudaStream_t s) {
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     auto kern = entropy ? k_policy_rows<T, true> : k_policy_rows<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), true, s, row_args(z), weight, p.old_logp,
+    return launch_rows(kern, z.rows, row_parts(ctx, z), true, s, row_args(z), w, p.old_logp,
                        p.ref_logp, p.adv, rule, logp, entropy, dz, dstride, ctx->ctrl);
   });
 }

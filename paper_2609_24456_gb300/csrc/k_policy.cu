@@ -1,12 +1,13 @@
 // k_policy.cu -- the clipped policy loss over the tokens of a packed batch, with
 // its gradients by the log-probabilities and the entropies.
 //
-// One pass over the tokens (16 to 32 bytes each), in chunks of 4 per thread, so
-// that sequences of any lengths load the CTAs alike.  A token's weight needs the
-// number of tokens that count, in the batch or in its sequence: a pass over the
-// mask (1 byte a token) counts them per chunk first, and a chunk adds up those
-// of the sequences that reach into it from outside.  A batch of one chunk
-// counts for itself and is one launch.
+// One pass over the tokens (16 to 32 bytes each).  Each CTA has a run of them, its
+// warps take tiles of 128 in turn, without barriers, whatever the sequences'
+// lengths.  A token's weight needs the number of tokens that count, in the batch
+// or in its sequence: the mask (1 byte a token) is counted by blocks of 512
+// first, and a warp per sequence makes its weight from the blocks inside it and
+// the bytes at its ends.  A batch of up to 4,096 tokens is one CTA that counts for
+// itself, in one launch.
 #include <cmath>
 
 #include "edp_loss.cuh"
@@ -14,22 +15,21 @@
 namespace edp {
 
 cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &rule,
-                               const float *weight, const PolicyTokens &p, float *logp,
+                               const RowWeights &w, const PolicyTokens &p, float *logp,
                                float *entropy, void *dz, uint64_t dstride, cudaStream_t s);
 
 namespace {
 
-constexpr int kThreads = 512;      // a chunk of 2,048 tokens
+constexpr int kThreads = 512;
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
-constexpr int kSums = 7;  // pg, kl, entropy; ratio, old kl; clipped above, below
+constexpr uint32_t kBlock = 512;     // tokens counted together
+constexpr int kSums = 8;  // pg, kl, entropy; ratio, old kl; clipped above, below; tokens
+constexpr int kFlush = 8;  // tiles (32 tokens a lane) between two additions to the sums
 
 struct Weighting {
-  const uint32_t *chunk;              // tokens that count, per chunk
-  const unsigned long long *tokens;   // and in all
-  bool by_mask;   // SEQ_MEAN: sequences' tokens are counted, not their lengths
-  bool by_total;  // TOKEN_MEAN: the divisor is *tokens
-  float fixed;    // otherwise, but for SEQ_MEAN: every weight
-  float divisor;  // SEQ_MEAN: sequences
+  const float *sequence;             // SEQ_MEAN: each sequence's weight
+  const unsigned long long *tokens;  // TOKEN_MEAN without norm: the divisor
+  float fixed;                       // otherwise: every weight
 };
 
 struct Range {
@@ -46,210 +46,213 @@ __device__ __forceinline__ uint32_t cta_sum(uint32_t v, uint32_t *red) {
   __syncthreads();
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
   __syncthreads();
-  uint32_t x = (threadIdx.x & 31) < NT / 32 ? red[threadIdx.x & 31] : 0;
+  const uint32_t x = (threadIdx.x & 31) < NT / 32 ? red[threadIdx.x & 31] : 0;
   return __reduce_add_sync(kAllLanes, x);
 }
 
-// Tokens that count, per chunk, and their total.
+// Tokens that count in t .. t + 15.
+template <bool VEC>
+__device__ __forceinline__ uint32_t count16(const TokenSet &s, uint64_t t, const Range &r) {
+  if (VEC && s.mask && !s.target && t >= r.first && t + 16 <= r.end) {
+    const uint4 m = *reinterpret_cast<const uint4 *>(s.mask + t);
+    auto some = [](uint32_t x) {  // bytes that are not 0
+      return __popc((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
+    };
+    return some(m.x) + some(m.y) + some(m.z) + some(m.w);
+  }
+  uint32_t n = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) n += __popc(token_bits<VEC>(s, t + 4 * k, r.first, r.end));
+  return n;
+}
+
+// Tokens that count, by blocks (a warp each) or in all.
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads)
-k_token_counts(TokenSet s, uint32_t *chunk, unsigned long long *total) {
+k_token_counts(TokenSet s, uint32_t *block, unsigned long long *total) {
   __shared__ uint32_t red[kThreads / 32];
   pdl_wait();
   pdl_launch();
   const Range r = token_range(s);
+  const int lane = threadIdx.x & 31;
+  const uint64_t step = (uint64_t)gridDim.x * (kThreads / 32);
   uint32_t sum = 0;
-  for (uint64_t c = blockIdx.x; c * 4 * kThreads < s.n; c += gridDim.x) {
-    const uint32_t bits = token_bits<VEC>(s, (c * kThreads + threadIdx.x) * 4, r.first, r.end);
-    if (chunk) {
-      const uint32_t n = cta_sum<kThreads>(__popc(bits), red);
-      if (threadIdx.x == 0) chunk[c] = n;
-    } else {
-      sum += __popc(bits);
+  for (uint64_t b = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+       b * kBlock < s.n; b += step) {
+    const uint32_t n = count16<VEC>(s, b * kBlock + 16 * lane, r);
+    if (block) {
+      const uint32_t all = __reduce_add_sync(kAllLanes, n);
+      if (lane == 0) block[b] = all;
     }
+    sum += n;
   }
-  if (chunk) return;
+  if (block) return;
   sum = cta_sum<kThreads>(sum, red);
   if (threadIdx.x == 0 && sum) atomicAdd(total, (unsigned long long)sum);
 }
 
-// Weights of a chunk's tokens, where each sequence has its own.
-template <int NT>
-struct ChunkWeights {
-  uint32_t pre[NT];   // tokens that count before a thread's, shifted by 4, and its bits
-  uint32_t red[NT / 32];
-  uint32_t lo, hi;    // the sequences of the chunk's first and last token
-  uint32_t before, after;  // tokens of lo before the chunk, of hi after it
+// Tokens that count among [a, b), below a block's worth, by a warp.
+__device__ __forceinline__ uint32_t count_few(const TokenSet &s, uint64_t a, uint64_t b) {
+  uint32_t n = 0;
+#pragma unroll 4
+  for (uint64_t t = a + (threadIdx.x & 31); t < b; t += 32)
+    n += (!s.mask || s.mask[t]) && (!s.target || (uint32_t)s.target[t] < s.vocab);
+  return n;
+}
 
-  // tokens that count among the chunk's first x
+// Each sequence's weight, 1 / (divisor tokens); block: NULL where every token counts.
+__global__ void __launch_bounds__(kThreads)
+k_sequence_weights(TokenSet s, const uint32_t *block, float divisor, float *weight) {
+  pdl_wait();
+  pdl_launch();
+  const int lane = threadIdx.x & 31;
+  const uint64_t step = (uint64_t)gridDim.x * (kThreads / 32);
+  for (uint64_t q = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); q < s.n_seq;
+       q += step) {
+    const uint64_t a = s.off[q], b = min(s.off[q + 1], s.n);
+    uint64_t n = b > a ? b - a : 0;
+    if (block && n) {
+      const uint64_t ka = (a + kBlock - 1) / kBlock, kb = b / kBlock;  // whole blocks
+      uint32_t some = 0;
+      if (ka >= kb) {
+        some = count_few(s, a, b);
+      } else {
+        for (uint64_t k = ka + lane; k < kb; k += 32) some += __ldcg(&block[k]);
+        some += count_few(s, a, ka * kBlock) + count_few(s, kb * kBlock, b);
+      }
+      n = __reduce_add_sync(kAllLanes, some);
+    }
+    if (lane == 0) weight[q] = n ? 1.f / (divisor * (float)n) : 0.f;
+  }
+}
+
+// Sequences' counts in a batch of one CTA: a prefix over its tokens.
+template <int NT>
+struct OneCta {
+  uint32_t pre[NT];  // tokens that count before a thread's, shifted by 4, and its bits
+  uint32_t red[NT / 32];
+
+  // tokens that count among the first x
   __device__ __forceinline__ uint32_t upto(uint32_t x) const {
     if (x >= 4u * NT) return (pre[NT - 1] >> 4) + __popc(pre[NT - 1] & 15u);
     const uint32_t p = pre[x >> 2];
     return (p >> 4) + __popc(p & ((1u << (x & 3u)) - 1u));
   }
-
-  template <bool VEC>
-  __device__ __forceinline__ void fill(const TokenSet &s, const Weighting &w, const Range &r,
-                                       uint64_t t0, uint32_t bits) {
+  __device__ __forceinline__ void fill(uint32_t bits) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    constexpr uint64_t C = 4ull * NT;
-    __syncthreads();  // the chunk before is done with
-    if (wid < 2) {
-      const uint64_t t = wid == 0 ? t0 : min(t0 + C, r.end) - 1;
-      const uint32_t q = sequence_of_warp(s.off, (uint32_t)s.n_seq, t);
-      if (lane == 0) (wid == 0 ? lo : hi) = q;
-    }
-    if (w.by_mask) {
-      uint32_t n = __popc(bits), incl = n;
+    const uint32_t n = __popc(bits);
+    uint32_t incl = n;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(kAllLanes, incl, o);
-        if (lane >= o) incl += y;
-      }
-      if (lane == 31) red[wid] = incl;
-      __syncthreads();
-      const uint32_t x = lane < wid ? red[lane] : 0;
-      pre[threadIdx.x] = ((__reduce_add_sync(kAllLanes, x) + incl - n) << 4) | bits;
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(kAllLanes, incl, o);
+      if (lane >= o) incl += y;
     }
+    if (lane == 31) red[wid] = incl;
     __syncthreads();
-    if (!w.by_mask) return;
-    // of the sequence that comes in from the left and of the one that goes on to
-    // the right: the chunks that they fill, and the part of the one at their end
-    const uint64_t a = s.off[lo], b = min(s.off[hi + 1], r.end);
-    uint32_t left = 0, right = 0;
-    const uint64_t c = t0 / C;
-    if (a < t0) {
-      const uint64_t ca = a / C;
-      for (uint64_t k = ca + 1 + threadIdx.x; k < c; k += NT) left += __ldcg(&w.chunk[k]);
-      left += __popc(token_bits<VEC>(s, ca * C + 4 * threadIdx.x, max(a, r.first), r.end));
-    }
-    if (b > t0 + C) {
-      const uint64_t cb = (b - 1) / C;
-      for (uint64_t k = c + 1 + threadIdx.x; k < cb; k += NT) right += __ldcg(&w.chunk[k]);
-      right += __popc(token_bits<VEC>(s, cb * C + 4 * threadIdx.x, r.first, b));
-    }
-    left = __reduce_add_sync(kAllLanes, left);
-    right = __reduce_add_sync(kAllLanes, right);
-    if (threadIdx.x == 0) before = after = 0;
+    const uint32_t x = lane < wid ? red[lane] : 0;
+    pre[threadIdx.x] = ((__reduce_add_sync(kAllLanes, x) + incl - n) << 4) | bits;
     __syncthreads();
-    if (lane == 0 && left) atomicAdd(&before, left);
-    if (lane == 0 && right) atomicAdd(&after, right);
-    __syncthreads();
-  }
-
-  // weights of a thread's tokens t .. t + 3
-  __device__ __forceinline__ void get(const TokenSet &s, const Weighting &w, const Range &r,
-                                      uint64_t t0, uint64_t t, uint32_t bits, float (&out)[4]) {
-    constexpr uint64_t C = 4ull * NT;
-    uint32_t q = 0;
-    uint64_t end = 0;
-    float each = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      out[i] = 0.f;
-      if (!(bits >> i & 1u)) continue;
-      if (t + i >= end) {
-        q = sequence_of(s.off, end ? q : lo, hi + 1, t + i);
-        const uint64_t a = s.off[q];
-        end = min(s.off[q + 1], r.end);
-        uint64_t n = end - a;
-        if (w.by_mask) {
-          n = upto((uint32_t)(end - t0 < C ? end - t0 : C)) - upto(a > t0 ? (uint32_t)(a - t0) : 0u);
-          if (a < t0) n += before;
-          if (end > t0 + C) n += after;
-        }
-        each = 1.f / (w.divisor * (float)n);
-      }
-      out[i] = each;
-    }
   }
 };
 
-enum class Weights { kFixed, kSequence, kGiven };
-
-// What the tokens weigh where all weigh the same; n: those of the one chunk, if
-// there is only one.
-__device__ __forceinline__ float same_weight(const Weighting &w, uint32_t n, bool one) {
-  if (!w.by_total) return w.fixed;
-  const unsigned long long k = one ? n : __ldcg(w.tokens);
-  return 1.f / (float)k;
-}
-
-// The weights alone, for the form from logits.
-template <bool VEC>
-__global__ void __launch_bounds__(kThreads)
-k_token_weights(TokenSet s, Weighting w, bool sequences, float *out) {
-  __shared__ ChunkWeights<kThreads> cw;
-  pdl_wait();
-  pdl_launch();
-  const Range r = token_range(s);
-  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * kThreads; t0 < s.n;
-       t0 += (uint64_t)gridDim.x * 4 * kThreads) {
-    const uint64_t t = t0 + 4 * threadIdx.x;
-    const uint32_t bits = token_bits<VEC>(s, t, r.first, r.end);
-    float v[4] = {};
-    if (sequences) {
-      if (t0 < r.end) {
-        cw.fill<VEC>(s, w, r, t0, bits);
-        cw.get(s, w, r, t0, t, bits, v);
-      }
-    } else {
-      const bool one = s.n <= 4 * kThreads;
-      const float f = same_weight(w, one ? cta_sum<kThreads>(__popc(bits), cw.red) : 0u, one);
+// What the tokens of a lane, t .. t + 3, weigh.  q0, q1: the sequences of the tile's
+// first and last token.
+template <typename F>
+__device__ __forceinline__ void sequence_weights(const TokenSet &s, uint64_t end, uint64_t t,
+                                                 uint32_t bits, uint32_t q0, uint32_t q1, F of,
+                                                 float (&w)[4]) {
+  uint32_t q = q0;
+  uint64_t next = 0;
+  float each = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = bits >> i & 1u ? f : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    w[i] = 0.f;
+    if (!(bits >> i & 1u)) continue;
+    if (t + i >= next) {
+      q = sequence_of(s.off, q, q1 + 1, t + i);
+      next = s.off[q + 1];
+      each = of(q, s.off[q], min(next, end));
     }
-    store4<VEC>(out, t, s.n, make_float4(v[0], v[1], v[2], v[3]));
+    w[i] = each;
   }
 }
 
-// The policy loss of every token, its gradients and the batch's sums.
-template <int NT, Weights W, bool VEC>
+// The policy loss of every token, its gradients and the batch's sums.  SEQ: a weight
+// for each sequence.  NT == kSmallThreads: one CTA, which counts for itself.
+template <int NT, bool SEQ, bool VEC>
 __global__ void __launch_bounds__(NT, 1536 / NT)
-k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, const float *given, float *loss,
+k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor, float *loss,
          float *dlogp, float *dentropy, Pair *part, Ctrl *ctrl) {
-  __shared__ ChunkWeights<W == Weights::kSequence ? NT : 32> cw;
-  __shared__ uint32_t red[NT / 32];
-  __shared__ Pair total[kSums + 1];
+  constexpr bool kOne = NT == kSmallThreads;
+  constexpr uint32_t kWarps = NT / 32;
+  __shared__ OneCta<kOne ? NT : 32> one;
+  __shared__ Pair total[kSums];
   pdl_wait();
-  Pair sum[kSums + 1];
-#pragma unroll
-  for (int k = 0; k <= kSums; ++k) sum[k] = Pair{0.f, 0.f};
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Range r = token_range(s);
-  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * NT; t0 < s.n;
-       t0 += (uint64_t)gridDim.x * 4 * NT) {
-    const uint64_t t = t0 + 4 * threadIdx.x;
+  float fixed = w.fixed;
+  if (!kOne && !SEQ && w.tokens) fixed = 1.f / (float)__ldcg(w.tokens);
+  Pair sum[kSums];
+#pragma unroll
+  for (int k = 0; k < kSums; ++k) sum[k] = Pair{0.f, 0.f};
+  float add[5] = {};
+  uint32_t above = 0, below = 0, tokens = 0;
+  auto flush = [&] {
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      pair_add(sum[k], add[k]);
+      add[k] = 0.f;
+    }
+  };
+  // the CTA's tiles, in turn by its warps
+  const uint64_t tiles = (s.n + kTile - 1) / kTile;
+  const uint64_t each = (tiles + gridDim.x - 1) / gridDim.x;
+  const uint64_t last = min(tiles, (blockIdx.x + 1) * each);
+  SeqWalk walk;
+  bool walking = false;
+  int kept = 0;
+  for (uint64_t tile = blockIdx.x * each + wid; tile < (kOne ? (uint64_t)kWarps : last);
+       tile += kWarps) {
+    const uint64_t t0 = tile * kTile, t = t0 + 4 * lane;
     const float4 lp = load4<VEC>(p.logp, t, s.n), od = load4<VEC>(p.old_logp, t, s.n);
     const float4 ad = load4<VEC>(p.adv, t, s.n);
     float4 rf = make_float4(0.f, 0.f, 0.f, 0.f), en = rf;
     if (p.ref_logp) rf = load4<VEC>(p.ref_logp, t, s.n);
     if (p.entropy) en = load4<VEC>(p.entropy, t, s.n);
-    uint32_t bits;
+    const uint32_t bits = token_bits<VEC>(s, t, r.first, r.end);
     float wt[4];
-    if (W == Weights::kGiven) {
-      const float4 g = load4<VEC>(given, t, s.n);
-      wt[0] = g.x, wt[1] = g.y, wt[2] = g.z, wt[3] = g.w;
-      bits = (g.x != 0.f) | (g.y != 0.f) << 1 | (g.z != 0.f) << 2 | (g.w != 0.f) << 3;
-    } else {
-      bits = token_bits<VEC>(s, t, r.first, r.end);
-      if (W == Weights::kSequence) {
-        wt[0] = wt[1] = wt[2] = wt[3] = 0.f;
-        if (t0 < r.end) {
-          cw.template fill<VEC>(s, w, r, t0, bits);
-          cw.get(s, w, r, t0, t, bits, wt);
+    if (kOne && SEQ) {
+      one.fill(bits);
+      sequence_weights(s, r.end, t, bits, 0, (uint32_t)s.n_seq - 1,
+                       [&](uint32_t, uint64_t a, uint64_t b) {
+                         return 1.f / (divisor * (float)(one.upto((uint32_t)b) -
+                                                         one.upto((uint32_t)a)));
+                       }, wt);
+    } else if (SEQ) {
+      wt[0] = wt[1] = wt[2] = wt[3] = 0.f;
+      if (t0 < r.end) {
+        const uint32_t n = (uint32_t)s.n_seq;
+        if (walking) walk.to(s.off, n, t0);
+        else walk.start(s.off, n, t0);
+        walking = true;
+        if (t0 + kTile <= walk.next) {
+          wt[0] = wt[1] = wt[2] = wt[3] = __ldcg(&w.sequence[walk.q]);
+        } else {
+          SeqWalk ahead = walk;
+          ahead.to(s.off, n, min(t0 + kTile, r.end) - 1);
+          sequence_weights(s, r.end, t, bits, walk.q, ahead.q,
+                           [&](uint32_t q, uint64_t, uint64_t) { return __ldcg(&w.sequence[q]); },
+                           wt);
         }
-      } else {
-        const bool one = NT == kSmallThreads;
-        const float f = same_weight(w, one && w.by_total ? cta_sum<NT>(__popc(bits), red) : 0u,
-                                    one);
-        wt[0] = wt[1] = wt[2] = wt[3] = f;
       }
+    } else {
+      if (kOne && w.tokens) fixed = 1.f / (float)cta_sum<NT>(__popc(bits), one.red);
+      wt[0] = wt[1] = wt[2] = wt[3] = fixed;
     }
     const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, o4[4] = {od.x, od.y, od.z, od.w};
     const float a4[4] = {ad.x, ad.y, ad.z, ad.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
     const float e4[4] = {en.x, en.y, en.z, en.w};
-    float g4[4], h4[4], add[5] = {};
-    uint32_t above = 0, below = 0;
+    float g4[4], h4[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       g4[i] = h4[i] = 0.f;
@@ -267,18 +270,22 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, const float *
       above += o.above;
       below += o.below;
     }
-#pragma unroll
-    for (int k = 0; k < 5; ++k) pair_add(sum[k], add[k]);
-    pair_add(sum[5], (float)above);
-    pair_add(sum[6], (float)below);
-    pair_add(sum[7], (float)__popc(bits));
+    tokens += __popc(bits);
+    if (++kept == kFlush) {
+      flush();
+      kept = 0;
+    }
     if (dlogp) store4<VEC>(dlogp, t, s.n, make_float4(g4[0], g4[1], g4[2], g4[3]));
     if (dentropy) store4<VEC>(dentropy, t, s.n, make_float4(h4[0], h4[1], h4[2], h4[3]));
   }
-  if (!grid_join<NT, kSums + 1>(sum, total, part, &ctrl->loss_ticket)) return;
+  flush();
+  sum[5] = pair_of(above);
+  sum[6] = pair_of(below);
+  sum[7] = pair_of(tokens);
+  if (!grid_join<NT, kSums>(sum, total, part, &ctrl->loss_ticket)) return;
   if (threadIdx.x == 0) {
-    double v[kSums + 1];
-    for (int k = 0; k <= kSums; ++k) v[k] = pair_value(total[k]);
+    double v[kSums];
+    for (int k = 0; k < kSums; ++k) v[k] = pair_value(total[k]);
     const double n = v[7] > 0.0 ? v[7] : 1.0;
     loss[0] = (float)(v[0] + (rule.kl_coef != 0.f ? (double)rule.kl_coef * v[1] : 0.0) -
                       (rule.entropy_coef != 0.f ? (double)rule.entropy_coef * v[2] : 0.0));
@@ -313,71 +320,80 @@ bool aligned_to(uintptr_t bytes, P... p) {
   return (((uintptr_t)p | ...) & (bytes - 1)) == 0;
 }
 
-// Chunks, at most `per_sm` CTAs per SM.
-unsigned chunk_grid(const edp_ctx *c, uint64_t n, int threads, unsigned per_sm) {
-  const uint64_t chunks = (n + 4ull * threads - 1) / (4ull * threads);
-  const uint64_t most = (uint64_t)per_sm * (uint64_t)c->coop_sms;
-  return (unsigned)(chunks < most ? chunks : most);
+unsigned at_most(uint64_t want, uint64_t most) {
+  return (unsigned)(want < 1 ? 1 : want < most ? want : most);
 }
 
 // The scratch of a call and what it is for.
 struct Plan {
   Weighting w;
-  bool sequences, counts, vec;
+  float divisor;
+  bool sequences;
   Pair *part;
-  uint32_t *chunk;
-  float *weight, *entropy;
+  float *entropy;
 };
 
-cudaError_t make_plan(edp_ctx *c, const TokenSet &set, bool vec, bool one_chunk, bool weights,
-                      bool entropy, cudaStream_t s, Plan *p) {
-  p->vec = vec;
+// Counts what the weights need, unless the batch's own CTA does (one_cta).
+cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool entropy,
+                         cudaStream_t s, Plan *p) {
+  const uint64_t sms = (uint64_t)c->coop_sms;
   p->sequences = set.reduce == EDP_REDUCE_SEQ_MEAN;
-  const bool chosen = set.mask || set.target;
+  p->divisor = (float)(set.norm > 0.0 ? set.norm : (double)set.n_seq);
+  const bool by_total = set.reduce == EDP_REDUCE_TOKEN_MEAN && !(set.norm > 0.0);
   p->w = Weighting{};
-  p->w.by_mask = p->sequences && chosen;
-  p->w.by_total = set.reduce == EDP_REDUCE_TOKEN_MEAN && !(set.norm > 0.0);
-  p->w.divisor = (float)(set.norm > 0.0 ? set.norm : (double)set.n_seq);
-  p->w.fixed = set.reduce == EDP_REDUCE_TOKEN_MEAN ? (float)(1.0 / set.norm)
-                                                   : 1.f / p->w.divisor;
-  p->counts = !one_chunk && (p->w.by_mask || p->w.by_total);
-  const size_t part = ((size_t)(kSums + 1) * 3 * c->coop_sms * sizeof(Pair) + 15) & ~(size_t)15;
-  const uint64_t chunks = (set.n + 4 * kThreads - 1) / (4 * kThreads);
-  const size_t chunk = p->w.by_mask ? (chunks * sizeof(uint32_t) + 15) & ~(size_t)15 : 0;
-  const size_t row = (set.n * sizeof(float) + 15) & ~(size_t)15;
+  p->w.fixed = 1.f / p->divisor;
+  const bool blocks = p->sequences && (set.mask || set.target) && !one_cta;
+  size_t at = 0;
+  auto take = [&](bool want, uint64_t bytes) {
+    const size_t a = at;
+    if (want) at += (bytes + 15) & ~(size_t)15;
+    return a;
+  };
+  const size_t part = take(true, kSums * 3 * sms * sizeof(Pair));
+  const size_t weight = take(p->sequences && !one_cta, set.n_seq * sizeof(float));
+  const size_t block = take(blocks, (set.n + kBlock - 1) / kBlock * sizeof(uint32_t));
+  const size_t ent = take(entropy, set.n * sizeof(float));
   void *blk = nullptr;
-  const cudaError_t e =
-      ctx_scratch(c, part + chunk + row * ((size_t)weights + (size_t)entropy), s, &blk);
+  cudaError_t e = ctx_scratch(c, at, s, &blk);
   if (e != cudaSuccess) return e;
   uint8_t *b = (uint8_t *)blk;
-  p->part = (Pair *)b;
-  p->chunk = p->w.by_mask ? (uint32_t *)(b + part) : nullptr;
-  p->weight = (float *)(b + part + chunk);
-  p->entropy = (float *)(b + part + chunk + (weights ? row : 0));
-  p->w.chunk = p->chunk;
-  p->w.tokens = &c->ctrl->loss_tokens;
-  return cudaSuccess;
-}
-
-cudaError_t launch_counts(edp_ctx *c, const TokenSet &set, const Plan &p, cudaStream_t s) {
-  if (!p.counts) return cudaSuccess;
-  auto kern = p.vec ? k_token_counts<true> : k_token_counts<false>;
-  return launch_pdl(kern, dim3(chunk_grid(c, set.n, kThreads, 4)), dim3(kThreads), s, set, p.chunk,
-                    &c->ctrl->loss_tokens);
-}
-
-template <Weights W>
-cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t,
-                          const PolicyRule &rule, const Plan &p, bool small, const float *given,
-                          float *loss, float *dlogp, float *dentropy, cudaStream_t s) {
-  if (small) {
-    auto kern = p.vec ? k_policy<kSmallThreads, W, true> : k_policy<kSmallThreads, W, false>;
-    return launch_pdl(kern, dim3(1), dim3(kSmallThreads), s, set, t, rule, p.w, given, loss, dlogp,
-                      dentropy, p.part, c->ctrl);
+  p->part = (Pair *)(b + part);
+  p->entropy = (float *)(b + ent);
+  if (by_total) p->w.tokens = &c->ctrl->loss_tokens;
+  if (one_cta) return cudaSuccess;
+  const unsigned warps = kThreads / 32;
+  if (blocks || by_total) {
+    auto kern = aligned_to(16, set.mask) ? k_token_counts<true> : k_token_counts<false>;
+    const uint64_t want = (set.n + kBlock * warps - 1) / (kBlock * warps);
+    e = launch_pdl(kern, dim3(at_most(want, 4 * sms)), dim3(kThreads), s, set,
+                   blocks ? (uint32_t *)(b + block) : nullptr, &c->ctrl->loss_tokens);
+    if (e != cudaSuccess) return e;
   }
-  auto kern = p.vec ? k_policy<kThreads, W, true> : k_policy<kThreads, W, false>;
-  return launch_pdl(kern, dim3(chunk_grid(c, set.n, kThreads, 3)), dim3(kThreads), s, set, t, rule,
-                    p.w, given, loss, dlogp, dentropy, p.part, c->ctrl);
+  if (p->sequences) {
+    p->w.sequence = (float *)(b + weight);
+    e = launch_pdl(k_sequence_weights, dim3(at_most((set.n_seq + warps - 1) / warps, 4 * sms)),
+                   dim3(kThreads), s, set,
+                   blocks ? (const uint32_t *)(b + block) : nullptr, p->divisor,
+                   (float *)(b + weight));
+  }
+  return e;
+}
+
+template <bool VEC>
+cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t,
+                          const PolicyRule &rule, const Plan &p, bool one_cta, float *loss,
+                          float *dlogp, float *dentropy, cudaStream_t s) {
+  auto go = [&](auto kern, unsigned grid, int threads) {
+    return launch_pdl(kern, dim3(grid), dim3(threads), s, set, t, rule, p.w, p.divisor, loss,
+                      dlogp, dentropy, p.part, c->ctrl);
+  };
+  if (one_cta)
+    return p.sequences ? go(k_policy<kSmallThreads, true, VEC>, 1, kSmallThreads)
+                       : go(k_policy<kSmallThreads, false, VEC>, 1, kSmallThreads);
+  const uint64_t want = (set.n + 4 * kThreads - 1) / (4 * kThreads);
+  const unsigned grid = at_most(want, 3ull * (uint64_t)c->coop_sms);
+  return p.sequences ? go(k_policy<kThreads, true, VEC>, grid, kThreads)
+                     : go(k_policy<kThreads, false, VEC>, grid, kThreads);
 }
 
 }  // namespace
@@ -385,46 +401,38 @@ cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t
 cudaError_t launch_policy_loss(edp_ctx *c, const edp_policy_config &cfg, const TokenSet &set,
                                const PolicyTokens &t, float *loss, float *dlogp,
                                float *dentropy, cudaStream_t s) {
+  const bool one_cta = set.n <= 4 * kSmallThreads;
+  Plan p;
+  const cudaError_t e = plan_weights(c, set, one_cta, false, s, &p);
+  if (e != cudaSuccess) return e;
   const bool vec = aligned_to(16, t.logp, t.old_logp, t.ref_logp, t.adv, t.entropy, dlogp,
                               dentropy) && aligned_to(4, set.mask);
-  const bool small = set.n <= 4 * kSmallThreads;
-  Plan p;
-  cudaError_t e = make_plan(c, set, vec, small, false, false, s, &p);
-  if (e != cudaSuccess) return e;
-  e = launch_counts(c, set, p, s);
-  if (e != cudaSuccess) return e;
   const PolicyRule rule = policy_rule(cfg);
-  return p.sequences ? launch_policy<Weights::kSequence>(c, set, t, rule, p, small, nullptr, loss,
-                                                         dlogp, dentropy, s)
-                     : launch_policy<Weights::kFixed>(c, set, t, rule, p, small, nullptr, loss,
-                                                      dlogp, dentropy, s);
+  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, loss, dlogp, dentropy, s)
+             : launch_policy<false>(c, set, t, rule, p, one_cta, loss, dlogp, dentropy, s);
 }
 
 cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
                                       const TokenSet &set, const PolicyTokens &t,
                                       const Logits &z, float *loss, float *logp, float *entropy,
                                       void *dz, uint64_t dstride, cudaStream_t s) {
-  const bool vec = aligned_to(16, t.old_logp, t.ref_logp, t.adv, logp, entropy) &&
-                   aligned_to(4, set.mask);
   const bool own_entropy = !entropy && cfg.entropy_coef > 0.0;
   Plan p;
-  cudaError_t e = make_plan(c, set, vec, set.n <= 4 * kThreads, true, own_entropy, s, &p);
+  cudaError_t e = plan_weights(c, set, false, own_entropy, s, &p);
   if (e != cudaSuccess) return e;
   if (own_entropy) entropy = p.entropy;
-  e = launch_counts(c, set, p, s);
-  if (e != cudaSuccess) return e;
-  auto kern = vec ? k_token_weights<true> : k_token_weights<false>;
-  e = launch_pdl(kern, dim3(chunk_grid(c, set.n, kThreads, 3)), dim3(kThreads), s, set, p.w,
-                 p.sequences, p.weight);
-  if (e != cudaSuccess) return e;
   const PolicyRule rule = policy_rule(cfg);
-  e = launch_policy_rows(c, z, rule, p.weight, t, logp, entropy, dz, dstride, s);
+  const RowWeights w{set.off, (uint32_t)set.n_seq, p.w.sequence, p.w.tokens, p.w.fixed};
+  e = launch_policy_rows(c, z, rule, w, t, logp, entropy, dz, dstride, s);
   if (e != cudaSuccess) return e;
   PolicyTokens q = t;
   q.logp = logp;
   q.entropy = entropy;
-  return launch_policy<Weights::kGiven>(c, set, q, rule, p, set.n <= 4 * kSmallThreads, p.weight,
-                                        loss, nullptr, nullptr, s);
+  const bool one_cta = set.n <= 4 * kSmallThreads;
+  const bool vec = aligned_to(16, t.old_logp, t.ref_logp, t.adv, logp, entropy) &&
+                   aligned_to(4, set.mask);
+  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, loss, nullptr, nullptr, s)
+             : launch_policy<false>(c, set, q, rule, p, one_cta, loss, nullptr, nullptr, s);
 }
 
 }  // namespace edp

@@ -3,22 +3,24 @@
 //
 // Three steps, since a token's gradient needs its pair's whole sequences: the
 // sums of logp - ref by sequence (9 bytes a token), the pairs, and the gradient
-// (1 byte read, 4 written).  The sums go by chunks of 4 tokens per thread: a
-// segmented scan gives every sequence's part of a chunk, and whoever wants a
-// sequence's sum adds its parts in order.  A sequence's gradients from its
-// pairs add up as whole numbers, in any order to the same bits.  A batch of one
-// chunk takes all three steps in one CTA.
+// (1 byte read, 4 written).  For the sums each warp has a run of tokens: within
+// a sequence its lanes add on their own; where sequences end in a tile, a
+// segmented scan gives each one's part of the run.  Whoever wants a sequence's
+// sum adds its parts in order.  A sequence's gradients from its pairs add up as
+// whole numbers, in any order to the same bits.  A batch of up to 4,096 tokens
+// takes all three steps in one CTA.
 #include "edp_loss.cuh"
 
 namespace edp {
 namespace {
 
-constexpr int kThreads = 512;        // a chunk of 2,048 tokens
+constexpr int kThreads = 512;
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
 constexpr int kPairThreads = 256;
 constexpr uint32_t kSmallPairs = 4096;
+constexpr uint32_t kLeastRun = 512;  // tokens of a warp
 
-// A sequence's part of a chunk.
+// A sequence's part of a run.
 struct alignas(16) SeqPart {
   float hi, lo;
   uint32_t n, pad;
@@ -30,11 +32,12 @@ struct SeqGrad {
 };
 
 struct PrefScratch {
-  SeqPart *inner;  // [n_seq] the part in the chunk where the sequence starts
-  SeqPart *head;   // [chunks] the part of the sequence that comes in from the left
+  SeqPart *inner;  // [n_seq] the part in the run where the sequence starts
+  SeqPart *head;   // [runs] the part of the sequence that comes in from the left
   SeqGrad *grad;   // [n_seq]
   uint32_t *bad;   // [n_seq] a gradient is not a finite number below 2^22
   Pair *part;
+  uint32_t run;    // tokens per warp, a multiple of a tile's
 };
 
 struct PrefRule {
@@ -61,118 +64,115 @@ __device__ __forceinline__ Run run_up(Run a, int o) {
   return {{__shfl_up_sync(kAllLanes, a.v.hi, o), __shfl_up_sync(kAllLanes, a.v.lo, o)},
           __shfl_up_sync(kAllLanes, a.n, o)};
 }
+__device__ __forceinline__ void run_add(Run &r, float lp, float ref) {
+  pair_add(r.v, lp);
+  pair_add(r.v, -ref);
+  ++r.n;
+}
 
-template <int NT>
-struct PrefShared {
-  uint32_t lo, hi;
-  Run warp[NT / 32];
-  uint32_t cut[NT / 32];
-};
-
-// Parts of the sequences in the chunk at t0 (which is below the last one's end).
-template <int NT, bool VEC>
-__device__ __forceinline__ void chunk_parts(const PrefIn &in, const PrefScratch &x, uint64_t t0,
-                                            uint64_t first, uint64_t end, PrefShared<NT> &sh) {
+// Parts of the sequences in tokens [begin, stop) of a warp; [first, end) are those
+// that the sequences hold.
+template <bool VEC>
+__device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x, uint64_t begin,
+                                          uint64_t stop, uint64_t first, uint64_t end) {
   const TokenSet &s = in.s;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  constexpr uint64_t C = 4ull * NT;
-  const uint64_t t = t0 + 4 * threadIdx.x, stop = min(t0 + C, end);
-  const float4 lp = load4<VEC>(in.logp, t, s.n);
-  float4 rf = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (in.ref) rf = load4<VEC>(in.ref, t, s.n);
-  const uint32_t bits = token_bits<VEC>(s, t, first, end);
-  __syncthreads();  // the chunk before is done with
-  if (wid < 2) {
-    const uint32_t q = sequence_of_warp(s.off, (uint32_t)s.n_seq, wid == 0 ? t0 : stop - 1);
-    if (lane == 0) (wid == 0 ? sh.lo : sh.hi) = q;
-  }
-  __syncthreads();
-  const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
-
-  // the runs of a thread's tokens: what its first run adds to the one before,
-  // whole runs in between, and the run that is open at its end
-  Run open{{0.f, 0.f}, 0}, closed = open;
-  uint32_t q = 0, closed_q = 0;
-  uint64_t qend = 0;
-  bool cut = false, pending = false;  // a run ended here; the first of them did, unwritten
-  auto emit = [&](uint32_t seq, const Run &r) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t n_seq = (uint32_t)s.n_seq;
+  stop = min(stop, end);
+  if (begin >= stop) return;
+  auto emit = [&](uint32_t q, const Run &r) {
     const SeqPart p{r.v.hi, r.v.lo, r.n, 0};
-    if (s.off[seq] >= t0) {
-      x.inner[seq] = p;
-      x.grad[seq] = SeqGrad{0, 0};
-      x.bad[seq] = 0;
+    if (s.off[q] >= begin) {
+      x.inner[q] = p;
+      x.grad[q] = SeqGrad{0, 0};
+      x.bad[q] = 0;
     } else {
-      x.head[t0 / C] = p;
+      x.head[begin / x.run] = p;
     }
   };
+  const Run none{{0.f, 0.f}, 0};
+  Run mine = none;  // a lane's share of the sequence that is open
+  SeqWalk walk;
+  walk.start(s.off, n_seq, begin);
+  for (uint64_t t0 = begin; t0 < stop; t0 += kTile) {
+    const uint64_t t = t0 + 4 * lane;
+    const float4 lp = load4<VEC>(in.logp, t, s.n);
+    float4 rf = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in.ref) rf = load4<VEC>(in.ref, t, s.n);
+    const uint32_t bits = token_bits<VEC>(s, t, first, stop);
+    const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
+    if (t0 + kTile < walk.next && t0 + kTile < stop) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (t + i >= stop || t + i < first) continue;
-    if (t + i >= qend) {
-      q = sequence_of(s.off, qend ? q : sh.lo, sh.hi + 1, t + i);
-      qend = min(s.off[q + 1], end);
+      for (int i = 0; i < 4; ++i)
+        if (bits >> i & 1u) run_add(mine, l4[i], r4[i]);
+      continue;
     }
-    if (bits >> i & 1u) {
-      pair_add(open.v, l4[i]);
-      pair_add(open.v, -r4[i]);
-      ++open.n;
-    }
-    if (t + i + 1 == qend || t + i + 1 == stop) {  // the run ends with this token
-      if (!cut && s.off[q] < t) {  // it may have begun in another thread
-        closed = open;
-        closed_q = q;
-        pending = true;
-      } else {
-        emit(q, open);
+    // sequences end in this tile, or the run does
+    SeqWalk ahead = walk;
+    ahead.to(s.off, n_seq, min(t0 + kTile, stop) - 1);
+    Run carry{warp_join(mine.v), __reduce_add_sync(kAllLanes, mine.n)};
+    mine = none;
+    Run open = none, closed = none;
+    uint32_t q = walk.q, closed_q = 0;
+    uint64_t next = 0;
+    bool cut = false, pending = false;  // one ended here; its start is in another lane's tokens
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (t + i >= stop || t + i < first) continue;
+      if (t + i >= next) {
+        q = sequence_of(s.off, q, ahead.q + 1, t + i);
+        next = min(s.off[q + 1], end);
       }
-      cut = true;
-      open = Run{{0.f, 0.f}, 0};
+      if (bits >> i & 1u) run_add(open, l4[i], r4[i]);
+      if (t + i + 1 == next || t + i + 1 == stop) {
+        if (!cut && s.off[q] < t) {
+          closed = open;
+          closed_q = q;
+          pending = true;
+        } else {
+          emit(q, open);
+        }
+        cut = true;
+        open = none;
+      }
     }
-  }
-  // what comes into each thread from those before it in the chunk
-  Run incl = open;
-  bool c = cut;
+    // what comes into each lane from those before it, since the last end
+    Run incl = open;
+    bool c = cut;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const Run y = run_up(incl, o);
-    const bool yc = __shfl_up_sync(kAllLanes, c, o);
-    if (lane >= o && !c) {
-      incl = run_join(y, incl);
-      c = yc;
+    for (int o = 1; o < 32; o <<= 1) {
+      const Run y = run_up(incl, o);
+      const bool yc = __shfl_up_sync(kAllLanes, c, o);
+      if (lane >= o && !c) {
+        incl = run_join(y, incl);
+        c = yc;
+      }
     }
-  }
-  if (lane == 31) {
-    sh.warp[wid] = incl;
-    sh.cut[wid] = c;
-  }
-  Run into = run_up(incl, 1);
-  bool into_cut = __shfl_up_sync(kAllLanes, c, 1);
-  if (lane == 0) {
-    into = Run{{0.f, 0.f}, 0};
-    into_cut = false;
-  }
-  __syncthreads();
-  if (!pending) return;
-  if (!into_cut) {
-    Run w{{0.f, 0.f}, 0};
-    for (int k = wid - 1; k >= 0; --k) {
-      w = run_join(sh.warp[k], w);
-      if (sh.cut[k]) break;
+    Run into = run_up(incl, 1);
+    bool into_cut = __shfl_up_sync(kAllLanes, c, 1);
+    if (lane == 0) {
+      into = none;
+      into_cut = false;
     }
-    into = run_join(w, into);
+    if (pending) {
+      if (!into_cut) into = run_join(carry, into);
+      emit(closed_q, run_join(into, closed));
+    }
+    if (lane == 31) mine = c ? incl : run_join(carry, incl);
+    walk = ahead;
+    walk.to(s.off, n_seq, min(t0 + kTile, stop - 1));
   }
-  emit(closed_q, run_join(into, closed));
 }
 
 // A sequence's sum and its number of tokens.
-template <uint64_t C>
 __device__ __forceinline__ Run sequence_sum(const TokenSet &s, const PrefScratch &x, uint64_t seq) {
   const uint64_t a = s.off[seq], b = min(s.off[seq + 1], s.n);
   if (b <= a) return {{0.f, 0.f}, 0};
   const float4 p = __ldcg(reinterpret_cast<const float4 *>(&x.inner[seq]));
   Run r{{p.x, p.y}, __float_as_uint(p.z)};
+  const uint64_t last = (b - 1) / x.run;
 #pragma unroll 4
-  for (uint64_t c = a / C + 1; c <= (b - 1) / C; ++c) {
+  for (uint64_t c = a / x.run + 1; c <= last; ++c) {
     const float4 h = __ldcg(reinterpret_cast<const float4 *>(&x.head[c]));
     r = run_join(r, Run{{h.x, h.y}, __float_as_uint(h.z)});
   }
@@ -195,7 +195,6 @@ __device__ __forceinline__ void grad_add(const PrefScratch &x, uint64_t seq, dou
 }
 
 // Pairs first, first + step, ...: their losses, gradients and sums.
-template <uint64_t C>
 __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
                                            const PrefScratch &x, const PrefOut &out,
                                            uint32_t first, uint32_t step, Pair (&sum)[4],
@@ -206,7 +205,7 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
     if ((uint64_t)c >= in.s.n_seq || (uint64_t)j >= in.s.n_seq) {
       flag(ctrl, DEVERR_INDEX, (unsigned long long)((uint64_t)c >= in.s.n_seq ? c : j));
     } else {
-      const Run rc = sequence_sum<C>(in.s, x, c), rj = sequence_sum<C>(in.s, x, j);
+      const Run rc = sequence_sum(in.s, x, c), rj = sequence_sum(in.s, x, j);
       const double kc = r.average && rc.n ? 1.0 / (double)rc.n : 1.0;
       const double kj = r.average && rj.n ? 1.0 / (double)rj.n : 1.0;
       const double uc = pair_value(rc.v) * kc, uj = pair_value(rj.v) * kj;
@@ -244,13 +243,12 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
   }
 }
 
-template <uint64_t C>
 __device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
                                             const PrefScratch &x, const PrefOut &out,
                                             uint64_t first, uint64_t step) {
   if (!out.ratio) return;
   for (uint64_t q = first; q < in.s.n_seq; q += step) {
-    const Run v = sequence_sum<C>(in.s, x, q);
+    const Run v = sequence_sum(in.s, x, q);
     out.ratio[q] = (float)(pair_value(v.v) * (r.average && v.n ? 1.0 / (double)v.n : 1.0));
   }
 }
@@ -274,50 +272,60 @@ __device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, 
   return fmaf(scale.hi, vh, fmaf(scale.hi, vl, scale.lo * vh));
 }
 
-template <int NT, bool VEC>
-__device__ __forceinline__ void chunk_grad(const PrefIn &in, const PrefScratch &x, df scale,
-                                           float *dlogp, uint64_t t0, uint64_t first,
-                                           uint64_t end, PrefShared<NT> &sh) {
+// Gradients of tokens [begin, stop) of a warp.
+template <bool VEC>
+__device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x, df scale,
+                                         float *dlogp, uint64_t begin, uint64_t stop,
+                                         uint64_t first, uint64_t end) {
   const TokenSet &s = in.s;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const uint64_t t = t0 + 4 * threadIdx.x;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (t0 < end) {
+  const uint32_t n_seq = (uint32_t)s.n_seq;
+  const int lane = threadIdx.x & 31;
+  SeqWalk walk;
+  if (begin < min(stop, end)) walk.start(s.off, n_seq, begin);
+  uint32_t known = 0xffffffffu;  // the sequence that g belongs to
+  float g = 0.f;
+  for (uint64_t t0 = begin; t0 < stop; t0 += kTile) {
+    const uint64_t t = t0 + 4 * lane;
     const uint32_t bits = token_bits<VEC>(s, t, first, end);
-    __syncthreads();
-    if (wid < 2) {
-      const uint32_t q = sequence_of_warp(s.off, (uint32_t)s.n_seq,
-                                          wid == 0 ? t0 : min(t0 + (uint64_t)(4 * NT), end) - 1);
-      if (lane == 0) (wid == 0 ? sh.lo : sh.hi) = q;
-    }
-    __syncthreads();
-    uint32_t q = 0;
-    uint64_t qend = 0;
-    float g = 0.f;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (t0 < end) {
+      walk.to(s.off, n_seq, t0);
+      if (t0 + kTile <= walk.next) {
+        if (walk.q != known) g = token_grad(x, walk.q, scale);
+        known = walk.q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (!(bits >> i & 1u)) continue;
-      if (t + i >= qend) {
-        q = sequence_of(s.off, qend ? q : sh.lo, sh.hi + 1, t + i);
-        qend = s.off[q + 1];
-        g = token_grad(x, q, scale);
+        for (int i = 0; i < 4; ++i) v[i] = bits >> i & 1u ? g : 0.f;
+      } else {
+        SeqWalk ahead = walk;
+        ahead.to(s.off, n_seq, min(t0 + kTile, end) - 1);
+        uint32_t q = walk.q;
+        uint64_t next = 0;
+        float each = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!(bits >> i & 1u)) continue;
+          if (t + i >= next) {
+            q = sequence_of(s.off, q, ahead.q + 1, t + i);
+            next = s.off[q + 1];
+            each = token_grad(x, q, scale);
+          }
+          v[i] = each;
+        }
+        walk = ahead;
       }
-      v[i] = g;
     }
+    store4<VEC>(dlogp, t, s.n, make_float4(v[0], v[1], v[2], v[3]));
   }
-  store4<VEC>(dlogp, t, s.n, make_float4(v[0], v[1], v[2], v[3]));
 }
 
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads)
 k_pref_parts(PrefIn in, PrefScratch x) {
-  __shared__ PrefShared<kThreads> sh;
   pdl_wait();
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
-  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * kThreads; t0 < end;
-       t0 += (uint64_t)gridDim.x * 4 * kThreads)
-    chunk_parts<kThreads, VEC>(in, x, t0, first, end, sh);
+  const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * x.run;
+  run_parts<VEC>(in, x, begin, begin + x.run, first, end);
 }
 
 __global__ void __launch_bounds__(kPairThreads)
@@ -328,8 +336,8 @@ k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, Ctrl *ctrl) {
   Pair sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
-  take_pairs<4ull * kThreads>(in, r, x, out, i, step, sum, ctrl);
-  take_ratios<4ull * kThreads>(in, r, x, out, i, step);
+  take_pairs(in, r, x, out, i, step, sum, ctrl);
+  take_ratios(in, r, x, out, i, step);
   pdl_launch();
   if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
     write_loss(r, in.n_pair, total, out.loss);
@@ -338,37 +346,35 @@ k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, Ctrl *ctrl) {
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads)
 k_pref_grad(PrefIn in, PrefScratch x, df scale, float *dlogp) {
-  __shared__ PrefShared<kThreads> sh;
   pdl_wait();
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
-  for (uint64_t t0 = (uint64_t)blockIdx.x * 4 * kThreads; t0 < in.s.n;
-       t0 += (uint64_t)gridDim.x * 4 * kThreads)
-    chunk_grad<kThreads, VEC>(in, x, scale, dlogp, t0, first, end, sh);
+  const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * x.run;
+  run_grad<VEC>(in, x, scale, dlogp, begin, min(begin + x.run, in.s.n), first, end);
 }
 
-// All three steps of a batch of one chunk.
+// All three steps of a batch of up to 4 kSmallThreads tokens, a tile per warp.
 template <bool VEC>
 __global__ void __launch_bounds__(kSmallThreads)
 k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *ctrl) {
-  constexpr uint64_t C = 4ull * kSmallThreads;
-  __shared__ PrefShared<kSmallThreads> sh;
   __shared__ Pair total[4];
   pdl_wait();
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
-  if (end) chunk_parts<kSmallThreads, VEC>(in, x, 0, first, end, sh);
+  const uint64_t begin = (uint64_t)(threadIdx.x >> 5) * x.run;
+  run_parts<VEC>(in, x, begin, begin + x.run, first, end);
   __threadfence();  // the pairs read around the first-level cache
   __syncthreads();
   Pair sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
-  take_pairs<C>(in, r, x, out, threadIdx.x, kSmallThreads, sum, ctrl);
-  take_ratios<C>(in, r, x, out, threadIdx.x, kSmallThreads);
+  take_pairs(in, r, x, out, threadIdx.x, kSmallThreads, sum, ctrl);
+  take_ratios(in, r, x, out, threadIdx.x, kSmallThreads);
   __threadfence();
   if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
     write_loss(r, in.n_pair, total, out.loss);
-  if (out.dlogp) chunk_grad<kSmallThreads, VEC>(in, x, scale, out.dlogp, 0, first, end, sh);
+  if (out.dlogp)
+    run_grad<VEC>(in, x, scale, out.dlogp, begin, min(begin + x.run, in.s.n), first, end);
 }
 
 }  // namespace
@@ -380,7 +386,11 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
                                    cudaStream_t s) {
   const uint64_t sms = (uint64_t)c->coop_sms;
   const bool small = set.n <= 4 * kSmallThreads && n_pair <= kSmallPairs;
-  const uint64_t chunks = (set.n + 4 * kThreads - 1) / (4 * kThreads);
+  // a run per warp of a full chip, so that all end together
+  const uint64_t warps = kThreads / 32, chip = 3 * warps * sms;
+  uint64_t run = (set.n + chip - 1) / chip;
+  run = small ? kTile : run < kLeastRun ? kLeastRun : (run + kTile - 1) / kTile * kTile;
+  const uint64_t runs = (set.n + run - 1) / run;
   const uint64_t want = ((n_pair > set.n_seq ? n_pair : set.n_seq) + kPairThreads - 1) / kPairThreads;
   const uint64_t pair_grid = want < 4 * sms ? want : 4 * sms;
   size_t at = 0;
@@ -390,14 +400,14 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
     return a;
   };
   const size_t inner = take(set.n_seq * sizeof(SeqPart)), grad = take(set.n_seq * sizeof(SeqGrad));
-  const size_t head = take(chunks * sizeof(SeqPart)), bad = take(set.n_seq * sizeof(uint32_t));
+  const size_t head = take(runs * sizeof(SeqPart)), bad = take(set.n_seq * sizeof(uint32_t));
   const size_t part = take(4 * pair_grid * sizeof(Pair));
   void *blk = nullptr;
   cudaError_t e = ctx_scratch(c, at, s, &blk);
   if (e != cudaSuccess) return e;
   uint8_t *b = (uint8_t *)blk;
   const PrefScratch x{(SeqPart *)(b + inner), (SeqPart *)(b + head), (SeqGrad *)(b + grad),
-                      (uint32_t *)(b + bad), (Pair *)(b + part)};
+                      (uint32_t *)(b + bad), (Pair *)(b + part), (uint32_t)run};
   PrefRule r;
   r.beta = cfg.beta;
   r.smooth = cfg.label_smoothing;
@@ -414,7 +424,7 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   if (small)
     return launch_pdl(vec ? k_pref_small<true> : k_pref_small<false>, dim3(1),
                       dim3(kSmallThreads), s, in, r, x, out, scale, c->ctrl);
-  const unsigned grid = (unsigned)(chunks < 4 * sms ? chunks : 4 * sms);
+  const unsigned grid = (unsigned)((runs + warps - 1) / warps);
   e = launch_pdl(vec ? k_pref_parts<true> : k_pref_parts<false>, dim3(grid), dim3(kThreads), s, in,
                  x);
   if (e != cudaSuccess) return e;
