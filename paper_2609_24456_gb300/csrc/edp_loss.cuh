@@ -61,64 +61,83 @@ struct RowWeights {
   float fixed;                       // or the weight of all
 };
 
-// One token: its policy loss and divergence, the ratio, whether it is clipped,
-// and the loss's derivative by logp (entropy apart), before weight and scale.
-struct PolicyToken {
-  float pg, kl, ratio, dlogp, old_kl;
-  bool above, below;
-};
-
-// e^q - 1 - q and, in em1, e^q - 1; e = e^q.  Below 1/2 the Taylor series, whose
-// first term left out is 2^-24 of the sum; above, the difference loses at most
-// three bits.
-__device__ __forceinline__ float exp_less_line(float q, float e, float *em1) {
-  float p = 1.f / 40320.f;  // 1/8!
+// e^q - 1 - q for |q| below 1: the Taylor series, whose first term left out is
+// 2^-24 of the sum.
+__device__ __forceinline__ float exp_less_line(float q) {
+  float p = 1.f / 3628800.f;  // 1/10!
+  p = fmaf(p, q, 1.f / 362880.f);
+  p = fmaf(p, q, 1.f / 40320.f);
   p = fmaf(p, q, 1.f / 5040.f);
   p = fmaf(p, q, 1.f / 720.f);
   p = fmaf(p, q, 1.f / 120.f);
   p = fmaf(p, q, 1.f / 24.f);
   p = fmaf(p, q, 1.f / 6.f);
   p = fmaf(p, q, 0.5f);
-  const float near = q * q * p;
-  const bool far = !(fabsf(q) < 0.5f);
-  *em1 = far ? e - 1.f : q + near;
-  return far ? *em1 - q : near;
+  return q * q * p;
+}
+// The same for any q, and in em1 e^q - 1: from 1 on the difference loses at most
+// two bits of e^q.
+__device__ __forceinline__ float exp_less_line(float q, float *em1) {
+  const float near = exp_less_line(q), e = ex2(q * (float)kLog2e) - 1.f;
+  const bool far = !(fabsf(q) < 1.f);
+  *em1 = far ? e : q + near;
+  return far ? e - q : near;
 }
 
-__device__ __forceinline__ PolicyToken policy_token(const PolicyRule &c, float logp, float old,
-                                                    float ref, bool has_ref, float adv) {
+// One token: its policy loss and divergence, the ratio less one, the divergence from
+// the old policy, and the loss's derivative by logp (entropy apart), before weight
+// and scale.  d = logp - old, q = ref - logp; with d, q and the advantage 0 all are 0.
+struct PolicyToken {
+  float pg, kl, ratio1, old_kl, dlogp;
+  bool above, below;
+};
+enum class Kl { kNone, kK3, kOther };  // which estimator, as far as the code goes
+
+// NEAR: |d| and |q| are below 1.
+template <Kl KL, bool NEAR>
+__device__ __forceinline__ PolicyToken policy_token(const PolicyRule &c, float d, float q,
+                                                    float adv) {
   PolicyToken o;
-  const float d = logp - old;
-  o.ratio = expf(d);
-  float em1;
-  o.old_kl = exp_less_line(d, o.ratio, &em1);
+  if (NEAR) {
+    o.old_kl = exp_less_line(d);
+    o.ratio1 = d + o.old_kl;
+  } else {
+    o.old_kl = exp_less_line(d, &o.ratio1);
+  }
+  const float r = o.ratio1 + 1.f;
   // the limits act on the logarithm, whose difference of two fp32 numbers is
   // one rounding away from the numbers that the caller gave
-  o.above = adv > 0.f && d > c.ln_high;
-  const bool dual = adv < 0.f && d > c.ln_dual;
-  o.below = dual || (adv < 0.f && d < c.ln_low);
-  const float used = o.above ? c.high : dual ? c.dual : o.below ? c.low : o.ratio;
+  const bool pos = adv > 0.f;
+  const bool up = d > (pos ? c.ln_high : c.ln_dual), down = !pos && d < c.ln_low;
+  const float used = up ? (pos ? c.high : c.dual) : down ? c.low : r;
+  o.pg = -used * adv;
   // an advantage of 0 takes nothing from a ratio that overflowed
-  o.pg = adv == 0.f && !isnan(d) ? 0.f : -used * adv;
-  o.dlogp = o.above || o.below ? 0.f : o.pg;
+  if (!NEAR && adv == 0.f) o.pg = d * 0.f;
+  o.dlogp = up || down ? 0.f : o.pg;
+  o.above = up && pos;
+  o.below = (up || down) && adv < 0.f;
   o.kl = 0.f;
-  if (has_ref) {
-    const float q = ref - logp;
-    float g = 1.f;
-    if (c.kl == EDP_KL_K1) {
+  if (KL != Kl::kNone) {
+    float g;  // minus the derivative
+    if (KL == Kl::kK3) {
+      if (NEAR) {
+        o.kl = exp_less_line(q);
+        g = q + o.kl;
+      } else {
+        o.kl = exp_less_line(q, &g);
+      }
+    } else if (c.kl == EDP_KL_K1) {
       o.kl = -q;
-    } else if (c.kl == EDP_KL_K2) {
-      o.kl = 0.5f * q * q;
-      g = -q;
+      g = -1.f;
     } else {
-      o.kl = exp_less_line(q, expf(q), &em1);
-      g = -em1;
+      o.kl = 0.5f * q * q;
+      g = q;
     }
-    if (c.kl_coef != 0.f) o.dlogp = fmaf(c.kl_coef, g, o.dlogp);
+    // without the coefficient the divergence is reported alone, whatever it is
+    if (c.kl_coef != 0.f) o.dlogp = fmaf(-c.kl_coef, g, o.dlogp);
   }
   return o;
 }
-
 
 // ---------------------------------------------------------------------------
 // Sums in pairs of fp32 numbers: hi is the running sum, lo the sum of its

@@ -342,6 +342,16 @@ __device__ __forceinline__ float row_weight(const RowWeights &w, uint64_t t) {
   return w.tokens ? 1.f / (float)__ldcg(w.tokens) : w.fixed;
 }
 
+// The policy loss's derivative by a row's log-probability, before weight and scale.
+__device__ __forceinline__ float row_policy(const PolicyRule &rule, float logp, float old,
+                                            const float *ref, float adv) {
+  const float d = logp - old;
+  if (!ref) return policy_token<Kl::kNone, false>(rule, d, 0.f, adv).dlogp;
+  const float q = *ref - logp;
+  return rule.kl == EDP_KL_K3 ? policy_token<Kl::kK3, false>(rule, d, q, adv).dlogp
+                              : policy_token<Kl::kOther, false>(rule, d, q, adv).dlogp;
+}
+
 // Log-probability, policy gradient and the logits' gradient of a row, by a
 // cluster of gridDim.y CTAs.
 template <typename T, bool ENT>
@@ -400,10 +410,10 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
     part_zero(d + first, n);
     return;
   }
-  const PolicyToken tok = policy_token(rule, o.logp, old_logp[t], ref_logp ? ref_logp[t] : 0.f,
-                                       ref_logp != nullptr, adv[t]);
   const float by = rule.grad_scale * w;
-  const RowGrad g = row_grad(o.m, o.s, ENT ? o.entropy : 0.f, by * tok.dlogp,
+  const RowGrad g = row_grad(o.m, o.s, ENT ? o.entropy : 0.f,
+                             by * row_policy(rule, o.logp, old_logp[t],
+                                             ref_logp ? ref_logp + t : nullptr, adv[t]),
                              ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
   part_grad<T, ENT>(row, d, first, n, target, g, a.c);
 }

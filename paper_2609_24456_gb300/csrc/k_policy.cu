@@ -9,6 +9,7 @@
 // the bytes at its ends.  A batch of up to 4,096 tokens is one CTA that counts for
 // itself, in one launch.
 #include <cmath>
+#include <type_traits>
 
 #include "edp_loss.cuh"
 
@@ -21,9 +22,10 @@ cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kPerSm = 2;  // CTAs of k_policy, in one wave
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
 constexpr uint32_t kBlock = 512;     // tokens counted together
-constexpr int kSums = 8;  // pg, kl, entropy; ratio, old kl; clipped above, below; tokens
+constexpr int kSums = 8;  // pg, kl, entropy; ratio - 1, old kl; clipped above, below; tokens
 constexpr int kFlush = 8;  // tiles (32 tokens a lane) between two additions to the sums
 
 struct Weighting {
@@ -50,15 +52,17 @@ __device__ __forceinline__ uint32_t cta_sum(uint32_t v, uint32_t *red) {
   return __reduce_add_sync(kAllLanes, x);
 }
 
+// Bytes that are not 0.
+__device__ __forceinline__ uint32_t some_bytes(uint32_t x) {
+  return __popc((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
+}
+
 // Tokens that count in t .. t + 15.
 template <bool VEC>
 __device__ __forceinline__ uint32_t count16(const TokenSet &s, uint64_t t, const Range &r) {
   if (VEC && s.mask && !s.target && t >= r.first && t + 16 <= r.end) {
     const uint4 m = *reinterpret_cast<const uint4 *>(s.mask + t);
-    auto some = [](uint32_t x) {  // bytes that are not 0
-      return __popc((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
-    };
-    return some(m.x) + some(m.y) + some(m.z) + some(m.w);
+    return some_bytes(m.x) + some_bytes(m.y) + some_bytes(m.z) + some_bytes(m.w);
   }
   uint32_t n = 0;
 #pragma unroll
@@ -179,8 +183,8 @@ __device__ __forceinline__ void sequence_weights(const TokenSet &s, uint64_t end
 
 // The policy loss of every token, its gradients and the batch's sums.  SEQ: a weight
 // for each sequence.  NT == kSmallThreads: one CTA, which counts for itself.
-template <int NT, bool SEQ, bool VEC>
-__global__ void __launch_bounds__(NT, 1536 / NT)
+template <int NT, bool SEQ, bool VEC, Kl KL>
+__global__ void __launch_bounds__(NT, NT == kSmallThreads ? 1 : kPerSm)
 k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor, float *loss,
          float *dlogp, float *dentropy, Pair *part, Ctrl *ctrl) {
   constexpr bool kOne = NT == kSmallThreads;
@@ -191,7 +195,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Range r = token_range(s);
   float fixed = w.fixed;
-  if (!kOne && !SEQ && w.tokens) fixed = 1.f / (float)__ldcg(w.tokens);
+  if (!kOne && !SEQ && w.tokens) fixed = 1.f / (float)max(__ldcg(w.tokens), 1ull);
   Pair sum[kSums];
 #pragma unroll
   for (int k = 0; k < kSums; ++k) sum[k] = Pair{0.f, 0.f};
@@ -204,81 +208,174 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
       add[k] = 0.f;
     }
   };
-  // the CTA's tiles, in turn by its warps
+  // the CTA's tokens c0 .. c0 + cn - 1, in tiles in turn by its warps; places
+  // within them are 32-bit numbers.  Tiles below `whole` count but for the mask.
   const uint64_t tiles = (s.n + kTile - 1) / kTile;
-  const uint64_t each = (tiles + gridDim.x - 1) / gridDim.x;
-  const uint64_t last = min(tiles, (blockIdx.x + 1) * each);
+  const uint64_t c0 = blockIdx.x * ((tiles + gridDim.x - 1) / gridDim.x) * kTile;
+  const uint64_t c1 = min(s.n, c0 + (tiles + gridDim.x - 1) / gridDim.x * kTile);
+  const uint32_t cn = kOne ? 4 * NT : c1 > c0 ? (uint32_t)(c1 - c0) : 0;
+  const uint32_t whole = VEC && !s.target && c0 >= r.first && r.end > c0
+                             ? (uint32_t)min((uint64_t)cn, r.end - c0) : 0;
+  const float *lpc = p.logp + c0, *odc = p.old_logp + c0, *adc = p.adv + c0;
+  const float *rfc = p.ref_logp + c0, *enc = p.entropy + c0;
+  const uint8_t *mc = s.mask + c0;
+  struct Tile {
+    float4 lp, od, ad, rf, en;
+    uint32_t m;  // a byte per token, 0: it does not count
+  };
+  const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto load = [&](uint32_t i) {
+    Tile x;
+    const uint32_t e = i + 4 * lane;
+    x.rf = x.en = none;
+    if (i + kTile <= whole) {
+      x.lp = *reinterpret_cast<const float4 *>(lpc + e);
+      x.od = *reinterpret_cast<const float4 *>(odc + e);
+      x.ad = *reinterpret_cast<const float4 *>(adc + e);
+      if (KL != Kl::kNone) x.rf = *reinterpret_cast<const float4 *>(rfc + e);
+      if (p.entropy) x.en = *reinterpret_cast<const float4 *>(enc + e);
+      x.m = s.mask ? *reinterpret_cast<const uint32_t *>(mc + e) : 0xffffffffu;
+    } else {
+      const uint64_t t = c0 + e;
+      x.lp = load4<VEC>(p.logp, t, s.n);
+      x.od = load4<VEC>(p.old_logp, t, s.n);
+      x.ad = load4<VEC>(p.adv, t, s.n);
+      if (KL != Kl::kNone) x.rf = load4<VEC>(p.ref_logp, t, s.n);
+      if (p.entropy) x.en = load4<VEC>(p.entropy, t, s.n);
+      const uint32_t bits = token_bits<VEC>(s, t, r.first, r.end);
+      x.m = (bits & 1u) | (bits & 2u) << 7 | (bits & 4u) << 14 | (bits & 8u) << 21;
+    }
+    return x;
+  };
   SeqWalk walk;
-  bool walking = false;
-  int kept = 0;
-  for (uint64_t tile = blockIdx.x * each + wid; tile < (kOne ? (uint64_t)kWarps : last);
-       tile += kWarps) {
-    const uint64_t t0 = tile * kTile, t = t0 + 4 * lane;
-    const float4 lp = load4<VEC>(p.logp, t, s.n), od = load4<VEC>(p.old_logp, t, s.n);
-    const float4 ad = load4<VEC>(p.adv, t, s.n);
-    float4 rf = make_float4(0.f, 0.f, 0.f, 0.f), en = rf;
-    if (p.ref_logp) rf = load4<VEC>(p.ref_logp, t, s.n);
-    if (p.entropy) en = load4<VEC>(p.entropy, t, s.n);
-    const uint32_t bits = token_bits<VEC>(s, t, r.first, r.end);
+  // where the walk's sequence and the one after it end in the CTA's tokens, and
+  // their weights
+  uint32_t next = 0, after = 0;
+  float here = 0.f, there = 0.f;
+  bool known = false;
+  auto place = [&](uint64_t t) {
+    return t > c0 ? (uint32_t)min(t - c0, (uint64_t)cn + kTile) : 0u;
+  };
+  Tile ahead;
+  const uint32_t share = (cn / kTile + kWarps - 1 + (cn % kTile != 0)) / kWarps * kTile;
+  const uint32_t stop = (uint32_t)min((uint64_t)cn, (uint64_t)(wid + 1) * share);
+  uint32_t i = wid * share;
+  if (false && i < stop) ahead = load(i);
+#pragma unroll 1
+  while (i < stop) {
+   const uint32_t group = min(stop, i + kFlush * kTile);
+#pragma unroll 1
+   for (; i < group; i += kTile) {
+    const Tile x = false ? ahead : load(i);
+    if (false && stop - i > kTile) ahead = load(i + kTile);
+    bool b[4];  // which of the lane's tokens count
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = x.m & (0xffu << (8 * k));
+    auto bits = [&] { return b[0] | b[1] << 1 | b[2] << 2 | b[3] << 3; };
     float wt[4];
     if (kOne && SEQ) {
-      one.fill(bits);
-      sequence_weights(s, r.end, t, bits, 0, (uint32_t)s.n_seq - 1,
+      one.fill(bits());
+      sequence_weights(s, r.end, c0 + i + 4 * lane, bits(), 0, (uint32_t)s.n_seq - 1,
                        [&](uint32_t, uint64_t a, uint64_t b) {
                          return 1.f / (divisor * (float)(one.upto((uint32_t)b) -
                                                          one.upto((uint32_t)a)));
                        }, wt);
     } else if (SEQ) {
-      wt[0] = wt[1] = wt[2] = wt[3] = 0.f;
-      if (t0 < r.end) {
-        const uint32_t n = (uint32_t)s.n_seq;
-        if (walking) walk.to(s.off, n, t0);
-        else walk.start(s.off, n, t0);
-        walking = true;
-        if (t0 + kTile <= walk.next) {
-          wt[0] = wt[1] = wt[2] = wt[3] = __ldcg(&w.sequence[walk.q]);
-        } else {
-          SeqWalk ahead = walk;
-          ahead.to(s.off, n, min(t0 + kTile, r.end) - 1);
-          sequence_weights(s, r.end, t, bits, walk.q, ahead.q,
-                           [&](uint32_t q, uint64_t, uint64_t) { return __ldcg(&w.sequence[q]); },
-                           wt);
+      const uint32_t n = (uint32_t)s.n_seq;
+      if (c0 + i >= r.end) {
+        wt[0] = wt[1] = wt[2] = wt[3] = 0.f;
+      } else {
+        if (i >= next) {  // on to the sequence of the tile's first token
+          if (known && after > i) {
+            ++walk.q;
+            next = after;
+            here = there;
+          } else {
+            if (known) {
+              walk.next = c0 + next;
+              walk.to(s.off, n, c0 + i);
+            } else {
+              walk.start(s.off, n, c0 + i);
+            }
+            next = place(walk.next);
+            here = __ldcg(&w.sequence[walk.q]);
+          }
+          known = true;
+          // and what will be wanted at its end
+          after = walk.q + 1 < n ? place(s.off[walk.q + 2]) : next;
+          there = walk.q + 1 < n ? __ldcg(&w.sequence[walk.q + 1]) : 0.f;
+        }
+        wt[0] = wt[1] = wt[2] = wt[3] = here;
+        if (i + kTile > next) {
+          if (i + kTile <= after || c0 + after >= r.end) {  // two sequences
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (i + 4 * lane + k >= next) wt[k] = there;
+          } else {
+            SeqWalk to = walk;
+            to.next = c0 + next;
+            to.to(s.off, n, min(c0 + i + kTile, r.end) - 1);
+            sequence_weights(s, r.end, c0 + i + 4 * lane, bits(), walk.q, to.q,
+                             [&](uint32_t q, uint64_t, uint64_t) {
+                               return __ldcg(&w.sequence[q]);
+                             }, wt);
+          }
         }
       }
     } else {
-      if (kOne && w.tokens) fixed = 1.f / (float)cta_sum<NT>(__popc(bits), one.red);
+      if (kOne && w.tokens) fixed = 1.f / (float)max(cta_sum<NT>(__popc(bits()), one.red), 1u);
       wt[0] = wt[1] = wt[2] = wt[3] = fixed;
     }
-    const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, o4[4] = {od.x, od.y, od.z, od.w};
-    const float a4[4] = {ad.x, ad.y, ad.z, ad.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
-    const float e4[4] = {en.x, en.y, en.z, en.w};
-    float g4[4], h4[4];
+    // what does not count is 0 from here on, whatever it held
+    const float l4[4] = {x.lp.x, x.lp.y, x.lp.z, x.lp.w};
+    const float o4[4] = {x.od.x, x.od.y, x.od.z, x.od.w};
+    const float a4[4] = {x.ad.x, x.ad.y, x.ad.z, x.ad.w};
+    const float r4[4] = {x.rf.x, x.rf.y, x.rf.z, x.rf.w};
+    const float e4[4] = {x.en.x, x.en.y, x.en.z, x.en.w};
+    float g4[4], d4[4], q4[4], adv4[4], most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      g4[i] = h4[i] = 0.f;
-      if (!(bits >> i & 1u)) continue;
-      const PolicyToken o =
-          policy_token(rule, l4[i], o4[i], r4[i], p.ref_logp != nullptr, a4[i]);
-      const float by = rule.grad_scale * wt[i];
-      g4[i] = by * o.dlogp;
-      h4[i] = -by * rule.entropy_coef;
-      add[0] = fmaf(wt[i], o.pg, add[0]);
-      add[1] = fmaf(wt[i], o.kl, add[1]);
-      add[2] = fmaf(wt[i], e4[i], add[2]);
-      add[3] += o.ratio;
-      add[4] += o.old_kl;
-      above += o.above;
-      below += o.below;
+    for (int k = 0; k < 4; ++k) {
+      d4[k] = b[k] ? l4[k] - o4[k] : 0.f;
+      q4[k] = KL != Kl::kNone && b[k] ? r4[k] - l4[k] : 0.f;
+      adv4[k] = b[k] ? a4[k] : 0.f;
+      most = fmaxf(most, fabsf(d4[k]));
+      if (KL == Kl::kK3) most = fmaxf(most, fabsf(q4[k]));
     }
-    tokens += __popc(bits);
-    if (++kept == kFlush) {
-      flush();
-      kept = 0;
+    auto take = [&](auto near) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const PolicyToken o =
+            policy_token<KL, decltype(near)::value>(rule, d4[k], q4[k], adv4[k]);
+        g4[k] = rule.grad_scale * wt[k] * o.dlogp;
+        add[0] = fmaf(wt[k], o.pg, add[0]);
+        if (KL != Kl::kNone) add[1] = fmaf(wt[k], o.kl, add[1]);
+        add[3] += o.ratio1;
+        add[4] += o.old_kl;
+        above += o.above;
+        below += o.below;
+      }
+    };
+    if (__any_sync(kAllLanes, most >= 1.f)) take(std::false_type{});
+    else take(std::true_type{});
+    if (p.entropy) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (b[k]) add[2] = fmaf(wt[k], e4[k], add[2]);
     }
-    if (dlogp) store4<VEC>(dlogp, t, s.n, make_float4(g4[0], g4[1], g4[2], g4[3]));
-    if (dentropy) store4<VEC>(dentropy, t, s.n, make_float4(h4[0], h4[1], h4[2], h4[3]));
+    tokens += some_bytes(x.m);
+    auto store = [&](float *out, float4 v) {
+      if (i + kTile <= whole) *reinterpret_cast<float4 *>(out + c0 + i + 4 * lane) = v;
+      else store4<VEC>(out, c0 + i + 4 * lane, s.n, v);
+    };
+    if (dlogp) store(dlogp, make_float4(g4[0], g4[1], g4[2], g4[3]));
+    if (dentropy) {
+      const float h = -rule.grad_scale * rule.entropy_coef;
+      store(dentropy, make_float4(b[0] ? h * wt[0] : 0.f, b[1] ? h * wt[1] : 0.f,
+                                  b[2] ? h * wt[2] : 0.f, b[3] ? h * wt[3] : 0.f));
+    }
+   }
+   flush();
   }
-  flush();
   sum[5] = pair_of(above);
   sum[6] = pair_of(below);
   sum[7] = pair_of(tokens);
@@ -294,7 +391,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
     loss[3] = (float)v[2];
     loss[4] = (float)(v[5] / n);
     loss[5] = (float)(v[6] / n);
-    loss[6] = (float)(v[3] / n);
+    loss[6] = v[7] > 0.0 ? (float)(1.0 + v[3] / n) : 0.f;
     loss[7] = (float)(v[4] / n);
     ctrl->loss_tokens = 0;
   }
@@ -349,7 +446,7 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
     if (want) at += (bytes + 15) & ~(size_t)15;
     return a;
   };
-  const size_t part = take(true, kSums * 3 * sms * sizeof(Pair));
+  const size_t part = take(true, kSums * kPerSm * sms * sizeof(Pair));
   const size_t weight = take(p->sequences && !one_cta, set.n_seq * sizeof(float));
   const size_t block = take(blocks, (set.n + kBlock - 1) / kBlock * sizeof(uint32_t));
   const size_t ent = take(entropy, set.n * sizeof(float));
@@ -387,13 +484,19 @@ cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t
     return launch_pdl(kern, dim3(grid), dim3(threads), s, set, t, rule, p.w, p.divisor, loss,
                       dlogp, dentropy, p.part, c->ctrl);
   };
-  if (one_cta)
-    return p.sequences ? go(k_policy<kSmallThreads, true, VEC>, 1, kSmallThreads)
-                       : go(k_policy<kSmallThreads, false, VEC>, 1, kSmallThreads);
   const uint64_t want = (set.n + 4 * kThreads - 1) / (4 * kThreads);
-  const unsigned grid = at_most(want, 3ull * (uint64_t)c->coop_sms);
-  return p.sequences ? go(k_policy<kThreads, true, VEC>, grid, kThreads)
-                     : go(k_policy<kThreads, false, VEC>, grid, kThreads);
+  const unsigned grid = at_most(want, (uint64_t)kPerSm * (uint64_t)c->coop_sms);
+  auto kind = [&](auto kl) {
+    constexpr Kl KL = decltype(kl)::value;
+    if (one_cta)
+      return p.sequences ? go(k_policy<kSmallThreads, true, VEC, KL>, 1, kSmallThreads)
+                         : go(k_policy<kSmallThreads, false, VEC, KL>, 1, kSmallThreads);
+    return p.sequences ? go(k_policy<kThreads, true, VEC, KL>, grid, kThreads)
+                       : go(k_policy<kThreads, false, VEC, KL>, grid, kThreads);
+  };
+  if (!t.ref_logp) return kind(std::integral_constant<Kl, Kl::kNone>{});
+  return rule.kl == EDP_KL_K3 ? kind(std::integral_constant<Kl, Kl::kK3>{})
+                              : kind(std::integral_constant<Kl, Kl::kOther>{});
 }
 
 }  // namespace

@@ -18,7 +18,7 @@ constexpr int kThreads = 512;
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
 constexpr int kPairThreads = 256;
 constexpr uint32_t kSmallPairs = 4096;
-constexpr uint32_t kLeastRun = 512;  // tokens of a warp
+constexpr uint32_t kLeastRun = kTile;  // tokens of a warp
 
 // A sequence's part of a run.
 struct alignas(16) SeqPart {
