@@ -274,6 +274,11 @@ struct SeqWalk {
   }
 };
 
+// Bytes that are not 0.
+__device__ __forceinline__ uint32_t some_bytes(uint32_t x) {
+  return __popc((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
+}
+
 // Which of the tokens t .. t + 3 count, as bits; t is a multiple of 4.  first,
 // end: the tokens that the sequences hold.
 template <bool VEC>

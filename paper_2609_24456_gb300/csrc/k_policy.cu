@@ -52,11 +52,6 @@ __device__ __forceinline__ uint32_t cta_sum(uint32_t v, uint32_t *red) {
   return __reduce_add_sync(kAllLanes, x);
 }
 
-// Bytes that are not 0.
-__device__ __forceinline__ uint32_t some_bytes(uint32_t x) {
-  return __popc((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u);
-}
-
 // Tokens that count in t .. t + 15.
 template <bool VEC>
 __device__ __forceinline__ uint32_t count16(const TokenSet &s, uint64_t t, const Range &r) {

@@ -15,10 +15,12 @@ namespace edp {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kPerSm = 2;            // CTAs of the sums, in one wave
+constexpr int kGradPerSm = 4;        // and of the gradient
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
-constexpr int kPairThreads = 256;
+constexpr int kPairThreads = 128;
 constexpr uint32_t kSmallPairs = 4096;
-constexpr uint32_t kLeastRun = kTile;  // tokens of a warp
+constexpr uint32_t kAtOnce = 4;  // tiles in flight per warp
 
 // A sequence's part of a run.
 struct alignas(16) SeqPart {
@@ -41,7 +43,9 @@ struct PrefScratch {
 };
 
 struct PrefRule {
-  double beta, smooth, margin, norm;
+  df beta, margin, half;  // half: 1 / (2 beta)
+  float smooth;
+  double norm;
   uint32_t kind, average;
 };
 
@@ -94,11 +98,44 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
   Run mine = none;  // a lane's share of the sequence that is open
   SeqWalk walk;
   walk.start(s.off, n_seq, begin);
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   for (uint64_t t0 = begin; t0 < stop; t0 += kTile) {
+    // tiles that the sequence goes through, kAtOnce of them in flight
+    if (VEC && t0 >= first) {
+      const uint64_t top = min(walk.next, stop), room = top > t0 ? top - t0 : 0;
+      for (uint32_t n = room > kTile ? (uint32_t)min((room - 1) / kTile, (uint64_t)x.run) : 0; n;) {
+        const uint32_t m = min(n, kAtOnce);
+        float4 lp[kAtOnce], rf[kAtOnce];
+        uint32_t mk[kAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+          const uint64_t t = t0 + k * kTile + 4 * lane;
+          lp[k] = rf[k] = zero;
+          mk[k] = 0;
+          if (k >= m) continue;
+          lp[k] = *reinterpret_cast<const float4 *>(in.logp + t);
+          if (in.ref) rf[k] = *reinterpret_cast<const float4 *>(in.ref + t);
+          mk[k] = s.mask ? *reinterpret_cast<const uint32_t *>(s.mask + t) : 0xffffffffu;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+          const float l4[4] = {lp[k].x, lp[k].y, lp[k].z, lp[k].w};
+          const float r4[4] = {rf[k].x, rf[k].y, rf[k].z, rf[k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool b = mk[k] & (0xffu << (8 * i));
+            pair_add(mine.v, b ? l4[i] : 0.f);
+            if (in.ref) pair_add(mine.v, b ? -r4[i] : 0.f);
+          }
+          mine.n += some_bytes(mk[k]);
+        }
+        t0 += m * kTile;
+        n -= m;
+      }
+    }
     const uint64_t t = t0 + 4 * lane;
     const float4 lp = load4<VEC>(in.logp, t, s.n);
-    float4 rf = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (in.ref) rf = load4<VEC>(in.ref, t, s.n);
+    const float4 rf = in.ref ? load4<VEC>(in.ref, t, s.n) : zero;
     const uint32_t bits = token_bits<VEC>(s, t, first, stop);
     const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
     if (t0 + kTile < walk.next && t0 + kTile < stop) {
@@ -179,19 +216,31 @@ __device__ __forceinline__ Run sequence_sum(const TokenSet &s, const PrefScratch
   return r;
 }
 
-constexpr double kHiUnit = 1.0 / 1048576.0;              // 2^-20
-constexpr double kLoUnit = 1.0 / 4611686018427387904.0;  // 2^-62
-constexpr double kGradMost = 4194304.0;                  // 2^22
+constexpr float kHiUnit = 1.f / 1048576.f;              // 2^-20
+constexpr float kLoUnit = 1.f / 4611686018427387904.f;  // 2^-62
+constexpr float kGradMost = 4194304.f;                  // 2^22
 
-__device__ __forceinline__ void grad_add(const PrefScratch &x, uint64_t seq, double v) {
-  if (!(fabs(v) < kGradMost)) {
+__device__ __forceinline__ df as_df(Pair a) {
+  return isfinite(a.hi) ? quick_two_sum(a.hi, a.lo) : df{a.hi, 0.f};
+}
+// x / n for a whole number n
+__device__ __forceinline__ df df_over(df x, uint32_t n) {
+  const float nh = (float)n, nl = (float)((long long)n - (long long)nh);
+  const float q = x.hi / nh;
+  const float rest = fmaf(-q, nl, fmaf(-q, nh, x.hi)) + x.lo;
+  return isfinite(q) ? quick_two_sum(q, rest / nh) : df{q, 0.f};
+}
+
+__device__ __forceinline__ void grad_add(const PrefScratch &x, uint64_t seq, df v) {
+  if (!(fabsf(v.hi) < kGradMost)) {
     x.bad[seq] = 1u;  // every writer writes the same
     return;
   }
-  const double h = rint(v * (1.0 / kHiUnit));
-  const double l = rint((v - h * kHiUnit) * (1.0 / kLoUnit));
-  if (h != 0.0) atomicAdd(&x.grad[seq].hi, (unsigned long long)(long long)h);
-  if (l != 0.0) atomicAdd(&x.grad[seq].lo, (unsigned long long)(long long)l);
+  const float h = rintf(v.hi * (1.f / kHiUnit));  // all of this is exact but for
+  const float rest = fmaf(-h, kHiUnit, v.hi);     // the roundings to whole units
+  const long long lo = __float2ll_rn(rest * (1.f / kLoUnit)) + __float2ll_rn(v.lo * (1.f / kLoUnit));
+  if (h != 0.f) atomicAdd(&x.grad[seq].hi, (unsigned long long)__float2ll_rn(h));
+  if (lo) atomicAdd(&x.grad[seq].lo, (unsigned long long)lo);
 }
 
 // Pairs first, first + step, ...: their losses, gradients and sums.
@@ -206,38 +255,42 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
       flag(ctrl, DEVERR_INDEX, (unsigned long long)((uint64_t)c >= in.s.n_seq ? c : j));
     } else {
       const Run rc = sequence_sum(in.s, x, c), rj = sequence_sum(in.s, x, j);
-      const double kc = r.average && rc.n ? 1.0 / (double)rc.n : 1.0;
-      const double kj = r.average && rj.n ? 1.0 / (double)rj.n : 1.0;
-      const double uc = pair_value(rc.v) * kc, uj = pair_value(rj.v) * kj;
-      const double h = uc - uj, d = r.beta * h - r.margin;
-      double g;  // by u of the chosen
-      if (r.kind == EDP_PREF_LOGISTIC) {
-        const float f = (float)d, e = expf(-fabsf(f));
-        const float tail = log1pf(e);  // -ln s(|d|)
-        const float up = tail + fmaxf(-f, 0.f), down = tail + fmaxf(f, 0.f);
-        const float m = (float)r.smooth;
-        l = m == 0.f ? up : fmaf(1.f - m, up, m * down);
-        // s(-d) (1 - e) - s(d) e = s(-d) - e
-        const float sd = f > 0.f ? e / (1.f + e) : 1.f / (1.f + e);
-        g = -r.beta * ((double)sd - r.smooth);
-      } else if (r.kind == EDP_PREF_HINGE) {
-        l = isnan(d) ? (float)d : (float)fmax(1.0 - d, 0.0);
-        g = d < 1.0 ? -r.beta : 0.0;
-      } else {
-        const double y = h - 0.5 / r.beta;
-        l = (float)(y * y);
-        g = 2.0 * y;
+      df uc = as_df(rc.v), uj = as_df(rj.v);
+      if (r.average) {
+        if (rc.n) uc = df_over(uc, rc.n);
+        if (rj.n) uj = df_over(uj, rj.n);
       }
-      if (isnan(d)) g = d;
-      grad_add(x, c, g * kc);
-      grad_add(x, j, -g * kj);
+      const df h = as_df(pair_join(Pair{uc.hi, uc.lo}, Pair{-uj.hi, -uj.lo}));
+      const df bh = df_mul(h, r.beta);
+      const float d = isfinite(bh.hi) ? df_add(bh, df{-r.margin.hi, -r.margin.lo}).hi : h.hi;
+      df g;  // by u of the chosen
+      if (r.kind == EDP_PREF_LOGISTIC) {
+        const float e = expf(-fabsf(d)), tail = log1pf(e);  // tail = -ln s(|d|)
+        const float up = tail + fmaxf(-d, 0.f), down = tail + fmaxf(d, 0.f);
+        l = r.smooth == 0.f ? up : fmaf(1.f - r.smooth, up, r.smooth * down);
+        // s(-d) (1 - e) - s(d) e = s(-d) - e
+        const float sd = d > 0.f ? e / (1.f + e) : 1.f / (1.f + e);
+        g = df{-r.beta.hi * (sd - r.smooth), 0.f};
+      } else if (r.kind == EDP_PREF_HINGE) {
+        const df y = df_add(df_add(df{1.f, 0.f}, r.margin), df{-bh.hi, -bh.lo});
+        l = y.hi > 0.f ? y.hi : isnan(d) ? d : d < 0.f ? -d : 0.f;
+        g = y.hi > 0.f ? df{-r.beta.hi, -r.beta.lo} : df{0.f, 0.f};
+      } else {
+        const df y = df_add(h, df{-r.half.hi, -r.half.lo});
+        l = isfinite(h.hi) ? y.hi * y.hi : h.hi * h.hi;
+        g = df{2.f * y.hi, 2.f * y.lo};
+      }
+      if (!isfinite(h.hi)) g = r.kind == EDP_PREF_SQUARE || isnan(d) ? df{h.hi, 0.f} : g;
+      grad_add(x, c, r.average && rc.n ? df_over(g, rc.n) : g);
+      const df m{-g.hi, -g.lo};
+      grad_add(x, j, r.average && rj.n ? df_over(m, rj.n) : m);
       pair_add(sum[0], l);
-      if (h > 0.0) pair_add(sum[1], 1.f);
-      const df bc = df_split(r.beta * uc), bj = df_split(r.beta * uj);
-      pair_add(sum[2], bc.hi);
-      pair_add(sum[2], bc.lo);
-      pair_add(sum[3], bj.hi);
-      pair_add(sum[3], bj.lo);
+      if (h.hi > 0.f) pair_add(sum[1], 1.f);
+      const df bc = df_mul(uc, r.beta), bj = df_mul(uj, r.beta);
+      pair_add(sum[2], isfinite(bc.hi) ? bc.hi : uc.hi);
+      if (isfinite(bc.hi)) pair_add(sum[2], bc.lo);
+      pair_add(sum[3], isfinite(bj.hi) ? bj.hi : uj.hi);
+      if (isfinite(bj.hi)) pair_add(sum[3], bj.lo);
     }
     if (out.pair_loss) out.pair_loss[i] = l;
   }
@@ -249,7 +302,8 @@ __device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
   if (!out.ratio) return;
   for (uint64_t q = first; q < in.s.n_seq; q += step) {
     const Run v = sequence_sum(in.s, x, q);
-    out.ratio[q] = (float)(pair_value(v.v) * (r.average && v.n ? 1.0 / (double)v.n : 1.0));
+    const df u = as_df(v.v);
+    out.ratio[q] = r.average && v.n ? df_over(u, v.n).hi : u.hi;
   }
 }
 
@@ -267,8 +321,8 @@ __device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, 
   const long long up = ((long long)g.y + (1ll << 41)) >> 42;
   const long long whole = (long long)g.x + up;
   const float h = (float)whole, rest = (float)(whole - (long long)h);
-  const float vh = h * (float)kHiUnit;
-  const float vl = fmaf(rest, (float)kHiUnit, (float)((long long)g.y - (up << 42)) * (float)kLoUnit);
+  const float vh = h * kHiUnit;
+  const float vl = fmaf(rest, kHiUnit, (float)((long long)g.y - (up << 42)) * kLoUnit);
   return fmaf(scale.hi, vh, fmaf(scale.hi, vl, scale.lo * vh));
 }
 
@@ -280,24 +334,57 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
   const TokenSet &s = in.s;
   const uint32_t n_seq = (uint32_t)s.n_seq;
   const int lane = threadIdx.x & 31;
+  stop = min(stop, s.n);
   SeqWalk walk;
-  if (begin < min(stop, end)) walk.start(s.off, n_seq, begin);
-  uint32_t known = 0xffffffffu;  // the sequence that g belongs to
-  float g = 0.f;
-  for (uint64_t t0 = begin; t0 < stop; t0 += kTile) {
+  uint64_t after = 0;           // where the sequence after the walk's ends
+  float here = 0.f, there = 0.f;  // gradients of both
+  bool known = false;
+  for (uint64_t t0 = begin; t0 < stop;) {
     const uint64_t t = t0 + 4 * lane;
-    const uint32_t bits = token_bits<VEC>(s, t, first, end);
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (t0 < end) {
-      walk.to(s.off, n_seq, t0);
-      if (t0 + kTile <= walk.next) {
-        if (walk.q != known) g = token_grad(x, walk.q, scale);
-        known = walk.q;
+      if (!known || t0 >= walk.next) {
+        if (known && after > t0) {
+          ++walk.q;
+          walk.next = after;
+          here = there;
+        } else {
+          if (known) walk.to(s.off, n_seq, t0);
+          else walk.start(s.off, n_seq, t0);
+          here = token_grad(x, walk.q, scale);
+        }
+        known = true;
+        // and what will be wanted at its end
+        const bool more = walk.q + 1 < n_seq;
+        after = more ? s.off[walk.q + 2] : walk.next;
+        there = more ? token_grad(x, walk.q + 1, scale) : 0.f;
+      }
+      // tiles within the sequence, kAtOnce of them in flight
+      const uint64_t top = min(walk.next, min(stop, end)), room = top > t0 ? top - t0 : 0;
+      if (VEC && t0 >= first && room >= kTile) {
+        const uint32_t m = (uint32_t)min(room / kTile, (uint64_t)kAtOnce);
+        uint32_t mk[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = bits >> i & 1u ? g : 0.f;
+        for (uint32_t k = 0; k < kAtOnce; ++k)
+          mk[k] = s.mask && k < m ? *reinterpret_cast<const uint32_t *>(s.mask + t + k * kTile)
+                                  : 0xffffffffu;
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k)
+          if (k < m)
+            *reinterpret_cast<float4 *>(dlogp + t + k * kTile) =
+                make_float4(mk[k] & 0xffu ? here : 0.f, mk[k] & 0xff00u ? here : 0.f,
+                            mk[k] & 0xff0000u ? here : 0.f, mk[k] & 0xff000000u ? here : 0.f);
+        t0 += m * kTile;
+        continue;
+      }
+      const uint32_t bits = token_bits<VEC>(s, t, first, end);
+      if (t0 + kTile <= after || after >= end) {  // two sequences
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = !(bits >> i & 1u) ? 0.f : t + i < walk.next ? here : there;
       } else {
-        SeqWalk ahead = walk;
-        ahead.to(s.off, n_seq, min(t0 + kTile, end) - 1);
+        SeqWalk to = walk;
+        to.to(s.off, n_seq, min(t0 + kTile, end) - 1);
         uint32_t q = walk.q;
         uint64_t next = 0;
         float each = 0.f;
@@ -305,21 +392,21 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
         for (int i = 0; i < 4; ++i) {
           if (!(bits >> i & 1u)) continue;
           if (t + i >= next) {
-            q = sequence_of(s.off, q, ahead.q + 1, t + i);
+            q = sequence_of(s.off, q, to.q + 1, t + i);
             next = s.off[q + 1];
             each = token_grad(x, q, scale);
           }
           v[i] = each;
         }
-        walk = ahead;
       }
     }
     store4<VEC>(dlogp, t, s.n, make_float4(v[0], v[1], v[2], v[3]));
+    t0 += kTile;
   }
 }
 
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kPerSm)
 k_pref_parts(PrefIn in, PrefScratch x) {
   pdl_wait();
   pdl_launch();
@@ -329,28 +416,31 @@ k_pref_parts(PrefIn in, PrefScratch x) {
 }
 
 __global__ void __launch_bounds__(kPairThreads)
-k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, Ctrl *ctrl) {
+k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, uint32_t pair_ctas, Ctrl *ctrl) {
   __shared__ Pair total[4];
   pdl_wait();
-  const uint32_t i = blockIdx.x * kPairThreads + threadIdx.x, step = gridDim.x * kPairThreads;
+  pdl_launch();
   Pair sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
-  take_pairs(in, r, x, out, i, step, sum, ctrl);
-  take_ratios(in, r, x, out, i, step);
-  pdl_launch();
+  if (blockIdx.x < pair_ctas)
+    take_pairs(in, r, x, out, blockIdx.x * kPairThreads + threadIdx.x, pair_ctas * kPairThreads,
+               sum, ctrl);
+  else
+    take_ratios(in, r, x, out, (blockIdx.x - pair_ctas) * kPairThreads + threadIdx.x,
+                (uint64_t)(gridDim.x - pair_ctas) * kPairThreads);
   if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
     write_loss(r, in.n_pair, total, out.loss);
 }
 
 template <bool VEC>
-__global__ void __launch_bounds__(kThreads)
-k_pref_grad(PrefIn in, PrefScratch x, df scale, float *dlogp) {
+__global__ void __launch_bounds__(kThreads, kGradPerSm)
+k_pref_grad(PrefIn in, PrefScratch x, df scale, uint32_t run, float *dlogp) {
   pdl_wait();
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
-  const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * x.run;
-  run_grad<VEC>(in, x, scale, dlogp, begin, min(begin + x.run, in.s.n), first, end);
+  const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * run;
+  run_grad<VEC>(in, x, scale, dlogp, begin, begin + run, first, end);
 }
 
 // All three steps of a batch of up to 4 kSmallThreads tokens, a tile per warp.
@@ -374,7 +464,7 @@ k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *
   if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
     write_loss(r, in.n_pair, total, out.loss);
   if (out.dlogp)
-    run_grad<VEC>(in, x, scale, out.dlogp, begin, min(begin + x.run, in.s.n), first, end);
+    run_grad<VEC>(in, x, scale, out.dlogp, begin, begin + x.run, first, end);
 }
 
 }  // namespace
@@ -387,12 +477,18 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   const uint64_t sms = (uint64_t)c->coop_sms;
   const bool small = set.n <= 4 * kSmallThreads && n_pair <= kSmallPairs;
   // a run per warp of a full chip, so that all end together
-  const uint64_t warps = kThreads / 32, chip = 3 * warps * sms;
-  uint64_t run = (set.n + chip - 1) / chip;
-  run = small ? kTile : run < kLeastRun ? kLeastRun : (run + kTile - 1) / kTile * kTile;
+  const uint64_t warps = kThreads / 32;
+  auto run_of = [&](uint64_t per_sm) {
+    const uint64_t chip = per_sm * warps * sms, each = (set.n + chip - 1) / chip;
+    return small ? (uint64_t)kTile : (each + kTile - 1) / kTile * kTile;
+  };
+  const uint64_t run = run_of(kPerSm), grad_run = run_of(kGradPerSm);
   const uint64_t runs = (set.n + run - 1) / run;
-  const uint64_t want = ((n_pair > set.n_seq ? n_pair : set.n_seq) + kPairThreads - 1) / kPairThreads;
-  const uint64_t pair_grid = want < 4 * sms ? want : 4 * sms;
+  auto ctas = [&](uint64_t n) {
+    const uint64_t want = (n + kPairThreads - 1) / kPairThreads;
+    return (uint32_t)(want < 4 * sms ? want : 4 * sms);
+  };
+  const uint32_t pair_ctas = ctas(n_pair), pair_grid = pair_ctas + (ratio ? ctas(set.n_seq) : 0);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t a = at;
@@ -409,12 +505,16 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   const PrefScratch x{(SeqPart *)(b + inner), (SeqPart *)(b + head), (SeqGrad *)(b + grad),
                       (uint32_t *)(b + bad), (Pair *)(b + part), (uint32_t)run};
   PrefRule r;
-  r.beta = cfg.beta;
-  r.smooth = cfg.label_smoothing;
-  r.margin = cfg.margin;
+  auto both = [](double v) {
+    const float hi = (float)v;
+    return df{hi, (float)(v - (double)hi)};
+  };
+  r.beta = both(cfg.beta);
+  r.smooth = (float)cfg.label_smoothing;
+  r.margin = both(cfg.margin);
+  r.half = both(0.5 / cfg.beta);
   r.norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
-  const double by = cfg.grad_scale / r.norm;
-  const df scale{(float)by, (float)(by - (double)(float)by)};
+  const df scale = both(cfg.grad_scale / r.norm);
   r.kind = cfg.kind;
   r.average = cfg.average;
   const PrefIn in{set, logp, ref, pair, n_pair};
@@ -428,11 +528,13 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   e = launch_pdl(vec ? k_pref_parts<true> : k_pref_parts<false>, dim3(grid), dim3(kThreads), s, in,
                  x);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(k_pref_pairs, dim3((unsigned)pair_grid), dim3(kPairThreads), s, in, r, x, out,
+  e = launch_pdl(k_pref_pairs, dim3(pair_grid), dim3(kPairThreads), s, in, r, x, out, pair_ctas,
                  c->ctrl);
   if (e != cudaSuccess || !dlogp) return e;
-  return launch_pdl(vec ? k_pref_grad<true> : k_pref_grad<false>, dim3(grid), dim3(kThreads), s,
-                    in, x, scale, dlogp);
+  const uint64_t grads = (set.n + grad_run - 1) / grad_run;
+  return launch_pdl(vec ? k_pref_grad<true> : k_pref_grad<false>,
+                    dim3((unsigned)((grads + warps - 1) / warps)), dim3(kThreads), s, in, x, scale,
+                    (uint32_t)grad_run, dlogp);
 }
 
 }  // namespace edp
