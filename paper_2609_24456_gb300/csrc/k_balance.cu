@@ -16,7 +16,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxExperts = 1024;
 constexpr uint64_t kOneCta = 32768;
-constexpr uint32_t kCountRows = 256;  // rows a CTA counts at a time
 constexpr float kProbUnits = 1099511627776.f;  // 2^40
 
 }  // namespace
@@ -44,21 +43,29 @@ struct BalanceArgs {
   uint64_t dstride;
 };
 
-// Rows r0, r0 + step, ... (each kCountRows) into hist; how many of them count.
-template <int NT>
-__device__ __forceinline__ uint32_t count_choices(const BalanceArgs &a, uint64_t r0, uint64_t step,
-                                                  uint32_t *hist, Ctrl *ctrl) {
+// Rows first, first + step, ... (a thread each) into hist; how many of them count.
+__device__ __forceinline__ uint32_t count_choices(const BalanceArgs &a, uint64_t first,
+                                                  uint64_t step, uint32_t *hist, Ctrl *ctrl) {
   uint32_t tokens = 0;
-  for (; r0 < a.rows; r0 += step) {
-    const uint32_t nr = (uint32_t)min((uint64_t)kCountRows, a.rows - r0);
-    for (uint32_t i = threadIdx.x; i < nr; i += NT) tokens += !a.mask || a.mask[r0 + i];
-    const int32_t *sel = a.sel + r0 * a.top;
-    for (uint32_t i = threadIdx.x; i < nr * a.top; i += NT) {
-      if (a.mask && !a.mask[r0 + i / a.top]) continue;
-      const int32_t e = sel[i];
-      if (e < 0) continue;
-      if ((uint32_t)e < a.E) atomicAdd(&hist[e], 1u);
-      else flag(ctrl, DEVERR_INDEX, (unsigned long long)e);
+  auto take = [&](int32_t e) {
+    if (e < 0) return;
+    if ((uint32_t)e < a.E) atomicAdd(&hist[e], 1u);
+    else flag(ctrl, DEVERR_INDEX, (unsigned long long)e);
+  };
+  const bool quads = a.top % 4 == 0 && ((uintptr_t)a.sel & 15u) == 0;
+  for (uint64_t t = first; t < a.rows; t += step) {
+    if (a.mask && !a.mask[t]) continue;
+    ++tokens;
+    const int32_t *sel = a.sel + t * a.top;
+    if (quads) {
+#pragma unroll 2
+      for (uint32_t k = 0; k < a.top; k += 4) {
+        const int4 e = *reinterpret_cast<const int4 *>(sel + k);
+        take(e.x), take(e.y), take(e.z), take(e.w);
+      }
+    } else {
+#pragma unroll 4
+      for (uint32_t k = 0; k < a.top; ++k) take(sel[k]);
     }
   }
   return tokens;
@@ -71,8 +78,8 @@ k_expert_counts(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   pdl_launch();
   for (uint32_t e = threadIdx.x; e < a.E; e += kThreads) hist[e] = 0;
   __syncthreads();
-  uint32_t n = count_choices<kThreads>(a, (uint64_t)blockIdx.x * kCountRows,
-                                       (uint64_t)gridDim.x * kCountRows, hist, ctrl);
+  uint32_t n = count_choices(a, (uint64_t)blockIdx.x * kThreads + threadIdx.x,
+                             (uint64_t)gridDim.x * kThreads, hist, ctrl);
   n = __reduce_add_sync(kAllLanes, n);
   if ((threadIdx.x & 31) == 0 && n) atomicAdd(&sums->tokens, (unsigned long long)n);
   __syncthreads();
@@ -80,18 +87,25 @@ k_expert_counts(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
     if (hist[e]) atomicAdd(&sums->count[e], hist[e]);
 }
 
+// CTAs per SM, by the elements of a lane.
+template <int N>
+constexpr int kBalancePerSm = N <= 4 ? 6 : N <= 8 ? 4 : N <= 16 ? 3 : N <= 32 ? 2 : 1;
+
 // L lanes per row, V loads of VN elements per lane: element i of lane l is in
 // column ((i / VN) L + l) VN + i % VN.
 template <typename T, int VN>
-__device__ __forceinline__ void load_row(const T *p, float (&v)[VN]) {
-  if constexpr (VN == 1) {
-    v[0] = to_f32(*p);
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4 *>(p);
-    const T *x = reinterpret_cast<const T *>(&w);
+struct Raw {
+  using type = uint4;
+};
+template <typename T>
+struct Raw<T, 1> {
+  using type = T;
+};
+template <typename T, int VN>
+__device__ __forceinline__ void unpack_row(const typename Raw<T, VN>::type &w, float (&v)[VN]) {
+  const T *x = reinterpret_cast<const T *>(&w);
 #pragma unroll
-    for (int i = 0; i < VN; ++i) v[i] = to_f32(x[i]);
-  }
+  for (int i = 0; i < VN; ++i) v[i] = to_f32(x[i]);
 }
 template <typename T, int VN>
 __device__ __forceinline__ void store_row(T *p, const float (&v)[VN]) {
@@ -106,26 +120,68 @@ __device__ __forceinline__ void store_row(T *p, const float (&v)[VN]) {
   }
 }
 
-// ONE: a single CTA, which counts the choices itself.
+__device__ __forceinline__ void copy16(void *shared, const void *global) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(shared)), "l"(global)
+               : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// ONE: a single CTA, which counts the choices itself.  Otherwise a lane's vectors
+// of its next rows are on their way to shared memory, in slots of its own: rows in
+// flight then cost no registers (71 MB of logits and gradients of 128 experts:
+// 44 us with one row ahead in registers).
 template <typename T, int L, int V, int VN, int NT, bool ONE>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, ONE ? 1 : kBalancePerSm<V * VN>)
 k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   constexpr int N = V * VN, kGroups = NT / L, kWarps = NT / 32;
   constexpr uint32_t kCols = (uint32_t)N * L;  // columns with room for all experts
-  __shared__ float col[kWarps][kCols <= kMaxExperts ? kCols : kMaxExperts];
+  constexpr int kDepth = ONE || VN == 1 ? 1 : V >= 8 ? 1 : V == 4 ? 2 : 4;
+  constexpr bool kRing = kDepth > 1;
+  constexpr size_t kRingBytes = kRing ? (size_t)kDepth * V * NT * 16 : 16;
+  constexpr size_t kColBytes = (size_t)kWarps * kCols * sizeof(float);
+  __shared__ alignas(16) uint8_t room[kRingBytes > kColBytes ? kRingBytes : kColBytes];
+  __shared__ alignas(16) float fs[kCols];
   __shared__ uint32_t hist[ONE ? kMaxExperts : 1];
   __shared__ uint32_t one_tokens;
   __shared__ bool last;
-  pdl_wait();
-  if (ONE) pdl_launch();
+  float(*col)[kCols] = reinterpret_cast<float(*)[kCols]>(room);  // once the ring is empty
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int l = threadIdx.x % L;
+  const uint64_t step = (uint64_t)gridDim.x * kGroups;
+  // the warp's groups take neighbouring rows and leave together
+  uint64_t t0 = (uint64_t)blockIdx.x * kGroups + (threadIdx.x / 32) * (32 / L);
+  using W = typename Raw<T, VN>::type;
+  W *ring = reinterpret_cast<W *>(room);
+  auto slot = [&](uint32_t d, int k) { return ((d % kDepth) * V + k) * NT + threadIdx.x; };
+  auto fetch = [&](uint64_t t, uint32_t d) {
+    if constexpr (kRing) {
+      const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const uint32_t e = ((uint32_t)k * L + l) * VN;
+        if (t < a.rows && e < a.E) copy16(&ring[slot(d, k)], row + e);
+      }
+      copies_end();
+    }
+  };
+  // Only the counts come from the kernel before, which waited for all that came
+  // before it: the first rows may be on their way while it runs.
+  if (ONE) pdl_wait();
+  uint32_t ahead = 0;
+  if constexpr (kRing)
+    for (; ahead < kDepth - 1; ++ahead) fetch(t0 + lane / L + ahead * step, ahead);
+  if (!ONE) pdl_wait();
+  if (ONE) pdl_launch();
   unsigned long long tokens;
   if (ONE) {
     for (uint32_t e = threadIdx.x; e < a.E; e += NT) hist[e] = 0;
     if (threadIdx.x == 0) one_tokens = 0;
     __syncthreads();
-    uint32_t n = count_choices<NT>(a, 0, kCountRows, hist, ctrl);
+    uint32_t n = count_choices(a, threadIdx.x, NT, hist, ctrl);
     n = __reduce_add_sync(kAllLanes, n);
     if (lane == 0 && n) atomicAdd(&one_tokens, n);
     __syncthreads();
@@ -136,44 +192,55 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   const float inv_n = 1.f / (float)(tokens ? tokens : 1);
   const float per = (float)a.E / (float)a.top * inv_n;  // f_e = counts[e] * per
   const float scale = a.scale * inv_n;
-  float f[N], ps[N];
+  for (uint32_t e = threadIdx.x; e < kCols; e += NT)
+    fs[e] = e < a.E ? (float)(ONE ? hist[e] : __ldcg(&sums->count[e])) * per : 0.f;
+  __syncthreads();
+  float ps[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t e = ((uint32_t)(i / VN) * L + l) * VN + i % VN;
-    f[i] = e < a.E ? (float)(ONE ? hist[e] : __ldcg(&sums->count[e])) * per : 0.f;
-    ps[i] = 0.f;
-  }
+  for (int i = 0; i < N; ++i) ps[i] = 0.f;
   bool nan = false;
-  const uint64_t step = (uint64_t)gridDim.x * kGroups;
-  // the warp's groups take neighbouring rows and leave together
-  for (uint64_t t0 = (uint64_t)blockIdx.x * kGroups + (threadIdx.x / 32) * (32 / L); t0 < a.rows;
-       t0 += step) {
+  bool next = t0 + lane / L < a.rows && (!a.mask || a.mask[t0 + lane / L]);
+  for (uint32_t d = 0; t0 < a.rows; t0 += step, ++d) {
     const uint64_t t = t0 + lane / L;
-    const bool in = t < a.rows, use = in && (!a.mask || a.mask[t]);
+    const bool in = t < a.rows, use = next;
+    next = t + step < a.rows && (!a.mask || a.mask[t + step]);
+    // a masked row is loaded too: whatever it holds goes no further
+    W w[V];
+    if constexpr (kRing) {
+      fetch(t + (kDepth - 1) * step, d + kDepth - 1);
+      copies_wait<kDepth - 1>();
+#pragma unroll
+      for (int k = 0; k < V; ++k) w[k] = ring[slot(d, k)];
+    } else {
+      const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const uint32_t e = ((uint32_t)k * L + l) * VN;
+        if (in && e < a.E) w[k] = *reinterpret_cast<const W *>(row + e);
+      }
+    }
     float y[N], m = kNegInf;
-    const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const uint32_t e = ((uint32_t)k * L + l) * VN;
       float v[VN];
-#pragma unroll
-      for (int i = 0; i < VN; ++i) v[i] = kNegInf;
-      if (use && e < a.E) load_row<T, VN>(row + e, v);
+      unpack_row<T, VN>(w[k], v);
 #pragma unroll
       for (int i = 0; i < VN; ++i) {
-        y[k * VN + i] = v[i];
-        m = fmaxf(m, v[i]);
+        y[k * VN + i] = use && e < a.E ? v[i] : kNegInf;
+        m = fmaxf(m, y[k * VN + i]);
       }
     }
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
     if (m == kNegInf) m = 0.f;
     float s = 0.f, fp = 0.f;
+    auto f = [&](int i) { return fs[((uint32_t)(i / VN) * L + l) * VN + i % VN]; };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       y[i] = ex2((y[i] - m) * (float)kLog2e);
       s += y[i];
-      fp = fmaf(y[i], f[i], fp);
+      fp = fmaf(y[i], f(i), fp);
     }
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) {
@@ -196,13 +263,15 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
         const uint32_t e = ((uint32_t)k * L + l) * VN;
         float v[VN];
 #pragma unroll
-        for (int i = 0; i < VN; ++i) v[i] = scale * y[k * VN + i] * (f[k * VN + i] - fp);
+        for (int i = 0; i < VN; ++i) v[i] = scale * y[k * VN + i] * (f(k * VN + i) - fp);
         if (e < a.E) store_row<T, VN>(d + e, v);
       }
     }
   }
   if (!ONE) pdl_launch();
   if (nan) atomicExch(&sums->nan, 1u);
+  if constexpr (kRing) copies_wait<0>();
+  __syncthreads();  // the ring's room is free
   // over the warp's groups, then its CTA's warps, in order
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -261,14 +330,14 @@ cudaError_t launch_shape(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cu
     return launch_pdl(k_balance<T, L, V, VN, NT, true>, dim3(1), dim3(NT), s, a, sums, c->ctrl);
   }
   const uint64_t sms = (uint64_t)c->coop_sms;
-  const uint64_t cb = (a.rows + kCountRows - 1) / kCountRows;
-  cudaError_t e = launch_pdl(k_expert_counts, dim3((unsigned)(cb < sms ? cb : sms)),
+  const uint64_t cb = (a.rows + kThreads - 1) / kThreads;
+  cudaError_t e = launch_pdl(k_expert_counts, dim3((unsigned)(cb < 4 * sms ? cb : 4 * sms)),
                              dim3(kThreads), s, a, sums, c->ctrl);
   if (e != cudaSuccess) return e;
   const uint64_t b = (a.rows * L + kThreads - 1) / kThreads;
+  const uint64_t wave = kBalancePerSm<V * VN> * sms;
   return launch_pdl(k_balance<T, L, V, VN, kThreads, false>,
-                    dim3((unsigned)(b < 4 * sms ? b : 4 * sms)), dim3(kThreads), s, a, sums,
-                    c->ctrl);
+                    dim3((unsigned)(b < wave ? b : wave)), dim3(kThreads), s, a, sums, c->ctrl);
 }
 
 template <typename T>
@@ -278,13 +347,13 @@ cudaError_t launch_type(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cud
   const bool vec = ((uintptr_t)a.z | (uintptr_t)a.dz | a.E * bytes | a.stride * bytes |
                     (a.dz ? a.dstride * bytes : 0)) % 16 == 0;
   if (vec) {
-    const uint32_t n = a.E / VN;  // vectors of a row
+    const uint32_t n = a.E / VN;  // vectors of a row, two per lane
     if (n <= 1) return launch_shape<T, 1, 1, VN>(c, a, sums, s);
-    if (n <= 2) return launch_shape<T, 2, 1, VN>(c, a, sums, s);
-    if (n <= 4) return launch_shape<T, 4, 1, VN>(c, a, sums, s);
-    if (n <= 8) return launch_shape<T, 8, 1, VN>(c, a, sums, s);
-    if (n <= 16) return launch_shape<T, 16, 1, VN>(c, a, sums, s);
-    if (n <= 32) return launch_shape<T, 32, 1, VN>(c, a, sums, s);
+    if (n <= 2) return launch_shape<T, 1, 2, VN>(c, a, sums, s);
+    if (n <= 4) return launch_shape<T, 2, 2, VN>(c, a, sums, s);
+    if (n <= 8) return launch_shape<T, 4, 2, VN>(c, a, sums, s);
+    if (n <= 16) return launch_shape<T, 8, 2, VN>(c, a, sums, s);
+    if (n <= 32) return launch_shape<T, 16, 2, VN>(c, a, sums, s);
     if (n <= 64) return launch_shape<T, 32, 2, VN>(c, a, sums, s);
     if (n <= 128) return launch_shape<T, 32, 4, VN>(c, a, sums, s);
     if constexpr (VN == 4) return launch_shape<T, 32, 8, VN>(c, a, sums, s);
