@@ -8,6 +8,8 @@
 // element, where rows do not lie on 16-byte boundaries); the softmax stays in
 // registers.  Counts and probabilities add up over CTAs as whole numbers, in
 // any order to the same bits.  Up to kOneCta elements one CTA does both steps.
+#include <type_traits>
+
 #include "edp_loss.cuh"
 
 namespace edp {
@@ -106,6 +108,36 @@ __device__ __forceinline__ void unpack_row(const typename Raw<T, VN>::type &w, f
   const T *x = reinterpret_cast<const T *>(&w);
 #pragma unroll
   for (int i = 0; i < VN; ++i) v[i] = to_f32(x[i]);
+}
+// A vector of -infinity.
+template <typename T, int VN>
+__device__ __forceinline__ typename Raw<T, VN>::type lowest_row() {
+  if constexpr (VN == 1) {
+    return from_f32<T>(kNegInf);
+  } else {
+    const uint32_t x = sizeof(T) == 4 ? 0xff800000u
+                       : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+    return make_uint4(x, x, x, x);
+  }
+}
+// The largest element (NaN apart), of 16-bit types two at a time.
+template <typename T, int V, int VN>
+__device__ __forceinline__ float row_max(const typename Raw<T, VN>::type (&w)[V]) {
+  if constexpr (VN == 8) {
+    using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2,
+                                         __nv_bfloat162>::type;
+    const T2 *x = reinterpret_cast<const T2 *>(w);
+    T2 m = x[0];
+#pragma unroll
+    for (int i = 1; i < 4 * V; ++i) m = __hmax2(m, x[i]);
+    return fmaxf(to_f32(m.x), to_f32(m.y));
+  } else {
+    const T *x = reinterpret_cast<const T *>(w);
+    float m = to_f32(x[0]);
+#pragma unroll
+    for (int i = 1; i < V * VN; ++i) m = fmaxf(m, to_f32(x[i]));
+    return m;
+  }
 }
 template <typename T, int VN>
 __device__ __forceinline__ void store_row(T *p, const float (&v)[VN]) {
@@ -219,17 +251,17 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
         if (in && e < a.E) w[k] = *reinterpret_cast<const W *>(row + e);
       }
     }
-    float y[N], m = kNegInf;
+    // what is not used is -infinity
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (!use || ((uint32_t)k * L + l) * VN >= a.E) w[k] = lowest_row<T, VN>();
+    float y[N], m = row_max<T, V, VN>(w);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint32_t e = ((uint32_t)k * L + l) * VN;
       float v[VN];
       unpack_row<T, VN>(w[k], v);
 #pragma unroll
-      for (int i = 0; i < VN; ++i) {
-        y[k * VN + i] = use && e < a.E ? v[i] : kNegInf;
-        m = fmaxf(m, y[k * VN + i]);
-      }
+      for (int i = 0; i < VN; ++i) y[k * VN + i] = v[i];
     }
 #pragma unroll
     for (int o = L / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
@@ -249,21 +281,19 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
     }
     if (use && s == 0.f && l == 0) flag(ctrl, DEVERR_ROW, t);  // no distribution: p = 0
     const float inv = s == 0.f ? 0.f : 1.f / s;
-    fp *= inv;
     nan |= isnan(inv);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      y[i] = __fmul_rn(y[i], inv);  // the same sums whether a gradient follows or not
-      ps[i] = __fadd_rn(ps[i], y[i]);
-    }
+    for (int i = 0; i < N; ++i) ps[i] = fmaf(y[i], inv, ps[i]);
     if (a.dz && in) {
+      // p (f - sum f p) = (y / s) (f - fp / s)
+      const float by = scale * inv, less = -by * (fp * inv);
       T *d = reinterpret_cast<T *>(a.dz) + t * a.dstride;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const uint32_t e = ((uint32_t)k * L + l) * VN;
         float v[VN];
 #pragma unroll
-        for (int i = 0; i < VN; ++i) v[i] = scale * y[k * VN + i] * (f(k * VN + i) - fp);
+        for (int i = 0; i < VN; ++i) v[i] = y[k * VN + i] * fmaf(f(k * VN + i), by, less);
         if (e < a.E) store_row<T, VN>(d + e, v);
       }
     }
