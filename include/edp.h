@@ -548,7 +548,7 @@ typedef enum { EDP_F32 = 0, EDP_BF16 = 1, EDP_F16 = 2 } edp_dtype;
  * -infinity, are written as 0 (S as 0) and reported by edp_sync
  * (EDP_ERR_INVALID).  NaN or +infinity in a row makes its outputs NaN.
  * Errors: EDP_ERR_INVALID for an unknown dtype, vocab == 0, stride < vocab,
- * rows or vocab >= 2^31, temperature not finite or not > 0, a NULL logits,
+ * rows or vocab >= 2^31, temperature outside [1e-6, 1e6], a NULL logits,
  * target or logp, arrays outside device memory, or logits not aligned to their
  * type.  rows == 0 does nothing. */
 EDP_API edp_status edp_token_logprob(edp_ctx *ctx, const void *logits, uint32_t dtype,

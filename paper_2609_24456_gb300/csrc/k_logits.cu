@@ -5,8 +5,12 @@
 // With z the row, T the temperature and m = max z, everything is in powers of
 // two: y_j = (z_j - m) log2(e) / T, S = sum 2^y_j, U = sum 2^y_j y_j, so that
 //   logp = (z_t - m) / T - ln S,  H = ln S - ln2 U / S,  p_j = 2^y_j / S.
-// One pass keeps (m, S, U) per thread; a larger maximum rescales S and U.
+// One pass keeps (m, S, U) per thread; a larger maximum rescales S and U.  Two
+// elements at a time where the instructions allow (F2), since the pass is as much
+// bound by issue as by memory.
 #include <cooperative_groups.h>
+
+#include <type_traits>
 
 #include "edp_loss.cuh"
 
@@ -21,64 +25,196 @@ constexpr int kUnroll = 4;  // 16-byte loads in flight per thread
 
 constexpr float kNoLog = -1e4f;  // stands for logarithms whose power of 2 is 0 in fp32
 
-// Running maximum and sums of a part of a row.
+// The difference z - m and its product with c cost an instruction more than one
+// fused z c - (m c), whose rounding of m c is the same for all of a row and is
+// taken out at its end.  The fused form overflows near the ends of fp32: a
+// bfloat16 row with a maximum beyond kFusedMost goes the careful way, as fp32
+// rows do.
+constexpr float kFusedMost = 1e29f;
+template <typename T>
+constexpr bool kFused = sizeof(T) == 2;
+
+// Two fp32 numbers in a 64-bit register: both in one instruction, each rounded as
+// on its own.
+struct F2 {
+  unsigned long long v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float x, float y) {
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+  }
+  __device__ __forceinline__ explicit F2(float x) : F2(x, x) {}
+  __device__ __forceinline__ float x() const {
+    float a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+    return a;
+  }
+  __device__ __forceinline__ float y() const {
+    float a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+    return b;
+  }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 ex2_both(F2 a) { return F2(ex2(a.x()), ex2(a.y())); }
+
+// A 16-byte vector as pairs of fp32 numbers.
+template <typename T>
+struct Vec16 {
+  static constexpr int kN = 16 / sizeof(T), kPairs = kN / 2;
+  __device__ static __forceinline__ F2 pair(const uint4 &w, int i) {
+    const T *x = reinterpret_cast<const T *>(&w);
+    return F2(to_f32(x[2 * i]), to_f32(x[2 * i + 1]));
+  }
+  __device__ static __forceinline__ void set(uint4 &w, int i, F2 v) {
+    T *x = reinterpret_cast<T *>(&w);
+    x[2 * i] = from_f32<T>(v.x());
+    x[2 * i + 1] = from_f32<T>(v.y());
+  }
+  // NaN apart
+  __device__ static __forceinline__ float max(const uint4 &w) {
+    float m = to_f32(reinterpret_cast<const T *>(&w)[0]);
+#pragma unroll
+    for (int i = 1; i < kN; ++i) m = fmaxf(m, to_f32(reinterpret_cast<const T *>(&w)[i]));
+    return m;
+  }
+};
+template <typename T2>
+__device__ __forceinline__ float max_of_pairs(const uint4 &w) {
+  const T2 *x = reinterpret_cast<const T2 *>(&w);
+  const T2 m = __hmax2(__hmax2(x[0], x[1]), __hmax2(x[2], x[3]));
+  return fmaxf(to_f32(m.x), to_f32(m.y));
+}
+template <>
+__device__ __forceinline__ float Vec16<__nv_bfloat16>::max(const uint4 &w) {
+  return max_of_pairs<__nv_bfloat162>(w);
+}
+template <>
+__device__ __forceinline__ float Vec16<__half>::max(const uint4 &w) {
+  return max_of_pairs<__half2>(w);
+}
+template <>
+__device__ __forceinline__ F2 Vec16<__nv_bfloat16>::pair(const uint4 &w, int i) {
+  const uint32_t x = (&w.x)[i];
+  return F2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ void Vec16<__nv_bfloat16>::set(uint4 &w, int i, F2 v) {
+  (&w.x)[i] = pack_bf16x2(v.x(), v.y());
+}
+template <>
+__device__ __forceinline__ void Vec16<__half>::set(uint4 &w, int i, F2 v) {
+  const __half2 h = __floats2half2_rn(v.x(), v.y());
+  (&w.x)[i] = *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Logarithms of a row relative to its maximum m.
+template <typename T, bool FUSED>
+struct RowLog {
+  float c, less;  // y = z c - less, or (z - less) c
+  __device__ __forceinline__ RowLog(float m, float c_) : c(c_) {
+    const bool none = m == kNegInf;  // nothing but -infinity so far
+    if (FUSED && std::is_same<T, __nv_bfloat16>::value) less = fmaxf(m, -kFusedMost) * c;
+    else if (FUSED) less = none ? 0.f : m * c;
+    else less = none ? 0.f : m;
+  }
+  __device__ __forceinline__ float of(float z) const {
+    return FUSED ? fmaf(z, c, -less) : (z - less) * c;
+  }
+  __device__ __forceinline__ F2 of(F2 z) const {
+    return FUSED ? fma2(z, F2(c), F2(-less)) : (z + F2(-less)) * F2(c);
+  }
+  // what takes logarithms relative to `from` to these
+  __device__ __forceinline__ float shift(const RowLog &from) const {
+    return FUSED ? from.less - less : (from.less - less) * c;
+  }
+};
+
+// -infinity has no product with its 0: a finite number stands for it, in bfloat16
+// before the logarithm (two at a time), else after.
+template <typename T, bool FUSED>
+__device__ __forceinline__ uint4 finite_words(uint4 w) {
+  if constexpr (FUSED && std::is_same<T, __nv_bfloat16>::value) {
+    const __nv_bfloat162 low = __float2bfloat162_rn(-10.f * kFusedMost);
+    __nv_bfloat162 *x = reinterpret_cast<__nv_bfloat162 *>(&w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __hmax2_nan(x[i], low);
+  }
+  return w;
+}
+template <typename T, bool FUSED>
+__device__ __forceinline__ F2 finite_log(F2 y) {
+  if constexpr (FUSED && std::is_same<T, __nv_bfloat16>::value) return y;
+  return F2(fmaxf(y.x(), kNoLog), fmaxf(y.y(), kNoLog));
+}
+
+// Running maximum and sums of a part of a row: S and U relative to the maximum.
 struct RowSum {
   float m, s, u;
 };
 
+template <typename T, bool FUSED>
 __device__ __forceinline__ RowSum row_join(RowSum a, RowSum b, float c) {
   const float m = fmaxf(a.m, b.m);
-  if (m == kNegInf) return {m, a.s + b.s, a.u + b.u};  // NaN among them stays
-  const float da = a.m == kNegInf ? 0.f : (a.m - m) * c;
-  const float db = b.m == kNegInf ? 0.f : (b.m - m) * c;
-  const float fa = ex2(da), fb = ex2(db);
-  // 2^(y + d) (y + d): a part whose factor underflowed has no product either
-  const float ua = fa > 0.f ? fa * fmaf(da, a.s, a.u) : 0.f;
-  const float ub = fb > 0.f ? fb * fmaf(db, b.s, b.u) : 0.f;
+  const RowLog<T, FUSED> log(m, c);
+  const float da = a.m == m ? 0.f : log.shift(RowLog<T, FUSED>(a.m, c));
+  const float db = b.m == m ? 0.f : log.shift(RowLog<T, FUSED>(b.m, c));
+  const float fa = a.m == kNegInf ? 1.f : ex2(da), fb = b.m == kNegInf ? 1.f : ex2(db);
+  // 2^(y + d) (y + d): a part whose factor underflowed has no product either, and
+  // one without a maximum has sums of 0 (or NaN, which stays)
+  const float ua = a.m == kNegInf ? a.u : fa > 0.f ? fa * fmaf(da, a.s, a.u) : 0.f;
+  const float ub = b.m == kNegInf ? b.u : fb > 0.f ? fb * fmaf(db, b.s, b.u) : 0.f;
   return {m, fmaf(fa, a.s, fb * b.s), ua + ub};
 }
 
-// N elements of one thread.
-template <bool ENT, int N>
-__device__ __forceinline__ void row_take(RowSum &a, const float (&v)[N], float c) {
-  float m = v[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+// A thread's sums, of even and odd places apart.
+struct LaneSum {
+  float m;
+  F2 s, u;
+};
+template <typename T, bool ENT, bool FUSED>
+__device__ __forceinline__ RowLog<T, FUSED> raise(LaneSum &a, float m, float c) {
   if (m > a.m) {
     if (a.m != kNegInf) {
-      const float d = (a.m - m) * c, f = ex2(d);
-      if (ENT) a.u = f > 0.f ? f * fmaf(d, a.s, a.u) : 0.f;
-      a.s *= f;
+      const float d = RowLog<T, FUSED>(m, c).shift(RowLog<T, FUSED>(a.m, c)), f = ex2(d);
+      if (ENT) a.u = f > 0.f ? F2(f) * fma2(F2(d), a.s, a.u) : F2(0.f);
+      a.s = F2(f) * a.s;
     }
     a.m = m;
   }
-  const float mm = a.m == kNegInf ? 0.f : a.m;
+  return RowLog<T, FUSED>(a.m, c);
+}
+// K vectors of one thread.
+template <typename T, bool ENT, bool FUSED, int K>
+__device__ __forceinline__ void take_vectors(LaneSum &a, const uint4 (&w)[K], float c) {
+  float m = Vec16<T>::max(w[0]);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float y = (v[i] - mm) * c;
-    const float e = ex2(y);
-    a.s += e;
-    // -infinity has no product
-    if (ENT) a.u = fmaf(e, fmaxf(y, kNoLog), a.u);
+  for (int k = 1; k < K; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
+  const RowLog<T, FUSED> log = raise<T, ENT, FUSED>(a, m, c);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint4 x = ENT ? finite_words<T, FUSED>(w[k]) : w[k];
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::kPairs; ++i) {
+      const F2 y = log.of(Vec16<T>::pair(x, i)), e = ex2_both(y);
+      a.s = a.s + e;
+      if (ENT) a.u = fma2(e, finite_log<T, FUSED>(y), a.u);
+    }
   }
 }
-
-template <typename T>
-struct Vec16 {
-  static constexpr int kN = 16 / sizeof(T);
-  __device__ static __forceinline__ void unpack(const uint4 &w, float (&v)[kN]) {
-    const T *x = reinterpret_cast<const T *>(&w);
-#pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] = to_f32(x[i]);
-  }
-  __device__ static __forceinline__ uint4 pack(const float (&v)[kN]) {
-    uint4 w;
-    T *x = reinterpret_cast<T *>(&w);
-#pragma unroll
-    for (int i = 0; i < kN; ++i) x[i] = from_f32<T>(v[i]);
-    return w;
-  }
-};
 
 // Elements [0, n) at p as those before the first 16-byte boundary, vectors, rest.
 template <typename T>
@@ -91,16 +227,16 @@ struct Span {
   }
 };
 
-template <typename T, bool ENT>
+template <typename T, bool ENT, bool FUSED>
 __device__ __forceinline__ RowSum part_sum(const T *p, uint32_t n, float c) {
   constexpr int N = Vec16<T>::kN;
-  RowSum a{kNegInf, 0.f, 0.f};
+  LaneSum a{kNegInf, F2(0.f), F2(0.f)};
   const Span<T> sp(p, n);
   if (threadIdx.x < sp.head + sp.tail) {
-    const uint32_t i = threadIdx.x < sp.head ? threadIdx.x
-                                             : threadIdx.x + sp.vecs * N;
-    const float v[1] = {to_f32(p[i])};
-    row_take<ENT, 1>(a, v, c);
+    const float v = to_f32(p[threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * N]);
+    const float y = raise<T, ENT, FUSED>(a, v, c).of(v), e = ex2(y);
+    a.s = a.s + F2(e, 0.f);
+    if (ENT) a.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), a.u);
   }
   const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
   uint32_t i = threadIdx.x;
@@ -108,34 +244,36 @@ __device__ __forceinline__ RowSum part_sum(const T *p, uint32_t n, float c) {
     uint4 w[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * kRowThreads];
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      float v[N];
-      Vec16<T>::unpack(w[k], v);
-      row_take<ENT, N>(a, v, c);
-    }
+    take_vectors<T, ENT, FUSED>(a, w, c);
   }
   for (; i < sp.vecs; i += kRowThreads) {
-    float v[N];
-    Vec16<T>::unpack(q[i], v);
-    row_take<ENT, N>(a, v, c);
+    const uint4 w[1] = {q[i]};
+    take_vectors<T, ENT, FUSED>(a, w, c);
   }
-  return a;
+  return {a.m, a.s.x() + a.s.y(), a.u.x() + a.u.y()};
 }
 
 // The CTA's sum, in thread 0; joined by lanes and warps in a fixed order.
+template <typename T, bool FUSED>
 __device__ __forceinline__ RowSum cta_join(RowSum a, float c, RowSum *red) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
-    const RowSum b{__shfl_down_sync(kAllLanes, a.m, o), __shfl_down_sync(kAllLanes, a.s, o),
-                   __shfl_down_sync(kAllLanes, a.u, o)};
-    a = row_join(a, b, c);
+    const RowSum b{__shfl_xor_sync(kAllLanes, a.m, o), __shfl_xor_sync(kAllLanes, a.s, o),
+                   __shfl_xor_sync(kAllLanes, a.u, o)};
+    a = row_join<T, FUSED>(a, b, c);
   }
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   if (lane == 0) red[wid] = a;
   __syncthreads();
-  if (threadIdx.x == 0)
-    for (int w = 1; w < kRowWarps; ++w) a = row_join(a, red[w], c);
+  if (wid == 0) {
+    a = lane < kRowWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f};
+#pragma unroll
+    for (int o = kRowWarps / 2; o; o >>= 1) {
+      const RowSum b{__shfl_xor_sync(kAllLanes, a.m, o), __shfl_xor_sync(kAllLanes, a.s, o),
+                     __shfl_xor_sync(kAllLanes, a.u, o)};
+      a = row_join<T, FUSED>(a, b, c);
+    }
+  }
   return a;
 }
 
@@ -156,10 +294,25 @@ __device__ __forceinline__ Row row_kind(const int32_t *target, const uint8_t *ma
   return x < 0 ? Row::kSkip : (uint32_t)x >= vocab ? Row::kBad : Row::kUse;
 }
 
+// Whether a row's sums hold (see kFusedMost); without a maximum they are 0.
+template <typename T>
+__device__ __forceinline__ bool sums_hold(const RowSum &a) {
+  return !std::is_same<T, __nv_bfloat16>::value || a.m == kNegInf || fabsf(a.m) <= kFusedMost;
+}
+// The sums relative to m itself, not to the rounded m c.
+template <typename T>
+__device__ __forceinline__ RowSum exact_sums(RowSum a, float c) {
+  if (!kFused<T> || a.m == kNegInf) return a;
+  const float d = -fmaf(a.m, c, -(a.m * c));
+  a.u = fmaf(d, a.s, a.u);  // 2^d is 1 + d ln 2 to 2^-38
+  const float f = d * kLn2;
+  return {a.m, fmaf(f, a.s, a.s), fmaf(f, a.u, a.u)};
+}
+
 struct RowOut {
   float logp, entropy, m, s;
 };
-// What the whole row's sum says (S = 0: no distribution).
+// What the whole row's sums say (S = 0: no distribution).
 __device__ __forceinline__ RowOut row_out(const RowSum &a, float zt, float inv_t) {
   if (a.m == kNegInf && !(a.s != a.s)) return {0.f, 0.f, 0.f, 0.f};
   const float ln = logf(a.s);
@@ -190,6 +343,7 @@ __global__ void __launch_bounds__(kRowThreads)
 k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl) {
   __shared__ RowSum red[kRowWarps];
   __shared__ RowSum parts[8];
+  __shared__ RowSum whole;
   pdl_wait();
   pdl_launch();
   const uint64_t t = blockIdx.x;
@@ -208,7 +362,8 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
   if (np > 1) cluster_arrive();
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
-  RowSum sum = cta_join(part_sum<T, ENT>(row + first, n, a.c), a.c, red);
+  constexpr bool F = kFused<T>;
+  RowSum sum = cta_join<T, F>(part_sum<T, ENT, F>(row + first, n, a.c), a.c, red);
   if (np > 1) {
     cluster_wait();  // every CTA has started, so that its shared memory is there
     if (threadIdx.x == 0) cg::this_cluster().map_shared_rank(parts, 0)[part] = sum;
@@ -216,7 +371,14 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
     cluster_wait();
     if (part) return;
     if (threadIdx.x == 0)
-      for (uint32_t k = 1; k < np; ++k) sum = row_join(sum, parts[k], a.c);
+      for (uint32_t k = 1; k < np; ++k) sum = row_join<T, F>(sum, parts[k], a.c);
+  }
+  if (F) {
+    if (threadIdx.x == 0) whole = exact_sums<T>(sum, a.c);
+    __syncthreads();
+    sum = whole;
+    if (!sums_hold<T>(sum))  // rare: one CTA, the careful way
+      sum = cta_join<T, false>(part_sum<T, ENT, false>(row, a.vocab, a.c), a.c, red);
   }
   if (threadIdx.x == 0) {
     const RowOut o = row_out(sum, to_f32(row[a.target[t]]), a.inv_t);
@@ -231,32 +393,64 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
 }
 
 // Gradient of a part of a row.  dz_j = (1/T) (g [j = t] - p_j (g + h (ln p_j + H)))
-// = p_j (A + B y_j) off the target, with ln p_j = ln2 y_j - ln S.
+// = 2^y_j (A + B y_j) off the target, with p_j = 2^y_j / S, ln p_j = ln2 y_j - ln S.
 struct RowGrad {
-  float m, inv_s, ga, gb;  // A and B, signed
-  float at;                // added at the target
+  float m, a, b;  // signed
+  float at;       // added at the target
 };
 __device__ __forceinline__ RowGrad row_grad(float m, float s, float entropy, float g, float h,
                                             float inv_t) {
   RowGrad r;
+  const float by = -inv_t / s;
   r.m = m;
-  r.inv_s = 1.f / s;
-  r.ga = -inv_t * (g + h * (entropy - logf(s)));
-  r.gb = -inv_t * h * kLn2;
+  r.a = by * (g + h * (entropy - logf(s)));
+  r.b = by * h * kLn2;
   r.at = inv_t * g;
   return r;
 }
-template <bool ENT>
-__device__ __forceinline__ float grad_of(float z, const RowGrad &g, float c) {
-  const float y = (z - g.m) * c;
-  const float p = ex2(y) * g.inv_s;
-  return p * (ENT ? fmaf(g.gb, fmaxf(y, kNoLog), g.ga) : g.ga);
+// y = RowLog's less d: what its rounding of m c left out, which 2^y / S and y take in.
+template <typename T, bool FUSED>
+__device__ __forceinline__ RowGrad exact_grad(RowGrad g, float c) {
+  if (!FUSED) return g;
+  const float d = -fmaf(g.m, c, -(g.m * c)), f = d * kLn2;
+  g.a = fmaf(d, g.b, g.a);
+  g.a = fmaf(f, g.a, g.a);
+  g.b = fmaf(f, g.b, g.b);
+  return g;
 }
 
-template <typename T, bool ENT>
+template <typename T, bool ENT, bool FUSED>
+struct GradOf {
+  RowLog<T, FUSED> log;
+  F2 a, b;
+  __device__ __forceinline__ GradOf(const RowGrad &g, float c) : log(g.m, c) {
+    const RowGrad x = exact_grad<T, FUSED>(g, c);
+    a = F2(x.a);
+    b = F2(x.b);
+  }
+  __device__ __forceinline__ F2 of(F2 z) const {
+    const F2 y = log.of(z), e = ex2_both(y);
+    return e * (ENT ? fma2(b, finite_log<T, FUSED>(y), a) : a);
+  }
+  __device__ __forceinline__ float of(float z) const {
+    if constexpr (FUSED && std::is_same<T, __nv_bfloat16>::value)
+      z = z == kNegInf ? -10.f * kFusedMost : z;
+    return of(F2(z, 0.f)).x();
+  }
+  __device__ __forceinline__ uint4 of(const uint4 &w) const {
+    const uint4 x = ENT ? finite_words<T, FUSED>(w) : w;
+    uint4 o;
+#pragma unroll
+    for (int i = 0; i < Vec16<T>::kPairs; ++i) Vec16<T>::set(o, i, of(Vec16<T>::pair(x, i)));
+    return o;
+  }
+};
+
+template <typename T, bool ENT, bool FUSED>
 __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t first, uint32_t n,
-                                          uint32_t target, const RowGrad &g, float c) {
+                                          uint32_t target, const RowGrad &grad, float c) {
   constexpr int N = Vec16<T>::kN;
+  const GradOf<T, ENT, FUSED> g(grad, c);
   p += first;
   d += first;
   const uint32_t at = target - first;  // beyond n: not in this part
@@ -266,7 +460,7 @@ __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t first, uint
     const Span<T> sp(p, n);
     if (threadIdx.x < sp.head + sp.tail) {
       const uint32_t i = threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * N;
-      d[i] = from_f32<T>(grad_of<ENT>(to_f32(p[i]), g, c));
+      d[i] = from_f32<T>(g.of(to_f32(p[i])));
     }
     const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
     uint4 *o = reinterpret_cast<uint4 *>(d + sp.head);
@@ -276,29 +470,25 @@ __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t first, uint
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * kRowThreads];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        float v[N];
-        Vec16<T>::unpack(w[k], v);
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = grad_of<ENT>(v[e], g, c);
-        o[i + k * kRowThreads] = Vec16<T>::pack(v);
-      }
+      for (int k = 0; k < kUnroll; ++k) o[i + k * kRowThreads] = g.of(w[k]);
     }
-    for (; i < sp.vecs; i += kRowThreads) {
-      float v[N];
-      Vec16<T>::unpack(q[i], v);
-#pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = grad_of<ENT>(v[e], g, c);
-      o[i] = Vec16<T>::pack(v);
-    }
+    for (; i < sp.vecs; i += kRowThreads) o[i] = g.of(q[i]);
   } else {
-    for (uint32_t i = threadIdx.x; i < n; i += kRowThreads)
-      d[i] = from_f32<T>(grad_of<ENT>(to_f32(p[i]), g, c));
+    for (uint32_t i = threadIdx.x; i < n; i += kRowThreads) d[i] = from_f32<T>(g.of(to_f32(p[i])));
   }
   if (at < n) {
     __syncthreads();
-    if (threadIdx.x == 0) d[at] = from_f32<T>(grad_of<ENT>(zt, g, c) + g.at);
+    if (threadIdx.x == 0) d[at] = from_f32<T>(g.of(zt) + grad.at);
   }
+}
+// The way that the row's maximum asks for.
+template <typename T, bool ENT>
+__device__ __forceinline__ void part_grad_any(const T *p, T *d, uint32_t first, uint32_t n,
+                                              uint32_t target, const RowGrad &g, float c) {
+  if (kFused<T> && sums_hold<T>(RowSum{g.m, 0.f, 0.f}))
+    part_grad<T, ENT, kFused<T>>(p, d, first, n, target, g, c);
+  else
+    part_grad<T, ENT, false>(p, d, first, n, target, g, c);
 }
 
 template <typename T>
@@ -331,8 +521,8 @@ k_token_logprob_grad(RowArgs a, const float *stats, const float *entropy, const 
   }
   const RowGrad g = row_grad(stats[2 * t], s, ENT ? entropy[t] : 0.f, dlogp[t],
                              ENT ? dentropy[t] : 0.f, a.inv_t);
-  part_grad<T, ENT>(reinterpret_cast<const T *>(a.z) + t * a.stride, d, first, n,
-                    (uint32_t)a.target[t], g, a.c);
+  part_grad_any<T, ENT>(reinterpret_cast<const T *>(a.z) + t * a.stride, d, first, n,
+                        (uint32_t)a.target[t], g, a.c);
 }
 
 // What row t weighs in the policy loss, found by a warp; 0 outside the sequences.
@@ -385,7 +575,8 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
   const uint32_t target = (uint32_t)a.target[t];
   const float zt = to_f32(row[target]);
   if (np > 1) cluster_arrive();
-  RowSum sum = cta_join(part_sum<T, ENT>(row + first, n, a.c), a.c, red);
+  constexpr bool F = kFused<T>;
+  RowSum sum = cta_join<T, F>(part_sum<T, ENT, F>(row + first, n, a.c), a.c, red);
   if (np > 1) {
     cluster_wait();  // every CTA has started, so that its shared memory is there
     if (threadIdx.x == 0)
@@ -395,11 +586,20 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
     cluster_wait();
     if (threadIdx.x == 0) {
       sum = parts[0];
-      for (uint32_t k = 1; k < np; ++k) sum = row_join(sum, parts[k], a.c);
+      for (uint32_t k = 1; k < np; ++k) sum = row_join<T, F>(sum, parts[k], a.c);
     }
   }
-  if (threadIdx.x == 0) whole = sum;
+  if (threadIdx.x == 0) whole = exact_sums<T>(sum, a.c);
   __syncthreads();
+  if (F && !sums_hold<T>(whole)) {  // rare: every CTA the whole row, the careful way
+    sum = cta_join<T, false>(part_sum<T, ENT, false>(row, a.vocab, a.c), a.c, red);
+    if (threadIdx.x == 0) whole = sum;
+    __syncthreads();
+    if (np > 1) {  // before one of them overwrites its part
+      cluster_arrive();
+      cluster_wait();
+    }
+  }
   const RowOut o = row_out(whole, zt, a.inv_t);
   if (part == 0 && threadIdx.x == 0) {
     if (o.s == 0.f) flag(ctrl, DEVERR_ROW, t);
@@ -415,7 +615,7 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
                              by * row_policy(rule, o.logp, old_logp[t],
                                              ref_logp ? ref_logp + t : nullptr, adv[t]),
                              ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
-  part_grad<T, ENT>(row, d, first, n, target, g, a.c);
+  part_grad_any<T, ENT>(row, d, first, n, target, g, a.c);
 }
 
 RowArgs row_args(const Logits &z) {

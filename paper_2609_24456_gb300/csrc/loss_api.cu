@@ -28,8 +28,8 @@ edp_status check_logits(edp_ctx *c, const char *who, const Logits &z, const void
   if (z.vocab == 0 || z.vocab > 0x7FFFFFFFu || z.rows > 0x7FFFFFFFull || z.stride < z.vocab ||
       z.stride > (1ull << 40))
     return fail(c, EDP_ERR_INVALID, "%s: need 0 < vocab <= stride, rows and vocab below 2^31", who);
-  if (!(z.temperature > 0.0) || !std::isfinite(z.temperature))
-    return fail(c, EDP_ERR_INVALID, "%s: temperature must be finite and > 0", who);
+  if (!(z.temperature >= 1e-6 && z.temperature <= 1e6))
+    return fail(c, EDP_ERR_INVALID, "%s: temperature must be in [1e-6, 1e6]", who);
   if (((uintptr_t)z.z | (uintptr_t)dz) % size_of(z.dtype))
     return fail(c, EDP_ERR_INVALID, "%s: logits are not aligned to their type", who);
   if (dz && (dstride < z.vocab || dstride > (1ull << 40) || (dz == z.z && dstride != z.stride)))
