@@ -166,20 +166,6 @@ struct RowSum {
   float m, s, u;
 };
 
-template <typename T, bool FUSED>
-__device__ __forceinline__ RowSum row_join(RowSum a, RowSum b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  const RowLog<T, FUSED> log(m, c);
-  const float da = a.m == m ? 0.f : log.shift(RowLog<T, FUSED>(a.m, c));
-  const float db = b.m == m ? 0.f : log.shift(RowLog<T, FUSED>(b.m, c));
-  const float fa = a.m == kNegInf ? 1.f : ex2(da), fb = b.m == kNegInf ? 1.f : ex2(db);
-  // 2^(y + d) (y + d): a part whose factor underflowed has no product either, and
-  // one without a maximum has sums of 0 (or NaN, which stays)
-  const float ua = a.m == kNegInf ? a.u : fa > 0.f ? fa * fmaf(da, a.s, a.u) : 0.f;
-  const float ub = b.m == kNegInf ? b.u : fb > 0.f ? fb * fmaf(db, b.s, b.u) : 0.f;
-  return {m, fmaf(fa, a.s, fb * b.s), ua + ub};
-}
-
 // A thread's sums, of even and odd places apart.
 struct LaneSum {
   float m;
@@ -227,7 +213,7 @@ struct Span {
   }
 };
 
-template <typename T, bool ENT, bool FUSED>
+template <typename T, bool ENT, bool FUSED, int NT = kRowThreads>
 __device__ __forceinline__ RowSum part_sum(const T *p, uint32_t n, float c) {
   constexpr int N = Vec16<T>::kN;
   LaneSum a{kNegInf, F2(0.f), F2(0.f)};
@@ -240,41 +226,88 @@ __device__ __forceinline__ RowSum part_sum(const T *p, uint32_t n, float c) {
   }
   const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
   uint32_t i = threadIdx.x;
-  for (; i + (kUnroll - 1) * kRowThreads < sp.vecs; i += kUnroll * kRowThreads) {
+  for (; i + (kUnroll - 1) * NT < sp.vecs; i += kUnroll * NT) {
     uint4 w[kUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * kRowThreads];
+    for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * NT];
     take_vectors<T, ENT, FUSED>(a, w, c);
   }
-  for (; i < sp.vecs; i += kRowThreads) {
+  for (; i < sp.vecs; i += NT) {
     const uint4 w[1] = {q[i]};
     take_vectors<T, ENT, FUSED>(a, w, c);
   }
   return {a.m, a.s.x() + a.s.y(), a.u.x() + a.u.y()};
 }
 
-// The CTA's sum, in thread 0; joined by lanes and warps in a fixed order.
-template <typename T, bool FUSED>
+// The two halves of a barrier of the cluster (all of whose CTAs are resident, so
+// that each arrives without waiting for another).
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+// The first, which only tells that the CTA has started.
+__device__ __forceinline__ void cluster_started() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// The sums of a warp's lanes, in all of them: first their maximum, to which each
+// lane's sums go over, then plain sums in a fixed order (LANES: the lanes that hold
+// any, the first of the warp).
+template <typename T, bool FUSED, int LANES = 32>
+__device__ __forceinline__ RowSum warp_sum(RowSum a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
+  if (a.m != kNegInf) {
+    const float d = RowLog<T, FUSED>(m, c).shift(RowLog<T, FUSED>(a.m, c));
+    const float f = a.m == m ? 1.f : ex2(d);
+    // 2^(y + d) (y + d): a part whose factor underflowed has no product either
+    a.u = a.m == m ? a.u : f > 0.f ? f * fmaf(d, a.s, a.u) : 0.f;
+    a.s *= f;
+  }  // else the sums are 0 (or NaN, which stays)
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) {
+    a.s += __shfl_xor_sync(kAllLanes, a.s, o);
+    a.u += __shfl_xor_sync(kAllLanes, a.u, o);
+  }
+  return {m, a.s, a.u};
+}
+
+// The CTA's sums, in its first warp.
+template <typename T, bool FUSED, int NT = kRowThreads>
 __device__ __forceinline__ RowSum cta_join(RowSum a, float c, RowSum *red) {
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const RowSum b{__shfl_xor_sync(kAllLanes, a.m, o), __shfl_xor_sync(kAllLanes, a.s, o),
-                   __shfl_xor_sync(kAllLanes, a.u, o)};
-    a = row_join<T, FUSED>(a, b, c);
-  }
+  a = warp_sum<T, FUSED>(a, c);
   if (lane == 0) red[wid] = a;
   __syncthreads();
-  if (wid == 0) {
-    a = lane < kRowWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f};
-#pragma unroll
-    for (int o = kRowWarps / 2; o; o >>= 1) {
-      const RowSum b{__shfl_xor_sync(kAllLanes, a.m, o), __shfl_xor_sync(kAllLanes, a.s, o),
-                     __shfl_xor_sync(kAllLanes, a.u, o)};
-      a = row_join<T, FUSED>(a, b, c);
-    }
-  }
+  if (wid == 0)
+    a = warp_sum<T, FUSED, NT / 32>(lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, c);
   return a;
+}
+
+// The sums of a row's parts, in every thread: each CTA's first warp gives its own to
+// all of the cluster and adds up what it was given.  Every CTA has started.
+template <typename T, bool FUSED>
+__device__ __forceinline__ RowSum cluster_join(RowSum a, float c, uint32_t part, uint32_t np,
+                                               RowSum *parts, RowSum *whole) {
+  if (np > 1) {
+    if (threadIdx.x < 32) {
+      // lane 0's, by each of the lanes to one CTA
+      const RowSum mine{__shfl_sync(kAllLanes, a.m, 0), __shfl_sync(kAllLanes, a.s, 0),
+                        __shfl_sync(kAllLanes, a.u, 0)};
+      if (threadIdx.x < np) cg::this_cluster().map_shared_rank(parts, threadIdx.x)[part] = mine;
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (threadIdx.x < 32)
+      a = warp_sum<T, FUSED, 8>(threadIdx.x < np ? parts[threadIdx.x] : RowSum{kNegInf, 0.f, 0.f},
+                                c);
+  }
+  if (threadIdx.x == 0) *whole = a;
+  __syncthreads();
+  return *whole;
 }
 
 // The part of a row that CTA `part` of `parts` takes, as whole vectors' worth.
@@ -319,15 +352,6 @@ __device__ __forceinline__ RowOut row_out(const RowSum &a, float zt, float inv_t
   return {(zt - a.m) * inv_t - ln, ln - kLn2 * (a.u / a.s), a.m, a.s};
 }
 
-// The two halves of a barrier of the cluster (all of whose CTAs are resident, so
-// that each arrives without waiting for another).
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 struct RowArgs {
   const void *z;
   uint64_t stride;
@@ -359,7 +383,7 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
     return;  // the whole cluster
   }
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
-  if (np > 1) cluster_arrive();
+  if (np > 1) cluster_started();
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   constexpr bool F = kFused<T>;
@@ -370,8 +394,9 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
     cluster_arrive();
     cluster_wait();
     if (part) return;
-    if (threadIdx.x == 0)
-      for (uint32_t k = 1; k < np; ++k) sum = row_join<T, F>(sum, parts[k], a.c);
+    if (threadIdx.x < 32)
+      sum = warp_sum<T, F, 8>(threadIdx.x < np ? parts[threadIdx.x] : RowSum{kNegInf, 0.f, 0.f},
+                              a.c);
   }
   if (F) {
     if (threadIdx.x == 0) whole = exact_sums<T>(sum, a.c);
@@ -446,14 +471,11 @@ struct GradOf {
   }
 };
 
-template <typename T, bool ENT, bool FUSED>
-__device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t first, uint32_t n,
-                                          uint32_t target, const RowGrad &grad, float c) {
+template <typename T, bool ENT, bool FUSED, int NT>
+__device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t n, uint32_t at,
+                                          const RowGrad &grad, float c) {
   constexpr int N = Vec16<T>::kN;
   const GradOf<T, ENT, FUSED> g(grad, c);
-  p += first;
-  d += first;
-  const uint32_t at = target - first;  // beyond n: not in this part
   const float zt = at < n ? to_f32(p[at]) : 0.f;
   __syncthreads();  // the target is read before it is overwritten (in place)
   if ((((uintptr_t)p ^ (uintptr_t)d) & 15u) == 0) {
@@ -465,40 +487,41 @@ __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t first, uint
     const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
     uint4 *o = reinterpret_cast<uint4 *>(d + sp.head);
     uint32_t i = threadIdx.x;
-    for (; i + (kUnroll - 1) * kRowThreads < sp.vecs; i += kUnroll * kRowThreads) {
+    for (; i + (kUnroll - 1) * NT < sp.vecs; i += kUnroll * NT) {
       uint4 w[kUnroll];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * kRowThreads];
+      for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * NT];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) o[i + k * kRowThreads] = g.of(w[k]);
+      for (int k = 0; k < kUnroll; ++k) o[i + k * NT] = g.of(w[k]);
     }
-    for (; i < sp.vecs; i += kRowThreads) o[i] = g.of(q[i]);
+    for (; i < sp.vecs; i += NT) o[i] = g.of(q[i]);
   } else {
-    for (uint32_t i = threadIdx.x; i < n; i += kRowThreads) d[i] = from_f32<T>(g.of(to_f32(p[i])));
+    for (uint32_t i = threadIdx.x; i < n; i += NT) d[i] = from_f32<T>(g.of(to_f32(p[i])));
   }
   if (at < n) {
     __syncthreads();
     if (threadIdx.x == 0) d[at] = from_f32<T>(g.of(zt) + grad.at);
   }
 }
-// The way that the row's maximum asks for.
-template <typename T, bool ENT>
-__device__ __forceinline__ void part_grad_any(const T *p, T *d, uint32_t first, uint32_t n,
-                                              uint32_t target, const RowGrad &g, float c) {
+// The way that the row's maximum asks for.  at: the target's place in the part, or
+// beyond n.
+template <typename T, bool ENT, int NT = kRowThreads>
+__device__ __forceinline__ void part_grad_any(const T *p, T *d, uint32_t n, uint32_t at,
+                                              const RowGrad &g, float c) {
   if (kFused<T> && sums_hold<T>(RowSum{g.m, 0.f, 0.f}))
-    part_grad<T, ENT, kFused<T>>(p, d, first, n, target, g, c);
+    part_grad<T, ENT, kFused<T>, NT>(p, d, n, at, g, c);
   else
-    part_grad<T, ENT, false>(p, d, first, n, target, g, c);
+    part_grad<T, ENT, false, NT>(p, d, n, at, g, c);
 }
 
-template <typename T>
+template <typename T, int NT = kRowThreads>
 __device__ __forceinline__ void part_zero(T *d, uint32_t n) {
   constexpr int N = Vec16<T>::kN;
   const Span<T> sp(d, n);
   if (threadIdx.x < sp.head + sp.tail)
     d[threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * N] = from_f32<T>(0.f);
   uint4 *o = reinterpret_cast<uint4 *>(d + sp.head);
-  for (uint32_t i = threadIdx.x; i < sp.vecs; i += kRowThreads) o[i] = make_uint4(0, 0, 0, 0);
+  for (uint32_t i = threadIdx.x; i < sp.vecs; i += NT) o[i] = make_uint4(0, 0, 0, 0);
 }
 
 template <typename T, bool ENT>
@@ -521,29 +544,32 @@ k_token_logprob_grad(RowArgs a, const float *stats, const float *entropy, const 
   }
   const RowGrad g = row_grad(stats[2 * t], s, ENT ? entropy[t] : 0.f, dlogp[t],
                              ENT ? dentropy[t] : 0.f, a.inv_t);
-  part_grad_any<T, ENT>(reinterpret_cast<const T *>(a.z) + t * a.stride, d, first, n,
-                        (uint32_t)a.target[t], g, a.c);
+  part_grad_any<T, ENT>(reinterpret_cast<const T *>(a.z) + t * a.stride + first, d + first, n,
+                        (uint32_t)a.target[t] - first, g, a.c);
 }
 
-// What row t weighs in the policy loss, found by a warp; 0 outside the sequences.
+__device__ __forceinline__ bool in_sequences(const RowWeights &w, uint64_t t) {
+  return !w.off || (t >= w.off[0] && t < w.off[w.n_seq]);
+}
+// What row t of the sequences weighs in the policy loss, found by a warp.
 __device__ __forceinline__ float row_weight(const RowWeights &w, uint64_t t) {
-  if (w.off && (t < w.off[0] || t >= w.off[w.n_seq])) return 0.f;
   if (w.sequence) return __ldcg(&w.sequence[sequence_of_warp(w.off, 0, w.n_seq, t)]);
   return w.tokens ? 1.f / (float)__ldcg(w.tokens) : w.fixed;
 }
 
 // The policy loss's derivative by a row's log-probability, before weight and scale.
 __device__ __forceinline__ float row_policy(const PolicyRule &rule, float logp, float old,
-                                            const float *ref, float adv) {
+                                            bool has_ref, float ref, float adv) {
   const float d = logp - old;
-  if (!ref) return policy_token<Kl::kNone, false>(rule, d, 0.f, adv).dlogp;
-  const float q = *ref - logp;
+  if (!has_ref) return policy_token<Kl::kNone, false>(rule, d, 0.f, adv).dlogp;
+  const float q = ref - logp;
   return rule.kl == EDP_KL_K3 ? policy_token<Kl::kK3, false>(rule, d, q, adv).dlogp
                               : policy_token<Kl::kOther, false>(rule, d, q, adv).dlogp;
 }
 
 // Log-probability, policy gradient and the logits' gradient of a row, by a
-// cluster of gridDim.y CTAs.
+// cluster of gridDim.y CTAs, with the logits read twice: for rows whose parts do
+// not fit shared memory (k_policy_resident).
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(kRowThreads)
 k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
@@ -560,8 +586,7 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
   row_part(a.vocab, part, np, &first, &n);
   T *d = reinterpret_cast<T *>(dz) + t * dstride;
   const Row kind = row_kind(a.target, a.mask, t, a.vocab);
-  const float w = kind == Row::kUse ? row_weight(weights, t) : 0.f;
-  if (w == 0.f) {
+  if (kind != Row::kUse || !in_sequences(weights, t)) {
     if (part == 0 && threadIdx.x == 0) {
       logp[t] = 0.f;
       if (entropy) entropy[t] = 0.f;
@@ -571,36 +596,28 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
     part_zero(d + first, n);
     return;  // the whole cluster
   }
+  const float w = row_weight(weights, t);
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
   const uint32_t target = (uint32_t)a.target[t];
   const float zt = to_f32(row[target]);
-  if (np > 1) cluster_arrive();
+  if (np > 1) cluster_started();
   constexpr bool F = kFused<T>;
   RowSum sum = cta_join<T, F>(part_sum<T, ENT, F>(row + first, n, a.c), a.c, red);
-  if (np > 1) {
-    cluster_wait();  // every CTA has started, so that its shared memory is there
-    if (threadIdx.x == 0)
-      for (uint32_t k = 0; k < np; ++k)
-        cg::this_cluster().map_shared_rank(parts, k)[part] = sum;
-    cluster_arrive();  // also: every CTA has read the target before one overwrites it
-    cluster_wait();
-    if (threadIdx.x == 0) {
-      sum = parts[0];
-      for (uint32_t k = 1; k < np; ++k) sum = row_join<T, F>(sum, parts[k], a.c);
-    }
-  }
-  if (threadIdx.x == 0) whole = exact_sums<T>(sum, a.c);
-  __syncthreads();
-  if (F && !sums_hold<T>(whole)) {  // rare: every CTA the whole row, the careful way
+  if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
+  // also: every CTA has read the target before one overwrites it
+  sum = exact_sums<T>(cluster_join<T, F>(sum, a.c, part, np, parts, &whole), a.c);
+  if (F && !sums_hold<T>(sum)) {  // rare: every CTA the whole row, the careful way
+    __syncthreads();
     sum = cta_join<T, false>(part_sum<T, ENT, false>(row, a.vocab, a.c), a.c, red);
     if (threadIdx.x == 0) whole = sum;
     __syncthreads();
+    sum = whole;
     if (np > 1) {  // before one of them overwrites its part
       cluster_arrive();
       cluster_wait();
     }
   }
-  const RowOut o = row_out(whole, zt, a.inv_t);
+  const RowOut o = row_out(sum, zt, a.inv_t);
   if (part == 0 && threadIdx.x == 0) {
     if (o.s == 0.f) flag(ctrl, DEVERR_ROW, t);
     logp[t] = o.logp;
@@ -612,10 +629,106 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
   }
   const float by = rule.grad_scale * w;
   const RowGrad g = row_grad(o.m, o.s, ENT ? o.entropy : 0.f,
-                             by * row_policy(rule, o.logp, old_logp[t],
-                                             ref_logp ? ref_logp + t : nullptr, adv[t]),
+                             by * row_policy(rule, o.logp, old_logp[t], ref_logp != nullptr,
+                                             ref_logp ? ref_logp[t] : 0.f, adv[t]),
                              ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
-  part_grad_any<T, ENT>(row, d, first, n, target, g, a.c);
+  part_grad_any<T, ENT>(row + first, d + first, n, target - first, g, a.c);
+}
+
+// The same with each CTA's part of the row in shared memory: read from memory once,
+// its gradient written once.  The part comes by bulk copies; the CTAs of other rows
+// on the SM take turns with it at waiting, computing and storing.
+constexpr int kResidentThreads = 256;
+constexpr uint32_t kResidentPart = 40 * 1024;       // bytes of a part, where the row allows
+constexpr uint32_t kResidentMost = 200 * 1024;
+constexpr uint64_t kRowWaitNs = 1000000000ull;      // bound of the wait for a part
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(kResidentThreads)
+k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
+                  const float *adv, PolicyRule rule, float *logp, float *entropy, void *dz,
+                  uint64_t dstride, Ctrl *ctrl) {
+  constexpr int NT = kResidentThreads;
+  constexpr bool F = kFused<T>;
+  extern __shared__ uint4 resident[];
+  __shared__ RowSum red[NT / 32];
+  __shared__ RowSum parts[8];
+  __shared__ RowSum whole;
+  __shared__ unsigned long long bar;
+  if (threadIdx.x == 0) {
+    mbar_init(&bar, 1);
+    mbar_init_fence();
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_launch();
+  const uint64_t t = blockIdx.x;
+  const uint32_t part = blockIdx.y, np = gridDim.y;
+  uint32_t first, n;
+  row_part(a.vocab, part, np, &first, &n);
+  T *d = reinterpret_cast<T *>(dz) + t * dstride + first;
+  const Row kind = row_kind(a.target, a.mask, t, a.vocab);
+  if (kind != Row::kUse || !in_sequences(weights, t)) {
+    if (part == 0 && threadIdx.x == 0) {
+      logp[t] = 0.f;
+      if (entropy) entropy[t] = 0.f;
+      if (kind == Row::kBad)
+        flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)a.target[t]);
+    }
+    part_zero<T, NT>(d, n);
+    return;  // the whole cluster
+  }
+  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+  const T *p = row + first;
+  // the part keeps its place within 16 bytes
+  T *held = reinterpret_cast<T *>(resident) + ((uintptr_t)p & 15u) / sizeof(T);
+  const Span<T> sp(p, n);
+  if (threadIdx.x == 0 && sp.vecs) {
+    mbar_arrive_tx(&bar, sp.vecs * 16);
+    bulk_load(held + sp.head, p + sp.head, sp.vecs * 16, &bar, policy_stream());
+  }
+  if (threadIdx.x < sp.head + sp.tail) {
+    const uint32_t i =
+        threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * Vec16<T>::kN;
+    held[i] = p[i];
+  }
+  if (np > 1) cluster_started();
+  const uint32_t target = (uint32_t)a.target[t];
+  const float zt = to_f32(row[target]);
+  const float w = row_weight(weights, t);
+  const float old = old_logp[t], ref = ref_logp ? ref_logp[t] : 0.f, ad = adv[t];
+  if (sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
+    if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
+    mbar_wait(&bar, 0, kRowWaitNs);  // bounded: the copy lands before the CTA ends
+  }
+  __syncthreads();
+  RowSum sum = cta_join<T, F, NT>(part_sum<T, ENT, F, NT>(held, n, a.c), a.c, red);
+  if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
+  // also: every CTA has read the target before one overwrites it
+  sum = exact_sums<T>(cluster_join<T, F>(sum, a.c, part, np, parts, &whole), a.c);
+  if (F && !sums_hold<T>(sum)) {  // rare: again, the careful way
+    if (np > 1) {  // the sums before have been read
+      cluster_arrive();
+      cluster_wait();
+    }
+    __syncthreads();
+    sum = cta_join<T, false, NT>(part_sum<T, ENT, false, NT>(held, n, a.c), a.c, red);
+    sum = cluster_join<T, false>(sum, a.c, part, np, parts, &whole);
+  }
+  const RowOut o = row_out(sum, zt, a.inv_t);
+  if (part == 0 && threadIdx.x == 0) {
+    if (o.s == 0.f) flag(ctrl, DEVERR_ROW, t);
+    logp[t] = o.logp;
+    if (entropy) entropy[t] = o.entropy;
+  }
+  if (o.s == 0.f) {
+    part_zero<T, NT>(d, n);
+    return;
+  }
+  const float by = rule.grad_scale * w;
+  const RowGrad g = row_grad(o.m, o.s, ENT ? o.entropy : 0.f,
+                             by * row_policy(rule, o.logp, old, ref_logp != nullptr, ref, ad),
+                             ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
+  part_grad_any<T, ENT, NT>(held, d, n, target - first, g, a.c);
 }
 
 RowArgs row_args(const Logits &z) {
@@ -640,12 +753,20 @@ uint32_t row_parts(const edp_ctx *c, const Logits &z) {
   return p;
 }
 
+// Shared memory that a part of a row takes at any alignment.
+size_t part_bytes(const Logits &z, uint32_t parts) {
+  const uint64_t size = z.dtype == EDP_F32 ? 4 : 2;
+  const uint64_t each = ((z.vocab + parts - 1) / parts + 7) & ~7ull;
+  return (size_t)(((each * size + 15) & ~15ull) + 16);
+}
+
 template <typename... KArgs, typename... Args>
 cudaError_t launch_rows(void (*kern)(KArgs...), uint64_t rows, uint32_t parts, bool cluster,
-                        cudaStream_t s, Args... args) {
+                        int threads, size_t smem, cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows, parts);
-  cfg.blockDim = dim3(kRowThreads);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -676,8 +797,8 @@ cudaError_t launch_token_logprob(edp_ctx *ctx, const Logits &z, float *logp, flo
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     auto kern = entropy ? k_token_logprob<T, true> : k_token_logprob<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), true, s, row_args(z), logp, entropy, stats,
-                       ctx->ctrl);
+    return launch_rows(kern, z.rows, row_parts(ctx, z), true, kRowThreads, 0, s, row_args(z), logp,
+                       entropy, stats, ctx->ctrl);
   });
 }
 
@@ -688,8 +809,8 @@ cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     auto kern = entropy ? k_token_logprob_grad<T, true> : k_token_logprob_grad<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), false, s, row_args(z), stats, entropy,
-                       dlogp, dentropy, dz, dstride, ctx->ctrl);
+    return launch_rows(kern, z.rows, row_parts(ctx, z), false, kRowThreads, 0, s, row_args(z), stats,
+                       entropy, dlogp, dentropy, dz, dstride, ctx->ctrl);
   });
 }
 
@@ -698,9 +819,19 @@ cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &
                                float *entropy, void *dz, uint64_t dstride, cudaStream_t s) {
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    auto kern = entropy ? k_policy_rows<T, true> : k_policy_rows<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), true, s, row_args(z), w, p.old_logp,
-                       p.ref_logp, p.adv, rule, logp, entropy, dz, dstride, ctx->ctrl);
+    uint32_t parts = row_parts(ctx, z);
+    while (parts < 8 && part_bytes(z, parts) > kResidentPart) parts *= 2;
+    const size_t bytes = part_bytes(z, parts);
+    auto go = [&](auto kern, int threads, size_t smem) {
+      return launch_rows(kern, z.rows, parts, true, threads, smem, s, row_args(z), w, p.old_logp,
+                         p.ref_logp, p.adv, rule, logp, entropy, dz, dstride, ctx->ctrl);
+    };
+    if (bytes > kResidentMost)
+      return go(entropy ? k_policy_rows<T, true> : k_policy_rows<T, false>, kRowThreads, 0);
+    auto kern = entropy ? k_policy_resident<T, true> : k_policy_resident<T, false>;
+    const cudaError_t e = cudaFuncSetAttribute(
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
+    return e != cudaSuccess ? e : go(kern, kResidentThreads, bytes);
   });
 }
 

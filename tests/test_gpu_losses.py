@@ -181,11 +181,21 @@ def test_policy_special_values(edp_lib):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,vocab", [(1, 3), (5, 1000), (40, 20_011), (333, 4097)])
+@pytest.mark.parametrize("rows,vocab", [(1, 3), (5, 1000), (40, 20_011), (333, 4097), (3, 152_064)])
 @pytest.mark.parametrize("reduce", [0, 1])
 def test_policy_from_logits(edp_lib, dtype, rows, vocab, reduce):
     """The fused form against the oracle's three steps, in place and not, and
     against the three calls."""
+    policy_from_logits(edp_lib, dtype, rows, vocab, reduce)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("f32", 420_011), ("bf16", 840_007)])
+def test_policy_from_logits_beyond_shared_memory(edp_lib, dtype, vocab):
+    """Rows whose eighth does not fit shared memory are read twice."""
+    policy_from_logits(edp_lib, dtype, 2, vocab, 0)
+
+
+def policy_from_logits(edp_lib, dtype, rows, vocab, reduce):
     edp, ring = edp_lib, ctx_of(edp_lib)
     rng = np.random.default_rng(rows)
     _, v, target, zd = make(rows, vocab, dtype, rows, banned=vocab > 100)
@@ -258,6 +268,38 @@ def test_policy_from_logits(edp_lib, dtype, rows, vocab, reduce):
         assert np.all(np.abs(to_np(l3) - loss) <= 1e-5 * (1 + np.abs(loss)))
         assert np.all(np.abs(to_np(d3.double())[use] - d[use]) <= 2 * bound + 2 * LEAST[dtype] +
                       2 * UNIT[dtype] * np.abs(ref_d))
+
+
+@pytest.mark.parametrize("vocab", [40, 20_000])
+def test_policy_from_logits_special_values(edp_lib, vocab):
+    """The type's lowest and largest values, one allowed token, NaN: the fused
+    form as the three calls."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    for dtype in ("bf16", "f16", "f32"):
+        _, v = view(6, vocab, dtype)
+        v.normal_(0, 1)
+        v[0, 1:] = torch.finfo(TYPES[dtype]).min
+        v[1, :] = torch.finfo(TYPES[dtype]).min
+        v[2, 1:] = -torch.inf
+        v[3, 5] = float("nan")
+        v[4, :] = torch.finfo(TYPES[dtype]).max
+        t = cuda(np.array([0, 5, 0, 0, 9, 7], np.int32))
+        a, b = torch.ones(6, device="cuda"), -torch.ones(6, device="cuda")
+        cfg = edp.make_policy_config(entropy_coef=.1)
+        lp, lp3, H, g, h = (torch.zeros(6, device="cuda") for _ in range(5))
+        st, loss, d = torch.zeros(6, 2, device="cuda"), torch.zeros(8, device="cuda"), \
+            torch.zeros_like(v)
+        edp.edp_token_logprob(ring.ctx, v, t, lp3, entropy=H, stats=st)
+        edp.edp_policy_loss(ring.ctx, cfg, lp3, b, a, 6, loss, entropy=H, dlogp=g, dentropy=h)
+        edp.edp_token_logprob_grad(ring.ctx, v, t, st, g, d, entropy=H, dentropy=h)
+        edp.edp_policy_loss_logits(ring.ctx, cfg, v, t, b, a, loss, lp, v)
+        edp.edp_sync(ring.ctx)
+        fine = [0, 1, 2, 4, 5]
+        assert np.all(np.abs(to_np(lp)[fine] - to_np(lp3)[fine]) <= 1e-5)
+        assert np.isnan(to_np(lp)[3]) and torch.isnan(v[3]).all() and torch.isnan(d[3]).all()
+        got, want = to_np(v.double())[fine], to_np(d.double())[fine]
+        # the same up to roundings of the type, and of 1e-5 of a gradient below 1
+        assert np.all(np.abs(got - want) <= 2e-5 + 2 * UNIT[dtype] * np.abs(want))
 
 
 def test_policy_from_logits_rows_without_distribution(edp_lib):
