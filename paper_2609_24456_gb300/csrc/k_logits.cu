@@ -311,9 +311,15 @@ __device__ __forceinline__ RowSum cluster_join(RowSum a, float c, uint32_t part,
 }
 
 // The part of a row that CTA `part` of `parts` takes, as whole vectors' worth.
+__device__ __forceinline__ uint32_t part_size(uint32_t vocab, uint32_t parts) {
+  return (((vocab + parts - 1) / parts) + 7u) & ~7u;
+}
+__device__ __forceinline__ uint32_t owner_of(uint32_t vocab, uint32_t column, uint32_t parts) {
+  return column / part_size(vocab, parts);
+}
 __device__ __forceinline__ void row_part(uint32_t vocab, uint32_t part, uint32_t parts,
                                          uint32_t *first, uint32_t *n) {
-  const uint32_t each = (((vocab + parts - 1) / parts) + 7u) & ~7u;
+  const uint32_t each = part_size(vocab, parts);
   const uint64_t lo = min((uint64_t)part * each, (uint64_t)vocab);
   *first = (uint32_t)lo;
   *n = (uint32_t)min((uint64_t)each, vocab - lo);
@@ -476,31 +482,40 @@ __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t n, uint32_t
                                           const RowGrad &grad, float c) {
   constexpr int N = Vec16<T>::kN;
   const GradOf<T, ENT, FUSED> g(grad, c);
-  const float zt = at < n ? to_f32(p[at]) : 0.f;
-  __syncthreads();  // the target is read before it is overwritten (in place)
+  // each thread reads what it writes (in place), the target among it
+  auto one = [&](uint32_t i) {
+    const float v = g.of(to_f32(p[i]));
+    d[i] = from_f32<T>(i == at ? v + grad.at : v);
+  };
   if ((((uintptr_t)p ^ (uintptr_t)d) & 15u) == 0) {
     const Span<T> sp(p, n);
-    if (threadIdx.x < sp.head + sp.tail) {
-      const uint32_t i = threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * N;
-      d[i] = from_f32<T>(g.of(to_f32(p[i])));
-    }
+    if (threadIdx.x < sp.head + sp.tail)
+      one(threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * N);
     const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
     uint4 *o = reinterpret_cast<uint4 *>(d + sp.head);
+    const uint32_t place = at - sp.head, hit = at >= sp.head ? place / N : 0xffffffffu;
+    auto many = [&](const uint4 &w, uint32_t i) {
+      uint4 x = g.of(w);
+      if (i == hit) {
+        const T *z = reinterpret_cast<const T *>(&w);
+        T *y = reinterpret_cast<T *>(&x);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e == place % N) y[e] = from_f32<T>(g.of(to_f32(z[e])) + grad.at);
+      }
+      o[i] = x;
+    };
     uint32_t i = threadIdx.x;
     for (; i + (kUnroll - 1) * NT < sp.vecs; i += kUnroll * NT) {
       uint4 w[kUnroll];
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) w[k] = q[i + k * NT];
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) o[i + k * NT] = g.of(w[k]);
+      for (int k = 0; k < kUnroll; ++k) many(w[k], i + k * NT);
     }
-    for (; i < sp.vecs; i += NT) o[i] = g.of(q[i]);
+    for (; i < sp.vecs; i += NT) many(q[i], i);
   } else {
-    for (uint32_t i = threadIdx.x; i < n; i += NT) d[i] = from_f32<T>(g.of(to_f32(p[i])));
-  }
-  if (at < n) {
-    __syncthreads();
-    if (threadIdx.x == 0) d[at] = from_f32<T>(g.of(zt) + grad.at);
+    for (uint32_t i = threadIdx.x; i < n; i += NT) one(i);
   }
 }
 // The way that the row's maximum asks for.  at: the target's place in the part, or
@@ -642,6 +657,21 @@ constexpr int kResidentThreads = 256;
 constexpr uint32_t kResidentPart = 40 * 1024;       // bytes of a part, where the row allows
 constexpr uint32_t kResidentMost = 200 * 1024;
 constexpr uint64_t kRowWaitNs = 1000000000ull;      // bound of the wait for a part
+enum class Rest { kGrad, kZero, kCareful };
+
+// v to `to` in the shared memory of the cluster's CTA `rank`, counted on its `bar`.
+__device__ __forceinline__ void send_float4(float4 *to, float4 v, unsigned long long *bar,
+                                            uint32_t rank) {
+  asm volatile(
+      "{\n\t.reg .b32 d, b;\n\t"
+      "mapa.shared::cluster.u32 d, %0, %2;\n\t"
+      "mapa.shared::cluster.u32 b, %1, %2;\n\t"
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [d], {%3, %4, %5, %6}, "
+      "[b];\n\t}"
+      ::"r"(smem_addr(to)), "r"(smem_addr(bar)), "r"(rank), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+      : "memory");
+}
+
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(kResidentThreads)
 k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
@@ -651,18 +681,23 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 resident[];
   __shared__ RowSum red[NT / 32];
-  __shared__ RowSum parts[8];
-  __shared__ RowSum whole;
-  __shared__ unsigned long long bar;
+  __shared__ float4 parts[2][8];  // what the cluster's CTAs send: m, S, U, the target's logit
+  __shared__ RowGrad grad;
+  __shared__ Rest rest;
+  __shared__ unsigned long long bar, sent[2];
+  const uint64_t t = blockIdx.x;
+  const uint32_t part = blockIdx.y, np = gridDim.y;
   if (threadIdx.x == 0) {
     mbar_init(&bar, 1);
+    for (int k = 0; k < 2; ++k) {
+      mbar_init(&sent[k], 1);
+      mbar_arrive_tx(&sent[k], np * sizeof(float4));
+    }
     mbar_init_fence();
   }
   __syncthreads();
   pdl_wait();
   pdl_launch();
-  const uint64_t t = blockIdx.x;
-  const uint32_t part = blockIdx.y, np = gridDim.y;
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   T *d = reinterpret_cast<T *>(dz) + t * dstride + first;
@@ -677,8 +712,7 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
     part_zero<T, NT>(d, n);
     return;  // the whole cluster
   }
-  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
-  const T *p = row + first;
+  const T *p = reinterpret_cast<const T *>(a.z) + t * a.stride + first;
   // the part keeps its place within 16 bytes
   T *held = reinterpret_cast<T *>(resident) + ((uintptr_t)p & 15u) / sizeof(T);
   const Span<T> sp(p, n);
@@ -692,43 +726,74 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
     held[i] = p[i];
   }
   if (np > 1) cluster_started();
-  const uint32_t target = (uint32_t)a.target[t];
-  const float zt = to_f32(row[target]);
-  const float w = row_weight(weights, t);
-  const float old = old_logp[t], ref = ref_logp ? ref_logp[t] : 0.f, ad = adv[t];
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const uint32_t at = (uint32_t)a.target[t] - first;  // beyond n: not in this part
+  float w = 0.f, old = 0.f, ref = 0.f, ad = 0.f;      // the first warp's, beside the copy
+  if (wid == 0) {
+    w = row_weight(weights, t);
+    old = old_logp[t];
+    if (ref_logp) ref = ref_logp[t];
+    ad = adv[t];
+  }
   if (sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
     if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
     mbar_wait(&bar, 0, kRowWaitNs);  // bounded: the copy lands before the CTA ends
   }
   __syncthreads();
-  RowSum sum = cta_join<T, F, NT>(part_sum<T, ENT, F, NT>(held, n, a.c), a.c, red);
-  if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
-  // also: every CTA has read the target before one overwrites it
-  sum = exact_sums<T>(cluster_join<T, F>(sum, a.c, part, np, parts, &whole), a.c);
-  if (F && !sums_hold<T>(sum)) {  // rare: again, the careful way
-    if (np > 1) {  // the sums before have been read
-      cluster_arrive();
-      cluster_wait();
+  // The first warp joins the CTA's sums, gives them to the cluster's other CTAs and
+  // takes theirs, and makes of all what the part's gradient needs.
+  auto finish = [&](auto fused, int round) {
+    constexpr bool FUSED = decltype(fused)::value;
+    RowSum sum = warp_sum<T, FUSED, NT / 32>(
+        lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+    float zt = at < n ? to_f32(held[at]) : 0.f;
+    bool whole = true;
+    if (np > 1) {
+      const float4 mine = make_float4(__shfl_sync(kAllLanes, sum.m, 0),
+                                      __shfl_sync(kAllLanes, sum.s, 0),
+                                      __shfl_sync(kAllLanes, sum.u, 0), zt);
+      if (lane < np) send_float4(&parts[round][part], mine, &sent[round], lane);
+      if (!mbar_wait(&sent[round], 0, kRowWaitNs)) {
+        if (lane == 0) flag(ctrl, DEVERR_TIMEOUT, t);
+        whole = mbar_wait(&sent[round], 0, kRowWaitNs);  // none of them comes after the end
+      }
+      const float4 x = lane < np ? parts[round][lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+      zt = __shfl_sync(kAllLanes, x.w, owner_of(a.vocab, (uint32_t)a.target[t], np));
+      sum = warp_sum<T, FUSED, 8>(RowSum{x.x, x.y, x.z}, a.c);
     }
+    if (FUSED) sum = exact_sums<T>(sum, a.c);
+    if (FUSED && !sums_hold<T>(sum)) {
+      if (lane == 0) rest = Rest::kCareful;
+      return;
+    }
+    if (lane) return;
+    const RowOut o = whole ? row_out(sum, zt, a.inv_t) : RowOut{0.f, 0.f, 0.f, 0.f};
+    if (part == 0) {
+      if (o.s == 0.f) flag(ctrl, DEVERR_ROW, t);
+      logp[t] = o.logp;
+      if (entropy) entropy[t] = o.entropy;
+    }
+    rest = o.s == 0.f ? Rest::kZero : Rest::kGrad;
+    const float by = rule.grad_scale * w;
+    grad = row_grad(o.m, o.s, ENT ? o.entropy : 0.f,
+                    by * row_policy(rule, o.logp, old, ref_logp != nullptr, ref, ad),
+                    ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
+  };
+  RowSum sum = warp_sum<T, F>(part_sum<T, ENT, F, NT>(held, n, a.c), a.c);
+  if (lane == 0) red[wid] = sum;
+  if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
+  __syncthreads();
+  if (wid == 0) finish(std::integral_constant<bool, F>{}, 0);
+  __syncthreads();
+  if (F && rest == Rest::kCareful) {  // rare: again, the careful way
+    sum = warp_sum<T, false>(part_sum<T, ENT, false, NT>(held, n, a.c), a.c);
+    if (lane == 0) red[wid] = sum;
     __syncthreads();
-    sum = cta_join<T, false, NT>(part_sum<T, ENT, false, NT>(held, n, a.c), a.c, red);
-    sum = cluster_join<T, false>(sum, a.c, part, np, parts, &whole);
+    if (wid == 0) finish(std::false_type{}, 1);
+    __syncthreads();
   }
-  const RowOut o = row_out(sum, zt, a.inv_t);
-  if (part == 0 && threadIdx.x == 0) {
-    if (o.s == 0.f) flag(ctrl, DEVERR_ROW, t);
-    logp[t] = o.logp;
-    if (entropy) entropy[t] = o.entropy;
-  }
-  if (o.s == 0.f) {
-    part_zero<T, NT>(d, n);
-    return;
-  }
-  const float by = rule.grad_scale * w;
-  const RowGrad g = row_grad(o.m, o.s, ENT ? o.entropy : 0.f,
-                             by * row_policy(rule, o.logp, old, ref_logp != nullptr, ref, ad),
-                             ENT ? -by * rule.entropy_coef : 0.f, a.inv_t);
-  part_grad_any<T, ENT, NT>(held, d, n, target - first, g, a.c);
+  if (rest == Rest::kZero) part_zero<T, NT>(d, n);
+  else part_grad_any<T, ENT, NT>(held, d, n, at, grad, a.c);
 }
 
 RowArgs row_args(const Logits &z) {
