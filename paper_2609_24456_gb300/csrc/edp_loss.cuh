@@ -49,6 +49,7 @@ struct PolicyRule {
   float low, high, dual;           // limits of the ratio; dual 0: none
   float ln_low, ln_high, ln_dual;  // and of its logarithm
   float kl_coef, entropy_coef, grad_scale;
+  df kl_both, less_entropy;        // both coefficients, the second negative
   uint32_t kl;
 };
 
@@ -161,8 +162,8 @@ __device__ __forceinline__ Pair pair_join(Pair a, Pair b) {
   const df s = two_sum(a.hi, b.hi);
   return {s.hi, __fadd_rn(__fadd_rn(a.lo, b.lo), s.lo)};
 }
-__device__ __forceinline__ double pair_value(Pair a) {
-  return isfinite(a.hi) ? (double)a.hi + (double)a.lo : (double)a.hi;
+__device__ __forceinline__ df as_df(Pair a) {
+  return isfinite(a.hi) ? quick_two_sum(a.hi, a.lo) : df{a.hi, 0.f};
 }
 __device__ __forceinline__ Pair pair_shfl_xor(Pair a, int o) {
   return {__shfl_xor_sync(kAllLanes, a.hi, o), __shfl_xor_sync(kAllLanes, a.lo, o)};

@@ -347,7 +347,7 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   __syncthreads();  // every thread has seen sums->nan
   if (threadIdx.x) return;
   for (int w = 1; w < kWarps; ++w) v = pair_join(v, red[w]);
-  a.loss[0] = a.coef * (float)pair_value(v);
+  a.loss[0] = a.coef * as_df(v).hi;
   sums->tokens = 0;
   sums->nan = 0;
   ctrl->loss_ticket = 0;

@@ -375,20 +375,26 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
   sum[6] = pair_of(below);
   sum[7] = pair_of(tokens);
   if (!grid_join<NT, kSums>(sum, total, part, &ctrl->loss_ticket)) return;
-  if (threadIdx.x == 0) {
-    double v[kSums];
-    for (int k = 0; k < kSums; ++k) v[k] = pair_value(total[k]);
-    const double n = v[7] > 0.0 ? v[7] : 1.0;
-    loss[0] = (float)(v[0] + (rule.kl_coef != 0.f ? (double)rule.kl_coef * v[1] : 0.0) -
-                      (rule.entropy_coef != 0.f ? (double)rule.entropy_coef * v[2] : 0.0));
-    loss[1] = (float)v[0];
-    loss[2] = (float)v[1];
-    loss[3] = (float)v[2];
-    loss[4] = (float)(v[5] / n);
-    loss[5] = (float)(v[6] / n);
-    loss[6] = v[7] > 0.0 ? (float)(1.0 + v[3] / n) : 0.f;
-    loss[7] = (float)(v[4] / n);
-    ctrl->loss_tokens = 0;
+  // an output per thread, in pairs: fp64 divisions one after another cost a microsecond
+  if (threadIdx.x < 8) {
+    const uint32_t k = threadIdx.x;
+    const float n = total[7].hi + total[7].lo;
+    if (k == 0) {
+      df l = as_df(total[0]);
+      if (rule.kl_coef != 0.f) l = df_add(l, df_mul(as_df(total[1]), rule.kl_both));
+      if (rule.entropy_coef != 0.f) l = df_add(l, df_mul(as_df(total[2]), rule.less_entropy));
+      // pairs lose infinities, plain numbers do not
+      loss[0] = isfinite(l.hi) ? l.hi
+                : total[0].hi + (rule.kl_coef != 0.f ? rule.kl_coef * total[1].hi : 0.f) -
+                      (rule.entropy_coef != 0.f ? rule.entropy_coef * total[2].hi : 0.f);
+      ctrl->loss_tokens = 0;
+    } else if (k < 4) {
+      loss[k] = as_df(total[k - 1]).hi;
+    } else {
+      const int from = k == 4 ? 5 : k == 5 ? 6 : k == 6 ? 3 : 4;
+      const float mean = n > 0.f ? as_df(total[from]).hi / n : 0.f;
+      loss[k] = k == 6 && n > 0.f ? 1.f + mean : mean;
+    }
   }
 }
 
@@ -404,6 +410,12 @@ PolicyRule policy_rule(const edp_policy_config &c) {
   r.entropy_coef = (float)c.entropy_coef;
   r.grad_scale = (float)c.grad_scale;
   r.kl = c.kl;
+  auto both = [](double v) {
+    const float hi = (float)v;
+    return df{hi, (float)(v - (double)hi)};
+  };
+  r.kl_both = both(c.kl_coef);
+  r.less_entropy = both(-c.entropy_coef);
   return r;
 }
 

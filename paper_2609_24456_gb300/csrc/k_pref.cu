@@ -44,8 +44,8 @@ struct PrefScratch {
 
 struct PrefRule {
   df beta, margin, half;  // half: 1 / (2 beta)
+  df per_norm, per_pair;  // 1 / norm and 1 / pairs
   float smooth;
-  double norm;
   uint32_t kind, average;
 };
 
@@ -220,9 +220,6 @@ constexpr float kHiUnit = 1.f / 1048576.f;              // 2^-20
 constexpr float kLoUnit = 1.f / 4611686018427387904.f;  // 2^-62
 constexpr float kGradMost = 4194304.f;                  // 2^22
 
-__device__ __forceinline__ df as_df(Pair a) {
-  return isfinite(a.hi) ? quick_two_sum(a.hi, a.lo) : df{a.hi, 0.f};
-}
 // x / n for a whole number n
 __device__ __forceinline__ df df_over(df x, uint32_t n) {
   const float nh = (float)n, nl = (float)((long long)n - (long long)nh);
@@ -307,10 +304,11 @@ __device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
   }
 }
 
-__device__ __forceinline__ void write_loss(const PrefRule &r, uint32_t n_pair, const Pair *total,
-                                           float *loss) {
-  loss[0] = (float)(pair_value(total[0]) / r.norm);
-  for (int k = 1; k < 4; ++k) loss[k] = (float)(pair_value(total[k]) / (double)n_pair);
+// An output by each of four threads.
+__device__ __forceinline__ void write_loss(const PrefRule &r, const Pair *total, float *loss) {
+  if (threadIdx.x >= 4) return;
+  const df v = as_df(total[threadIdx.x]), by = threadIdx.x ? r.per_pair : r.per_norm;
+  loss[threadIdx.x] = isfinite(v.hi) ? df_mul(v, by).hi : v.hi;
 }
 
 // The gradient of each token of a sequence, rounded once.
@@ -429,8 +427,8 @@ k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, uint32_t pair_ct
   else
     take_ratios(in, r, x, out, (blockIdx.x - pair_ctas) * kPairThreads + threadIdx.x,
                 (uint64_t)(gridDim.x - pair_ctas) * kPairThreads);
-  if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
-    write_loss(r, in.n_pair, total, out.loss);
+  if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
+    write_loss(r, total, out.loss);
 }
 
 template <bool VEC>
@@ -461,8 +459,8 @@ k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *
   take_pairs(in, r, x, out, threadIdx.x, kSmallThreads, sum, ctrl);
   take_ratios(in, r, x, out, threadIdx.x, kSmallThreads);
   __threadfence();
-  if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket) && threadIdx.x == 0)
-    write_loss(r, in.n_pair, total, out.loss);
+  if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
+    write_loss(r, total, out.loss);
   if (out.dlogp)
     run_grad<VEC>(in, x, scale, out.dlogp, begin, begin + x.run, first, end);
 }
@@ -513,8 +511,10 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   r.smooth = (float)cfg.label_smoothing;
   r.margin = both(cfg.margin);
   r.half = both(0.5 / cfg.beta);
-  r.norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
-  const df scale = both(cfg.grad_scale / r.norm);
+  const double norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
+  r.per_norm = both(1.0 / norm);
+  r.per_pair = both(1.0 / (double)n_pair);
+  const df scale = both(cfg.grad_scale / norm);
   r.kind = cfg.kind;
   r.average = cfg.average;
   const PrefIn in{set, logp, ref, pair, n_pair};
