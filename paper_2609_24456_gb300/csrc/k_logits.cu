@@ -685,7 +685,7 @@ template <typename T, bool ENT>
 __global__ void __launch_bounds__(kResidentThreads)
 k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
                   const float *adv, PolicyRule rule, float *logp, float *entropy, void *dz,
-                  uint64_t dstride, Ctrl *ctrl) {
+                  uint64_t dstride, bool early, Ctrl *ctrl) {
   constexpr int NT = kResidentThreads;
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 resident[];
@@ -705,7 +705,9 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
     mbar_init_fence();
   }
   __syncthreads();
-  pdl_wait();
+  // early: the kernel before is of this call, waited for all that came before it and
+  // writes the weights alone
+  if (!early) pdl_wait();
   pdl_launch();
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
@@ -719,6 +721,7 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
         flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)a.target[t]);
     }
     part_zero<T, NT>(d, n);
+    if (early) pdl_wait();  // so that what waits for this kernel finds the weights
     return;  // the whole cluster
   }
   const T *p = reinterpret_cast<const T *>(a.z) + t * a.stride + first;
@@ -738,6 +741,7 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const uint32_t at = (uint32_t)a.target[t] - first;  // beyond n: not in this part
   float w = 0.f, old = 0.f, ref = 0.f, ad = 0.f;      // the first warp's, beside the copy
+  if (early) pdl_wait();
   if (wid == 0) {
     w = row_weight(weights, t);
     old = old_logp[t];
@@ -890,7 +894,8 @@ cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float
 
 cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &rule,
                                const RowWeights &w, const PolicyTokens &p, float *logp,
-                               float *entropy, void *dz, uint64_t dstride, cudaStream_t s) {
+                               float *entropy, void *dz, uint64_t dstride, bool early,
+                               cudaStream_t s) {
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     uint32_t parts = row_parts(ctx, z);
@@ -899,16 +904,17 @@ cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &
     while (parts < 8 && z.rows * parts < 8ull * ctx->coop_sms && part_bytes(z, parts) > kLeastPart)
       parts *= 2;
     const size_t bytes = part_bytes(z, parts);
-    auto go = [&](auto kern, int threads, size_t smem) {
-      return launch_rows(kern, z.rows, parts, true, threads, smem, s, row_args(z), w, p.old_logp,
-                         p.ref_logp, p.adv, rule, logp, entropy, dz, dstride, ctx->ctrl);
-    };
     if (bytes > kResidentMost)
-      return go(entropy ? k_policy_rows<T, true> : k_policy_rows<T, false>, kRowThreads, 0);
+      return launch_rows(entropy ? k_policy_rows<T, true> : k_policy_rows<T, false>, z.rows, parts,
+                         true, kRowThreads, 0, s, row_args(z), w, p.old_logp, p.ref_logp, p.adv,
+                         rule, logp, entropy, dz, dstride, ctx->ctrl);
     auto kern = entropy ? k_policy_resident<T, true> : k_policy_resident<T, false>;
     const cudaError_t e = cudaFuncSetAttribute(
         kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
-    return e != cudaSuccess ? e : go(kern, kResidentThreads, bytes);
+    if (e != cudaSuccess) return e;
+    return launch_rows(kern, z.rows, parts, true, kResidentThreads, bytes, s, row_args(z), w,
+                       p.old_logp, p.ref_logp, p.adv, rule, logp, entropy, dz, dstride, early,
+                       ctx->ctrl);
   });
 }
 

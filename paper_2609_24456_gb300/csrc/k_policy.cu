@@ -17,7 +17,8 @@ namespace edp {
 
 cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &rule,
                                const RowWeights &w, const PolicyTokens &p, float *logp,
-                               float *entropy, void *dz, uint64_t dstride, cudaStream_t s);
+                               float *entropy, void *dz, uint64_t dstride, bool early,
+                               cudaStream_t s);
 
 namespace {
 
@@ -102,8 +103,11 @@ __device__ __forceinline__ uint32_t count_few(const TokenSet &s, uint64_t a, uin
 // Each sequence's weight, 1 / (divisor tokens); block: NULL where every token counts.
 __global__ void __launch_bounds__(kThreads)
 k_sequence_weights(TokenSet s, const uint32_t *block, float divisor, float *weight) {
+  // behind k_token_counts, which waited for all that came before this call, what comes
+  // after this kernel may start at once and read what it does not wait for
+  if (block) pdl_launch();
   pdl_wait();
-  pdl_launch();
+  if (!block) pdl_launch();
   const int lane = threadIdx.x & 31;
   const uint64_t step = (uint64_t)gridDim.x * (kThreads / 32);
   for (uint64_t q = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); q < s.n_seq;
@@ -181,12 +185,14 @@ __device__ __forceinline__ void sequence_weights(const TokenSet &s, uint64_t end
 template <int NT, bool SEQ, bool VEC, Kl KL>
 __global__ void __launch_bounds__(NT, NT == kSmallThreads ? 1 : kPerSm)
 k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor, float *loss,
-         float *dlogp, float *dentropy, Pair *part, Ctrl *ctrl) {
+         float *dlogp, float *dentropy, Pair *part, bool early, Ctrl *ctrl) {
   constexpr bool kOne = NT == kSmallThreads;
   constexpr uint32_t kWarps = NT / 32;
   __shared__ OneCta<kOne ? NT : 32> one;
   __shared__ Pair total[kSums];
-  pdl_wait();
+  // early (one CTA): the kernel before is of this call and writes logp and entropy
+  // alone; the rest is there already
+  if (!kOne || !early) pdl_wait();
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Range r = token_range(s);
   float fixed = w.fixed;
@@ -224,19 +230,19 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
     const uint32_t e = i + 4 * lane;
     x.rf = x.en = none;
     if (i + kTile <= whole) {
-      x.lp = *reinterpret_cast<const float4 *>(lpc + e);
+      if (!kOne) x.lp = *reinterpret_cast<const float4 *>(lpc + e);
       x.od = *reinterpret_cast<const float4 *>(odc + e);
       x.ad = *reinterpret_cast<const float4 *>(adc + e);
       if (KL != Kl::kNone) x.rf = *reinterpret_cast<const float4 *>(rfc + e);
-      if (p.entropy) x.en = *reinterpret_cast<const float4 *>(enc + e);
+      if (!kOne && p.entropy) x.en = *reinterpret_cast<const float4 *>(enc + e);
       x.m = s.mask ? *reinterpret_cast<const uint32_t *>(mc + e) : 0xffffffffu;
     } else {
       const uint64_t t = c0 + e;
-      x.lp = load4<VEC>(p.logp, t, s.n);
+      if (!kOne) x.lp = load4<VEC>(p.logp, t, s.n);
       x.od = load4<VEC>(p.old_logp, t, s.n);
       x.ad = load4<VEC>(p.adv, t, s.n);
       if (KL != Kl::kNone) x.rf = load4<VEC>(p.ref_logp, t, s.n);
-      if (p.entropy) x.en = load4<VEC>(p.entropy, t, s.n);
+      if (!kOne && p.entropy) x.en = load4<VEC>(p.entropy, t, s.n);
       const uint32_t bits = token_bits<VEC>(s, t, r.first, r.end);
       x.m = (bits & 1u) | (bits & 2u) << 7 | (bits & 4u) << 14 | (bits & 8u) << 21;
     }
@@ -251,18 +257,15 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
   auto place = [&](uint64_t t) {
     return t > c0 ? (uint32_t)min(t - c0, (uint64_t)cn + kTile) : 0u;
   };
-  Tile ahead;
   const uint32_t share = (cn / kTile + kWarps - 1 + (cn % kTile != 0)) / kWarps * kTile;
   const uint32_t stop = (uint32_t)min((uint64_t)cn, (uint64_t)(wid + 1) * share);
   uint32_t i = wid * share;
-  if (false && i < stop) ahead = load(i);
 #pragma unroll 1
   while (i < stop) {
    const uint32_t group = min(stop, i + kFlush * kTile);
 #pragma unroll 1
    for (; i < group; i += kTile) {
-    const Tile x = false ? ahead : load(i);
-    if (false && stop - i > kTile) ahead = load(i + kTile);
+    Tile x = load(i);
     bool b[4];  // which of the lane's tokens count
 #pragma unroll
     for (int k = 0; k < 4; ++k) b[k] = x.m & (0xffu << (8 * k));
@@ -320,6 +323,11 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
     } else {
       if (kOne && w.tokens) fixed = 1.f / (float)max(cta_sum<NT>(__popc(bits()), one.red), 1u);
       wt[0] = wt[1] = wt[2] = wt[3] = fixed;
+    }
+    if (kOne) {
+      if (early) pdl_wait();
+      x.lp = load4<VEC>(p.logp, c0 + i + 4 * lane, s.n);
+      if (p.entropy) x.en = load4<VEC>(p.entropy, c0 + i + 4 * lane, s.n);
     }
     // what does not count is 0 from here on, whatever it held
     const float l4[4] = {x.lp.x, x.lp.y, x.lp.z, x.lp.w};
@@ -433,6 +441,7 @@ struct Plan {
   Weighting w;
   float divisor;
   bool sequences;
+  bool early;  // k_token_counts runs first
   Pair *part;
   float *entropy;
 };
@@ -447,6 +456,7 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
   p->w = Weighting{};
   p->w.fixed = 1.f / p->divisor;
   const bool blocks = p->sequences && (set.mask || set.target) && !one_cta;
+  p->early = !one_cta && (blocks || by_total);
   size_t at = 0;
   auto take = [&](bool want, uint64_t bytes) {
     const size_t a = at;
@@ -485,11 +495,11 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
 
 template <bool VEC>
 cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t,
-                          const PolicyRule &rule, const Plan &p, bool one_cta, float *loss,
-                          float *dlogp, float *dentropy, cudaStream_t s) {
+                          const PolicyRule &rule, const Plan &p, bool one_cta, bool early,
+                          float *loss, float *dlogp, float *dentropy, cudaStream_t s) {
   auto go = [&](auto kern, unsigned grid, int threads) {
     return launch_pdl(kern, dim3(grid), dim3(threads), s, set, t, rule, p.w, p.divisor, loss,
-                      dlogp, dentropy, p.part, c->ctrl);
+                      dlogp, dentropy, p.part, early, c->ctrl);
   };
   const uint64_t want = (set.n + 4 * kThreads - 1) / (4 * kThreads);
   const unsigned grid = at_most(want, (uint64_t)kPerSm * (uint64_t)c->coop_sms);
@@ -518,8 +528,8 @@ cudaError_t launch_policy_loss(edp_ctx *c, const edp_policy_config &cfg, const T
   const bool vec = aligned_to(16, t.logp, t.old_logp, t.ref_logp, t.adv, t.entropy, dlogp,
                               dentropy) && aligned_to(4, set.mask);
   const PolicyRule rule = policy_rule(cfg);
-  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, loss, dlogp, dentropy, s)
-             : launch_policy<false>(c, set, t, rule, p, one_cta, loss, dlogp, dentropy, s);
+  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, false, loss, dlogp, dentropy, s)
+             : launch_policy<false>(c, set, t, rule, p, one_cta, false, loss, dlogp, dentropy, s);
 }
 
 cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
@@ -533,7 +543,7 @@ cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
   if (own_entropy) entropy = p.entropy;
   const PolicyRule rule = policy_rule(cfg);
   const RowWeights w{set.off, (uint32_t)set.n_seq, p.w.sequence, p.w.tokens, p.w.fixed};
-  e = launch_policy_rows(c, z, rule, w, t, logp, entropy, dz, dstride, s);
+  e = launch_policy_rows(c, z, rule, w, t, logp, entropy, dz, dstride, p.early, s);
   if (e != cudaSuccess) return e;
   PolicyTokens q = t;
   q.logp = logp;
@@ -541,8 +551,8 @@ cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
   const bool one_cta = set.n <= 4 * kSmallThreads;
   const bool vec = aligned_to(16, t.old_logp, t.ref_logp, t.adv, logp, entropy) &&
                    aligned_to(4, set.mask);
-  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, loss, nullptr, nullptr, s)
-             : launch_policy<false>(c, set, q, rule, p, one_cta, loss, nullptr, nullptr, s);
+  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, true, loss, nullptr, nullptr, s)
+             : launch_policy<false>(c, set, q, rule, p, one_cta, true, loss, nullptr, nullptr, s);
 }
 
 }  // namespace edp
