@@ -821,13 +821,15 @@ RowArgs row_args(const Logits &z) {
   return a;
 }
 
-// CTAs per row: one for at least two waves of rows, else so many (up to 8, a
-// portable cluster) that the chip has work, each with two vectors per thread.
-uint32_t row_parts(const edp_ctx *c, const Logits &z) {
+// CTAs per row: up to 8 (a portable cluster), each with two vectors per thread, until
+// there are per_sm for each SM.  Where they join their sums (per_sm 2) fewer and larger
+// parts are faster (500 rows of 152,064: 25 us with 1 CTA each, 38 with 4); the
+// gradient's need not wait for one another (16 per SM: 48 us, 53 with 2).
+uint32_t row_parts(const edp_ctx *c, const Logits &z, uint64_t per_sm) {
   const uint64_t size = z.dtype == EDP_F32 ? 4 : 2;
   const uint64_t least = (uint64_t)kRowThreads * 32 / size;
   uint32_t p = 1;
-  while (p < 8 && z.rows * p < 2ull * c->coop_sms && z.vocab >= 2 * p * least) p *= 2;
+  while (p < 8 && z.rows * p < per_sm * (uint64_t)c->coop_sms && z.vocab >= 2 * p * least) p *= 2;
   return p;
 }
 
@@ -875,7 +877,7 @@ cudaError_t launch_token_logprob(edp_ctx *ctx, const Logits &z, float *logp, flo
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     auto kern = entropy ? k_token_logprob<T, true> : k_token_logprob<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), true, kRowThreads, 0, s, row_args(z), logp,
+    return launch_rows(kern, z.rows, row_parts(ctx, z, 2), true, kRowThreads, 0, s, row_args(z), logp,
                        entropy, stats, ctx->ctrl);
   });
 }
@@ -887,8 +889,8 @@ cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
     auto kern = entropy ? k_token_logprob_grad<T, true> : k_token_logprob_grad<T, false>;
-    return launch_rows(kern, z.rows, row_parts(ctx, z), false, kRowThreads, 0, s, row_args(z), stats,
-                       entropy, dlogp, dentropy, dz, dstride, ctx->ctrl);
+    return launch_rows(kern, z.rows, row_parts(ctx, z, 16), false, kRowThreads, 0, s, row_args(z),
+                       stats, entropy, dlogp, dentropy, dz, dstride, ctx->ctrl);
   });
 }
 
@@ -898,7 +900,7 @@ cudaError_t launch_policy_rows(edp_ctx *ctx, const Logits &z, const PolicyRule &
                                cudaStream_t s) {
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    uint32_t parts = row_parts(ctx, z);
+    uint32_t parts = row_parts(ctx, z, 2);
     while (parts < 8 && part_bytes(z, parts) > kResidentPart) parts *= 2;
     // few rows: smaller parts, so that the last of them are a small share
     while (parts < 8 && z.rows * parts < 8ull * ctx->coop_sms && part_bytes(z, parts) > kLeastPart)

@@ -7,7 +7,7 @@
 // a sequence its lanes add on their own; where sequences end in a tile, a
 // segmented scan gives each one's part of the run.  Whoever wants a sequence's
 // sum adds its parts in order.  A sequence's gradients from its pairs add up as
-// whole numbers, in any order to the same bits.  A batch of up to 4,096 tokens
+// whole numbers, in any order to the same bits.  A batch of up to 8,192 tokens
 // takes all three steps in one CTA.
 #include "edp_loss.cuh"
 
@@ -17,7 +17,8 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kPerSm = 2;            // CTAs of the sums, in one wave
 constexpr int kGradPerSm = 4;        // and of the gradient
-constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
+constexpr int kSmallThreads = 1024;  // a batch of up to 8,192 tokens, in one CTA
+constexpr uint32_t kSmallRun = 2 * kTile;
 constexpr int kPairThreads = 128;
 constexpr uint32_t kSmallPairs = 4096;
 constexpr uint32_t kAtOnce = 4;  // tiles in flight per warp
@@ -84,9 +85,10 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
   const uint32_t n_seq = (uint32_t)s.n_seq;
   stop = min(stop, end);
   if (begin >= stop) return;
-  auto emit = [&](uint32_t q, const Run &r) {
+  // the part of sequence q, which starts at `start`
+  auto emit = [&](uint32_t q, uint64_t start, const Run &r) {
     const SeqPart p{r.v.hi, r.v.lo, r.n, 0};
-    if (s.off[q] >= begin) {
+    if (start >= begin) {
       x.inner[q] = p;
       x.grad[q] = SeqGrad{0, 0};
       x.bad[q] = 0;
@@ -96,8 +98,12 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
   };
   const Run none{{0.f, 0.f}, 0};
   Run mine = none;  // a lane's share of the sequence that is open
+  // the sequence of the tile's first token, and where the one after it ends
   SeqWalk walk;
   walk.start(s.off, n_seq, begin);
+  uint64_t start = s.off[walk.q];
+  auto end_after = [&](uint32_t q) { return q + 1 < n_seq ? s.off[q + 2] : ~0ull; };
+  uint64_t after = end_after(walk.q);
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   for (uint64_t t0 = begin; t0 < stop; t0 += kTile) {
     // tiles that the sequence goes through, kAtOnce of them in flight
@@ -138,36 +144,51 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
     const float4 rf = in.ref ? load4<VEC>(in.ref, t, s.n) : zero;
     const uint32_t bits = token_bits<VEC>(s, t, first, stop);
     const float l4[4] = {lp.x, lp.y, lp.z, lp.w}, r4[4] = {rf.x, rf.y, rf.z, rf.w};
-    if (t0 + kTile < walk.next && t0 + kTile < stop) {
+    // up to one end in this tile: the lanes go on adding, and give their shares at it
+    if (t0 + kTile < walk.next || t0 + kTile < after) {
+      const bool ends = walk.next <= t0 + kTile;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (bits >> i & 1u) run_add(mine, l4[i], r4[i]);
+        if ((bits >> i & 1u) && t + i < walk.next) run_add(mine, l4[i], r4[i]);
+      if (!ends) continue;
+      const Run all{warp_join(mine.v), __reduce_add_sync(kAllLanes, mine.n)};
+      if (lane == 0 && walk.next > start && walk.next > begin) emit(walk.q, start, all);
+      mine = none;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((bits >> i & 1u) && t + i >= walk.next) run_add(mine, l4[i], r4[i]);
+      start = walk.next;
+      walk.next = after;
+      ++walk.q;
+      after = end_after(walk.q);
       continue;
     }
-    // sequences end in this tile, or the run does
+    // several
     SeqWalk ahead = walk;
     ahead.to(s.off, n_seq, min(t0 + kTile, stop) - 1);
     Run carry{warp_join(mine.v), __reduce_add_sync(kAllLanes, mine.n)};
     mine = none;
     Run open = none, closed = none;
     uint32_t q = walk.q, closed_q = 0;
-    uint64_t next = 0;
+    uint64_t from = 0, next = 0, closed_from = 0;
     bool cut = false, pending = false;  // one ended here; its start is in another lane's tokens
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (t + i >= stop || t + i < first) continue;
       if (t + i >= next) {
         q = sequence_of(s.off, q, ahead.q + 1, t + i);
-        next = min(s.off[q + 1], end);
+        from = s.off[q];
+        next = s.off[q + 1];
       }
       if (bits >> i & 1u) run_add(open, l4[i], r4[i]);
-      if (t + i + 1 == next || t + i + 1 == stop) {
-        if (!cut && s.off[q] < t) {
+      if (t + i + 1 == next) {
+        if (!cut && from < t) {
           closed = open;
           closed_q = q;
+          closed_from = from;
           pending = true;
         } else {
-          emit(q, open);
+          emit(q, from, open);
         }
         cut = true;
         open = none;
@@ -193,11 +214,19 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
     }
     if (pending) {
       if (!into_cut) into = run_join(carry, into);
-      emit(closed_q, run_join(into, closed));
+      emit(closed_q, closed_from, run_join(into, closed));
     }
     if (lane == 31) mine = c ? incl : run_join(carry, incl);
     walk = ahead;
-    walk.to(s.off, n_seq, min(t0 + kTile, stop - 1));
+    // on to what the next tile starts in; past the last sequence there is none
+    if (t0 + kTile < stop) walk.to(s.off, n_seq, t0 + kTile);
+    start = s.off[walk.q];
+    after = end_after(walk.q);
+  }
+  // the sequence that the run leaves open
+  if (walk.q < n_seq && start < stop && walk.next > stop) {
+    const Run all{warp_join(mine.v), __reduce_add_sync(kAllLanes, mine.n)};
+    if (lane == 0) emit(walk.q, start, all);
   }
 }
 
@@ -441,7 +470,7 @@ k_pref_grad(PrefIn in, PrefScratch x, df scale, uint32_t run, float *dlogp) {
   run_grad<VEC>(in, x, scale, dlogp, begin, begin + run, first, end);
 }
 
-// All three steps of a batch of up to 4 kSmallThreads tokens, a tile per warp.
+// All three steps of a batch of up to 8,192 tokens, two tiles per warp.
 template <bool VEC>
 __global__ void __launch_bounds__(kSmallThreads)
 k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *ctrl) {
@@ -473,12 +502,12 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
                                    float *ratio, float *pair_loss, float *dlogp,
                                    cudaStream_t s) {
   const uint64_t sms = (uint64_t)c->coop_sms;
-  const bool small = set.n <= 4 * kSmallThreads && n_pair <= kSmallPairs;
+  const bool small = set.n <= kSmallRun * (kSmallThreads / 32) && n_pair <= kSmallPairs;
   // a run per warp of a full chip, so that all end together
   const uint64_t warps = kThreads / 32;
   auto run_of = [&](uint64_t per_sm) {
     const uint64_t chip = per_sm * warps * sms, each = (set.n + chip - 1) / chip;
-    return small ? (uint64_t)kTile : (each + kTile - 1) / kTile * kTile;
+    return small ? (uint64_t)kSmallRun : (each + kTile - 1) / kTile * kTile;
   };
   const uint64_t run = run_of(kPerSm), grad_run = run_of(kGradPerSm);
   const uint64_t runs = (set.n + run - 1) / run;
