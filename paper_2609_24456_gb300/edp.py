@@ -633,11 +633,18 @@ def make_preference_config(beta, kind=EDP_PREF_LOGISTIC, label_smoothing=0.0, ma
                                  int(bool(average)))
 
 
+_dtypes = {}  # edp_dtype by torch type, filled as types are met (torch is not imported here)
+
+
 def _dtype(t):
-    name = str(t.dtype)
-    if name not in ("torch.float32", "torch.bfloat16", "torch.float16"):
-        raise TypeError("logits of %s: float32, bfloat16 or float16" % name)
-    return {"torch.float32": EDP_F32, "torch.bfloat16": EDP_BF16, "torch.float16": EDP_F16}[name]
+    code = _dtypes.get(t.dtype)
+    if code is None:
+        name = str(t.dtype)
+        if name not in ("torch.float32", "torch.bfloat16", "torch.float16"):
+            raise TypeError("logits of %s: float32, bfloat16 or float16" % name)
+        code = _dtypes[t.dtype] = {"torch.float32": EDP_F32, "torch.bfloat16": EDP_BF16,
+                                   "torch.float16": EDP_F16}[name]
+    return code
 
 
 def _rows(t):
