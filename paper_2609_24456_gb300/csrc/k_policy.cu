@@ -190,13 +190,13 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
   constexpr uint32_t kWarps = NT / 32;
   __shared__ OneCta<kOne ? NT : 32> one;
   __shared__ Pair total[kSums];
-  // early (one CTA): the kernel before is of this call and writes logp and entropy
-  // alone; the rest is there already
-  if (!kOne || !early) pdl_wait();
+  // early: the kernel before is of this call and waited, itself or the one before it,
+  // for all that came before; it writes logp and entropy (one CTA) or the weights alone
+  if (!early) pdl_wait();
+  bool waited = !early;
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const Range r = token_range(s);
   float fixed = w.fixed;
-  if (!kOne && !SEQ && w.tokens) fixed = 1.f / (float)max(__ldcg(w.tokens), 1ull);
   Pair sum[kSums];
 #pragma unroll
   for (int k = 0; k < kSums; ++k) sum[k] = Pair{0.f, 0.f};
@@ -266,6 +266,10 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
 #pragma unroll 1
    for (; i < group; i += kTile) {
     Tile x = load(i);
+    if (!kOne && !waited) {
+      pdl_wait();
+      waited = true;
+    }
     bool b[4];  // which of the lane's tokens count
 #pragma unroll
     for (int k = 0; k < 4; ++k) b[k] = x.m & (0xffu << (8 * k));
@@ -321,11 +325,13 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
         }
       }
     } else {
+      if (!kOne && w.tokens) fixed = 1.f / (float)max(__ldcg(w.tokens), 1ull);
       if (kOne && w.tokens) fixed = 1.f / (float)max(cta_sum<NT>(__popc(bits()), one.red), 1u);
       wt[0] = wt[1] = wt[2] = wt[3] = fixed;
     }
     if (kOne) {
-      if (early) pdl_wait();
+      if (!waited) pdl_wait();
+      waited = true;
       x.lp = load4<VEC>(p.logp, c0 + i + 4 * lane, s.n);
       if (p.entropy) x.en = load4<VEC>(p.entropy, c0 + i + 4 * lane, s.n);
     }
@@ -379,6 +385,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
    }
    flush();
   }
+  if (!waited) pdl_wait();  // a warp without tokens: before the CTA's sums go out
   sum[5] = pair_of(above);
   sum[6] = pair_of(below);
   sum[7] = pair_of(tokens);
@@ -528,8 +535,8 @@ cudaError_t launch_policy_loss(edp_ctx *c, const edp_policy_config &cfg, const T
   const bool vec = aligned_to(16, t.logp, t.old_logp, t.ref_logp, t.adv, t.entropy, dlogp,
                               dentropy) && aligned_to(4, set.mask);
   const PolicyRule rule = policy_rule(cfg);
-  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, false, loss, dlogp, dentropy, s)
-             : launch_policy<false>(c, set, t, rule, p, one_cta, false, loss, dlogp, dentropy, s);
+  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s)
+             : launch_policy<false>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s);
 }
 
 cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
@@ -551,8 +558,9 @@ cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
   const bool one_cta = set.n <= 4 * kSmallThreads;
   const bool vec = aligned_to(16, t.old_logp, t.ref_logp, t.adv, logp, entropy) &&
                    aligned_to(4, set.mask);
-  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, true, loss, nullptr, nullptr, s)
-             : launch_policy<false>(c, set, q, rule, p, one_cta, true, loss, nullptr, nullptr, s);
+  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr, s)
+             : launch_policy<false>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr,
+                                    s);
 }
 
 }  // namespace edp

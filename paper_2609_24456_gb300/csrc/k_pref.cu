@@ -357,7 +357,7 @@ __device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, 
 template <bool VEC>
 __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x, df scale,
                                          float *dlogp, uint64_t begin, uint64_t stop,
-                                         uint64_t first, uint64_t end) {
+                                         uint64_t first, uint64_t end, bool wait) {
   const TokenSet &s = in.s;
   const uint32_t n_seq = (uint32_t)s.n_seq;
   const int lane = threadIdx.x & 31;
@@ -366,6 +366,8 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
   uint64_t after = 0;           // where the sequence after the walk's ends
   float here = 0.f, there = 0.f;  // gradients of both
   bool known = false;
+  if (begin < min(stop, end)) walk.start(s.off, n_seq, begin);
+  if (wait) pdl_wait();  // for the gradients: the offsets and the mask are inputs
   for (uint64_t t0 = begin; t0 < stop;) {
     const uint64_t t = t0 + 4 * lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -377,7 +379,6 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
           here = there;
         } else {
           if (known) walk.to(s.off, n_seq, t0);
-          else walk.start(s.off, n_seq, t0);
           here = token_grad(x, walk.q, scale);
         }
         known = true;
@@ -463,11 +464,11 @@ k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, uint32_t pair_ct
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads, kGradPerSm)
 k_pref_grad(PrefIn in, PrefScratch x, df scale, uint32_t run, float *dlogp) {
-  pdl_wait();
+  // behind k_pref_pairs, whose call waited for all that came before it
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
   const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * run;
-  run_grad<VEC>(in, x, scale, dlogp, begin, begin + run, first, end);
+  run_grad<VEC>(in, x, scale, dlogp, begin, begin + run, first, end, true);
 }
 
 // All three steps of a batch of up to 8,192 tokens, two tiles per warp.
@@ -491,7 +492,7 @@ k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *
   if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
     write_loss(r, total, out.loss);
   if (out.dlogp)
-    run_grad<VEC>(in, x, scale, out.dlogp, begin, begin + x.run, first, end);
+    run_grad<VEC>(in, x, scale, out.dlogp, begin, begin + x.run, first, end, false);
 }
 
 }  // namespace
