@@ -174,6 +174,30 @@ __device__ __forceinline__ Pair warp_join(Pair a) {
   return a;
 }
 
+// K sums of a warp's lanes at once, K a power of two: in each step a lane hands over
+// half of the sums that it still has for as many of the other half.  Sum k ends in
+// lanes k 32/K and on; the order is fixed.
+template <int K>
+__device__ __forceinline__ Pair warp_join_all(const Pair (&mine)[K]) {
+  Pair v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = mine[k];
+  const int lane = threadIdx.x & 31;
+  int o = 16;
+#pragma unroll
+  for (int h = K / 2; h; h /= 2, o /= 2) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const Pair give = upper ? v[i] : v[i + h], keep = upper ? v[i + h] : v[i];
+      v[i] = pair_join(keep, pair_shfl_xor(give, o));
+    }
+  }
+#pragma unroll
+  for (; o; o >>= 1) v[0] = pair_join(v[0], pair_shfl_xor(v[0], o));
+  return v[0];
+}
+
 // K sums over the grid: the pairs of every thread of every CTA joined in a fixed
 // order.  True in the last CTA to arrive, where total[] (shared) then holds them.
 // part: [K][gridDim.x]; ticket: 0 before and after.
@@ -184,13 +208,10 @@ __device__ __forceinline__ bool grid_join(const Pair (&mine)[K], Pair *total, Pa
   __shared__ Pair red[K][NT / 32];
   __shared__ bool last;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const Pair v = warp_join(mine[k]);
-    if (lane == 0) red[k][wid] = v;
-  }
+  Pair v = warp_join_all(mine);
+  if (lane % (32 / K) == 0) red[lane / (32 / K)][wid] = v;
   __syncthreads();
-  Pair v{0.f, 0.f};
+  v = Pair{0.f, 0.f};
   if (wid < K) {
     if (lane < NT / 32) v = red[wid][lane];
     v = warp_join(v);

@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxExperts = 1024;
-constexpr uint64_t kOneCta = 32768;
+constexpr uint64_t kOneCta = 16384;
 constexpr float kProbUnits = 1099511627776.f;  // 2^40
 
 }  // namespace

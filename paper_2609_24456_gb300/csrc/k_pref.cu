@@ -481,14 +481,14 @@ k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
   const uint64_t begin = (uint64_t)(threadIdx.x >> 5) * x.run;
   run_parts<VEC>(in, x, begin, begin + x.run, first, end);
-  __threadfence();  // the pairs read around the first-level cache
   __syncthreads();
   Pair sum[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
-  take_pairs(in, r, x, out, threadIdx.x, kSmallThreads, sum, ctrl);
-  take_ratios(in, r, x, out, threadIdx.x, kSmallThreads);
-  __threadfence();
+  constexpr uint32_t kHalf = kSmallThreads / 2;  // the ratios by warps of their own
+  if (threadIdx.x < kHalf) take_pairs(in, r, x, out, threadIdx.x, kHalf, sum, ctrl);
+  else take_ratios(in, r, x, out, threadIdx.x - kHalf, kHalf);
+  // the barriers of the join order the CTA's gradients before their use
   if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
     write_loss(r, total, out.loss);
   if (out.dlogp)
