@@ -373,8 +373,10 @@ cudaError_t launch_shape(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cu
   if (e != cudaSuccess) return e;
   const uint64_t b = (a.rows * L + kThreads - 1) / kThreads;
   const uint64_t wave = kBalancePerSm<V * VN> * sms;
-  return launch_pdl(k_balance<T, L, V, VN, kThreads, false>,
-                    dim3((unsigned)(b < wave ? b : wave)), dim3(kThreads), s, a, sums, c->ctrl);
+  e = launch_pdl(k_balance<T, L, V, VN, kThreads, false>,
+                 dim3((unsigned)(b < wave ? b : wave)), dim3(kThreads), s, a, sums, c->ctrl);
+  if (e != cudaSuccess) cudaMemsetAsync(sums, 0, sizeof *sums, s);  // the counts go no further
+  return e;
 }
 
 template <typename T>

@@ -32,6 +32,7 @@ constexpr int kFlush = 8;  // tiles (32 tokens a lane) between two additions to 
 struct Weighting {
   const float *sequence;             // SEQ_MEAN: each sequence's weight
   const unsigned long long *tokens;  // TOKEN_MEAN without norm: the divisor
+  bool by_range;                     // the same where every token of the sequences counts
   float fixed;                       // otherwise: every weight
 };
 
@@ -325,6 +326,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
         }
       }
     } else {
+      if (w.by_range) fixed = r.end > r.first ? 1.f / (float)(r.end - r.first) : 0.f;
       if (!kOne && w.tokens) fixed = 1.f / (float)max(__ldcg(w.tokens), 1ull);
       if (kOne && w.tokens) fixed = 1.f / (float)max(cta_sum<NT>(__popc(bits()), one.red), 1u);
       wt[0] = wt[1] = wt[2] = wt[3] = fixed;
@@ -459,10 +461,13 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
   const uint64_t sms = (uint64_t)c->coop_sms;
   p->sequences = set.reduce == EDP_REDUCE_SEQ_MEAN;
   p->divisor = (float)(set.norm > 0.0 ? set.norm : (double)set.n_seq);
-  const bool by_total = set.reduce == EDP_REDUCE_TOKEN_MEAN && !(set.norm > 0.0);
+  const bool chosen = set.mask || set.target;
+  const bool mean = set.reduce == EDP_REDUCE_TOKEN_MEAN && !(set.norm > 0.0);
+  const bool by_total = mean && chosen;
   p->w = Weighting{};
   p->w.fixed = 1.f / p->divisor;
-  const bool blocks = p->sequences && (set.mask || set.target) && !one_cta;
+  p->w.by_range = mean && !chosen;
+  const bool blocks = p->sequences && chosen && !one_cta;
   p->early = !one_cta && (blocks || by_total);
   size_t at = 0;
   auto take = [&](bool want, uint64_t bytes) {
@@ -500,6 +505,11 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
   return e;
 }
 
+// The count that k_policy would have set back to 0, after a launch that failed.
+void forget_count(edp_ctx *c, const Plan &p, cudaStream_t s) {
+  if (p.w.tokens) cudaMemsetAsync(&c->ctrl->loss_tokens, 0, sizeof c->ctrl->loss_tokens, s);
+}
+
 template <bool VEC>
 cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t,
                           const PolicyRule &rule, const Plan &p, bool one_cta, bool early,
@@ -530,13 +540,15 @@ cudaError_t launch_policy_loss(edp_ctx *c, const edp_policy_config &cfg, const T
                                float *dentropy, cudaStream_t s) {
   const bool one_cta = set.n <= 4 * kSmallThreads;
   Plan p;
-  const cudaError_t e = plan_weights(c, set, one_cta, false, s, &p);
+  cudaError_t e = plan_weights(c, set, one_cta, false, s, &p);
   if (e != cudaSuccess) return e;
   const bool vec = aligned_to(16, t.logp, t.old_logp, t.ref_logp, t.adv, t.entropy, dlogp,
                               dentropy) && aligned_to(4, set.mask);
   const PolicyRule rule = policy_rule(cfg);
-  return vec ? launch_policy<true>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s)
-             : launch_policy<false>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s);
+  e = vec ? launch_policy<true>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s)
+          : launch_policy<false>(c, set, t, rule, p, one_cta, p.early, loss, dlogp, dentropy, s);
+  if (e != cudaSuccess) forget_count(c, p, s);
+  return e;
 }
 
 cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
@@ -551,16 +563,20 @@ cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
   const PolicyRule rule = policy_rule(cfg);
   const RowWeights w{set.off, (uint32_t)set.n_seq, p.w.sequence, p.w.tokens, p.w.fixed};
   e = launch_policy_rows(c, z, rule, w, t, logp, entropy, dz, dstride, p.early, s);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess) {
+    forget_count(c, p, s);
+    return e;
+  }
   PolicyTokens q = t;
   q.logp = logp;
   q.entropy = entropy;
   const bool one_cta = set.n <= 4 * kSmallThreads;
   const bool vec = aligned_to(16, t.old_logp, t.ref_logp, t.adv, logp, entropy) &&
                    aligned_to(4, set.mask);
-  return vec ? launch_policy<true>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr, s)
-             : launch_policy<false>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr,
-                                    s);
+  e = vec ? launch_policy<true>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr, s)
+          : launch_policy<false>(c, set, q, rule, p, one_cta, one_cta, loss, nullptr, nullptr, s);
+  if (e != cudaSuccess) forget_count(c, p, s);
+  return e;
 }
 
 }  // namespace edp

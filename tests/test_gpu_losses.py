@@ -181,7 +181,8 @@ def test_policy_special_values(edp_lib):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("rows,vocab", [(1, 3), (5, 1000), (40, 20_011), (333, 4097), (3, 152_064)])
+@pytest.mark.parametrize("rows,vocab", [(1, 3), (5, 1000), (40, 20_011), (333, 4097), (3, 152_064),
+                                        (5000, 130)])
 @pytest.mark.parametrize("reduce", [0, 1])
 def test_policy_from_logits(edp_lib, dtype, rows, vocab, reduce):
     """The fused form against the oracle's three steps, in place and not, and
@@ -620,6 +621,59 @@ def test_losses_on_streams_and_in_a_graph(edp_lib):
     torch.cuda.synchronize()
     for x, y, w in zip(a, b, c):
         assert torch.equal(x, y) and torch.equal(x, w)
+    edp.edp_sync(ring.ctx)
+
+
+def test_losses_between_calls_that_share_their_scratch(edp_lib):
+    """Advantages, packing and each loss in turn on one stream, without waiting
+    between them, give the bits that each gives on its own."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    rng = np.random.default_rng(8)
+    off = offsets(rng, 60, 300)
+    n = int(off[-1])
+    logp, old, ref, adv, _ = (cuda(x.astype(np.float32)) for x in policy_case(rng, n))
+    d_off, pair = cuda(off.astype(np.uint64)), cuda(rng.integers(0, 60, (50, 2)))
+    tokens = cuda(rng.integers(0, 9, n).astype(np.int32))
+    idx = torch.arange(60, device="cuda")
+    mask = cuda((rng.random(n) < .8).astype(np.uint8))
+    T, E = 64, 200
+    r, v = torch.randn(T, E, device="cuda"), torch.randn(T + 1, E, device="cuda")
+    d = torch.zeros(T, E, dtype=torch.uint8, device="cuda")
+    z = torch.randn(n, 64, device="cuda")
+    sel = cuda(rng.integers(0, 64, (n, 2)).astype(np.int32))
+    seq = edp.make_policy_config(reduce=edp.EDP_REDUCE_SEQ_MEAN)
+    one = edp.make_policy_config()
+    pref = edp.make_preference_config(.2)
+
+    def calls(wait):
+        out = [torch.zeros(T, E, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"),
+               torch.zeros(61, dtype=torch.int64, device="cuda")]
+        out += [torch.zeros(n, device="cuda") for _ in range(3)]
+        out += [torch.zeros(8, device="cuda") for _ in range(2)]
+        out += [torch.zeros(4, device="cuda"), torch.zeros(1, device="cuda"),
+                torch.zeros(64, dtype=torch.int64, device="cuda"), torch.zeros_like(z)]
+        todo = [
+            lambda: edp.edp_policy_loss(ring.ctx, seq, logp, old, adv, n, out[6], mask=mask,
+                                        off=d_off, n_seq=60, dlogp=out[3]),
+            lambda: edp.edp_gae(ring.ctx, r, v, d, T, E, .99, .95, adv_norm=out[0]),
+            lambda: edp.edp_preference_loss(ring.ctx, pref, logp, d_off, 60, n, pair, 50, out[8],
+                                            ref_logp=ref, mask=mask, dlogp=out[4]),
+            lambda: edp.edp_pack_deliver(ring.ctx, tokens, d_off, 60, idx, 60, out[1], out[2], n),
+            lambda: edp.edp_balance_loss(ring.ctx, z, sel, .1, out[9], out[10], mask=mask,
+                                         dlogits=out[11]),
+            lambda: edp.edp_policy_loss(ring.ctx, one, logp, old, adv, n, out[7], mask=mask,
+                                        dlogp=out[5])]
+        for f in todo:
+            f()
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return out
+
+    want = calls(True)
+    for _ in range(5):
+        for a, b in zip(calls(False), want):
+            assert torch.equal(a, b)
     edp.edp_sync(ring.ctx)
 
 
