@@ -19,6 +19,7 @@ constexpr int kPerSm = 2;            // CTAs of the sums, in one wave
 constexpr int kGradPerSm = 4;        // and of the gradient
 constexpr int kSmallThreads = 1024;  // a batch of up to 8,192 tokens, in one CTA
 constexpr uint32_t kSmallRun = 2 * kTile;
+constexpr uint32_t kSmallSeqs = 512;
 constexpr int kPairThreads = 128;
 constexpr uint32_t kSmallPairs = 4096;
 constexpr uint32_t kAtOnce = 4;  // tiles in flight per warp
@@ -230,16 +231,25 @@ __device__ __forceinline__ void run_parts(const PrefIn &in, const PrefScratch &x
   }
 }
 
+// What another thread of the call wrote: in shared memory (LOCAL: of one CTA), or read
+// around the first-level cache.
+template <bool LOCAL, typename V>
+__device__ __forceinline__ V fresh(const V *p) {
+  if constexpr (LOCAL) return *p;
+  else return __ldcg(p);
+}
+
 // A sequence's sum and its number of tokens.
+template <bool LOCAL>
 __device__ __forceinline__ Run sequence_sum(const TokenSet &s, const PrefScratch &x, uint64_t seq) {
   const uint64_t a = s.off[seq], b = min(s.off[seq + 1], s.n);
   if (b <= a) return {{0.f, 0.f}, 0};
-  const float4 p = __ldcg(reinterpret_cast<const float4 *>(&x.inner[seq]));
+  const float4 p = fresh<LOCAL>(reinterpret_cast<const float4 *>(&x.inner[seq]));
   Run r{{p.x, p.y}, __float_as_uint(p.z)};
   const uint64_t last = (b - 1) / x.run;
 #pragma unroll 4
   for (uint64_t c = a / x.run + 1; c <= last; ++c) {
-    const float4 h = __ldcg(reinterpret_cast<const float4 *>(&x.head[c]));
+    const float4 h = fresh<LOCAL>(reinterpret_cast<const float4 *>(&x.head[c]));
     r = run_join(r, Run{{h.x, h.y}, __float_as_uint(h.z)});
   }
   return r;
@@ -270,6 +280,7 @@ __device__ __forceinline__ void grad_add(const PrefScratch &x, uint64_t seq, df 
 }
 
 // Pairs first, first + step, ...: their losses, gradients and sums.
+template <bool LOCAL>
 __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
                                            const PrefScratch &x, const PrefOut &out,
                                            uint32_t first, uint32_t step, Pair (&sum)[4],
@@ -280,7 +291,7 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
     if ((uint64_t)c >= in.s.n_seq || (uint64_t)j >= in.s.n_seq) {
       flag(ctrl, DEVERR_INDEX, (unsigned long long)((uint64_t)c >= in.s.n_seq ? c : j));
     } else {
-      const Run rc = sequence_sum(in.s, x, c), rj = sequence_sum(in.s, x, j);
+      const Run rc = sequence_sum<LOCAL>(in.s, x, c), rj = sequence_sum<LOCAL>(in.s, x, j);
       df uc = as_df(rc.v), uj = as_df(rj.v);
       if (r.average) {
         if (rc.n) uc = df_over(uc, rc.n);
@@ -322,12 +333,13 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
   }
 }
 
+template <bool LOCAL>
 __device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
                                             const PrefScratch &x, const PrefOut &out,
                                             uint64_t first, uint64_t step) {
   if (!out.ratio) return;
   for (uint64_t q = first; q < in.s.n_seq; q += step) {
-    const Run v = sequence_sum(in.s, x, q);
+    const Run v = sequence_sum<LOCAL>(in.s, x, q);
     const df u = as_df(v.v);
     out.ratio[q] = r.average && v.n ? df_over(u, v.n).hi : u.hi;
   }
@@ -341,9 +353,10 @@ __device__ __forceinline__ void write_loss(const PrefRule &r, const Pair *total,
 }
 
 // The gradient of each token of a sequence, rounded once.
+template <bool LOCAL>
 __device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, df scale) {
-  if (__ldcg(&x.bad[seq])) return __int_as_float(0x7fc00000);
-  const ulonglong2 g = __ldcg(reinterpret_cast<const ulonglong2 *>(&x.grad[seq]));
+  if (fresh<LOCAL>(&x.bad[seq])) return __int_as_float(0x7fc00000);
+  const ulonglong2 g = fresh<LOCAL>(reinterpret_cast<const ulonglong2 *>(&x.grad[seq]));
   // what is whole units of 2^-20 in lo goes to hi, so that neither cancels much
   const long long up = ((long long)g.y + (1ll << 41)) >> 42;
   const long long whole = (long long)g.x + up;
@@ -354,7 +367,7 @@ __device__ __forceinline__ float token_grad(const PrefScratch &x, uint32_t seq, 
 }
 
 // Gradients of tokens [begin, stop) of a warp.
-template <bool VEC>
+template <bool VEC, bool LOCAL>
 __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x, df scale,
                                          float *dlogp, uint64_t begin, uint64_t stop,
                                          uint64_t first, uint64_t end, bool wait) {
@@ -379,13 +392,13 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
           here = there;
         } else {
           if (known) walk.to(s.off, n_seq, t0);
-          here = token_grad(x, walk.q, scale);
+          here = token_grad<LOCAL>(x, walk.q, scale);
         }
         known = true;
         // and what will be wanted at its end
         const bool more = walk.q + 1 < n_seq;
         after = more ? s.off[walk.q + 2] : walk.next;
-        there = more ? token_grad(x, walk.q + 1, scale) : 0.f;
+        there = more ? token_grad<LOCAL>(x, walk.q + 1, scale) : 0.f;
       }
       // tiles within the sequence, kAtOnce of them in flight
       const uint64_t top = min(walk.next, min(stop, end)), room = top > t0 ? top - t0 : 0;
@@ -422,7 +435,7 @@ __device__ __forceinline__ void run_grad(const PrefIn &in, const PrefScratch &x,
           if (t + i >= next) {
             q = sequence_of(s.off, q, to.q + 1, t + i);
             next = s.off[q + 1];
-            each = token_grad(x, q, scale);
+            each = token_grad<LOCAL>(x, q, scale);
           }
           v[i] = each;
         }
@@ -452,10 +465,10 @@ k_pref_pairs(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, uint32_t pair_ct
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
   if (blockIdx.x < pair_ctas)
-    take_pairs(in, r, x, out, blockIdx.x * kPairThreads + threadIdx.x, pair_ctas * kPairThreads,
+    take_pairs<false>(in, r, x, out, blockIdx.x * kPairThreads + threadIdx.x, pair_ctas * kPairThreads,
                sum, ctrl);
   else
-    take_ratios(in, r, x, out, (blockIdx.x - pair_ctas) * kPairThreads + threadIdx.x,
+    take_ratios<false>(in, r, x, out, (blockIdx.x - pair_ctas) * kPairThreads + threadIdx.x,
                 (uint64_t)(gridDim.x - pair_ctas) * kPairThreads);
   if (grid_join<kPairThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
     write_loss(r, total, out.loss);
@@ -468,14 +481,19 @@ k_pref_grad(PrefIn in, PrefScratch x, df scale, uint32_t run, float *dlogp) {
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
   const uint64_t begin = ((uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * run;
-  run_grad<VEC>(in, x, scale, dlogp, begin, begin + run, first, end, true);
+  run_grad<VEC, false>(in, x, scale, dlogp, begin, begin + run, first, end, true);
 }
 
-// All three steps of a batch of up to 8,192 tokens, two tiles per warp.
+// All three steps of a batch of up to 8,192 tokens, two tiles per warp, and up to
+// kSmallSeqs sequences, whose sums and gradients stay in shared memory.
 template <bool VEC>
 __global__ void __launch_bounds__(kSmallThreads)
-k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *ctrl) {
+k_pref_small(PrefIn in, PrefRule r, PrefOut out, df scale, Ctrl *ctrl) {
+  __shared__ SeqPart inner[kSmallSeqs], head[kSmallThreads / 32];
+  __shared__ alignas(16) SeqGrad grad[kSmallSeqs];
+  __shared__ uint32_t bad[kSmallSeqs];
   __shared__ Pair total[4];
+  const PrefScratch x{inner, head, grad, bad, nullptr, kSmallRun};
   pdl_wait();
   pdl_launch();
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
@@ -486,13 +504,13 @@ k_pref_small(PrefIn in, PrefRule r, PrefScratch x, PrefOut out, df scale, Ctrl *
 #pragma unroll
   for (int k = 0; k < 4; ++k) sum[k] = Pair{0.f, 0.f};
   constexpr uint32_t kHalf = kSmallThreads / 2;  // the ratios by warps of their own
-  if (threadIdx.x < kHalf) take_pairs(in, r, x, out, threadIdx.x, kHalf, sum, ctrl);
-  else take_ratios(in, r, x, out, threadIdx.x - kHalf, kHalf);
+  if (threadIdx.x < kHalf) take_pairs<true>(in, r, x, out, threadIdx.x, kHalf, sum, ctrl);
+  else take_ratios<true>(in, r, x, out, threadIdx.x - kHalf, kHalf);
   // the barriers of the join order the CTA's gradients before their use
   if (grid_join<kSmallThreads, 4>(sum, total, x.part, &ctrl->loss_ticket))
     write_loss(r, total, out.loss);
   if (out.dlogp)
-    run_grad<VEC>(in, x, scale, out.dlogp, begin, begin + x.run, first, end, false);
+    run_grad<VEC, true>(in, x, scale, out.dlogp, begin, begin + x.run, first, end, false);
 }
 
 }  // namespace
@@ -503,12 +521,35 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
                                    float *ratio, float *pair_loss, float *dlogp,
                                    cudaStream_t s) {
   const uint64_t sms = (uint64_t)c->coop_sms;
-  const bool small = set.n <= kSmallRun * (kSmallThreads / 32) && n_pair <= kSmallPairs;
+  const bool small = set.n <= kSmallRun * (kSmallThreads / 32) && n_pair <= kSmallPairs &&
+                     set.n_seq <= kSmallSeqs;
+  PrefRule r;
+  auto both = [](double v) {
+    const float hi = (float)v;
+    return df{hi, (float)(v - (double)hi)};
+  };
+  r.beta = both(cfg.beta);
+  r.smooth = (float)cfg.label_smoothing;
+  r.margin = both(cfg.margin);
+  r.half = both(0.5 / cfg.beta);
+  const double norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
+  r.per_norm = both(1.0 / norm);
+  r.per_pair = both(1.0 / (double)n_pair);
+  const df scale = both(cfg.grad_scale / norm);
+  r.kind = cfg.kind;
+  r.average = cfg.average;
+  const PrefIn in{set, logp, ref, pair, n_pair};
+  const PrefOut out{loss, ratio, pair_loss, dlogp};
+  const bool vec = (((uintptr_t)logp | (uintptr_t)ref | (uintptr_t)dlogp) & 15) == 0 &&
+                   ((uintptr_t)set.mask & 3) == 0;
+  if (small)
+    return launch_pdl(vec ? k_pref_small<true> : k_pref_small<false>, dim3(1),
+                      dim3(kSmallThreads), s, in, r, out, scale, c->ctrl);
   // a run per warp of a full chip, so that all end together
   const uint64_t warps = kThreads / 32;
   auto run_of = [&](uint64_t per_sm) {
     const uint64_t chip = per_sm * warps * sms, each = (set.n + chip - 1) / chip;
-    return small ? (uint64_t)kSmallRun : (each + kTile - 1) / kTile * kTile;
+    return (each + kTile - 1) / kTile * kTile;
   };
   const uint64_t run = run_of(kPerSm), grad_run = run_of(kGradPerSm);
   const uint64_t runs = (set.n + run - 1) / run;
@@ -532,28 +573,6 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
   uint8_t *b = (uint8_t *)blk;
   const PrefScratch x{(SeqPart *)(b + inner), (SeqPart *)(b + head), (SeqGrad *)(b + grad),
                       (uint32_t *)(b + bad), (Pair *)(b + part), (uint32_t)run};
-  PrefRule r;
-  auto both = [](double v) {
-    const float hi = (float)v;
-    return df{hi, (float)(v - (double)hi)};
-  };
-  r.beta = both(cfg.beta);
-  r.smooth = (float)cfg.label_smoothing;
-  r.margin = both(cfg.margin);
-  r.half = both(0.5 / cfg.beta);
-  const double norm = cfg.norm > 0.0 ? cfg.norm : (double)n_pair;
-  r.per_norm = both(1.0 / norm);
-  r.per_pair = both(1.0 / (double)n_pair);
-  const df scale = both(cfg.grad_scale / norm);
-  r.kind = cfg.kind;
-  r.average = cfg.average;
-  const PrefIn in{set, logp, ref, pair, n_pair};
-  const PrefOut out{loss, ratio, pair_loss, dlogp};
-  const bool vec = (((uintptr_t)logp | (uintptr_t)ref | (uintptr_t)dlogp) & 15) == 0 &&
-                   ((uintptr_t)set.mask & 3) == 0;
-  if (small)
-    return launch_pdl(vec ? k_pref_small<true> : k_pref_small<false>, dim3(1),
-                      dim3(kSmallThreads), s, in, r, x, out, scale, c->ctrl);
   const unsigned grid = (unsigned)((runs + warps - 1) / warps);
   e = launch_pdl(vec ? k_pref_parts<true> : k_pref_parts<false>, dim3(grid), dim3(kThreads), s, in,
                  x);
