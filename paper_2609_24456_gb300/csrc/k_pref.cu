@@ -489,18 +489,24 @@ k_pref_grad(PrefIn in, PrefScratch x, df scale, uint32_t run, float *dlogp) {
   run_grad<VEC, false>(in, x, scale, dlogp, begin, begin + run, first, end, true);
 }
 
-// All three steps of a batch of up to 8,192 tokens, two tiles per warp, and up to
-// kSmallSeqs sequences, whose sums and gradients stay in shared memory.
+// All three steps of a batch of up to 8,192 tokens, one or two tiles per warp (run:
+// tokens), and up to kSmallSeqs sequences, whose offsets, sums and gradients stay in
+// shared memory.
 template <bool VEC>
 __global__ void __launch_bounds__(kSmallThreads)
-k_pref_small(PrefIn in, PrefRule r, PrefOut out, df scale, Ctrl *ctrl) {
+k_pref_small(PrefIn in, PrefRule r, PrefOut out, df scale, uint32_t run, Ctrl *ctrl) {
+  __shared__ uint64_t off[kSmallSeqs + 1];
   __shared__ SeqPart inner[kSmallSeqs], head[kSmallThreads / 32];
   __shared__ alignas(16) SeqGrad grad[kSmallSeqs];
   __shared__ uint32_t bad[kSmallSeqs];
   __shared__ Pair total[4];
-  const PrefScratch x{inner, head, grad, bad, nullptr, kSmallRun};
+  const PrefScratch x{inner, head, grad, bad, nullptr, run};
   pdl_wait();
   pdl_launch();
+  // one round trip for the offsets, which every search goes to
+  for (uint32_t q = threadIdx.x; q <= in.s.n_seq; q += kSmallThreads) off[q] = in.s.off[q];
+  __syncthreads();
+  in.s.off = off;
   const uint64_t first = in.s.off[0], end = min(in.s.off[in.s.n_seq], in.s.n);
   const uint64_t begin = (uint64_t)(threadIdx.x >> 5) * x.run;
   run_parts<VEC>(in, x, begin, begin + x.run, first, end);
@@ -549,7 +555,8 @@ cudaError_t launch_preference_loss(edp_ctx *c, const edp_preference_config &cfg,
                    ((uintptr_t)set.mask & 3) == 0;
   if (small)
     return launch_pdl(vec ? k_pref_small<true> : k_pref_small<false>, dim3(1),
-                      dim3(kSmallThreads), s, in, r, out, scale, c->ctrl);
+                      dim3(kSmallThreads), s, in, r, out, scale,
+                      set.n <= 4 * kSmallThreads ? kTile : kSmallRun, c->ctrl);
   // a run per warp of a full chip, so that all end together
   const uint64_t warps = kThreads / 32;
   auto run_of = [&](uint64_t per_sm) {
