@@ -53,15 +53,6 @@ struct PolicyRule {
   uint32_t kl;
 };
 
-// What a row of logits weighs in the policy loss, by its token's place.
-struct RowWeights {
-  const uint64_t *off;
-  uint32_t n_seq;
-  const float *sequence;             // each sequence's weight,
-  const unsigned long long *tokens;  // or the divisor of all,
-  float fixed;                       // or the weight of all
-};
-
 // e^q - 1 - q for |q| below 1: the Taylor series, whose first term left out is
 // 2^-24 of the sum.
 __device__ __forceinline__ float exp_less_line(float q) {
@@ -327,6 +318,40 @@ __device__ __forceinline__ uint32_t token_bits(const TokenSet &s, uint64_t t, ui
       if ((bits >> i & 1u) && (uint32_t)s.target[t + i] >= s.vocab) bits &= ~(1u << i);
   }
   return bits;
+}
+
+// What a row of logits weighs in the policy loss, by its token's place.
+struct RowWeights {
+  TokenSet set;
+  bool count;                        // the row counts for itself (few rows), else:
+  const float *sequence;             // each sequence's weight,
+  const unsigned long long *tokens;  // or the divisor of all,
+  float fixed;                       // or the weight of all
+  float divisor;                     // by sequences: their number
+};
+__device__ __forceinline__ bool in_sequences(const RowWeights &w, uint64_t t) {
+  return !w.set.off || (t >= w.set.off[0] && t < w.set.off[w.set.n_seq]);
+}
+// What row t of the sequences weighs, found by a warp.
+__device__ __forceinline__ float row_weight(const RowWeights &w, uint64_t t) {
+  const TokenSet &s = w.set;
+  const bool by_sequence = s.reduce == EDP_REDUCE_SEQ_MEAN;
+  if (!w.count) {
+    if (w.sequence) return __ldcg(&w.sequence[sequence_of_warp(s.off, 0, (uint32_t)s.n_seq, t)]);
+    return w.tokens ? 1.f / (float)__ldcg(w.tokens) : w.fixed;
+  }
+  uint64_t a = 0, b = s.n;
+  if (s.off) {
+    const uint32_t q = by_sequence ? sequence_of_warp(s.off, 0, (uint32_t)s.n_seq, t) : 0;
+    a = s.off[q];
+    b = min(s.off[by_sequence ? q + 1 : s.n_seq], s.n);
+  }
+  uint32_t n = 0;
+#pragma unroll 2
+  for (uint64_t i = (a & ~3ull) + 4 * (threadIdx.x & 31); i < b; i += 128)
+    n += __popc(token_bits<false>(s, i, a, b));
+  n = __reduce_add_sync(kAllLanes, n);
+  return 1.f / ((by_sequence ? w.divisor : 1.f) * (float)n);
 }
 
 // Elements t .. t + 3 of an array of n; NaN-safe: what is beyond n is 0.

@@ -574,15 +574,6 @@ k_token_logprob_grad(RowArgs a, const float *stats, const float *entropy, const 
                         (uint32_t)a.target[t] - first, g, a.c);
 }
 
-__device__ __forceinline__ bool in_sequences(const RowWeights &w, uint64_t t) {
-  return !w.off || (t >= w.off[0] && t < w.off[w.n_seq]);
-}
-// What row t of the sequences weighs in the policy loss, found by a warp.
-__device__ __forceinline__ float row_weight(const RowWeights &w, uint64_t t) {
-  if (w.sequence) return __ldcg(&w.sequence[sequence_of_warp(w.off, 0, w.n_seq, t)]);
-  return w.tokens ? 1.f / (float)__ldcg(w.tokens) : w.fixed;
-}
-
 // The policy loss's derivative by a row's log-probability, before weight and scale.
 __device__ __forceinline__ float row_policy(const PolicyRule &rule, float logp, float old,
                                             bool has_ref, float ref, float adv) {

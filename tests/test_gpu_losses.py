@@ -182,6 +182,7 @@ def test_policy_special_values(edp_lib):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows,vocab", [(1, 3), (5, 1000), (40, 20_011), (333, 4097), (3, 152_064),
+                                        (128, 130), (129, 130), (640, 65), (641, 65),
                                         (5000, 130)])
 @pytest.mark.parametrize("reduce", [0, 1])
 def test_policy_from_logits(edp_lib, dtype, rows, vocab, reduce):
