@@ -527,11 +527,12 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
  * All arrays are device memory.  mask (uint8 per token, or NULL: all ones)
  * leaves out the tokens where it is 0: their log-probabilities, advantages and
  * logits may hold anything, their outputs and gradients are 0.  Outputs overlap
- * no input, but for a gradient in its logits' place.  Arithmetic is fp32, sums over tokens fp32 pairs or
- * fp64, each output rounded once to its type; no result depends on the order
- * in which threads run.  edp_policy_loss*, edp_preference_loss and
- * edp_balance_loss use the scratch that edp_gae and edp_pack_deliver use and
- * must be ordered with them and each other; edp_token_logprob* use none.
+ * no input, but for a gradient in its logits' place.  Arithmetic is fp32, sums
+ * over tokens fp32 pairs or fp64, each output rounded once to its type; no
+ * result depends on the order in which threads run.  edp_policy_loss*,
+ * edp_preference_loss and edp_balance_loss use the scratch that edp_gae and
+ * edp_pack_deliver use and must be ordered with them and each other;
+ * edp_token_logprob* use none.
  * ------------------------------------------------------------------------- */
 
 /* Element type of logits and of their gradient. */
