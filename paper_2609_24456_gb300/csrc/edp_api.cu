@@ -236,7 +236,9 @@ namespace {
 constexpr size_t kLeastScratch = 4096;
 
 // Grow-only block (*blk, *have bytes) to at least `want` bytes; the first
-// `zero_head` bytes of a new block are zeroed.
+// `zero_head` bytes of a new block are zeroed, on `s`: the kernels that read
+// them run there, and a stream that does not wait for the default one would
+// not wait for a cudaMemset.
 cudaError_t grow(edp_ctx *ctx, void **blk, size_t *have, size_t want, size_t zero_head,
                  cudaStream_t s) {
   if (want <= *have) return cudaSuccess;
@@ -257,7 +259,7 @@ cudaError_t grow(edp_ctx *ctx, void **blk, size_t *have, size_t want, size_t zer
   want = (want + 255) & ~(size_t)255;
   void *p = al(ctx->cfg.alloc_user, want);
   if (!p) return cudaErrorMemoryAllocation;
-  if (zero_head && cudaMemset(p, 0, zero_head) != cudaSuccess) {
+  if (zero_head && cudaMemsetAsync(p, 0, zero_head, s) != cudaSuccess) {
     cudaGetLastError();
     fr(ctx->cfg.alloc_user, p);
     return cudaErrorMemoryAllocation;
