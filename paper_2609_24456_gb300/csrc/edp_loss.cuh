@@ -78,7 +78,8 @@ __device__ __forceinline__ float exp_less_line(float q, float *em1) {
 
 // One token: its policy loss and divergence, the ratio less one, the divergence from
 // the old policy, and the loss's derivative by logp (entropy apart), before weight
-// and scale.  d = logp - old, q = ref - logp; with d, q and the advantage 0 all are 0.
+// and scale.  d = logp - old, q = ref - logp; with d, q and the advantage 0 all are 0
+// but the derivative with EDP_KL_K1, whose divergence falls with logp everywhere.
 struct PolicyToken {
   float pg, kl, ratio1, old_kl, dlogp;
   bool above, below;

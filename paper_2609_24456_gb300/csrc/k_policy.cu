@@ -351,7 +351,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
       x.lp = load4<VEC>(p.logp, c0 + i + 4 * lane, s.n);
       if (p.entropy) x.en = load4<VEC>(p.entropy, c0 + i + 4 * lane, s.n);
     }
-    // what does not count is 0 from here on, whatever it held
+    // what does not count is 0 from here on, whatever it held, and so is its gradient
     const float l4[4] = {x.lp.x, x.lp.y, x.lp.z, x.lp.w};
     const float o4[4] = {x.od.x, x.od.y, x.od.z, x.od.w};
     const float a4[4] = {x.ad.x, x.ad.y, x.ad.z, x.ad.w};
@@ -371,7 +371,7 @@ k_policy(TokenSet s, PolicyTokens p, PolicyRule rule, Weighting w, float divisor
       for (int k = 0; k < 4; ++k) {
         const PolicyToken o =
             policy_token<KL, decltype(near)::value>(rule, d4[k], q4[k], adv4[k]);
-        g4[k] = rule.grad_scale * wt[k] * o.dlogp;
+        g4[k] = b[k] ? rule.grad_scale * wt[k] * o.dlogp : 0.f;
         add[0] = fmaf(wt[k], o.pg, add[0]);
         if (KL != Kl::kNone) add[1] = fmaf(wt[k], o.kl, add[1]);
         add[3] += o.ratio1;
