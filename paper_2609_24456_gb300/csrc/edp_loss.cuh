@@ -104,8 +104,8 @@ __device__ __forceinline__ PolicyToken policy_token(const PolicyRule &c, float d
   const bool up = d > (pos ? c.ln_high : c.ln_dual), down = !pos && d < c.ln_low;
   const float used = up ? (pos ? c.high : c.dual) : down ? c.low : r;
   o.pg = -used * adv;
-  // an advantage of 0 takes nothing from a ratio that overflowed
-  if (!NEAR && adv == 0.f) o.pg = d * 0.f;
+  // an advantage of 0 takes nothing from any ratio, one that overflowed among them
+  if (!NEAR && adv == 0.f && !isnan(d)) o.pg = 0.f;
   o.dlogp = up || down ? 0.f : o.pg;
   o.above = up && pos;
   o.below = (up || down) && adv < 0.f;
