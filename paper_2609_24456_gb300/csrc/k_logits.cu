@@ -38,10 +38,10 @@ constexpr float kNoLog = -1e4f;  // stands for logarithms whose power of 2 is 0 
 
 // The difference z - m and its product with c cost an instruction more than one
 // fused z c - (m c), whose rounding of m c is the same for all of a row and is
-// taken out at its end.  The fused form overflows near the ends of fp32: a
-// bfloat16 row with a maximum beyond kFusedMost goes the careful way, as fp32
-// rows do.
-constexpr float kFusedMost = 1e29f;
+// taken out at its end.  What is taken out grows with m c: a 16-bit row with |m c|
+// beyond kFusedMost (a largest logit of 181,704 at temperature 1, of 182 at 0.001)
+// goes the careful way, as fp32 rows do.  Up to there the rounding is at most 2^-7.
+constexpr float kFusedMost = 262144.f;
 template <typename T>
 constexpr bool kFused = sizeof(T) == 2;
 
@@ -137,10 +137,11 @@ template <typename T, bool FUSED>
 struct RowLog {
   float c, less;  // y = z c - less, or (z - less) c
   __device__ __forceinline__ RowLog(float m, float c_) : c(c_) {
-    const bool none = m == kNegInf;  // nothing but -infinity so far
-    if (FUSED && std::is_same<T, __nv_bfloat16>::value) less = fmaxf(m, -kFusedMost) * c;
-    else if (FUSED) less = none ? 0.f : m * c;
-    else less = none ? 0.f : m;
+    // a part with low numbers or -infinity alone is taken relative to the lowest maximum
+    // that the fused form has, so that its sums stay finite (they go over as they are to
+    // a row whose maximum is there or higher; another row goes the careful way)
+    if (FUSED) less = fmaxf(m * c, -kFusedMost);
+    else less = m == kNegInf ? 0.f : m;
   }
   __device__ __forceinline__ float of(float z) const {
     return FUSED ? fmaf(z, c, -less) : (z - less) * c;
@@ -154,12 +155,16 @@ struct RowLog {
   }
 };
 
-// -infinity has no product with its 0: a finite number stands for it, in bfloat16
-// before the logarithm (two at a time), else after.
+// -infinity has no product with its 0, nor has a logarithm that overflows once it is
+// scaled: a number whose power of 2 is 0 all the same stands for them, in bfloat16
+// before the logarithm (two at a time), else after.  kLowLogit is so low that at any
+// temperature 2^(z c) is 0 beside every maximum of the fused form, and so high that an
+// entropy gradient's product with it is finite up to a dentropy of 8e26 T^2.
+constexpr float kLowLogit = -4e11f;
 template <typename T, bool FUSED>
 __device__ __forceinline__ uint4 finite_words(uint4 w) {
   if constexpr (FUSED && std::is_same<T, __nv_bfloat16>::value) {
-    const __nv_bfloat162 low = __float2bfloat162_rn(-10.f * kFusedMost);
+    const __nv_bfloat162 low = __float2bfloat162_rn(kLowLogit);
     __nv_bfloat162 *x = reinterpret_cast<__nv_bfloat162 *>(&w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __hmax2_nan(x[i], low);
@@ -344,18 +349,23 @@ __device__ __forceinline__ Row row_kind(const int32_t *target, const uint8_t *ma
   return x < 0 ? Row::kSkip : (uint32_t)x >= vocab ? Row::kBad : Row::kUse;
 }
 
-// Whether a row's sums hold (see kFusedMost); without a maximum they are 0.
-template <typename T>
-__device__ __forceinline__ bool sums_hold(const RowSum &a) {
-  return !std::is_same<T, __nv_bfloat16>::value || a.m == kNegInf || fabsf(a.m) <= kFusedMost;
+// Whether the sums of a row with maximum m hold (see kFusedMost); without a maximum
+// they are 0.
+__device__ __forceinline__ bool sums_hold(float m, float c) {
+  return m == kNegInf || fabsf(m * c) <= kFusedMost;
+}
+// 2^d - 1 to 2^-24 for |d| up to 2^-7: the first two terms of its series
+__device__ __forceinline__ float exp2_less_1(float d) {
+  const float x = d * kLn2;
+  return fmaf(0.5f * x, x, x);
 }
 // The sums relative to m itself, not to the rounded m c.
 template <typename T>
 __device__ __forceinline__ RowSum exact_sums(RowSum a, float c) {
   if (!kFused<T> || a.m == kNegInf) return a;
   const float d = -fmaf(a.m, c, -(a.m * c));
-  a.u = fmaf(d, a.s, a.u);  // 2^d is 1 + d ln 2 to 2^-38
-  const float f = d * kLn2;
+  a.u = fmaf(d, a.s, a.u);
+  const float f = exp2_less_1(d);
   return {a.m, fmaf(f, a.s, a.s), fmaf(f, a.u, a.u)};
 }
 
@@ -419,7 +429,7 @@ k_token_logprob(RowArgs a, float *logp, float *entropy, float *stats, Ctrl *ctrl
     if (threadIdx.x == 0) whole = exact_sums<T>(sum, a.c);
     __syncthreads();
     sum = whole;
-    if (!sums_hold<T>(sum))  // rare: one CTA, the careful way
+    if (!sums_hold(sum.m, a.c))  // rare: one CTA, the careful way
       sum = cta_join<T, false>(part_sum<T, ENT, false>(row, a.vocab, a.c), a.c, red);
   }
   if (threadIdx.x == 0) {
@@ -454,7 +464,7 @@ __device__ __forceinline__ RowGrad row_grad(float m, float s, float entropy, flo
 template <typename T, bool FUSED>
 __device__ __forceinline__ RowGrad exact_grad(RowGrad g, float c) {
   if (!FUSED) return g;
-  const float d = -fmaf(g.m, c, -(g.m * c)), f = d * kLn2;
+  const float d = -fmaf(g.m, c, -(g.m * c)), f = exp2_less_1(d);
   g.a = fmaf(d, g.b, g.a);
   g.a = fmaf(f, g.a, g.a);
   g.b = fmaf(f, g.b, g.b);
@@ -475,8 +485,7 @@ struct GradOf {
     return e * (ENT ? fma2(b, finite_log<T, FUSED>(y), a) : a);
   }
   __device__ __forceinline__ float of(float z) const {
-    if constexpr (FUSED && std::is_same<T, __nv_bfloat16>::value)
-      z = z == kNegInf ? -10.f * kFusedMost : z;
+    if constexpr (ENT && FUSED && std::is_same<T, __nv_bfloat16>::value) z = z < kLowLogit ? kLowLogit : z;
     return of(F2(z, 0.f)).x();
   }
   __device__ __forceinline__ uint4 of(const uint4 &w) const {
@@ -534,7 +543,7 @@ __device__ __forceinline__ void part_grad(const T *p, T *d, uint32_t n, uint32_t
 template <typename T, bool ENT, int NT = kRowThreads>
 __device__ __forceinline__ void part_grad_any(const T *p, T *d, uint32_t n, uint32_t at,
                                               const RowGrad &g, float c) {
-  if (kFused<T> && sums_hold<T>(RowSum{g.m, 0.f, 0.f}))
+  if (kFused<T> && sums_hold(g.m, c))
     part_grad<T, ENT, kFused<T>, NT>(p, d, n, at, g, c);
   else
     part_grad<T, ENT, false, NT>(p, d, n, at, g, c);
@@ -623,7 +632,7 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
   if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
   // also: every CTA has read the target before one overwrites it
   sum = exact_sums<T>(cluster_join<T, F>(sum, a.c, part, np, parts, &whole), a.c);
-  if (F && !sums_hold<T>(sum)) {  // rare: every CTA the whole row, the careful way
+  if (F && !sums_hold(sum.m, a.c)) {  // rare: every CTA the whole row, the careful way
     __syncthreads();
     sum = cta_join<T, false>(part_sum<T, ENT, false>(row, a.vocab, a.c), a.c, red);
     if (threadIdx.x == 0) whole = sum;
@@ -665,6 +674,12 @@ constexpr uint32_t kResidentPart = 80 * 1024;       // bytes of a part, where th
 constexpr uint32_t kResidentMost = 200 * 1024;
 constexpr uint32_t kLeastPart = 32 * 1024;
 constexpr uint64_t kRowWaitNs = 1000000000ull;      // bound of the wait for a part
+// CTAs per SM, which bound the registers (56 and 40): as many as parts of 76 KB allow of
+// the 16-bit forms, whose two ways spill at 40 (f16 without entropy, 4,096 rows of 152,064:
+// 412 us, 379 at 54); fp32 has one way, and where its parts are small more CTAs (515 rows
+// of 32,003: 37.0 us, 41.3 with 3).
+template <typename T>
+constexpr int kResidentCtas = kFused<T> ? 3 : 4;
 enum class Rest { kGrad, kZero, kCareful };
 
 // No preference for what leaves the second-level cache first: with the streaming
@@ -689,7 +704,7 @@ __device__ __forceinline__ void send_float4(float4 *to, float4 v, unsigned long 
 }
 
 template <typename T, bool ENT>
-__global__ void __launch_bounds__(kResidentThreads)
+__global__ void __launch_bounds__(kResidentThreads, kResidentCtas<T>)
 k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const float *ref_logp,
                   const float *adv, PolicyRule rule, float *logp, float *entropy, void *dz,
                   uint64_t dstride, bool early, Ctrl *ctrl) {
@@ -782,7 +797,7 @@ k_policy_resident(RowArgs a, RowWeights weights, const float *old_logp, const fl
       sum = warp_sum<T, FUSED, 8>(RowSum{x.x, x.y, x.z}, a.c);
     }
     if (FUSED) sum = exact_sums<T>(sum, a.c);
-    if (FUSED && !sums_hold<T>(sum)) {
+    if (FUSED && !sums_hold(sum.m, a.c)) {
       if (lane == 0) rest = Rest::kCareful;
       return;
     }
