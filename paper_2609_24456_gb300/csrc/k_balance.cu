@@ -23,7 +23,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxExperts = 1024;
 constexpr uint64_t kOneCta = 16384;
-constexpr float kProbUnits = 1099511627776.f;  // 2^40
+// An expert's probabilities add up in units of 2^-40 or, from so many rows on that all of
+// them on one expert would pass 64 bits, of 2^-32.
+constexpr float kProbUnits = 1099511627776.f;    // 2^40
+constexpr float kProbUnitsMany = 4294967296.f;   // 2^32
+constexpr uint64_t kManyRows = 1ull << 23;
 
 }  // namespace
 
@@ -31,7 +35,7 @@ constexpr float kProbUnits = 1099511627776.f;  // 2^40
 struct BalanceSums {
   unsigned long long tokens;
   uint32_t nan, pad;
-  unsigned long long prob[kMaxExperts];  // in units of 2^-40
+  unsigned long long prob[kMaxExperts];  // in units of BalanceArgs::unit
   uint32_t count[kMaxExperts];
 };
 
@@ -44,6 +48,7 @@ struct BalanceArgs {
   const int32_t *sel;
   const uint8_t *mask;
   float coef, scale;  // coef, grad_scale coef
+  float units, unit;  // of the probabilities' sums: how many are 1, and 1 / units
   float *loss, *prob;
   int64_t *counts;
   void *dz;
@@ -321,7 +326,7 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) v += col[w][e];
     if (ONE) col[0][e] = v;
-    else if (v > 0.f) atomicAdd(&sums->prob[e], (unsigned long long)__float2ull_rn(v * kProbUnits));
+    else if (v > 0.f) atomicAdd(&sums->prob[e], (unsigned long long)__float2ull_rn(v * a.units));
   }
   __threadfence();
   __syncthreads();
@@ -336,7 +341,7 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   for (uint32_t e = threadIdx.x; e < a.E; e += NT) {
     const uint32_t n = ONE ? hist[e] : __ldcg(&sums->count[e]);
     float p = ONE ? col[0][e]
-                  : (float)__ldcg(&sums->prob[e]) * (1.f / kProbUnits);
+                  : (float)__ldcg(&sums->prob[e]) * a.unit;
     p = bad ? __int_as_float(0x7fc00000) : p * inv_n;
     if (a.prob) a.prob[e] = p;
     a.counts[e] = n;
@@ -417,8 +422,10 @@ cudaError_t launch_balance_loss(edp_ctx *c, const Logits &z, const int32_t *sel,
   cudaError_t e = ctx_zeroed_scratch(c, sizeof(BalanceSums), s, &blk);
   if (e != cudaSuccess) return e;
   BalanceSums *sums = (BalanceSums *)blk;
+  const float units = z.rows > kManyRows ? kProbUnitsMany : kProbUnits;
   const BalanceArgs a{z.z, z.rows, z.stride, z.vocab, top, sel, z.mask, (float)coef,
-                      (float)(grad_scale * coef), loss, prob, counts, dz, dstride};
+                      (float)(grad_scale * coef), units, 1.f / units, loss, prob, counts, dz,
+                      dstride};
   switch (z.dtype) {
     case EDP_BF16: return launch_type<__nv_bfloat16>(c, a, sums, s);
     case EDP_F16: return launch_type<__half>(c, a, sums, s);
