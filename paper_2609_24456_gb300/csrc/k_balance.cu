@@ -36,7 +36,7 @@ struct BalanceSums {
   unsigned long long tokens;
   uint32_t nan, pad;
   unsigned long long prob[kMaxExperts];  // in units of BalanceArgs::unit
-  uint32_t count[kMaxExperts];
+  unsigned long long count[kMaxExperts];
 };
 
 namespace {
@@ -96,7 +96,7 @@ k_expert_counts(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   if ((threadIdx.x & 31) == 0 && n) atomicAdd(&sums->tokens, (unsigned long long)n);
   __syncthreads();
   for (uint32_t e = threadIdx.x; e < a.E; e += kThreads)
-    if (hist[e]) atomicAdd(&sums->count[e], hist[e]);
+    if (hist[e]) atomicAdd(&sums->count[e], (unsigned long long)hist[e]);
 }
 
 // CTAs per SM, by the elements of a lane.
@@ -339,12 +339,12 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   const bool bad = __ldcg(&sums->nan) != 0;
   Pair v{0.f, 0.f};
   for (uint32_t e = threadIdx.x; e < a.E; e += NT) {
-    const uint32_t n = ONE ? hist[e] : __ldcg(&sums->count[e]);
+    const unsigned long long n = ONE ? hist[e] : __ldcg(&sums->count[e]);
     float p = ONE ? col[0][e]
                   : (float)__ldcg(&sums->prob[e]) * a.unit;
     p = bad ? __int_as_float(0x7fc00000) : p * inv_n;
     if (a.prob) a.prob[e] = p;
-    a.counts[e] = n;
+    a.counts[e] = (int64_t)n;
     pair_add(v, (float)n * per * p);
     if (!ONE) {
       sums->prob[e] = 0;
