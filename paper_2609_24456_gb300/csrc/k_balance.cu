@@ -23,6 +23,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxExperts = 1024;
 constexpr uint64_t kOneCta = 16384;
+// Rows of a lane: its fp32 sums of so many probabilities are good to 2^-16 at the worst
+// before they go over to whole numbers.  More rows take more CTAs than one wave.
+constexpr uint64_t kLaneRows = 256;
 // An expert's probabilities add up in units of 2^-40 or, from so many rows on that all of
 // them on one expert would pass 64 bits, of 2^-32.
 constexpr float kProbUnits = 1099511627776.f;    // 2^40
@@ -377,9 +380,10 @@ cudaError_t launch_shape(edp_ctx *c, const BalanceArgs &a, BalanceSums *sums, cu
                              dim3(kThreads), s, a, sums, c->ctrl);
   if (e != cudaSuccess) return e;
   const uint64_t b = (a.rows * L + kThreads - 1) / kThreads;
-  const uint64_t wave = kBalancePerSm<V * VN> * sms;
+  const uint64_t wave = kBalancePerSm<V * VN> * sms, least = (b + kLaneRows - 1) / kLaneRows;
+  const uint64_t most = wave > least ? wave : least;
   e = launch_pdl(k_balance<T, L, V, VN, kThreads, false>,
-                 dim3((unsigned)(b < wave ? b : wave)), dim3(kThreads), s, a, sums, c->ctrl);
+                 dim3((unsigned)(b < most ? b : most)), dim3(kThreads), s, a, sums, c->ctrl);
   if (e != cudaSuccess) cudaMemsetAsync(sums, 0, sizeof *sums, s);  // the counts go no further
   return e;
 }

@@ -6,6 +6,7 @@ from test_gpu_logprob import ctx_of
 
 pytestmark = pytest.mark.gpu
 
+
 def test_choices_of_one_expert(edp_lib):
     ring = ctx_of(edp_lib)
     rows, top = 2**26 + 3, 64
