@@ -138,7 +138,9 @@ k_sequence_weights(TokenSet s, const uint32_t *block, float divisor, float *weig
         for (uint64_t k = ka + lane; k < kb; k += 32) some += __ldcg(&block[k]);
         some += count_few(s, a, ka * kBlock) + count_few(s, kb * kBlock, b);
       }
-      n = __reduce_add_sync(kAllLanes, some);
+      // a lane's count fits 32 bits up to 2^37 tokens (2 TB), the sequence's need not
+      n = ((uint64_t)__reduce_add_sync(kAllLanes, some >> 16) << 16) +
+          __reduce_add_sync(kAllLanes, some & 0xffffu);
     }
     if (lane == 0) weight[q] = n ? 1.f / (divisor * (float)n) : 0.f;
   }

@@ -245,17 +245,21 @@ __device__ __forceinline__ V fresh(const V *p) {
 }
 
 // A sequence's sum and its number of tokens.
+struct SeqSum {
+  Pair v;
+  uint64_t n;
+};
 template <bool LOCAL>
-__device__ __forceinline__ Run sequence_sum(const TokenSet &s, const PrefScratch &x, uint64_t seq) {
+__device__ __forceinline__ SeqSum sequence_sum(const TokenSet &s, const PrefScratch &x, uint64_t seq) {
   const uint64_t a = s.off[seq], b = min(s.off[seq + 1], s.n);
   if (b <= a) return {{0.f, 0.f}, 0};
   const float4 p = fresh<LOCAL>(reinterpret_cast<const float4 *>(&x.inner[seq]));
-  Run r{{p.x, p.y}, __float_as_uint(p.z)};
+  SeqSum r{{p.x, p.y}, __float_as_uint(p.z)};
   const uint64_t last = (b - 1) / x.run;
 #pragma unroll 4
   for (uint64_t c = a / x.run + 1; c <= last; ++c) {
     const float4 h = fresh<LOCAL>(reinterpret_cast<const float4 *>(&x.head[c]));
-    r = run_join(r, Run{{h.x, h.y}, __float_as_uint(h.z)});
+    r = SeqSum{pair_join(r.v, Pair{h.x, h.y}), r.n + __float_as_uint(h.z)};
   }
   return r;
 }
@@ -265,7 +269,7 @@ constexpr float kLoUnit = 1.f / 4611686018427387904.f;  // 2^-62
 constexpr float kGradMost = 4194304.f;                  // 2^22
 
 // x / n for a whole number n
-__device__ __forceinline__ df df_over(df x, uint32_t n) {
+__device__ __forceinline__ df df_over(df x, uint64_t n) {
   const float nh = (float)n, nl = (float)((long long)n - (long long)nh);
   const float q = x.hi / nh;
   const float rest = fmaf(-q, nl, fmaf(-q, nh, x.hi)) + x.lo;
@@ -296,7 +300,7 @@ __device__ __forceinline__ void take_pairs(const PrefIn &in, const PrefRule &r,
     if ((uint64_t)c >= in.s.n_seq || (uint64_t)j >= in.s.n_seq) {
       flag(ctrl, DEVERR_INDEX, (unsigned long long)((uint64_t)c >= in.s.n_seq ? c : j));
     } else {
-      const Run rc = sequence_sum<LOCAL>(in.s, x, c), rj = sequence_sum<LOCAL>(in.s, x, j);
+      const SeqSum rc = sequence_sum<LOCAL>(in.s, x, c), rj = sequence_sum<LOCAL>(in.s, x, j);
       df uc = as_df(rc.v), uj = as_df(rj.v);
       if (r.average) {
         if (rc.n) uc = df_over(uc, rc.n);
@@ -344,7 +348,7 @@ __device__ __forceinline__ void take_ratios(const PrefIn &in, const PrefRule &r,
                                             uint64_t first, uint64_t step) {
   if (!out.ratio) return;
   for (uint64_t q = first; q < in.s.n_seq; q += step) {
-    const Run v = sequence_sum<LOCAL>(in.s, x, q);
+    const SeqSum v = sequence_sum<LOCAL>(in.s, x, q);
     const df u = as_df(v.v);
     out.ratio[q] = r.average && v.n ? df_over(u, v.n).hi : u.hi;
   }
