@@ -524,7 +524,8 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
  * ones before it gives the tokens shifted by one, and masks each sequence's
  * last row.  Any context of the GPU serves; its ring is not used.
  *
- * All arrays are device memory.  mask (uint8 per token, or NULL: all ones)
+ * All arrays are device memory, aligned to their elements' type (else
+ * EDP_ERR_INVALID).  mask (uint8 per token, or NULL: all ones)
  * leaves out the tokens where it is 0: their log-probabilities, advantages and
  * logits may hold anything, their outputs and gradients are 0.  Outputs overlap
  * no input, but for a gradient in its logits' place.  Arithmetic is fp32, sums

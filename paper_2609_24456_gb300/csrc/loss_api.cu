@@ -16,6 +16,18 @@ bool device_arrays(const edp_ctx *ctx, std::initializer_list<const void *> ps) {
   return true;
 }
 
+// Addresses at multiples of their elements' size: of 4 bytes and of 8.
+bool aligned_arrays(std::initializer_list<const void *> fours,
+                    std::initializer_list<const void *> eights) {
+  uintptr_t a = 0, b = 0;
+  for (const void *p : fours) a |= (uintptr_t)p;
+  for (const void *p : eights) b |= (uintptr_t)p;
+  return !(a & 3u) && !(b & 7u);
+}
+edp_status not_aligned(edp_ctx *ctx, const char *who) {
+  return fail(ctx, EDP_ERR_INVALID, "%s: arrays are not aligned to their type", who);
+}
+
 size_t size_of(uint32_t dtype) { return dtype == EDP_F32 ? 4 : 2; }
 
 bool in_order(double lo, double x) { return std::isfinite(x) && x >= lo; }
@@ -85,6 +97,8 @@ edp_status edp_token_logprob(edp_ctx *ctx, const void *logits, uint32_t dtype, u
   if (st != EDP_OK) return st;
   if (!logp || !device_arrays(ctx, {logits, target, mask, logp, entropy, stats}))
     return fail(ctx, EDP_ERR_INVALID, "edp_token_logprob: arrays must be device memory");
+  if (!aligned_arrays({target, logp, entropy, stats}, {}))
+    return not_aligned(ctx, "edp_token_logprob");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const cudaError_t e =
@@ -113,6 +127,8 @@ edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint32_t dty
                 "edp_token_logprob_grad: entropy and dentropy go together");
   if (!device_arrays(ctx, {logits, target, mask, stats, entropy, dlogp, dentropy, dlogits}))
     return fail(ctx, EDP_ERR_INVALID, "edp_token_logprob_grad: arrays must be device memory");
+  if (!aligned_arrays({target, stats, entropy, dlogp, dentropy}, {}))
+    return not_aligned(ctx, "edp_token_logprob_grad");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const cudaError_t e = launch_token_logprob_grad(ctx, z, stats, entropy, dlogp, dentropy,
@@ -140,6 +156,8 @@ edp_status edp_policy_loss(edp_ctx *ctx, const edp_policy_config *cfg, const flo
   if (!logp || !device_arrays(ctx, {logp, old_logp, ref_logp, adv, entropy, mask, off, loss,
                                     dlogp, dentropy}))
     return fail(ctx, EDP_ERR_INVALID, "edp_policy_loss: arrays must be device memory");
+  if (!aligned_arrays({logp, old_logp, ref_logp, adv, entropy, loss, dlogp, dentropy}, {off}))
+    return not_aligned(ctx, "edp_policy_loss");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const cudaError_t e =
@@ -174,6 +192,8 @@ edp_status edp_policy_loss_logits(edp_ctx *ctx, const edp_policy_config *cfg,
   if (!device_arrays(ctx, {logits, target, old_logp, ref_logp, adv, mask, off, loss, logp,
                            entropy, dlogits}))
     return fail(ctx, EDP_ERR_INVALID, "edp_policy_loss_logits: arrays must be device memory");
+  if (!aligned_arrays({target, old_logp, ref_logp, adv, loss, logp, entropy}, {off}))
+    return not_aligned(ctx, "edp_policy_loss_logits");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const cudaError_t e = launch_policy_loss_logits(ctx, *cfg, set, p, z, loss, logp, entropy,
@@ -213,6 +233,8 @@ edp_status edp_preference_loss(edp_ctx *ctx, const edp_preference_config *cfg,
                 "2^20");
   if (!device_arrays(ctx, {logp, ref_logp, mask, off, pair, loss, seq_ratio, pair_loss, dlogp}))
     return fail(ctx, EDP_ERR_INVALID, "edp_preference_loss: arrays must be device memory");
+  if (!aligned_arrays({logp, ref_logp, loss, seq_ratio, pair_loss, dlogp}, {off, pair}))
+    return not_aligned(ctx, "edp_preference_loss");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const TokenSet set{mask, off, nullptr, 0, EDP_REDUCE_SEQ_SUM, n_seq, n_tokens, 0.0};
@@ -245,6 +267,7 @@ edp_status edp_balance_loss(edp_ctx *ctx, const void *logits, uint32_t dtype, ui
     return fail(ctx, EDP_ERR_INVALID, "edp_balance_loss: coef and grad_scale must be finite");
   if (!device_arrays(ctx, {logits, sel, mask, loss, counts, prob, dlogits}))
     return fail(ctx, EDP_ERR_INVALID, "edp_balance_loss: arrays must be device memory");
+  if (!aligned_arrays({sel, loss, prob}, {counts})) return not_aligned(ctx, "edp_balance_loss");
   DeviceGuard dg(ctx->cfg.device);
   EDP_TRACE(__func__);
   const cudaError_t e = launch_balance_loss(ctx, z, sel, top, coef, grad_scale, loss, counts,
