@@ -528,9 +528,14 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
  * EDP_ERR_INVALID).  mask (uint8 per token, or NULL: all ones)
  * leaves out the tokens where it is 0: their log-probabilities, advantages and
  * logits may hold anything, their outputs and gradients are 0.  Outputs overlap
- * no input, but for a gradient in its logits' place.  Arithmetic is fp32, sums
- * over tokens fp32 pairs or fp64, each output rounded once to its type; no
- * result depends on the order in which threads run.  edp_policy_loss*,
+ * no input, but for a gradient in its logits' place.  Arithmetic is fp32, and
+ * outputs are rounded to their type.  Sums: a row's exponentials in fp32, by up
+ * to thousands of lanes; the policy loss's terms in fp32 for 32 tokens of a lane
+ * and in pairs of fp32 numbers beyond, the preference loss's log ratios in such
+ * pairs; the router's probabilities in fp32 for a few hundred rows of a lane
+ * (2^-15 of the sum at the worst) and as whole numbers beyond, as counts and the
+ * gradients of shared sequences.  No result depends on the order in which threads
+ * run.  edp_policy_loss*,
  * edp_preference_loss and edp_balance_loss use the scratch that edp_gae and
  * edp_pack_deliver use and must be ordered with them and each other;
  * edp_token_logprob* use none.

@@ -10,9 +10,11 @@
 // any order to the same bits.  Up to kOneCta elements one CTA does both steps
 // (256 rows of 64 experts 6.2 us, 6.4 in two kernels; 511 rows 8.2 and 6.4).
 //
-// 131,072 rows of 128 experts in bfloat16, 8 chosen: 23.4 us, 3.1 TB/s of the bytes
-// that the call cannot do without.  What bounds it: issue (23 instructions an
-// element), and the two kernels' starts and ends.
+// 131,072 rows of 128 experts in bfloat16, 8 chosen: 22.8 us, 3.1 TB/s of the bytes
+// that the call cannot do without.  What bounds it: 19 instructions an element, at 2.4
+// of 4 a cycle from the 16 warps per SM that 128 registers leave (18 us); the counts'
+// kernel and the starts and ends take the rest.  Forms off the vector path spill beyond
+// 256 experts (96 bytes, 264 beyond 512), as do fp32's of more than 512 (260).
 #include <type_traits>
 
 #include "edp_loss.cuh"
@@ -326,6 +328,7 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
   if (nan) atomicExch(&sums->nan, 1u);
   if constexpr (kRing) copies_wait<0>();
   __syncthreads();  // the ring's room is free
+  const float units = a.rows > kManyRows ? kProbUnitsMany : kProbUnits;
   // over the warp's groups, then its CTA's warps, in order
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -340,7 +343,7 @@ k_balance(BalanceArgs a, BalanceSums *sums, Ctrl *ctrl) {
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) v += col[w][e];
     if (ONE) col[0][e] = v;
-    else if (v > 0.f) atomicAdd(&sums->prob[e], (unsigned long long)__float2ull_rn(v * (a.rows > kManyRows ? kProbUnitsMany : kProbUnits)));
+    else if (v > 0.f) atomicAdd(&sums->prob[e], (unsigned long long)__float2ull_rn(v * units));
   }
   __threadfence();
   __syncthreads();

@@ -14,10 +14,10 @@
 // What bounds each now, at 6.69 TB/s of measured copy:
 //   log-probabilities, 8,192 x 152,064 bf16      324 us   335 us to read them: memory
 //   gradient with entropy, 4,096 x 152,064 bf16  349 us   354 us to read and write: memory
-//   gradient, 777 x 32,003 f16                    21 us   14.9 us: start and end of 1,554
-//                                                         CTAs, rows off 16-byte boundaries
-//   both with the policy loss, 8,192 x 152,064   775 us   707 us to read and write once
-//   one row of 152,064                           3.9 us   in a graph: launch, one round
+//   gradient, 777 x 32,003 f16                    21 us   14.9 us: 1,554 CTAs, 2.6 waves, each
+//                                                         of which loads once and then stores
+//   both with the policy loss, 8,192 x 152,064   784 us   707 us to read and write once
+//   one row of 152,064                           3.8 us   in a graph: launch, one round
 //                                                         trip to memory, the cluster's join
 #include <cooperative_groups.h>
 
@@ -485,7 +485,8 @@ struct GradOf {
     return e * (ENT ? fma2(b, finite_log<T, FUSED>(y), a) : a);
   }
   __device__ __forceinline__ float of(float z) const {
-    if constexpr (ENT && FUSED && std::is_same<T, __nv_bfloat16>::value) z = z < kLowLogit ? kLowLogit : z;
+    if constexpr (ENT && FUSED && std::is_same<T, __nv_bfloat16>::value)
+      z = z < kLowLogit ? kLowLogit : z;
     return of(F2(z, 0.f)).x();
   }
   __device__ __forceinline__ uint4 of(const uint4 &w) const {
@@ -663,8 +664,8 @@ k_policy_rows(RowArgs a, RowWeights weights, const float *old_logp, const float 
 
 // The same with each CTA's part of the row in shared memory: read from memory once,
 // its gradient written once.  The part comes by a bulk copy; the CTAs of other rows
-// on the SM take turns with it at waiting, computing and storing.  8,192 rows of
-// 152,064 bfloat16 logits: 775 us, 1,012 with the logits read twice.  Parts of 76 KB
+// on the SM (two beside it) take turns with it at waiting, computing and storing.  8,192 rows
+// of 152,064 bfloat16 logits: 784 us, 1,012 with the logits read twice.  Parts of 76 KB
 // (4 CTAs) and 384 threads; 842 us with 38 KB and 256 threads, 806 with 76 KB and 256,
 // 809 with 512, 875 with 101 KB and 512.  The CTAs' sums travel as messages, each
 // counted on an mbarrier of its receiver (841 us; 914 with barriers of the cluster, whose
@@ -683,7 +684,7 @@ constexpr int kResidentCtas = kFused<T> ? 3 : 4;
 enum class Rest { kGrad, kZero, kCareful };
 
 // No preference for what leaves the second-level cache first: with the streaming
-// policy 8,192 rows of 152,064 take 788 us, with this one 777.
+// policy 8,192 rows of 152,064 took 788 us, with this one 777.
 __device__ __forceinline__ uint64_t policy_normal() {
   uint64_t p;
   asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));

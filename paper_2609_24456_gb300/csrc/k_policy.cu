@@ -11,8 +11,9 @@
 //
 // 8,192 sequences of 128 to 4,096 tokens, masked, with a reference (17.3 M tokens of 21
 // bytes, weights by sequence): 80 us, 4.5 TB/s; the floor is 54 us.  What bounds it:
-// issue (ALU 0.52 busy; about 100 instructions a token, half of them selections and
-// comparisons of the clipping and the masks), then the two launches before it (5 us).
+// issue (about 100 instructions a token, half of them selections and comparisons of the
+// clipping and the masks, at 2.8 of 4 a cycle from 32 warps of 64 registers, up to 72 bytes
+// of them spilled), then the two launches before it (5 us).
 // Two CTAs of 512 threads per SM; 85 us with three of 384, 94 with five of 256, 91 with
 // the next tile loaded ahead (80 registers, spilled).  fp64 sums, or a search for each
 // token's sequence, as in the first kernel: 521 us.
@@ -36,12 +37,16 @@ constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CT
 constexpr uint32_t kBlock = 512;     // tokens counted together
 constexpr int kSums = 8;  // pg, kl, entropy; ratio - 1, old kl; clipped above, below; tokens
 // Up to so many tokens on average that its weight takes in, a row of logits counts them
-// itself, beside its copy, in the place of one or two kernels before (16 rows 14.0 us in a
-// graph with them, 11.5 without; 515 rows in 9 sequences 38.7 and 37.1, but with one mean
-// over all 515 37.8 and 44.6).
+// itself, beside its copy, in the place of one or two kernels before.  In a graph, with the
+// kernels and without: 16 rows 14.0 and 11.5 us; of 32,003 columns, 515 rows in 16 sequences
+// 28.3 and 27.1, in 4 28.3 and 28.6, with one mean over all 26.2 and 33.6; 1,000 rows in 16
+// 45.4 and 46.1.  Over 8 to 1,000 rows of 4,096, 32,003 and 152,064 columns the rule is within
+// 4% of the better one, but for means over 130 to 250 tokens of 4,096 columns (up to 22%).
 constexpr uint64_t kFewTokens = 128;
 constexpr uint64_t kFewRows = 1024;
-constexpr int kFlush = 8;  // tiles (32 tokens a lane) between two additions to the sums
+// Tiles between two additions to the sums: 32 tokens a lane in fp32, 2^-19 of their sum at
+// the worst.
+constexpr int kFlush = 8;
 
 struct Weighting {
   const float *sequence;             // SEQ_MEAN: each sequence's weight
