@@ -36,32 +36,9 @@ constexpr int kPerSm = 2;  // CTAs of k_policy, in one wave
 constexpr int kSmallThreads = 1024;  // a batch of up to 4,096 tokens, in one CTA
 constexpr uint32_t kBlock = 512;     // tokens counted together
 constexpr int kSums = 8;  // pg, kl, entropy; ratio - 1, old kl; clipped above, below; tokens
-// Up to so many tokens on average that its weight takes in, a row of logits counts them
-// itself, beside its copy, in the place of one or two kernels before.  In a graph, with the
-// kernels and without: 16 rows 14.0 and 11.5 us; of 32,003 columns, 515 rows in 16 sequences
-// 28.3 and 27.1, in 4 28.3 and 28.6, with one mean over all 26.2 and 33.6; 1,000 rows in 16
-// 45.4 and 46.1.  Over 8 to 1,000 rows of 4,096, 32,003 and 152,064 columns the rule is within
-// 4% of the better one, but for means over 130 to 250 tokens of 4,096 columns (up to 22%).
-constexpr uint64_t kFewTokens = 128;
-constexpr uint64_t kFewRows = 1024;
 // Tiles between two additions to the sums: 32 tokens a lane in fp32, 2^-19 of their sum at
 // the worst.
 constexpr int kFlush = 8;
-
-struct Weighting {
-  const float *sequence;             // SEQ_MEAN: each sequence's weight
-  const unsigned long long *tokens;  // TOKEN_MEAN without norm: the divisor
-  bool by_range;                     // the same where every token of the sequences counts
-  float fixed;                       // otherwise: every weight
-};
-
-struct Range {
-  uint64_t first, end;  // the tokens that the sequences hold
-};
-__device__ __forceinline__ Range token_range(const TokenSet &s) {
-  if (!s.off) return {0, s.n};
-  return {s.off[0], min(s.off[s.n_seq], s.n)};
-}
 
 template <int NT>
 __device__ __forceinline__ uint32_t cta_sum(uint32_t v, uint32_t *red) {
@@ -466,18 +443,9 @@ unsigned at_most(uint64_t want, uint64_t most) {
   return (unsigned)(want < 1 ? 1 : want < most ? want : most);
 }
 
-// The scratch of a call and what it is for.
-struct Plan {
-  Weighting w;
-  float divisor;
-  bool sequences;
-  bool early;  // k_token_counts runs first
-  Pair *part;
-  float *entropy;
-};
+}  // namespace
 
-// Counts what the weights need, unless the batch's own CTA does (one_cta).
-cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool entropy,
+cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool per_token,
                          cudaStream_t s, Plan *p) {
   const uint64_t sms = (uint64_t)c->coop_sms;
   p->sequences = set.reduce == EDP_REDUCE_SEQ_MEAN;
@@ -499,13 +467,13 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
   const size_t part = take(true, kSums * kPerSm * sms * sizeof(Pair));
   const size_t weight = take(p->sequences && !one_cta, set.n_seq * sizeof(float));
   const size_t block = take(blocks, (set.n + kBlock - 1) / kBlock * sizeof(uint32_t));
-  const size_t ent = take(entropy, set.n * sizeof(float));
+  const size_t own = take(per_token, set.n * sizeof(float));
   void *blk = nullptr;
   cudaError_t e = ctx_scratch(c, at, s, &blk);
   if (e != cudaSuccess) return e;
   uint8_t *b = (uint8_t *)blk;
   p->part = (Pair *)(b + part);
-  p->entropy = (float *)(b + ent);
+  p->per_token = (float *)(b + own);
   if (by_total) p->w.tokens = &c->ctrl->loss_tokens;
   if (one_cta) return cudaSuccess;
   const unsigned warps = kThreads / 32;
@@ -526,10 +494,11 @@ cudaError_t plan_weights(edp_ctx *c, const TokenSet &set, bool one_cta, bool ent
   return e;
 }
 
-// The count that k_policy would have set back to 0, after a launch that failed.
 void forget_count(edp_ctx *c, const Plan &p, cudaStream_t s) {
   if (p.w.tokens) cudaMemsetAsync(&c->ctrl->loss_tokens, 0, sizeof c->ctrl->loss_tokens, s);
 }
+
+namespace {
 
 template <bool VEC>
 cudaError_t launch_policy(edp_ctx *c, const TokenSet &set, const PolicyTokens &t,
@@ -582,7 +551,7 @@ cudaError_t launch_policy_loss_logits(edp_ctx *c, const edp_policy_config &cfg,
   const bool few = set.n <= kFewRows && set.n <= kFewTokens * means;
   cudaError_t e = plan_weights(c, set, few, own_entropy, s, &p);
   if (e != cudaSuccess) return e;
-  if (own_entropy) entropy = p.entropy;
+  if (own_entropy) entropy = p.per_token;
   const PolicyRule rule = policy_rule(cfg);
   const bool counted = p.sequences || p.w.tokens;
   const RowWeights w{set, few && counted, p.w.sequence, p.w.tokens, p.w.fixed, p.divisor};
