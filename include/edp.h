@@ -13,8 +13,9 @@
  *   delivery   -> edp_sample            (uniform, prioritized, shuffle)
  *                 edp_deliver           (gather + transform + collate)
  *   callback   -> edp_update_priorities / edp_update_priorities_td
- *   learner    -> edp_token_logprob*, edp_policy_loss*, edp_preference_loss,
- *                 edp_balance_loss (the losses of an LLM learner on its batch)
+ *   learner    -> edp_token_logprob*, edp_token_top, edp_policy_loss*,
+ *                 edp_preference_loss, edp_balance_loss, edp_distill_loss (the
+ *                 losses of an LLM learner on its batch, a teacher's lists)
  *   sharding   -> edp_tree_total, edp_route_prioritized, edp_sample_targets,
  *                 edp_batch_qmin, edp_is_weights, edp_gae_stats,
  *                 edp_gae_normalize (a buffer split across GPUs, Sec. 5.1)
@@ -535,10 +536,10 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
  * pairs; the router's probabilities in fp32 for a few hundred rows of a lane
  * (2^-15 of the sum at the worst) and as whole numbers beyond, as counts and the
  * gradients of shared sequences.  No result depends on the order in which threads
- * run.  edp_policy_loss*,
- * edp_preference_loss and edp_balance_loss use the scratch that edp_gae and
- * edp_pack_deliver use and must be ordered with them and each other;
- * edp_token_logprob* use none.
+ * run.  edp_policy_loss*, edp_preference_loss, edp_balance_loss and
+ * edp_distill_loss use the scratch that edp_gae and edp_pack_deliver use and must
+ * be ordered with them and each other; edp_token_logprob* and edp_token_top use
+ * none.
  * ------------------------------------------------------------------------- */
 
 /* Element type of logits and of their gradient. */
@@ -582,6 +583,32 @@ EDP_API edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint
                                           const float *entropy, const float *dlogp,
                                           const float *dentropy, void *dlogits,
                                           uint64_t dstride, edp_stream stream);
+
+/* The likeliest tokens of each row, with their log-probabilities: what an actor
+ * reports beside the token that it took, and what a teacher leaves for
+ * edp_distill_loss.  Logits, temperature, m, S and logp, entropy and stats as for
+ * edp_token_logprob.  For row t:
+ *   ids[t]      = its `top` largest logits' tokens, the largest first, equal ones
+ *                 in the order of their index (int32 [rows][top])
+ *   top_logp[t] = their log-probabilities       (float [rows][top])
+ *   rest[t]     = the logarithm of the probability of all tokens that are not in
+ *                 the list, -infinity where there is none (float [rows] or NULL)
+ * A token whose logit is -infinity is in no list: an entry without a token has id
+ * -1 and log-probability -infinity.  target, logp, entropy, rest and stats may be
+ * NULL (logp needs target, which may be given without it).  Rows left out by mask
+ * or by a negative target have an empty list and 0 in the other outputs; so has a
+ * row with a target >= vocab, or whose logits are all -infinity, which edp_sync
+ * reports (EDP_ERR_INVALID).  NaN or +infinity in a row makes its ids -1 and its
+ * numbers NaN.
+ * Errors: as edp_token_logprob, and EDP_ERR_INVALID for top outside [1, 128], NULL
+ * ids or top_logp, logp without target, or a vocabulary whose row takes more than
+ * 1.5 MiB (786,432 logits of 16 bits, 393,216 of 32). */
+EDP_API edp_status edp_token_top(edp_ctx *ctx, const void *logits, uint32_t dtype,
+                                 uint64_t rows, uint32_t vocab, uint64_t stride,
+                                 const int32_t *target, const uint8_t *mask,
+                                 double temperature, uint32_t top, int32_t *ids,
+                                 float *top_logp, float *logp, float *entropy, float *rest,
+                                 float *stats, edp_stream stream);
 
 /* How token losses become one number. */
 typedef enum {
@@ -734,6 +761,59 @@ EDP_API edp_status edp_balance_loss(edp_ctx *ctx, const void *logits, uint32_t d
                                     double coef, double grad_scale, float *loss,
                                     int64_t *counts, float *prob, void *dlogits,
                                     uint64_t dstride, edp_stream stream);
+
+/* Divergences of a student's classes q from a teacher's p. */
+typedef enum {
+  EDP_DISTILL_FORWARD = 0, /* sum p ln(p / q) */
+  EDP_DISTILL_REVERSE = 1, /* sum q ln(q / p) */
+  EDP_DISTILL_MIX = 2      /* b sum p ln(p / m) + (1 - b) sum q ln(q / m),
+                              m = b p + (1 - b) q, b = beta (Agarwal et al. 2023) */
+} edp_distill_kind;
+
+typedef struct {
+  double beta;                /* MIX: 0 < beta < 1; else 0 */
+  double teacher_temperature; /* of the lists without rest, in [1e-6, 1e6]; 1 with it */
+  double norm;                /* as in edp_policy_config */
+  double grad_scale;          /* factor of the gradient */
+  uint32_t kind;              /* edp_distill_kind */
+  uint32_t reduce;            /* edp_reduce */
+  uint32_t reserved[2];       /* must be 0 */
+} edp_distill_config;
+
+/* Distillation from a teacher's lists over a packed batch: the divergence of the
+ * student's distribution q = softmax(logits / temperature) from the teacher's,
+ * reduced as the policy loss is, and the gradient of the logits.  Row t's list is
+ * ids[t] and value[t] (int32 and float [rows][top], as edp_token_top writes them);
+ * an entry whose id is negative, or whose value is -infinity, is no entry.
+ *   With rest (float [rows]): p_i = exp(value_i) for the entries and exp(rest[t])
+ * for one class that holds all other tokens, whose q is the sum of theirs.
+ *   Without it: FORWARD alone, with p = softmax(value / teacher_temperature) over
+ * the entries, whatever the values leave out; q stays that of the whole vocabulary.
+ *   L = sum_t w_t l_t, with w_t as for edp_policy_loss;  dlogits = grad_scale
+ *   dL/dlogits of the type of the logits, 0 in the rows left out
+ * p is taken as it is given, whatever it sums to.  loss (float [1]) = L;
+ * row_loss (float [rows], or NULL) = l_t before its weight.  mask, off, n_seq and
+ * the tokens outside them as for edp_policy_loss; a list of a row left out is not
+ * read.  dlogits may be NULL (the loss alone), or the logits' own array (with
+ * dstride == stride).
+ * A list that holds a token twice, or an id >= vocab, and a row whose logits are
+ * all -infinity add 0 to the loss, have gradient 0 and are reported by edp_sync
+ * (EDP_ERR_INVALID).  A class with p > 0 and q = 0 makes FORWARD infinite (its
+ * gradient stays finite), one with q > 0 and p = 0 REVERSE (its row's gradient is
+ * then NaN); NaN or +infinity in a row or its list makes loss and gradient NaN.
+ * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, top outside
+ * [1, 128], a NULL logits, ids, value or loss, REVERSE or MIX without rest, rows ==
+ * 0, logits, dlogits and vocab as for edp_token_top, off and n_seq as for
+ * edp_policy_loss, or arrays outside device memory; EDP_ERR_OOM when the scratch
+ * cannot be allocated. */
+EDP_API edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg,
+                                    const void *logits, uint32_t dtype, uint64_t rows,
+                                    uint32_t vocab, uint64_t stride, double temperature,
+                                    const int32_t *ids, const float *value, uint32_t top,
+                                    const float *rest, const uint8_t *mask,
+                                    const uint64_t *off, uint64_t n_seq, float *loss,
+                                    float *row_loss, void *dlogits, uint64_t dstride,
+                                    edp_stream stream);
 
 /* Wait for `stream`, then report (and clear) asynchronous CUDA errors and
  * device-side flags recorded since the previous edp_sync. */

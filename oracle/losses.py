@@ -141,3 +141,99 @@ def balance(z, sel, keep, coef, grad_scale=1.0):
     prob = p.sum(0) / N
     grad = grad_scale * coef / N * p * (f - (p @ f)[:, None])
     return coef * float(f @ prob), counts, prob, grad
+
+
+FORWARD, REVERSE, MIX = range(3)
+
+
+def token_top(z, top, temperature=1.0):
+    """(ids, logp, rest) of rows z with a finite logit each: the largest first, ties
+    by their index; -1 and -inf where no token with a probability is left."""
+    z = np.asarray(z, np.float64)
+    ids, logp = np.full((len(z), top), -1), np.full((len(z), top), -np.inf)
+    rest = np.full(len(z), -np.inf)
+    for t, row in enumerate(z):
+        order = np.lexsort((np.arange(len(row)), -row))[:top]
+        order = order[row[order] > -np.inf]
+        y = (row - row.max()) / temperature
+        ln = np.log(np.exp(y).sum())
+        ids[t, :len(order)], logp[t, :len(order)] = order, y[order] - ln
+        out = np.delete(y, order)
+        out = out[out > -np.inf]
+        if len(out):  # relative to its own maximum: none of it is lost beside the list
+            rest[t] = out.max() + np.log(np.exp(out - out.max()).sum()) - ln
+    return ids, logp, rest
+
+
+def weights(keep, off=None, reduce=TOKEN_MEAN, norm=0.0):
+    """What each of the tokens weighs in the batch's loss."""
+    keep = np.asarray(keep, bool).copy()
+    n = len(keep)
+    seq = sequences(off, n) if off is not None else np.zeros(n, int)
+    keep &= seq >= 0
+    n_seq = len(off) - 1 if off is not None else 1
+    per = np.bincount(seq[keep], minlength=n_seq)
+    w = np.zeros(n)
+    for t in np.flatnonzero(keep):
+        w[t] = 1 / ((norm or n_seq) * per[seq[t]]) if reduce == SEQ_MEAN else \
+            1 / (norm or (keep.sum() if reduce == TOKEN_MEAN else n_seq))
+    return w
+
+
+def _log_sum(x):
+    x = x[x > -np.inf]
+    return x.max() + np.log(np.exp(x - x.max()).sum()) if len(x) else -np.inf
+
+
+def _times(w, log):
+    return np.where(w == 0, 0.0, w * np.where(w == 0, 0.0, log))
+
+
+def distill_row(z, ids, value, rest=None, kind=FORWARD, beta=0.0, temperature=1.0,
+                teacher_temperature=1.0):
+    """(loss, d loss / d z) of one row with a finite logit."""
+    z = np.asarray(z, np.float64)
+    x = z / temperature
+    lnq = x - _log_sum(x)
+    q = np.exp(lnq)
+    here = [k for k in range(len(ids)) if ids[k] >= 0 and value[k] > -np.inf]
+    at = np.array([ids[k] for k in here], int)
+    lp = np.array([value[k] for k in here], np.float64)
+    others = np.delete(np.arange(len(z)), at)
+    if rest is None:
+        lp = lp / teacher_temperature
+        lp = lp - _log_sum(lp) if len(lp) else lp
+        lp = np.append(lp, -np.inf)
+    else:
+        lp = np.append(lp, rest)
+    lq = np.append(lnq[at], _log_sum(lnq[others]))
+    P, Q = np.exp(lp), np.exp(lq)
+    cls = np.full(len(z), len(here))
+    cls[at] = np.arange(len(here))
+    with np.errstate(all="ignore"):
+        if kind == FORWARD:
+            loss, qf = _times(P, lp - lq).sum(), -P
+        elif kind == REVERSE:
+            loss = _times(Q, lq - lp).sum()
+            qf = _times(Q, lq - lp + 1)
+        else:
+            m = np.logaddexp(np.log(beta) + lp, np.log1p(-beta) + lq)
+            qf = (1 - beta) * _times(Q, lq - m)
+            loss = beta * _times(P, lp - m).sum() + qf.sum()
+        # q_j f'_b = (q_j / Q_b) (Q_b f'_b): a token's share of its class
+        share = np.where(lq[cls] > -np.inf, np.exp(lnq - lq[cls]), 0.0)
+        share[at] = 1.0
+        return loss, (share * qf[cls] - q * qf.sum()) / temperature
+
+
+def distill(z, ids, value, rest, keep, off=None, kind=FORWARD, beta=0.0, reduce=TOKEN_MEAN,
+            norm=0.0, temperature=1.0, teacher_temperature=1.0, grad_scale=1.0):
+    """(loss, row losses, gradient of the logits)."""
+    z = np.asarray(z, np.float64)
+    w = weights(keep, off, reduce, norm)
+    each, grad = np.zeros(len(z)), np.zeros_like(z)
+    for t in np.flatnonzero(w):
+        each[t], g = distill_row(z[t], ids[t], value[t], None if rest is None else rest[t], kind,
+                                 beta, temperature, teacher_temperature)
+        grad[t] = grad_scale * w[t] * g
+    return float((w * each)[w > 0].sum()), each, grad

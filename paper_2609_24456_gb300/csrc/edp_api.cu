@@ -1432,6 +1432,10 @@ edp_status edp_sync(edp_ctx *ctx, edp_stream stream) {
     return fail(ctx, EDP_ERR_INVALID,
                 "device: a packed output or a sum of shard totals exceeds its capacity "
                 "(%llu, flags 0x%x)", bi, h.err);
+  if (!(h.err & DEVERR_INDEX) && (h.err & DEVERR_TWICE))
+    return fail(ctx, EDP_ERR_INVALID,
+                "device: a teacher's list that holds a token twice (first row %llu, flags 0x%x)",
+                bi, h.err);
   if (!(h.err & DEVERR_INDEX))
     return fail(ctx, EDP_ERR_INVALID,
                 "device: a row of logits that are all -infinity (first row %llu, flags 0x%x)",

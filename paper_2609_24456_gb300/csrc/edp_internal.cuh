@@ -23,6 +23,7 @@ enum : uint32_t {
   DEVERR_TREE = 8u,     // a tree descent found no child holding its target
   DEVERR_OVERFLOW = 16u,  // packed output larger than its buffer (clipped)
   DEVERR_ROW = 32u,       // a row of logits that are all -infinity
+  DEVERR_TWICE = 64u,     // a teacher's list that holds a token twice
 };
 
 // Small device-resident control block (one per context).
@@ -569,6 +570,9 @@ struct PolicyTokens {
 };
 cudaError_t launch_token_logprob(edp_ctx *ctx, const Logits &z, float *logp, float *entropy,
                                  float *stats, cudaStream_t s);
+cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_t *ids,
+                             float *top_logp, float *logp, float *entropy, float *rest,
+                             float *stats, cudaStream_t s);
 cudaError_t launch_token_logprob_grad(edp_ctx *ctx, const Logits &z, const float *stats,
                                       const float *entropy, const float *dlogp,
                                       const float *dentropy, void *dz, uint64_t dstride,
@@ -587,6 +591,10 @@ cudaError_t launch_preference_loss(edp_ctx *ctx, const edp_preference_config &cf
 cudaError_t launch_balance_loss(edp_ctx *ctx, const Logits &z, const int32_t *sel, uint32_t top,
                                 double coef, double grad_scale, float *loss, int64_t *counts,
                                 float *prob, void *dz, uint64_t dstride, cudaStream_t s);
+cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, const TokenSet &set,
+                                const Logits &z, const int32_t *ids, const float *value,
+                                uint32_t top, const float *rest, float *loss, float *row_loss,
+                                void *dz, uint64_t dstride, cudaStream_t s);
 
 // Scratch owned by the context, grown on demand.  Growing allocates, and
 // first waits for the device (the old block may still be in use); neither

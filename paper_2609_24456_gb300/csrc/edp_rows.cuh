@@ -253,9 +253,10 @@ __device__ __forceinline__ void cluster_wait() {
 
 // The sums of a warp's lanes, in all of them: first their maximum, to which each
 // lane's sums go over, then plain sums in a fixed order (LANES: the lanes that hold
-// any, the first of the warp).
+// any, the first of the warp; a power of two).
 template <typename T, bool FUSED, int LANES = 32>
 __device__ __forceinline__ RowSum warp_sum(RowSum a, float c) {
+  static_assert((LANES & (LANES - 1)) == 0, "halved in each step");
   float m = a.m;
 #pragma unroll
   for (int o = LANES / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, o));
@@ -274,6 +275,9 @@ __device__ __forceinline__ RowSum warp_sum(RowSum a, float c) {
   return {m, a.s, a.u};
 }
 
+// The lanes that as many warps' sums take.
+constexpr int lanes_for(int warps) { return warps <= 8 ? 8 : warps <= 16 ? 16 : 32; }
+
 // The CTA's sums, in its first warp.
 template <typename T, bool FUSED, int NT = kRowThreads>
 __device__ __forceinline__ RowSum cta_join(RowSum a, float c, RowSum *red) {
@@ -282,7 +286,8 @@ __device__ __forceinline__ RowSum cta_join(RowSum a, float c, RowSum *red) {
   if (lane == 0) red[wid] = a;
   __syncthreads();
   if (wid == 0)
-    a = warp_sum<T, FUSED, NT / 32>(lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, c);
+    a = warp_sum<T, FUSED, lanes_for(NT / 32)>(
+        lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, c);
   return a;
 }
 

@@ -1,5 +1,6 @@
 // loss_api.cu -- the C ABI of the losses over a packed batch: argument checks
-// and dispatch to k_logits.cu, k_policy.cu, k_pref.cu and k_balance.cu.
+// and dispatch to k_logits.cu, k_top.cu, k_policy.cu, k_pref.cu, k_balance.cu and
+// k_distill.cu.
 #include <cmath>
 #include <initializer_list>
 
@@ -34,8 +35,9 @@ bool in_order(double lo, double x) { return std::isfinite(x) && x >= lo; }
 
 // Shape and type of logits, and of their gradient where it is given.
 edp_status check_logits(edp_ctx *c, const char *who, const Logits &z, const void *dz,
-                        uint64_t dstride) {
-  if (!z.z || !z.target) return fail(c, EDP_ERR_INVALID, "%s: NULL logits or target", who);
+                        uint64_t dstride, bool targets = true) {
+  if (!z.z || (targets && !z.target))
+    return fail(c, EDP_ERR_INVALID, "%s: NULL logits or target", who);
   if (z.dtype > EDP_F16) return fail(c, EDP_ERR_INVALID, "%s: unknown dtype", who);
   if (z.vocab == 0 || z.vocab > 0x7FFFFFFFu || z.rows > 0x7FFFFFFFull || z.stride < z.vocab ||
       z.stride > (1ull << 40))
@@ -47,6 +49,24 @@ edp_status check_logits(edp_ctx *c, const char *who, const Logits &z, const void
   if (dz && (dstride < z.vocab || dstride > (1ull << 40) || (dz == z.z && dstride != z.stride)))
     return fail(c, EDP_ERR_INVALID,
                 "%s: dstride must be >= vocab, and the logits' own in their array", who);
+  return EDP_OK;
+}
+
+// The kernels with lists hold a row in the shared memory of 8 CTAs at the most.
+constexpr uint64_t kMostRowBytes = 3ull << 19;
+edp_status check_lists(edp_ctx *c, const char *who, const Logits &z, uint32_t top) {
+  if (top == 0 || top > 128) return fail(c, EDP_ERR_INVALID, "%s: need 0 < top <= 128", who);
+  if (z.vocab * size_of(z.dtype) > kMostRowBytes)
+    return fail(c, EDP_ERR_INVALID, "%s: a row of logits takes more than 1.5 MiB", who);
+  return EDP_OK;
+}
+
+edp_status check_tokens(edp_ctx *c, const char *who, const TokenSet &s) {
+  if (s.n == 0 || s.n >= (1ull << 40))
+    return fail(c, EDP_ERR_INVALID, "%s: need 0 < tokens < 2^40", who);
+  if ((s.off != nullptr) != (s.n_seq != 0) || s.n_seq > 0x7FFFFFFFull ||
+      (!s.off && s.reduce != EDP_REDUCE_TOKEN_MEAN))
+    return fail(c, EDP_ERR_INVALID, "%s: off and n_seq go together, and by sequences both", who);
   return EDP_OK;
 }
 
@@ -68,12 +88,26 @@ edp_status check_policy(edp_ctx *c, const char *who, const edp_policy_config *g,
     return fail(c, EDP_ERR_INVALID, "%s: kl_coef needs ref_logp", who);
   if (g->entropy_coef > 0.0 && !has_entropy)
     return fail(c, EDP_ERR_INVALID, "%s: entropy_coef needs entropy", who);
-  if (s.n == 0 || s.n >= (1ull << 40))
-    return fail(c, EDP_ERR_INVALID, "%s: need 0 < tokens < 2^40", who);
-  if ((s.off != nullptr) != (s.n_seq != 0) || s.n_seq > 0x7FFFFFFFull ||
-      (!s.off && g->reduce != EDP_REDUCE_TOKEN_MEAN))
-    return fail(c, EDP_ERR_INVALID, "%s: off and n_seq go together, and by sequences both", who);
-  return EDP_OK;
+  return check_tokens(c, who, s);
+}
+
+edp_status check_distill(edp_ctx *c, const char *who, const edp_distill_config *g,
+                         const TokenSet &s, bool has_rest) {
+  if (!g) return fail(c, EDP_ERR_INVALID, "%s: NULL argument", who);
+  if (g->kind > EDP_DISTILL_MIX || g->reduce > EDP_REDUCE_SEQ_SUM || g->reserved[0] ||
+      g->reserved[1])
+    return fail(c, EDP_ERR_INVALID, "%s: unknown kind or reduce, or reserved fields set", who);
+  if (g->kind == EDP_DISTILL_MIX ? !(g->beta > 0.0 && g->beta < 1.0) : g->beta != 0.0)
+    return fail(c, EDP_ERR_INVALID, "%s: need 0 < beta < 1 with MIX, 0 else", who);
+  if (has_rest ? g->teacher_temperature != 1.0
+               : !(g->teacher_temperature >= 1e-6 && g->teacher_temperature <= 1e6))
+    return fail(c, EDP_ERR_INVALID,
+                "%s: teacher_temperature must be in [1e-6, 1e6], and 1 with rest", who);
+  if (!has_rest && g->kind != EDP_DISTILL_FORWARD)
+    return fail(c, EDP_ERR_INVALID, "%s: REVERSE and MIX need rest", who);
+  if (!in_order(0.0, g->norm) || !std::isfinite(g->grad_scale))
+    return fail(c, EDP_ERR_INVALID, "%s: norm and grad_scale must be finite, norm >= 0", who);
+  return check_tokens(c, who, s);
 }
 
 void count_traffic(edp_ctx *c, uint64_t read, uint64_t write) {
@@ -138,6 +172,69 @@ edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint32_t dty
                 rows * (vocab * size_of(dtype) + 16 + (mask != nullptr) +
                         8 * (entropy != nullptr)),
                 rows * vocab * size_of(dtype));
+  return EDP_OK;
+}
+
+edp_status edp_token_top(edp_ctx *ctx, const void *logits, uint32_t dtype, uint64_t rows,
+                         uint32_t vocab, uint64_t stride, const int32_t *target,
+                         const uint8_t *mask, double temperature, uint32_t top, int32_t *ids,
+                         float *top_logp, float *logp, float *entropy, float *rest,
+                         float *stats, edp_stream stream) {
+  if (!ctx) return EDP_ERR_INVALID;
+  if (rows == 0) return EDP_OK;
+  const Logits z{logits, dtype, vocab, rows, stride, target, mask, temperature};
+  edp_status st = check_logits(ctx, "edp_token_top", z, nullptr, 0, false);
+  if (st == EDP_OK) st = check_lists(ctx, "edp_token_top", z, top);
+  if (st != EDP_OK) return st;
+  if (!ids || !top_logp || (logp && !target))
+    return fail(ctx, EDP_ERR_INVALID, "edp_token_top: NULL ids or top_logp, or logp without target");
+  if (!device_arrays(ctx, {logits, target, mask, ids, top_logp, logp, entropy, rest, stats}))
+    return fail(ctx, EDP_ERR_INVALID, "edp_token_top: arrays must be device memory");
+  if (!aligned_arrays({target, ids, top_logp, logp, entropy, rest, stats}, {}))
+    return not_aligned(ctx, "edp_token_top");
+  DeviceGuard dg(ctx->cfg.device);
+  EDP_TRACE(__func__);
+  const cudaError_t e = launch_token_top(ctx, z, top, ids, top_logp, logp, entropy, rest, stats,
+                                         (cudaStream_t)stream);
+  if (e != cudaSuccess) return launch_fail(ctx, e, "edp_token_top");
+  count_traffic(ctx,
+                rows * (vocab * size_of(dtype) + 4 * (target != nullptr) + (mask != nullptr)),
+                rows * (8ull * top + 4 * (logp != nullptr) + 4 * (entropy != nullptr) +
+                        4 * (rest != nullptr) + 8 * (stats != nullptr)));
+  return EDP_OK;
+}
+
+edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg, const void *logits,
+                            uint32_t dtype, uint64_t rows, uint32_t vocab, uint64_t stride,
+                            double temperature, const int32_t *ids, const float *value,
+                            uint32_t top, const float *rest, const uint8_t *mask,
+                            const uint64_t *off, uint64_t n_seq, float *loss, float *row_loss,
+                            void *dlogits, uint64_t dstride, edp_stream stream) {
+  if (!ctx) return EDP_ERR_INVALID;
+  const Logits z{logits, dtype, vocab, rows, stride, nullptr, mask, temperature};
+  const TokenSet set{mask, off, nullptr, vocab, cfg ? cfg->reduce : 0, n_seq, rows,
+                     cfg ? cfg->norm : 0.0};
+  edp_status st = check_distill(ctx, "edp_distill_loss", cfg, set, rest != nullptr);
+  if (st == EDP_OK) st = check_logits(ctx, "edp_distill_loss", z, dlogits, dstride, false);
+  if (st == EDP_OK) st = check_lists(ctx, "edp_distill_loss", z, top);
+  if (st != EDP_OK) return st;
+  if (!ids || !value || !loss)
+    return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: NULL ids, value or loss");
+  if (!device_arrays(ctx, {logits, ids, value, rest, mask, off, loss, row_loss, dlogits}))
+    return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: arrays must be device memory");
+  if (!aligned_arrays({ids, value, rest, loss, row_loss}, {off}))
+    return not_aligned(ctx, "edp_distill_loss");
+  DeviceGuard dg(ctx->cfg.device);
+  EDP_TRACE(__func__);
+  const cudaError_t e = launch_distill_loss(ctx, *cfg, set, z, ids, value, top, rest, loss,
+                                            row_loss, dlogits, dstride, (cudaStream_t)stream);
+  if (e != cudaSuccess) return launch_fail(ctx, e, "edp_distill_loss");
+  count_traffic(ctx,
+                rows * (vocab * size_of(dtype) + 8ull * top + 4 * (rest != nullptr) +
+                        (mask != nullptr)) +
+                    (off ? 8 * (n_seq + 1) : 0),
+                rows * (vocab * size_of(dtype) * (dlogits != nullptr) +
+                        4 * (row_loss != nullptr)) + 4);
   return EDP_OK;
 }
 

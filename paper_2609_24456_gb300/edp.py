@@ -87,6 +87,7 @@ EDP_F32, EDP_BF16, EDP_F16 = range(3)
 EDP_REDUCE_TOKEN_MEAN, EDP_REDUCE_SEQ_MEAN, EDP_REDUCE_SEQ_SUM = range(3)
 EDP_KL_K1, EDP_KL_K2, EDP_KL_K3 = range(3)
 EDP_PREF_LOGISTIC, EDP_PREF_SQUARE, EDP_PREF_HINGE = range(3)
+EDP_DISTILL_FORWARD, EDP_DISTILL_REVERSE, EDP_DISTILL_MIX = range(3)
 
 
 class edp_policy_config(C.Structure):
@@ -101,6 +102,12 @@ class edp_preference_config(C.Structure):
     _fields_ = [("beta", C.c_double), ("label_smoothing", C.c_double),
                 ("margin", C.c_double), ("norm", C.c_double), ("grad_scale", C.c_double),
                 ("kind", C.c_uint32), ("average", C.c_uint32), ("reserved", C.c_uint32 * 2)]
+
+
+class edp_distill_config(C.Structure):
+    _fields_ = [("beta", C.c_double), ("teacher_temperature", C.c_double),
+                ("norm", C.c_double), ("grad_scale", C.c_double), ("kind", C.c_uint32),
+                ("reduce", C.c_uint32), ("reserved", C.c_uint32 * 2)]
 
 
 EDP_PLACE_HOST_PAGEABLE, EDP_PLACE_HOST_PINNED, EDP_PLACE_GPU, EDP_PLACE_GPU_HOST = range(4)
@@ -168,6 +175,11 @@ SIGNATURES = {
                                     _VP, _VP]),
     "edp_token_logprob_grad": (C.c_int, [_VP, _VP, _U32, _U64, _U32, _U64, _VP, _VP, _D, _VP,
                                          _VP, _VP, _VP, _VP, _U64, _VP]),
+    "edp_token_top": (C.c_int, [_VP, _VP, _U32, _U64, _U32, _U64, _VP, _VP, _D, _U32] +
+                      [_VP] * 7),
+    "edp_distill_loss": (C.c_int, [_VP, C.POINTER(edp_distill_config), _VP, _U32, _U64, _U32,
+                                   _U64, _D, _VP, _VP, _U32, _VP, _VP, _VP, _U64, _VP, _VP, _VP,
+                                   _U64, _VP]),
     "edp_policy_loss": (C.c_int, [_VP, C.POINTER(edp_policy_config)] + [_VP] * 7 +
                         [_U64, _U64, _VP, _VP, _VP, _VP]),
     "edp_policy_loss_logits": (C.c_int, [_VP, C.POINTER(edp_policy_config), _VP, _U32, _U64, _U32,
@@ -632,6 +644,11 @@ def make_preference_config(beta, kind=EDP_PREF_LOGISTIC, label_smoothing=0.0, ma
                                  int(bool(average)))
 
 
+def make_distill_config(kind=EDP_DISTILL_FORWARD, reduce=EDP_REDUCE_TOKEN_MEAN, beta=0.0,
+                        teacher_temperature=1.0, norm=0.0, grad_scale=1.0):
+    return edp_distill_config(beta, teacher_temperature, norm, grad_scale, kind, reduce)
+
+
 _dtypes = {}  # edp_dtype by torch type, filled as types are met (torch is not imported here)
 
 
@@ -790,6 +807,42 @@ def edp_balance_loss(ctx, logits, sel, coef, loss, counts, mask=None, prob=None,
         _arr(mask, _mask, rows, who), coef, grad_scale, _vec(loss, who),
         _arr(counts, _i64, experts, who), _vec(prob, who), d, dstride,
         stream_handle(stream)), who)
+
+
+def _lists(x, rows, who):
+    """Entries per row of the lists x."""
+    if x.dim() != 2 or x.shape[0] != rows:
+        raise ValueError("%s: lists are 2-D tensors with a row for each of the logits'" % who)
+    return x.shape[1]
+
+
+def edp_token_top(ctx, logits, ids, top_logp, target=None, logp=None, mask=None,
+                  temperature=1.0, entropy=None, rest=None, stats=None, stream=None):
+    """The likeliest tokens of each row: ids and top_logp [rows][top]."""
+    who = "edp_token_top"
+    p, dt, rows, vocab, stride = _rows(logits)
+    top = _lists(ids, rows, who)
+    return _check(ctx, lib().edp_token_top(
+        ctx, p, dt, rows, vocab, stride, _arr(target, _i32, rows, who),
+        _arr(mask, _mask, rows, who), temperature, top, _arr(ids, _i32, rows * top, who),
+        _arr(top_logp, _f32, rows * top, who), _vec(logp, who), _vec(entropy, who),
+        _vec(rest, who), _vec(stats, who), stream_handle(stream)), who)
+
+
+def edp_distill_loss(ctx, cfg: edp_distill_config, logits, ids, value, loss, rest=None,
+                     mask=None, off=None, n_seq=0, temperature=1.0, row_loss=None,
+                     dlogits=None, stream=None):
+    """Loss of the student's logits against a teacher's lists [rows][top], and their
+    gradient; dlogits may be the logits."""
+    who = "edp_distill_loss"
+    p, dt, rows, vocab, stride = _rows(logits)
+    d, dstride = _grad_rows(dlogits, logits)
+    top = _lists(ids, rows, who)
+    return _check(ctx, lib().edp_distill_loss(
+        ctx, C.byref(cfg), p, dt, rows, vocab, stride, temperature,
+        _arr(ids, _i32, rows * top, who), _arr(value, _f32, rows * top, who), top,
+        _vec(rest, who), _arr(mask, _mask, rows, who), _arr(off, _u64, n_seq + 1, who), n_seq,
+        _vec(loss, who), _vec(row_loss, who), d, dstride, stream_handle(stream)), who)
 
 
 def edp_save(ctx, path, stream=None):
