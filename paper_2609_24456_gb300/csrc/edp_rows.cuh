@@ -182,12 +182,9 @@ __device__ __forceinline__ RowLog<T, FUSED> raise(LaneSum &a, float m, float c) 
   }
   return RowLog<T, FUSED>(a.m, c);
 }
-// K vectors of one thread.
+// K vectors of one thread, whose largest number is m.
 template <typename T, bool ENT, bool FUSED, int K>
-__device__ __forceinline__ void take_vectors(LaneSum &a, const uint4 (&w)[K], float c) {
-  float m = Vec16<T>::max(w[0]);
-#pragma unroll
-  for (int k = 1; k < K; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
+__device__ __forceinline__ void add_vectors(LaneSum &a, const uint4 (&w)[K], float m, float c) {
   const RowLog<T, FUSED> log = raise<T, ENT, FUSED>(a, m, c);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -199,6 +196,13 @@ __device__ __forceinline__ void take_vectors(LaneSum &a, const uint4 (&w)[K], fl
       if (ENT) a.u = fma2(e, finite_log<T, FUSED>(y), a.u);
     }
   }
+}
+template <typename T, bool ENT, bool FUSED, int K>
+__device__ __forceinline__ void take_vectors(LaneSum &a, const uint4 (&w)[K], float c) {
+  float m = Vec16<T>::max(w[0]);
+#pragma unroll
+  for (int k = 1; k < K; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
+  add_vectors<T, ENT, FUSED>(a, w, m, c);
 }
 
 // Elements [0, n) at p as those before the first 16-byte boundary, vectors, rest.

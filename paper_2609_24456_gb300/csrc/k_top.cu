@@ -2,14 +2,16 @@
 // log-probability of a given token, the entropy, and the logarithm of what is outside of
 // the list.
 //
-// One pass over memory: a cluster of CTAs holds the row in shared memory and passes over
-// it twice there.  First each thread's largest logit: a warp's r-th largest of those, and
-// the least of the warps' ones, is a bound that at least the K largest logits of the part
-// reach, and of tens of thousands hardly more than two or three times as many.  They are
-// collected, ranked by counting (value, then index: all different, so that the order does
-// not depend on the threads'), and the K first leave the row for the list.  Then the sums
-// of exponentials of the others, from which `rest` comes without cancellation.  The row's
-// first CTA merges the parts' lists.
+// One pass over memory.  A CTA of each row (or of each part of a row, joined by a cluster)
+// looks at its first rounds of vectors for a bound that a little more than the K largest
+// logits reach, most likely: each lane's largest, a warp's r-th largest of those, and of the
+// warps' the one that lies right.  Then it passes over all: numbers that reach the bound are
+// collected as candidates, the others go into the sums of exponentials, so that `rest` comes
+// without cancellation.  Fewer than K candidates ask for another pass with a lower bound
+// (the warps' least; one row in a hundred or less), too many (logits that are equal by the
+// hundred) for a search of the bound by halving.  The candidates are ordered by value, then
+// index (all different, so that nothing depends on the order in which they came), and those
+// behind the list join the sums.  A row's first CTA merges its parts' lists.
 #include <cmath>
 
 #include "edp_rows.cuh"
@@ -17,9 +19,13 @@
 namespace edp {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 256;
+constexpr int kCtas = 4;    // per SM, which bounds the registers
+constexpr int kStages = 2;  // rounds in shared memory or on their way there
 constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMostParts = 8;
+constexpr uint32_t kNoted = 160;  // vectors of a warp that wait to be looked at
+constexpr uint32_t kRoom = 1056;  // for candidates: all numbers of a part of 4 warps' vectors
 
 using Key = unsigned long long;  // order of the logit, then 2^32 - 1 - column; 0: none
 
@@ -48,49 +54,177 @@ __device__ __forceinline__ void send_key(Key *to, Key v, unsigned long long *bar
       : "memory");
 }
 
-// A part of a row in shared memory, by one CTA's threads: vectors i, i + threads, ... and
-// the first of them one number each of those before and behind the vectors.
+// A vector of logits at -infinity.
 template <typename T>
-struct Held {
-  const T *at;
+__device__ __forceinline__ uint4 no_logits() {
+  const uint32_t x = std::is_same<T, float>::value           ? 0xff800000u
+                     : std::is_same<T, __nv_bfloat16>::value ? 0xff80ff80u
+                                                             : 0xfc00fc00u;
+  return make_uint4(x, x, x, x);
+}
+__device__ __forceinline__ RowSum row_sum(const LaneSum &a) {
+  return {a.m, a.s.x() + a.s.y(), a.u.x() + a.u.y()};
+}
+
+// 16 bytes to shared memory, beside the thread; groups of such copies, and waiting for all
+// but the last N groups.
+__device__ __forceinline__ void async_load(uint4 *to, const uint4 *from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from)
+               : "memory");
+}
+__device__ __forceinline__ void async_mark() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// A part of a row as its CTA's threads pass over it: the vectors in segments of a warp's 32,
+// kUnroll segments per warp and round, and the numbers before and behind the vectors by the
+// first threads.  Round g takes segments g, g + rounds, g + 2 rounds, ..., so that the
+// first round's are spread evenly over the part.
+template <typename T>
+struct Part {
+  const T *p;
+  uint32_t first;  // its first column
   Span<T> sp;
+  uint32_t rounds;
+  __device__ __forceinline__ Part(const T *p_, uint32_t first_, uint32_t n)
+      : p(p_), first(first_), sp(p_, n) {
+    rounds = max(1u, (sp.vecs + 32 * kWarps * kUnroll - 1) / (32 * kWarps * kUnroll));
+  }
+  __device__ __forceinline__ uint32_t vec_at(uint32_t g, int k) const {
+    return ((k * kWarps + (threadIdx.x >> 5)) * rounds + g) * 32 + (threadIdx.x & 31);
+  }
+  __device__ __forceinline__ uint32_t column(uint32_t vec) const {
+    return first + sp.head + vec * Vec16<T>::kN;
+  }
+  __device__ __forceinline__ uint4 vec(uint32_t i) const {
+    return reinterpret_cast<const uint4 *>(p + sp.head)[i];
+  }
+  // Round g of this thread's vectors to its own places, and from there.
+  __device__ __forceinline__ void fetch(uint4 *ring, uint32_t g) const {
+    if (g < rounds) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const uint32_t i = vec_at(g, k);
+        if (i < sp.vecs)
+          async_load(ring + (g % kStages * kUnroll + k) * kThreads + threadIdx.x,
+                     reinterpret_cast<const uint4 *>(p + sp.head) + i);
+      }
+    }
+    async_mark();
+  }
+  __device__ __forceinline__ void start(uint4 *ring) const {
+#pragma unroll
+    for (int g = 0; g < kStages; ++g) fetch(ring, g);
+  }
+  __device__ __forceinline__ void load(uint4 (&w)[kUnroll], const uint4 *ring, uint32_t g) const {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k)
+      w[k] = vec_at(g, k) < sp.vecs ? ring[(g % kStages * kUnroll + k) * kThreads + threadIdx.x]
+                                    : no_logits<T>();
+  }
   __device__ __forceinline__ bool single() const { return threadIdx.x < sp.head + sp.tail; }
   __device__ __forceinline__ uint32_t single_at() const {
     return threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * Vec16<T>::kN;
   }
-  __device__ __forceinline__ const uint4 *vecs() const {
-    return reinterpret_cast<const uint4 *>(at + sp.head);
-  }
-  // f(number, place) of this thread's numbers that are `least` or more
+  // f(number, column) of this thread's numbers
   template <typename F>
-  __device__ __forceinline__ void each(float least, F f) const {
-    if (single()) {
-      const float v = to_f32(at[single_at()]);
-      if (v >= least) f(v, single_at());
-    }
+  __device__ __forceinline__ void each(F f) const {
+    if (single()) f(to_f32(p[single_at()]), first + single_at());
     for (uint32_t i = threadIdx.x; i < sp.vecs; i += kThreads) {
-      const uint4 w = vecs()[i];
-      if (!(Vec16<T>::max(w) >= least)) continue;
+      const uint4 w = vec(i);
 #pragma unroll
-      for (int k = 0; k < Vec16<T>::kN; ++k) {
-        const float v = to_f32(reinterpret_cast<const T *>(&w)[k]);
-        if (v >= least) f(v, sp.head + i * Vec16<T>::kN + k);
-      }
+      for (int k = 0; k < Vec16<T>::kN; ++k)
+        f(to_f32(reinterpret_cast<const T *>(&w)[k]), column(i) + k);
     }
-  }
-  __device__ __forceinline__ float largest() const {
-    float m = single() ? to_f32(at[single_at()]) : kNegInf;
-    uint32_t i = threadIdx.x;
-    for (; i + 3 * kThreads < sp.vecs; i += 4 * kThreads) {
-      float x[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = Vec16<T>::max(vecs()[i + k * kThreads]);
-      m = fmaxf(m, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-    }
-    for (; i < sp.vecs; i += kThreads) m = fmaxf(m, Vec16<T>::max(vecs()[i]));
-    return m;
   }
 };
+
+// Which numbers are candidates: those above `least`, and of those equal to it the ones in
+// columns before `end`.
+struct Bound {
+  float least;
+  uint32_t end;
+  __device__ __forceinline__ bool holds(float v, uint32_t column) const {
+    return v > least || (v == least && column < end);
+  }
+};
+struct Candidates {
+  Key *list;
+  uint32_t *count;
+  __device__ __forceinline__ void add(float v, uint32_t column) const {
+    const uint32_t at = atomicAdd(count, 1u);
+    if (at < kRoom) list[at] = key_of(v, column);
+  }
+};
+
+// One pass, which was started: candidates go to the list, the sums are of all others.
+// A vector that has a candidate is taken out whole and noted; each lane looks at one of the
+// noted ones at the end (or when there is no room for another round's), which costs a round
+// without any a vote and one with some a few instructions for each of its vectors.
+template <typename T, bool ENT, bool FUSED>
+__device__ __forceinline__ LaneSum take_part(const Part<T> &x, uint4 *ring, Bound b,
+                                             const Candidates &to, uint32_t *noted, float c) {
+  LaneSum a{kNegInf, F2(0.f), F2(0.f)};
+  if (x.single()) {
+    const uint32_t at = x.single_at();
+    const float v = to_f32(x.p[at]);
+    if (b.holds(v, x.first + at)) {
+      to.add(v, x.first + at);
+    } else {
+      const float y = raise<T, ENT, FUSED>(a, v, c).of(v), e = ex2(y);
+      a.s = a.s + F2(e, 0.f);
+      if (ENT) a.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), a.u);
+    }
+  }
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t n = 0;
+  for (uint32_t g = 0; g < x.rounds; ++g) {
+    async_wait<kStages - 1>();
+    uint4 w[kUnroll];
+    x.load(w, ring, g);
+    float m[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) m[k] = Vec16<T>::max(w[k]);
+    float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+    if (__any_sync(kAllLanes, most >= b.least)) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const bool hit = m[k] >= b.least;
+        const uint32_t all = __ballot_sync(kAllLanes, hit);
+        if (hit) {
+          noted[n + __popc(all & ((1u << lane) - 1u))] = x.vec_at(g, k);
+          w[k] = no_logits<T>();
+          m[k] = kNegInf;
+        }
+        n += __popc(all);
+      }
+      most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+    }
+    add_vectors<T, ENT, FUSED>(a, w, most, c);
+    x.fetch(ring, g + kStages);
+    if (n > (g + 1 < x.rounds ? kNoted - 32 * kUnroll : 0)) {
+      __syncwarp();
+#pragma unroll 1
+      for (uint32_t i = lane; i < n; i += 32) {
+        uint4 v[1] = {x.vec(noted[i])};
+        const uint32_t column = x.column(noted[i]);
+        T *z = reinterpret_cast<T *>(&v[0]);
+#pragma unroll
+        for (int e = 0; e < Vec16<T>::kN; ++e)
+          if (b.holds(to_f32(z[e]), column + e)) {
+            to.add(to_f32(z[e]), column + e);
+            z[e] = from_f32<T>(kNegInf);
+          }
+        take_vectors<T, ENT, FUSED>(a, v, c);
+      }
+      n = 0;
+      __syncwarp();
+    }
+  }
+  return a;
+}
 
 // The count over the CTA's threads, in all of them.  red: kWarps numbers, free before.
 __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
@@ -103,22 +237,22 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
   return n;
 }
 
-// The candidates of a part more of whose numbers reach the bound `lo` than the list has
-// room for: halving between lo and the largest until a bound leaves K to `cap` of them, or
-// until the K-th largest number is known; of those equal to it the first in the row come
-// in, up to a column found by halving again.  Rare (numbers that are equal by the
-// hundred, as masked ones are), so it only has to end: 64 passes at the most.
+// A bound that K to kRoom numbers hold, by halving from `lo` on (which K or more reach,
+// unless it is the lowest): or, where numbers are equal by the hundred, exactly K.  Rare, so
+// that it only has to end: 64 counts at the most.
 template <typename T>
-__device__ __forceinline__ void collect_slowly(const Held<T> &h, uint32_t n, uint32_t first,
-                                               uint32_t lo, uint32_t K, uint32_t cap, Key *list,
-                                               uint32_t *count, uint32_t *red) {
+__device__ __forceinline__ Bound search_bound(const T *p, uint32_t first, uint32_t n, uint32_t lo,
+                                           uint32_t K, uint32_t *red) {
+  const Part<T> x(p, first, n);
   auto reach = [&](uint32_t bound) {
     uint32_t c = 0;
-    h.each(of_order(bound), [&](float, uint32_t) { ++c; });
+    x.each([&](float v, uint32_t) { c += v >= of_order(bound); });
     return cta_count(c, red);
   };
-  uint32_t hi = 0xff800001u, some = cap + 1;  // nothing is above +infinity
-  while (hi - lo > 1 && some > cap) {
+  uint32_t hi = 0xff800001u, some = kRoom + 1;  // nothing is above +infinity
+  if (lo == kLeastOrder) some = reach(lo);
+  if (some < K) return {of_order(lo), 0xffffffffu};
+  while (hi - lo > 1 && some > kRoom) {
     const uint32_t mid = lo + (hi - lo) / 2, c = reach(mid);
     if (c >= K) {
       lo = mid;
@@ -127,33 +261,72 @@ __device__ __forceinline__ void collect_slowly(const Held<T> &h, uint32_t n, uin
       hi = mid;
     }
   }
-  uint32_t end = n;  // numbers equal to lo count before this place
-  if (some > cap) {
-    const uint32_t above = reach(hi);
-    uint32_t a = 0;  // fewer than K - above of them before a, as many before end
-    while (end - a > 1) {
-      const uint32_t mid = a + (end - a) / 2;
-      uint32_t c = 0;
-      h.each(of_order(lo), [&](float v, uint32_t i) { c += order_of(v + 0.f) == lo && i < mid; });
-      if (cta_count(c, red) + above >= K) end = mid;
-      else a = mid;
-    }
+  const float least = of_order(lo);
+  if (some <= kRoom) return {least, 0xffffffffu};
+  // of the numbers equal to it those before a column: fewer than needed before a, as many
+  // before b
+  const uint32_t above = reach(hi);
+  uint32_t a = first, b = first + n;
+  while (b - a > 1) {
+    const uint32_t mid = a + (b - a) / 2;
+    uint32_t c = 0;
+    x.each([&](float v, uint32_t column) { c += v == least && column < mid; });
+    if (cta_count(c, red) + above >= K) b = mid;
+    else a = mid;
   }
-  if (threadIdx.x == 0) *count = 0;
-  __syncthreads();
-  h.each(of_order(lo), [&](float v, uint32_t i) {
-    if (i < end || order_of(v + 0.f) > lo) {
-      const uint32_t at = atomicAdd(count, 1u);
-      if (at < cap) list[at] = key_of(v, first + i);
+  return {least, b};
+}
+
+// The r-th largest (MAX) or smallest of a warp's numbers, r <= 32; ties by lane.
+template <bool MAX>
+__device__ __forceinline__ uint32_t warp_nth(uint32_t x, uint32_t r) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t best = 0;
+  for (uint32_t k = 0; k < r; ++k) {
+    best = MAX ? __reduce_max_sync(kAllLanes, x) : __reduce_min_sync(kAllLanes, x);
+    if (lane == __ffs(__ballot_sync(kAllLanes, x == best)) - 1) x = MAX ? 0u : 0xffffffffu;
+  }
+  return best;
+}
+
+// A warp's keys, the largest first.
+__device__ __forceinline__ Key warp_sorted(Key x) {
+  const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+  for (uint32_t size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (uint32_t by = size / 2; by; by /= 2) {
+      const Key y = __shfl_xor_sync(kAllLanes, x, by);
+      const bool large = ((lane & by) == 0) == ((lane & size) == 0 || size == 32);
+      x = large == (y > x) ? y : x;
     }
-  });
-  __syncthreads();
+  return x;
+}
+// How many keys of `runs` descending runs of `each` (at most 2^k = most) are larger, four
+// runs at a time side by side.
+__device__ __forceinline__ uint32_t larger_in_runs(const Key *keys, uint32_t each, uint32_t runs,
+                                                   uint32_t most, Key key) {
+  uint32_t sum = 0;
+  for (uint32_t q = 0; q < runs; q += 4) {
+    uint32_t at[4] = {0, 0, 0, 0};
+    for (uint32_t step = most; step; step >>= 1) {
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint32_t to = min(at[j] + step, each);
+        const Key x = keys[min(q + j, runs - 1) * each + to - 1];
+        at[j] = x > key ? to : at[j];
+      }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) sum += q + j < runs ? at[j] : 0;
+  }
+  return sum;
 }
 
 struct TopOut {
   int32_t *ids;
   float *top_logp, *logp, *entropy, *rest, *stats;
-  uint32_t top, cap;  // cap: room for candidates
+  uint32_t top;
 };
 
 __device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
@@ -168,32 +341,33 @@ __device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
   if (o.stats) o.stats[2 * t] = o.stats[2 * t + 1] = 0.f;
 }
 
-// A cluster of gridDim.y CTAs per row, each with its part in shared memory.
+// A cluster of gridDim.y CTAs per row, each a part of it.
 template <typename T, bool ENT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kCtas)
 k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 shared_words[];
-  __shared__ RowSum red[kWarps];
-  __shared__ uint32_t bound[kWarps];
+  __shared__ RowSum red[kWarps], left[kWarps];
+  __shared__ uint32_t bound[kWarps], counts[kWarps], noted[kWarps][kNoted];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S, U
   __shared__ uint32_t count;
-  __shared__ bool careful;
-  __shared__ unsigned long long bar, sent;
+  __shared__ unsigned long long sent;
   const uint64_t t = blockIdx.x;
   const uint32_t part = blockIdx.y, np = gridDim.y, K = o.top;
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  Key *list = reinterpret_cast<Key *>(shared_words);  // [cap], of even length
-  Key *inbox = list + o.cap;                          // [np][K]; the lists of the parts
-  uint4 *room = shared_words + (o.cap + np * K + 1) / 2;
+  Key *list = reinterpret_cast<Key *>(shared_words);  // [kRoom], as they come
+  Key *inbox = list + kRoom;                          // [np][K], the lists of the parts
+  uint4 *ring = shared_words + (kRoom + (np > 1 ? np * K : 0) + 1) / 2;
+  Key *sorted = reinterpret_cast<Key *>(ring);        // [kRoom], in order, after the passes
+  static_assert(kRoom * sizeof(Key) <= sizeof(uint4) * kStages * kUnroll * kThreads, "in the ring");
   if (threadIdx.x == 0) {
-    mbar_init(&bar, 1);
-    mbar_init(&sent, 1);
-    if (np > 1 && part == 0) mbar_arrive_tx(&sent, np * (K * sizeof(Key) + sizeof(float4)));
-    mbar_init_fence();
+    if (np > 1) {
+      mbar_init(&sent, 1);
+      if (part == 0) mbar_arrive_tx(&sent, np * (K * sizeof(Key) + sizeof(float4)));
+      mbar_init_fence();
+    }
     count = 0;
   }
-  __syncthreads();
   pdl_wait();
   pdl_launch();
   const int32_t target = a.target ? a.target[t] : 0;
@@ -208,85 +382,125 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   }
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
-  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride, *p = row + first;
-  // the part keeps its place within 16 bytes
-  T *held = reinterpret_cast<T *>(room) + ((uintptr_t)p & 15u) / sizeof(T);
-  const Held<T> h{held, Span<T>(p, n)};
-  if (threadIdx.x == 0 && h.sp.vecs) {
-    mbar_arrive_tx(&bar, h.sp.vecs * 16);
-    bulk_load(held + h.sp.head, p + h.sp.head, h.sp.vecs * 16, &bar, policy_normal());
-  }
-  if (h.single()) held[h.single_at()] = p[h.single_at()];
-  if (np > 1) cluster_started();
+  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+  const Part<T> x(row + first, first, n);
+  x.start(ring);
   const float zt = a.target && part == 0 ? to_f32(row[target]) : 0.f;
-  if (h.sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
-    if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
-    mbar_wait(&bar, 0, kRowWaitNs);  // bounded: the copy lands before the CTA ends
-  }
-  // A bound that at least K numbers reach: from warps all of whose lanes have a vector.
-  const uint32_t full = min((uint32_t)kWarps, h.sp.vecs / 32);
-  const uint32_t need = full ? (K + full - 1) / full : 33;
-  const float mine = h.largest();
-  if (need <= 32) {
-    uint32_t left = order_of(mine + 0.f), best = 0;
-    for (uint32_t k = 0; k < need; ++k) {
-      best = __reduce_max_sync(kAllLanes, left);
-      if (lane == __ffs(__ballot_sync(kAllLanes, left == best)) - 1) left = 0;
+  // The first rounds' numbers, each lane's largest: a bound that K of the part reach (where
+  // they are all, the least of the warps' r-th largest; else one that 2.5 K most likely do).
+  const uint32_t sample = min(x.rounds, (uint32_t)kStages);
+  const uint32_t full = x.rounds > 1 ? kWarps : min((uint32_t)kWarps, x.sp.vecs / 32);
+  uint32_t r = 33, nth = 1;
+  if (full) {
+    if (x.rounds == sample) {
+      r = (K + full - 1) / full;
+    } else {
+      const float per_warp = 2.5f * (float)(K * sample) / (float)(x.rounds * kWarps);
+      r = max(1u, (uint32_t)(per_warp + 0.5f));
+      nth = r > 1 ? kWarps * 2 / 5 : max(1u, (uint32_t)(kWarps * __expf(-per_warp)));
     }
+  }
+  uint32_t lo = kLeastOrder, lower = kLeastOrder;
+  if (r <= 32) {
+    float m = kNegInf;
+    async_wait<0>();
+    for (uint32_t g = 0; g < sample; ++g) {
+      uint4 w[kUnroll];
+      x.load(w, ring, g);
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
+    }
+    const uint32_t best = warp_nth<true>(order_of(m + 0.f), r);
     if (lane == 0) bound[wid] = best;
+  }
+  if (np > 1) cluster_started();
+  __syncthreads();
+  if (r <= 32) {
+    const uint32_t each = lane < full ? bound[lane] : 0xffffffffu;
+    lower = max(lo, __reduce_min_sync(kAllLanes, each));
+    lo = nth > 1 ? max(lo, warp_nth<false>(each, nth)) : lower;
+  }
+  const Candidates to{list, &count};
+  Bound b{of_order(lo), 0xffffffffu};
+  uint32_t found;
+  RowSum sum;
+  for (bool again = false, searched = false;;) {
+    if (again) {
+      if (threadIdx.x == 0) count = 0;
+      x.start(ring);
+      __syncthreads();
+    }
+    again = true;
+    sum = warp_sum<T, F>(row_sum(take_part<T, ENT, F>(x, ring, b, to, noted[wid], a.c)), a.c);
+    if (lane == 0) red[wid] = sum;
+    __syncthreads();
+    found = count;
+    if (searched || (found <= kRoom && (found >= K || lo == kLeastOrder))) break;
+    __syncthreads();
+    if (found <= kRoom && lo != lower) {
+      lo = lower;
+      b.least = of_order(lo);
+    } else {
+      b = search_bound<T>(row + first, first, n, found > kRoom ? lo : kLeastOrder, K, counts);
+      searched = true;
+    }
+  }
+  sum = exact_sums<T>(
+      warp_sum<T, F, lanes_for(kWarps)>(lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f},
+                                        a.c), a.c);
+  sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
+         __shfl_sync(kAllLanes, sum.u, 0)};
+  if (F && !sums_hold(sum.m, a.c)) {  // rare: again, the careful way
+    __syncthreads();
+    if (threadIdx.x == 0) count = 0;
+    x.start(ring);
+    __syncthreads();
+    sum = warp_sum<T, false>(row_sum(take_part<T, ENT, false>(x, ring, b, to, noted[wid], a.c)), a.c);
+    if (lane == 0) red[wid] = sum;
+    __syncthreads();
+    sum = warp_sum<T, false, lanes_for(kWarps)>(
+        lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+  }
+  found = min(found, kRoom);  // (in bounds even if someone writes the row meanwhile)
+  // In order: runs of 32 sorted by a warp each, then a key's place is its place in its own
+  // run and the number of larger keys in each of the others.
+  const uint32_t runs = (found + 31) / 32;
+  for (uint32_t q = wid; q < runs; q += kWarps) {
+    const uint32_t i = 32 * q + lane;
+    const Key key = warp_sorted(i < found ? list[i] : 0);
+    list[i] = key;
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < found; i += kThreads) {
+    const Key key = list[i];
+    sorted[larger_in_runs(list, 32, runs, 32, key)] = key;
   }
   if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
   __syncthreads();
-  uint32_t lo = kLeastOrder;
-  if (need <= 32)
-    lo = max(lo, __reduce_min_sync(kAllLanes, lane < full ? bound[lane] : 0xffffffffu));
-  const float least = of_order(lo);
-  if (mine >= least)
-    h.each(least, [&](float v, uint32_t i) {
-      const uint32_t at = atomicAdd(&count, 1u);
-      if (at < o.cap) list[at] = key_of(v, first + i);
-    });
-  __syncthreads();
-  if (count > o.cap) collect_slowly<T>(h, n, first, lo, K, o.cap, list, &count, bound);
-  const uint32_t found = count;
-  // Ranked by counting; the first K leave the row.
-  for (uint32_t i = threadIdx.x; i < max(found, K); i += kThreads) {
-    if (i >= found) {
-      if (i < K) {
-        if (np > 1) send_key(inbox + part * K + i, 0, &sent, 0);
-        else inbox[i] = 0;
-      }
-      continue;
-    }
-    const Key key = list[i];
-    uint32_t r = 0;
-    for (uint32_t j = 0; j + 2 <= found; j += 2) {
-      const ulonglong2 two = *reinterpret_cast<const ulonglong2 *>(list + j);
-      r += (two.x > key) + (two.y > key);
-    }
-    if (found & 1) r += list[found - 1] > key;
-    if (r < K) {
-      if (np > 1) send_key(inbox + part * K + r, key, &sent, 0);
-      else inbox[r] = key;
-      held[column_of(key) - first] = from_f32<T>(kNegInf);
-    }
+  for (uint32_t i = threadIdx.x; i < K; i += kThreads) {
+    if (np > 1) send_key(inbox + part * K + i, i < found ? sorted[i] : 0, &sent, 0);
+    else if (i >= found) sorted[i] = 0;
   }
-  __syncthreads();
-  RowSum sum = warp_sum<T, F>(part_sum<T, ENT, F, kThreads>(held, n, a.c), a.c);
-  if (lane == 0) red[wid] = sum;
+  // Candidates behind the list join the others.
+  LaneSum drop{kNegInf, F2(0.f), F2(0.f)};
+  auto drop_key = [&](Key key) {
+    const float z = value_of(key), y = raise<T, ENT, false>(drop, z, a.c).of(z), e = ex2(y);
+    drop.s = drop.s + F2(e, 0.f);
+    if (ENT) drop.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), drop.u);
+  };
+  for (uint32_t i = K + threadIdx.x; i < found; i += kThreads) drop_key(sorted[i]);
+  {
+    const RowSum mine = warp_sum<T, false>(row_sum(drop), a.c);
+    if (lane == 0) left[wid] = mine;
+  }
   __syncthreads();
   if (wid == 0) {
-    sum = exact_sums<T>(warp_sum<T, F, lanes_for(kWarps)>(lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f},
-                                           a.c), a.c);
-    if (lane == 0) careful = F && !sums_hold(sum.m, a.c);
-  }
-  __syncthreads();
-  if (careful) {  // rare: again, the careful way
-    sum = warp_sum<T, false>(part_sum<T, ENT, false, kThreads>(held, n, a.c), a.c);
-    if (lane == 0) red[wid] = sum;
-    __syncthreads();
-    if (wid == 0)
-      sum = warp_sum<T, false, lanes_for(kWarps)>(lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+    static_assert(kWarps <= 16, "and the sums of the others in lane 16");
+    sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
+           __shfl_sync(kAllLanes, sum.u, 0)};
+    sum = warp_sum<T, false>(lane < kWarps ? left[lane]
+                             : lane == 16  ? sum
+                                           : RowSum{kNegInf, 0.f, 0.f}, a.c);
   }
   if (np > 1) {
     if (threadIdx.x == 0)
@@ -301,49 +515,36 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       write_none(o, t);
       return;
     }
-    // What of the parts' lists is not of the row's joins the others.
-    LaneSum drop{kNegInf, F2(0.f), F2(0.f)};
+    // A key's place in the row's list: how many are larger in each of the parts' lists.
+    drop = {kNegInf, F2(0.f), F2(0.f)};
+    uint32_t have = 0;  // keys in all lists: the row's list may be shorter than K
     for (uint32_t i = threadIdx.x; i < np * K; i += kThreads) {
       const Key key = inbox[i];
-      const uint32_t own = i / K;
-      uint32_t r = i - own * K;
-      if (!key) {
-        continue;
-      }
-      for (uint32_t q = 0; q < np; ++q) {
-        if (q == own) continue;
-        uint32_t b = 0, e = K;  // list q: keys before b are larger, those from e on are not
-        while (b < e) {
-          const uint32_t mid = (b + e) / 2;
-          if (inbox[q * K + mid] > key) b = mid + 1;
-          else e = mid;
-        }
-        r += b;
-      }
-      if (r < K) {
-        list[r] = key;
-      } else {
-        const float z = value_of(key), y = raise<T, ENT, false>(drop, z, a.c).of(z), e = ex2(y);
-        drop.s = drop.s + F2(e, 0.f);
-        if (ENT) drop.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), drop.u);
-      }
+      if (!key) continue;
+      ++have;
+      const uint32_t rank = larger_in_runs(inbox, K, np, 128, key);
+      if (rank < K) list[rank] = key;
     }
-    uint32_t have = 0;  // keys in all lists: the row's list may be shorter than K
-    for (uint32_t i = threadIdx.x; i < np * K; i += kThreads) have += inbox[i] != 0;
-    have = cta_count(have, bound);
+    have = cta_count(have, counts);
     for (uint32_t i = have + threadIdx.x; i < K; i += kThreads) list[i] = 0;
-    const RowSum dropped = cta_join<T, false, kThreads>(
-        RowSum{drop.m, drop.s.x() + drop.s.y(), drop.u.x() + drop.u.y()}, a.c, red);
+    __syncthreads();
+    // What of the parts' lists is not of the row's joins the others, too.
+    const Key last = list[K - 1];
+    for (uint32_t i = threadIdx.x; i < np * K; i += kThreads) {
+      const Key key = inbox[i];
+      if (key && key < last) drop_key(key);
+    }
+    const RowSum mine = warp_sum<T, false>(row_sum(drop), a.c);
+    if (lane == 0) left[wid] = mine;
+    __syncthreads();
     if (wid) return;
-    const float4 x = lane < np ? sums[lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
-    const RowSum d0{__shfl_sync(kAllLanes, dropped.m, 0), __shfl_sync(kAllLanes, dropped.s, 0),
-                    __shfl_sync(kAllLanes, dropped.u, 0)};
-    sum = warp_sum<T, false, 16>(lane == kMostParts ? d0 : RowSum{x.x, x.y, x.z}, a.c);
+    const float4 y = lane - 16 < np ? sums[lane - 16] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+    sum = warp_sum<T, false>(lane < kWarps ? left[lane] : RowSum{y.x, y.y, y.z}, a.c);
   }
   if (wid) return;
   sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
          __shfl_sync(kAllLanes, sum.u, 0)};
-  const Key *top = np > 1 ? list : inbox;
+  const Key *top = np > 1 ? list : sorted;
   const bool any = top[0] != 0;
   const float M = any ? value_of(top[0]) : kNegInf;
   float S = 0.f, U = 0.f;
@@ -401,18 +602,17 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
 cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_t *ids,
                              float *top_logp, float *logp, float *entropy, float *rest,
                              float *stats, cudaStream_t s) {
-  const TopOut o{ids, top_logp, logp, entropy, rest, stats, top, top <= 64 ? 256u : 512u};
+  const TopOut o{ids, top_logp, logp, entropy, rest, stats, top};
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    uint32_t parts = row_parts(ctx, z, 2);
-    while (parts < kMostParts && part_bytes(z, parts) > kResidentPart) parts *= 2;
+    const uint32_t parts = row_parts(ctx, z, 2);
     auto kern = entropy ? k_token_top<T, true> : k_token_top<T, false>;
-    const size_t lists = ((o.cap + parts * top + 1) / 2) * 16;
+    const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
+    const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + kStages * kUnroll * kThreads);
     const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kResidentMost + 16 * 1024));
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
     if (e != cudaSuccess) return e;
-    return launch_rows(kern, z.rows, parts, true, kThreads, lists + part_bytes(z, parts), s,
-                       row_args(z), o, ctx->ctrl);
+    return launch_rows(kern, z.rows, parts, true, kThreads, bytes, s, row_args(z), o, ctx->ctrl);
   });
 }
 
