@@ -182,27 +182,27 @@ __device__ __forceinline__ RowLog<T, FUSED> raise(LaneSum &a, float m, float c) 
   }
   return RowLog<T, FUSED>(a.m, c);
 }
-// K vectors of one thread, whose largest number is m.
-template <typename T, bool ENT, bool FUSED, int K>
-__device__ __forceinline__ void add_vectors(LaneSum &a, const uint4 (&w)[K], float m, float c) {
-  const RowLog<T, FUSED> log = raise<T, ENT, FUSED>(a, m, c);
+// The sums of a vector's numbers relative to `log`.
+template <typename T, bool ENT, bool FUSED>
+__device__ __forceinline__ void add_vector(F2 &s, F2 &u, const uint4 &w,
+                                           const RowLog<T, FUSED> &log) {
+  const uint4 x = ENT ? finite_words<T, FUSED>(w) : w;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const uint4 x = ENT ? finite_words<T, FUSED>(w[k]) : w[k];
-#pragma unroll
-    for (int i = 0; i < Vec16<T>::kPairs; ++i) {
-      const F2 y = log.of(Vec16<T>::pair(x, i)), e = ex2_both(y);
-      a.s = a.s + e;
-      if (ENT) a.u = fma2(e, finite_log<T, FUSED>(y), a.u);
-    }
+  for (int i = 0; i < Vec16<T>::kPairs; ++i) {
+    const F2 y = log.of(Vec16<T>::pair(x, i)), e = ex2_both(y);
+    s = s + e;
+    if (ENT) u = fma2(e, finite_log<T, FUSED>(y), u);
   }
 }
+// K vectors of one thread.
 template <typename T, bool ENT, bool FUSED, int K>
 __device__ __forceinline__ void take_vectors(LaneSum &a, const uint4 (&w)[K], float c) {
   float m = Vec16<T>::max(w[0]);
 #pragma unroll
   for (int k = 1; k < K; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
-  add_vectors<T, ENT, FUSED>(a, w, m, c);
+  const RowLog<T, FUSED> log = raise<T, ENT, FUSED>(a, m, c);
+#pragma unroll
+  for (int k = 0; k < K; ++k) add_vector<T, ENT, FUSED>(a.s, a.u, w[k], log);
 }
 
 // Elements [0, n) at p as those before the first 16-byte boundary, vectors, rest.

@@ -24,7 +24,8 @@ constexpr int kCtas = 4;    // per SM, which bounds the registers
 constexpr int kStages = 2;  // rounds in shared memory or on their way there
 constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMostParts = 8;
-constexpr uint32_t kNoted = 160;  // vectors of a warp that wait to be looked at
+constexpr uint32_t kNoted = 8;    // vectors of a thread that wait to be looked at
+constexpr float kLeastSum = 0x1p-64f;
 constexpr uint32_t kRoom = 1056;  // for candidates: all numbers of a part of 4 warps' vectors
 
 using Key = unsigned long long;  // order of the logit, then 2^32 - 1 - column; 0: none
@@ -88,12 +89,20 @@ struct Part {
   uint32_t first;  // its first column
   Span<T> sp;
   uint32_t rounds;
+  // this thread's first vector; from one of its segments of a round to the next; the rounds
+  // that have all of them
+  const uint4 *mine;
+  uint32_t apart, whole;
   __device__ __forceinline__ Part(const T *p_, uint32_t first_, uint32_t n)
       : p(p_), first(first_), sp(p_, n) {
     rounds = max(1u, (sp.vecs + 32 * kWarps * kUnroll - 1) / (32 * kWarps * kUnroll));
+    apart = 32 * kWarps * rounds;
+    const uint32_t at = vec_at(0, 0, threadIdx.x & 31), last = at + (kUnroll - 1) * apart;
+    mine = reinterpret_cast<const uint4 *>(p + sp.head) + at;
+    whole = last < sp.vecs ? min(rounds, (sp.vecs - last + 31) / 32) : 0;
   }
-  __device__ __forceinline__ uint32_t vec_at(uint32_t g, int k) const {
-    return ((k * kWarps + (threadIdx.x >> 5)) * rounds + g) * 32 + (threadIdx.x & 31);
+  __device__ __forceinline__ uint32_t vec_at(uint32_t g, uint32_t k, uint32_t lane) const {
+    return ((k * kWarps + (threadIdx.x >> 5)) * rounds + g) * 32 + lane;
   }
   __device__ __forceinline__ uint32_t column(uint32_t vec) const {
     return first + sp.head + vec * Vec16<T>::kN;
@@ -101,15 +110,18 @@ struct Part {
   __device__ __forceinline__ uint4 vec(uint32_t i) const {
     return reinterpret_cast<const uint4 *>(p + sp.head)[i];
   }
-  // Round g of this thread's vectors to its own places, and from there.
+  // Round g of this thread's vectors to its own places, -infinity where there are none.
   __device__ __forceinline__ void fetch(uint4 *ring, uint32_t g) const {
-    if (g < rounds) {
+    uint4 *to = ring + g % kStages * (kUnroll * kThreads) + threadIdx.x;
+    const uint4 *from = mine + 32 * g;
+    if (g < whole) {
 #pragma unroll
+      for (int k = 0; k < kUnroll; ++k) async_load(to + k * kThreads, from + k * apart);
+    } else if (g < rounds) {
+#pragma unroll 1
       for (int k = 0; k < kUnroll; ++k) {
-        const uint32_t i = vec_at(g, k);
-        if (i < sp.vecs)
-          async_load(ring + (g % kStages * kUnroll + k) * kThreads + threadIdx.x,
-                     reinterpret_cast<const uint4 *>(p + sp.head) + i);
+        if (vec_at(g, k, threadIdx.x & 31) < sp.vecs) async_load(to + k * kThreads, from + k * apart);
+        else to[k * kThreads] = no_logits<T>();
       }
     }
     async_mark();
@@ -121,8 +133,7 @@ struct Part {
   __device__ __forceinline__ void load(uint4 (&w)[kUnroll], const uint4 *ring, uint32_t g) const {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k)
-      w[k] = vec_at(g, k) < sp.vecs ? ring[(g % kStages * kUnroll + k) * kThreads + threadIdx.x]
-                                    : no_logits<T>();
+      w[k] = ring[(g % kStages * kUnroll + k) * kThreads + threadIdx.x];
   }
   __device__ __forceinline__ bool single() const { return threadIdx.x < sp.head + sp.tail; }
   __device__ __forceinline__ uint32_t single_at() const {
@@ -159,24 +170,78 @@ struct Candidates {
   }
 };
 
-// One pass, which was started: candidates go to the list, the sums are of all others.
-// A vector that has a candidate is taken out whole and noted; each lane looks at one of the
-// noted ones at the end (or when there is no room for another round's), which costs a round
-// without any a vote and one with some a few instructions for each of its vectors.
+// A number's share of the sums relative to `log`.
 template <typename T, bool ENT, bool FUSED>
-__device__ __forceinline__ LaneSum take_part(const Part<T> &x, uint4 *ring, Bound b,
-                                             const Candidates &to, uint32_t *noted, float c) {
-  LaneSum a{kNegInf, F2(0.f), F2(0.f)};
+__device__ __forceinline__ void add_one(F2 &s, F2 &u, const RowLog<T, FUSED> &log, float v) {
+  const float y = log.of(v), e = ex2(y);
+  s = s + F2(e, 0.f);
+  if (ENT) u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), u);
+}
+// The sums of a vector's numbers but its candidates, which go to the list.
+template <typename T, bool ENT, bool FUSED>
+__device__ __forceinline__ void add_but(F2 &s, F2 &u, const RowLog<T, FUSED> &log, const uint4 &w,
+                                        uint32_t column, const Bound &b, const Candidates &to) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < Vec16<T>::kPairs; ++i) {
+    const F2 z = Vec16<T>::pair(w, i);
+    const bool x = b.holds(z.x(), column + 2 * i), y = b.holds(z.y(), column + 2 * i + 1);
+    bits |= (x ? 1u : 0u) << 2 * i | (y ? 2u : 0u) << 2 * i;
+    const F2 l = log.of(F2(x ? kNegInf : z.x(), y ? kNegInf : z.y())), e = ex2_both(l);
+    s = s + e;
+    if (ENT) u = fma2(e, F2(fmaxf(l.x(), kNoLog), fmaxf(l.y(), kNoLog)), u);
+  }
+  for (; bits; bits &= bits - 1) {
+    const uint32_t e = __ffs(bits) - 1, word = e * sizeof(T) / 4;
+    const uint32_t x = word < 2 ? word ? w.y : w.x : word == 2 ? w.z : w.w;
+    const uint32_t half = sizeof(T) == 2 ? x >> (e & 1) * 16 : x;
+    to.add(to_f32(*reinterpret_cast<const T *>(&half)), column + e);
+  }
+}
+
+// Calls f(note, lane) for each of the notes of a warp's lanes, n of each, in a lane per
+// note; they are in the lanes' columns of `notes`.
+template <typename F>
+__device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t upto = n;  // of this lane and those before
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const uint32_t x = __shfl_up_sync(kAllLanes, upto, o);
+    if (lane >= o) upto += x;
+  }
+  const uint32_t all = __shfl_sync(kAllLanes, upto, 31);
+  __syncwarp();
+  for (uint32_t i = lane; i < ((all + 31) & ~31u); i += 32) {
+    uint32_t owner = 0, before = 0;  // the lane of note i, and the notes before it
+#pragma unroll
+    for (int step = 16; step; step /= 2) {
+      const uint32_t x = __shfl_sync(kAllLanes, upto, owner + step - 1);
+      if (x <= i) {
+        owner += step;
+        before = x;
+      }
+    }
+    if (i < all) f(notes[32 * (i - before) + owner], owner);
+  }
+  __syncwarp();
+}
+
+// One pass, which was started: candidates go to the list, the sums are of all others, all
+// relative to `ref`, which none of them is above.  So no maximum is kept (with one, 8,192
+// rows of 152,064 bfloat16 logits took 470 us, without XXX).  A vector that has a candidate is
+// taken out whole and noted; the warp looks at those at the end, or when a lane may have no
+// room for another round's.
+template <typename T, bool ENT, bool FUSED>
+__device__ __forceinline__ RowSum take_part(const Part<T> &x, uint4 *ring, Bound b, float ref,
+                                            const Candidates &to, uint32_t *noted, float c) {
+  const RowLog<T, FUSED> log(ref, c);
+  F2 s(0.f), u(0.f);
   if (x.single()) {
     const uint32_t at = x.single_at();
     const float v = to_f32(x.p[at]);
-    if (b.holds(v, x.first + at)) {
-      to.add(v, x.first + at);
-    } else {
-      const float y = raise<T, ENT, FUSED>(a, v, c).of(v), e = ex2(y);
-      a.s = a.s + F2(e, 0.f);
-      if (ENT) a.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), a.u);
-    }
+    if (b.holds(v, x.first + at)) to.add(v, x.first + at);
+    else add_one<T, ENT, FUSED>(s, u, log, v);
   }
   const uint32_t lane = threadIdx.x & 31;
   uint32_t n = 0;
@@ -187,43 +252,41 @@ __device__ __forceinline__ LaneSum take_part(const Part<T> &x, uint4 *ring, Boun
     float m[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) m[k] = Vec16<T>::max(w[k]);
-    float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-    if (__any_sync(kAllLanes, most >= b.least)) {
+    if (fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) >= b.least) {
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const bool hit = m[k] >= b.least;
-        const uint32_t all = __ballot_sync(kAllLanes, hit);
-        if (hit) {
-          noted[n + __popc(all & ((1u << lane) - 1u))] = x.vec_at(g, k);
+      for (int k = 0; k < kUnroll; ++k)
+        if (m[k] >= b.least) {
+          noted[32 * n++ + lane] = kUnroll * g + k;
           w[k] = no_logits<T>();
-          m[k] = kNegInf;
         }
-        n += __popc(all);
-      }
-      most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
     }
-    add_vectors<T, ENT, FUSED>(a, w, most, c);
-    x.fetch(ring, g + kStages);
-    if (n > (g + 1 < x.rounds ? kNoted - 32 * kUnroll : 0)) {
-      __syncwarp();
-#pragma unroll 1
-      for (uint32_t i = lane; i < n; i += 32) {
-        uint4 v[1] = {x.vec(noted[i])};
-        const uint32_t column = x.column(noted[i]);
-        T *z = reinterpret_cast<T *>(&v[0]);
 #pragma unroll
-        for (int e = 0; e < Vec16<T>::kN; ++e)
-          if (b.holds(to_f32(z[e]), column + e)) {
-            to.add(to_f32(z[e]), column + e);
-            z[e] = from_f32<T>(kNegInf);
-          }
-        take_vectors<T, ENT, FUSED>(a, v, c);
-      }
+    for (int k = 0; k < kUnroll; ++k) add_vector<T, ENT, FUSED>(s, u, w[k], log);
+    x.fetch(ring, g + kStages);
+    if (__any_sync(kAllLanes, n > (g + 1 < x.rounds ? kNoted - kUnroll : 0))) {
+      each_note(noted, n, [&](uint32_t note, uint32_t owner) {
+        const uint32_t at = x.vec_at(note / kUnroll, note % kUnroll, owner);
+        add_but<T, ENT, FUSED>(s, u, log, x.vec(at), x.column(at), b, to);
+      });
       n = 0;
-      __syncwarp();
     }
   }
-  return a;
+  return {ref, s.x() + s.y(), u.x() + u.y()};
+}
+// The same relative to each thread's maximum, where the sums ask for that: rare.
+template <typename T, bool ENT>
+__device__ __forceinline__ RowSum take_carefully(const Part<T> &x, Bound b, const Candidates &to,
+                                                 float c) {
+  LaneSum a{kNegInf, F2(0.f), F2(0.f)};
+  auto one = [&](float v, uint32_t column) {
+    if (b.holds(v, column)) {
+      to.add(v, column);
+    } else {
+      add_one<T, ENT, false>(a.s, a.u, raise<T, ENT, false>(a, v, c), v);
+    }
+  };
+  x.each(one);
+  return row_sum(a);
 }
 
 // The count over the CTA's threads, in all of them.  red: kWarps numbers, free before.
@@ -348,7 +411,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 shared_words[];
   __shared__ RowSum red[kWarps], left[kWarps];
-  __shared__ uint32_t bound[kWarps], counts[kWarps], noted[kWarps][kNoted];
+  __shared__ uint32_t bound[kWarps], counts[kWarps], noted[kWarps][kNoted * 32];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S, U
   __shared__ uint32_t count;
   __shared__ unsigned long long sent;
@@ -424,42 +487,46 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   Bound b{of_order(lo), 0xffffffffu};
   uint32_t found;
   RowSum sum;
-  for (bool again = false, searched = false;;) {
+  for (bool again = false, searched = false, careful = false;;) {
+    // nothing but -infinity and NaN is left out by the lowest bound
+    const bool all = lo == kLeastOrder && b.end == 0xffffffffu;
+    const float ref = all ? 0.f : b.least;
+    careful |= F && !sums_hold(ref, a.c);
     if (again) {
       if (threadIdx.x == 0) count = 0;
-      x.start(ring);
+      if (!careful) x.start(ring);
       __syncthreads();
     }
     again = true;
-    sum = warp_sum<T, F>(row_sum(take_part<T, ENT, F>(x, ring, b, to, noted[wid], a.c)), a.c);
+    sum = careful ? take_carefully<T, ENT>(x, b, to, a.c)
+                  : take_part<T, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
+    sum = warp_sum<T, false>(sum, a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
     found = count;
-    if (searched || (found <= kRoom && (found >= K || lo == kLeastOrder))) break;
+    const bool enough = searched || (found <= kRoom && (found >= K || all));
+    if (enough) {
+      sum = warp_sum<T, false, lanes_for(kWarps)>(
+          lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+      if (!careful) sum = exact_sums<T>(sum, a.c);
+      sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
+             __shfl_sync(kAllLanes, sum.u, 0)};
+      if (all) sum.m = kNegInf;  // (0 or NaN)
+      // with sums as low as this the numbers lose bits or are lost: relative to their own
+      // maximum they are not
+      if (careful || all || !(sum.s < kLeastSum)) break;
+      careful = true;
+    }
     __syncthreads();
+    if (enough) continue;
     if (found <= kRoom && lo != lower) {
       lo = lower;
       b.least = of_order(lo);
     } else {
       b = search_bound<T>(row + first, first, n, found > kRoom ? lo : kLeastOrder, K, counts);
+      lo = order_of(b.least);
       searched = true;
     }
-  }
-  sum = exact_sums<T>(
-      warp_sum<T, F, lanes_for(kWarps)>(lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f},
-                                        a.c), a.c);
-  sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
-         __shfl_sync(kAllLanes, sum.u, 0)};
-  if (F && !sums_hold(sum.m, a.c)) {  // rare: again, the careful way
-    __syncthreads();
-    if (threadIdx.x == 0) count = 0;
-    x.start(ring);
-    __syncthreads();
-    sum = warp_sum<T, false>(row_sum(take_part<T, ENT, false>(x, ring, b, to, noted[wid], a.c)), a.c);
-    if (lane == 0) red[wid] = sum;
-    __syncthreads();
-    sum = warp_sum<T, false, lanes_for(kWarps)>(
-        lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
   }
   found = min(found, kRoom);  // (in bounds even if someone writes the row meanwhile)
   // In order: runs of 32 sorted by a warp each, then a key's place is its place in its own
