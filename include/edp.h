@@ -601,8 +601,7 @@ EDP_API edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint
  * reports (EDP_ERR_INVALID).  NaN or +infinity in a row makes its ids -1 and its
  * numbers NaN.
  * Errors: as edp_token_logprob, and EDP_ERR_INVALID for top outside [1, 128], NULL
- * ids or top_logp, logp without target, or a vocabulary whose row takes more than
- * 1.5 MiB (786,432 logits of 16 bits, 393,216 of 32). */
+ * ids or top_logp, or logp without target. */
 EDP_API edp_status edp_token_top(edp_ctx *ctx, const void *logits, uint32_t dtype,
                                  uint64_t rows, uint32_t vocab, uint64_t stride,
                                  const int32_t *target, const uint8_t *mask,
@@ -803,8 +802,9 @@ typedef struct {
  * then NaN); NaN or +infinity in a row or its list makes loss and gradient NaN.
  * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, top outside
  * [1, 128], a NULL logits, ids, value or loss, REVERSE or MIX without rest, rows ==
- * 0, logits, dlogits and vocab as for edp_token_top, off and n_seq as for
- * edp_policy_loss, or arrays outside device memory; EDP_ERR_OOM when the scratch
+ * 0, a vocabulary whose row takes more than 1.5 MiB (786,432 logits of 16 bits,
+ * 393,216 of 32), logits and dlogits as for edp_policy_loss_logits, off and n_seq as
+ * for edp_policy_loss, or arrays outside device memory; EDP_ERR_OOM when the scratch
  * cannot be allocated. */
 EDP_API edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg,
                                     const void *logits, uint32_t dtype, uint64_t rows,

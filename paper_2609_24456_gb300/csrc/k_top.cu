@@ -4,14 +4,15 @@
 //
 // One pass over memory.  A CTA of each row (or of each part of a row, joined by a cluster)
 // looks at its first rounds of vectors for a bound that a little more than the K largest
-// logits reach, most likely: each lane's largest, a warp's r-th largest of those, and of the
-// warps' the one that lies right.  Then it passes over all: numbers that reach the bound are
-// collected as candidates, the others go into the sums of exponentials, so that `rest` comes
-// without cancellation.  Fewer than K candidates ask for another pass with a lower bound
-// (the warps' least; one row in a hundred or less), too many (logits that are equal by the
-// hundred) for a search of the bound by halving.  The candidates are ordered by value, then
-// index (all different, so that nothing depends on the order in which they came), and those
-// behind the list join the sums.  A row's first CTA merges its parts' lists.
+// logits reach, most likely (first_bound).  Then it passes over all: numbers that reach the
+// bound are collected as candidates, the others go into the sums of exponentials, so that
+// `rest` comes without cancellation.  Fewer than K candidates (a row in some hundred) ask for
+// another pass with the next lower bound of the sample, more than there is room for with the
+// next higher one; where that leads nowhere (logits that are equal by the hundred) the bound
+// is searched by halving.  The candidates are ordered by value, then index (all different, so
+// that nothing depends on the order in which they came), and those behind the list join the
+// sums.  A row's first CTA merges its parts' lists.
+#include <algorithm>
 #include <cmath>
 
 #include "edp_rows.cuh"
@@ -19,10 +20,8 @@
 namespace edp {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kCtas = 4;    // per SM, which bounds the registers
+constexpr int kLanes = 1024;  // threads per SM, which bounds the registers
 constexpr int kStages = 2;  // rounds in shared memory or on their way there
-constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMostParts = 8;
 constexpr uint32_t kNoted = 8;    // vectors of a thread that wait to be looked at
 constexpr float kLeastSum = 0x1p-64f;
@@ -83,7 +82,7 @@ __device__ __forceinline__ void async_wait() {
 // kUnroll segments per warp and round, and the numbers before and behind the vectors by the
 // first threads.  Round g takes segments g, g + rounds, g + 2 rounds, ..., so that the
 // first round's are spread evenly over the part.
-template <typename T>
+template <typename T, int NT>
 struct Part {
   const T *p;
   uint32_t first;  // its first column
@@ -95,14 +94,14 @@ struct Part {
   uint32_t apart, whole;
   __device__ __forceinline__ Part(const T *p_, uint32_t first_, uint32_t n)
       : p(p_), first(first_), sp(p_, n) {
-    rounds = max(1u, (sp.vecs + 32 * kWarps * kUnroll - 1) / (32 * kWarps * kUnroll));
-    apart = 32 * kWarps * rounds;
+    rounds = max(1u, (sp.vecs + 32 * (NT / 32) * kUnroll - 1) / (32 * (NT / 32) * kUnroll));
+    apart = 32 * (NT / 32) * rounds;
     const uint32_t at = vec_at(0, 0, threadIdx.x & 31), last = at + (kUnroll - 1) * apart;
     mine = reinterpret_cast<const uint4 *>(p + sp.head) + at;
     whole = last < sp.vecs ? min(rounds, (sp.vecs - last + 31) / 32) : 0;
   }
   __device__ __forceinline__ uint32_t vec_at(uint32_t g, uint32_t k, uint32_t lane) const {
-    return ((k * kWarps + (threadIdx.x >> 5)) * rounds + g) * 32 + lane;
+    return ((k * (NT / 32) + (threadIdx.x >> 5)) * rounds + g) * 32 + lane;
   }
   __device__ __forceinline__ uint32_t column(uint32_t vec) const {
     return first + sp.head + vec * Vec16<T>::kN;
@@ -112,16 +111,16 @@ struct Part {
   }
   // Round g of this thread's vectors to its own places, -infinity where there are none.
   __device__ __forceinline__ void fetch(uint4 *ring, uint32_t g) const {
-    uint4 *to = ring + g % kStages * (kUnroll * kThreads) + threadIdx.x;
+    uint4 *to = ring + g % kStages * (kUnroll * NT) + threadIdx.x;
     const uint4 *from = mine + 32 * g;
     if (g < whole) {
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) async_load(to + k * kThreads, from + k * apart);
+      for (int k = 0; k < kUnroll; ++k) async_load(to + k * NT, from + k * apart);
     } else if (g < rounds) {
 #pragma unroll 1
       for (int k = 0; k < kUnroll; ++k) {
-        if (vec_at(g, k, threadIdx.x & 31) < sp.vecs) async_load(to + k * kThreads, from + k * apart);
-        else to[k * kThreads] = no_logits<T>();
+        if (vec_at(g, k, threadIdx.x & 31) < sp.vecs) async_load(to + k * NT, from + k * apart);
+        else to[k * NT] = no_logits<T>();
       }
     }
     async_mark();
@@ -133,21 +132,30 @@ struct Part {
   __device__ __forceinline__ void load(uint4 (&w)[kUnroll], const uint4 *ring, uint32_t g) const {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k)
-      w[k] = ring[(g % kStages * kUnroll + k) * kThreads + threadIdx.x];
+      w[k] = ring[(g % kStages * kUnroll + k) * NT + threadIdx.x];
   }
   __device__ __forceinline__ bool single() const { return threadIdx.x < sp.head + sp.tail; }
   __device__ __forceinline__ uint32_t single_at() const {
     return threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * Vec16<T>::kN;
   }
-  // f(number, column) of this thread's numbers
+  // f(number, column) of this thread's numbers, streamed as the passes are (with -infinity
+  // beyond the vectors), for the rare passes: small code.
   template <typename F>
-  __device__ __forceinline__ void each(F f) const {
+  __device__ __forceinline__ void each(uint4 *ring, F f) const {
+    start(ring);
     if (single()) f(to_f32(p[single_at()]), first + single_at());
-    for (uint32_t i = threadIdx.x; i < sp.vecs; i += kThreads) {
-      const uint4 w = vec(i);
+#pragma unroll 1
+    for (uint32_t g = 0; g < rounds; ++g) {
+      async_wait<kStages - 1>();
+#pragma unroll 1
+      for (uint32_t k = 0; k < kUnroll; ++k) {
+        const uint4 w = ring[(g % kStages * kUnroll + k) * NT + threadIdx.x];
+        const uint32_t at = column(vec_at(g, k, threadIdx.x & 31));
 #pragma unroll
-      for (int k = 0; k < Vec16<T>::kN; ++k)
-        f(to_f32(reinterpret_cast<const T *>(&w)[k]), column(i) + k);
+        for (int e = 0; e < Vec16<T>::kN; ++e)
+          f(to_f32(reinterpret_cast<const T *>(&w)[e]), at + e);
+      }
+      fetch(ring, g + kStages);
     }
   }
 };
@@ -191,6 +199,7 @@ __device__ __forceinline__ void add_but(F2 &s, F2 &u, const RowLog<T, FUSED> &lo
     s = s + e;
     if (ENT) u = fma2(e, F2(fmaxf(l.x(), kNoLog), fmaxf(l.y(), kNoLog)), u);
   }
+#pragma unroll 1
   for (; bits; bits &= bits - 1) {
     const uint32_t e = __ffs(bits) - 1, word = e * sizeof(T) / 4;
     const uint32_t x = word < 2 ? word ? w.y : w.x : word == 2 ? w.z : w.w;
@@ -212,6 +221,7 @@ __device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f
   }
   const uint32_t all = __shfl_sync(kAllLanes, upto, 31);
   __syncwarp();
+#pragma unroll 1
   for (uint32_t i = lane; i < ((all + 31) & ~31u); i += 32) {
     uint32_t owner = 0, before = 0;  // the lane of note i, and the notes before it
 #pragma unroll
@@ -229,11 +239,11 @@ __device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f
 
 // One pass, which was started: candidates go to the list, the sums are of all others, all
 // relative to `ref`, which none of them is above.  So no maximum is kept (with one, 8,192
-// rows of 152,064 bfloat16 logits took 470 us, without XXX).  A vector that has a candidate is
+// rows of 152,064 bfloat16 logits took 470 us, without 433).  A vector that has a candidate is
 // taken out whole and noted; the warp looks at those at the end, or when a lane may have no
 // room for another round's.
-template <typename T, bool ENT, bool FUSED>
-__device__ __forceinline__ RowSum take_part(const Part<T> &x, uint4 *ring, Bound b, float ref,
+template <typename T, int NT, bool ENT, bool FUSED>
+__device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, Bound b, float ref,
                                             const Candidates &to, uint32_t *noted, float c) {
   const RowLog<T, FUSED> log(ref, c);
   F2 s(0.f), u(0.f);
@@ -274,9 +284,9 @@ __device__ __forceinline__ RowSum take_part(const Part<T> &x, uint4 *ring, Bound
   return {ref, s.x() + s.y(), u.x() + u.y()};
 }
 // The same relative to each thread's maximum, where the sums ask for that: rare.
-template <typename T, bool ENT>
-__device__ __forceinline__ RowSum take_carefully(const Part<T> &x, Bound b, const Candidates &to,
-                                                 float c) {
+template <typename T, int NT, bool ENT>
+__device__ __forceinline__ RowSum take_carefully(const Part<T, NT> &x, uint4 *ring, Bound b,
+                                                 const Candidates &to, float c) {
   LaneSum a{kNegInf, F2(0.f), F2(0.f)};
   auto one = [&](float v, uint32_t column) {
     if (b.holds(v, column)) {
@@ -285,59 +295,55 @@ __device__ __forceinline__ RowSum take_carefully(const Part<T> &x, Bound b, cons
       add_one<T, ENT, false>(a.s, a.u, raise<T, ENT, false>(a, v, c), v);
     }
   };
-  x.each(one);
+  x.each(ring, one);
   return row_sum(a);
 }
 
-// The count over the CTA's threads, in all of them.  red: kWarps numbers, free before.
+// The count over the CTA's threads, in all of them.  red: a number per warp, free before.
+template <int NT>
 __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
   n = __reduce_add_sync(kAllLanes, n);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = n;
   __syncthreads();
   const uint32_t lane = threadIdx.x & 31;
-  n = __reduce_add_sync(kAllLanes, lane < kWarps ? red[lane] : 0u);
+  n = __reduce_add_sync(kAllLanes, lane < (NT / 32) ? red[lane] : 0u);
   __syncthreads();
   return n;
 }
 
 // A bound that K to kRoom numbers hold, by halving from `lo` on (which K or more reach,
-// unless it is the lowest): or, where numbers are equal by the hundred, exactly K.  Rare, so
-// that it only has to end: 64 counts at the most.
-template <typename T>
-__device__ __forceinline__ Bound search_bound(const T *p, uint32_t first, uint32_t n, uint32_t lo,
-                                           uint32_t K, uint32_t *red) {
-  const Part<T> x(p, first, n);
-  auto reach = [&](uint32_t bound) {
-    uint32_t c = 0;
-    x.each([&](float v, uint32_t) { c += v >= of_order(bound); });
-    return cta_count(c, red);
-  };
+// unless it is the lowest): or, where numbers are equal by the hundred, exactly K, with an end
+// among those equal to it, found by halving too.  Rare, so that it only has to end: 64 counts
+// at the most.
+template <typename T, int NT>
+__device__ __forceinline__ Bound search_bound(const Part<T, NT> &x, uint4 *ring, uint32_t n,
+                                              uint32_t lo, uint32_t K, uint32_t *red) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  enum { kLowest, kValue, kColumn } look = lo == kLeastOrder ? kLowest : kValue;
   uint32_t hi = 0xff800001u, some = kRoom + 1;  // nothing is above +infinity
-  if (lo == kLeastOrder) some = reach(lo);
-  if (some < K) return {of_order(lo), 0xffffffffu};
-  while (hi - lo > 1 && some > kRoom) {
-    const uint32_t mid = lo + (hi - lo) / 2, c = reach(mid);
-    if (c >= K) {
+  uint32_t a = x.first, b = x.first + n;        // too few with the end a, enough with b
+  for (;;) {
+    if (look == kValue && some <= kRoom) return {of_order(lo), kAll};
+    if (look == kValue && hi - lo <= 1) look = kColumn;
+    if (look == kColumn && b - a <= 1) return {of_order(lo), b};
+    const uint32_t mid = look == kValue ? lo + (hi - lo) / 2 : lo;
+    const uint32_t column = look == kColumn ? a + (b - a) / 2 : kAll;
+    const Bound probe{of_order(mid), column};
+    uint32_t c = 0;
+    x.each(ring, [&](float v, uint32_t at) { c += probe.holds(v, at); });
+    c = cta_count<NT>(c, red);
+    if (look == kColumn) {
+      (c >= K ? b : a) = column;
+    } else if (c >= K) {
       lo = mid;
       some = c;
+      look = kValue;
+    } else if (look == kLowest) {
+      return probe;
     } else {
       hi = mid;
     }
   }
-  const float least = of_order(lo);
-  if (some <= kRoom) return {least, 0xffffffffu};
-  // of the numbers equal to it those before a column: fewer than needed before a, as many
-  // before b
-  const uint32_t above = reach(hi);
-  uint32_t a = first, b = first + n;
-  while (b - a > 1) {
-    const uint32_t mid = a + (b - a) / 2;
-    uint32_t c = 0;
-    x.each([&](float v, uint32_t column) { c += v == least && column < mid; });
-    if (cta_count(c, red) + above >= K) b = mid;
-    else a = mid;
-  }
-  return {least, b};
 }
 
 // The r-th largest (MAX) or smallest of a warp's numbers, r <= 32; ties by lane.
@@ -345,6 +351,7 @@ template <bool MAX>
 __device__ __forceinline__ uint32_t warp_nth(uint32_t x, uint32_t r) {
   const uint32_t lane = threadIdx.x & 31;
   uint32_t best = 0;
+#pragma unroll 1
   for (uint32_t k = 0; k < r; ++k) {
     best = MAX ? __reduce_max_sync(kAllLanes, x) : __reduce_min_sync(kAllLanes, x);
     if (lane == __ffs(__ballot_sync(kAllLanes, x == best)) - 1) x = MAX ? 0u : 0xffffffffu;
@@ -370,8 +377,10 @@ __device__ __forceinline__ Key warp_sorted(Key x) {
 __device__ __forceinline__ uint32_t larger_in_runs(const Key *keys, uint32_t each, uint32_t runs,
                                                    uint32_t most, Key key) {
   uint32_t sum = 0;
+#pragma unroll 1
   for (uint32_t q = 0; q < runs; q += 4) {
     uint32_t at[4] = {0, 0, 0, 0};
+#pragma unroll
     for (uint32_t step = most; step; step >>= 1) {
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) {
@@ -390,10 +399,13 @@ struct TopOut {
   int32_t *ids;
   float *top_logp, *logp, *entropy, *rest, *stats;
   uint32_t top;
+  uint32_t rank, among;  // the bound of a sample: see first_bound
 };
 
+template <int NT>
 __device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
-  for (uint32_t k = threadIdx.x; k < o.top; k += kThreads) {
+#pragma unroll 1
+  for (uint32_t k = threadIdx.x; k < o.top; k += NT) {
     o.ids[t * o.top + k] = -1;
     o.top_logp[t * o.top + k] = kNegInf;
   }
@@ -404,14 +416,38 @@ __device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
   if (o.stats) o.stats[2 * t] = o.stats[2 * t + 1] = 0.f;
 }
 
+// The threads' sums and those that lanes 0 .. n - 1 of each warp have in `more`, in all.
+template <typename T, int NT>
+__device__ __forceinline__ RowSum joined(const RowSum &mine, const RowSum &more, uint32_t n,
+                                         RowSum *left, float c) {
+  static_assert(NT / 32 + kMostParts <= 32, "a lane each");
+  const uint32_t lane = threadIdx.x & 31;
+  const RowSum a = warp_sum<T, false>(mine, c);
+  if (lane == 0) left[threadIdx.x >> 5] = a;
+  const uint32_t from = lane - (NT / 32);
+  RowSum b{__shfl_sync(kAllLanes, more.m, from), __shfl_sync(kAllLanes, more.s, from),
+           __shfl_sync(kAllLanes, more.u, from)};
+  __syncthreads();
+  if (lane < (NT / 32)) b = left[lane];
+  else if (from >= n) b = {kNegInf, 0.f, 0.f};
+  b = warp_sum<T, false, 32>(b, c);
+  return {__shfl_sync(kAllLanes, b.m, 0), __shfl_sync(kAllLanes, b.s, 0),
+          __shfl_sync(kAllLanes, b.u, 0)};
+}
+__device__ __forceinline__ float warp_add(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
+  return x;
+}
+
 // A cluster of gridDim.y CTAs per row, each a part of it.
-template <typename T, bool ENT>
-__global__ void __launch_bounds__(kThreads, kCtas)
+template <typename T, int NT, bool ENT>
+__global__ void __launch_bounds__(NT, kLanes / NT)
 k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 shared_words[];
-  __shared__ RowSum red[kWarps], left[kWarps];
-  __shared__ uint32_t bound[kWarps], counts[kWarps], noted[kWarps][kNoted * 32];
+  __shared__ RowSum red[(NT / 32)], left[(NT / 32)];
+  __shared__ uint32_t bound[(NT / 32)], counts[(NT / 32)], noted[(NT / 32)][kNoted * 32];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S, U
   __shared__ uint32_t count;
   __shared__ unsigned long long sent;
@@ -422,7 +458,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   Key *inbox = list + kRoom;                          // [np][K], the lists of the parts
   uint4 *ring = shared_words + (kRoom + (np > 1 ? np * K : 0) + 1) / 2;
   Key *sorted = reinterpret_cast<Key *>(ring);        // [kRoom], in order, after the passes
-  static_assert(kRoom * sizeof(Key) <= sizeof(uint4) * kStages * kUnroll * kThreads, "in the ring");
+  static_assert(kRoom * sizeof(Key) <= sizeof(uint4) * kStages * kUnroll * NT, "in the ring");
   if (threadIdx.x == 0) {
     if (np > 1) {
       mbar_init(&sent, 1);
@@ -437,7 +473,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   const bool skip = (a.mask && !a.mask[t]) || target < 0;
   if (skip || (uint32_t)target >= a.vocab) {
     if (part == 0) {
-      write_none(o, t);
+      write_none<NT>(o, t);
       if (!skip && threadIdx.x == 0)
         flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)target);
     }
@@ -446,27 +482,19 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
-  const Part<T> x(row + first, first, n);
+  const Part<T, NT> x(row + first, first, n);
   x.start(ring);
   const float zt = a.target && part == 0 ? to_f32(row[target]) : 0.f;
-  // The first rounds' numbers, each lane's largest: a bound that K of the part reach (where
-  // they are all, the least of the warps' r-th largest; else one that 2.5 K most likely do).
+  // The first rounds' numbers, each lane's largest, give a bound that K of the part reach:
+  // where they are all, the least of the warps' r-th largest; else see first_bound.
   const uint32_t sample = min(x.rounds, (uint32_t)kStages);
-  const uint32_t full = x.rounds > 1 ? kWarps : min((uint32_t)kWarps, x.sp.vecs / 32);
-  uint32_t r = 33, nth = 1;
-  if (full) {
-    if (x.rounds == sample) {
-      r = (K + full - 1) / full;
-    } else {
-      const float per_warp = 2.5f * (float)(K * sample) / (float)(x.rounds * kWarps);
-      r = max(1u, (uint32_t)(per_warp + 0.5f));
-      nth = r > 1 ? kWarps * 2 / 5 : max(1u, (uint32_t)(kWarps * __expf(-per_warp)));
-    }
-  }
-  uint32_t lo = kLeastOrder, lower = kLeastOrder;
+  const uint32_t full = x.rounds > 1 ? NT / 32 : min(NT / 32u, x.sp.vecs / 32);
+  const uint32_t r = x.rounds > sample ? o.rank : full ? (K + full - 1) / full : 33;
+  uint32_t nth = x.rounds > sample ? o.among : 1;
   if (r <= 32) {
     float m = kNegInf;
     async_wait<0>();
+#pragma unroll 1
     for (uint32_t g = 0; g < sample; ++g) {
       uint4 w[kUnroll];
       x.load(w, ring, g);
@@ -478,15 +506,18 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   }
   if (np > 1) cluster_started();
   __syncthreads();
-  if (r <= 32) {
-    const uint32_t each = lane < full ? bound[lane] : 0xffffffffu;
-    lower = max(lo, __reduce_min_sync(kAllLanes, each));
-    lo = nth > 1 ? max(lo, warp_nth<false>(each, nth)) : lower;
-  }
+  auto bound_at = [&](uint32_t i) {
+    return r > 32 || i - 1 >= full
+               ? kLeastOrder
+               : max(kLeastOrder, warp_nth<false>(lane < full ? bound[lane] : 0xffffffffu, i));
+  };
+  uint32_t lo = bound_at(nth);
   const Candidates to{list, &count};
   Bound b{of_order(lo), 0xffffffffu};
-  uint32_t found;
+  uint32_t found, reached = kLeastOrder;  // reached: by too many
+  bool many = false, few = false;  // so far
   RowSum sum;
+#pragma unroll 1
   for (bool again = false, searched = false, careful = false;;) {
     // nothing but -infinity and NaN is left out by the lowest bound
     const bool all = lo == kLeastOrder && b.end == 0xffffffffu;
@@ -498,16 +529,16 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       __syncthreads();
     }
     again = true;
-    sum = careful ? take_carefully<T, ENT>(x, b, to, a.c)
-                  : take_part<T, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
+    sum = careful ? take_carefully<T, NT, ENT>(x, ring, b, to, a.c)
+                  : take_part<T, NT, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
     sum = warp_sum<T, false>(sum, a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
     found = count;
     const bool enough = searched || (found <= kRoom && (found >= K || all));
     if (enough) {
-      sum = warp_sum<T, false, lanes_for(kWarps)>(
-          lane < kWarps ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+      sum = warp_sum<T, false, lanes_for(NT / 32)>(
+          lane < (NT / 32) ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
       if (!careful) sum = exact_sums<T>(sum, a.c);
       sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
              __shfl_sync(kAllLanes, sum.u, 0)};
@@ -519,11 +550,17 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
     }
     __syncthreads();
     if (enough) continue;
-    if (found <= kRoom && lo != lower) {
-      lo = lower;
+    // the next of the warps' numbers, unless there is none or that leads back
+    const bool over = found > kRoom;
+    if (over) reached = lo;
+    (over ? many : few) = true;
+    uint32_t next = lo;
+    while (next == lo && nth - 1 < full) next = bound_at(nth += over ? 1 : -1);
+    if (nth - 1 < full && !(many && few)) {
+      lo = next;
       b.least = of_order(lo);
     } else {
-      b = search_bound<T>(row + first, first, n, found > kRoom ? lo : kLeastOrder, K, counts);
+      b = search_bound<T, NT>(x, ring, n, reached, K, counts);
       lo = order_of(b.least);
       searched = true;
     }
@@ -532,44 +569,36 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   // In order: runs of 32 sorted by a warp each, then a key's place is its place in its own
   // run and the number of larger keys in each of the others.
   const uint32_t runs = (found + 31) / 32;
-  for (uint32_t q = wid; q < runs; q += kWarps) {
+#pragma unroll 1
+  for (uint32_t q = wid; q < runs; q += (NT / 32)) {
     const uint32_t i = 32 * q + lane;
     const Key key = warp_sorted(i < found ? list[i] : 0);
     list[i] = key;
   }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < found; i += kThreads) {
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < found; i += NT) {
     const Key key = list[i];
     sorted[larger_in_runs(list, 32, runs, 32, key)] = key;
   }
   if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < K; i += kThreads) {
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < K; i += NT) {
     if (np > 1) send_key(inbox + part * K + i, i < found ? sorted[i] : 0, &sent, 0);
     else if (i >= found) sorted[i] = 0;
   }
   // Candidates behind the list join the others.
   LaneSum drop{kNegInf, F2(0.f), F2(0.f)};
   auto drop_key = [&](Key key) {
-    const float z = value_of(key), y = raise<T, ENT, false>(drop, z, a.c).of(z), e = ex2(y);
-    drop.s = drop.s + F2(e, 0.f);
-    if (ENT) drop.u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), drop.u);
+    const float z = value_of(key);
+    add_one<T, ENT, false>(drop.s, drop.u, raise<T, ENT, false>(drop, z, a.c), z);
   };
-  for (uint32_t i = K + threadIdx.x; i < found; i += kThreads) drop_key(sorted[i]);
-  {
-    const RowSum mine = warp_sum<T, false>(row_sum(drop), a.c);
-    if (lane == 0) left[wid] = mine;
-  }
-  __syncthreads();
-  if (wid == 0) {
-    static_assert(kWarps <= 16, "and the sums of the others in lane 16");
-    sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
-           __shfl_sync(kAllLanes, sum.u, 0)};
-    sum = warp_sum<T, false>(lane < kWarps ? left[lane]
-                             : lane == 16  ? sum
-                                           : RowSum{kNegInf, 0.f, 0.f}, a.c);
-  }
+#pragma unroll 1
+  for (uint32_t i = K + threadIdx.x; i < found; i += NT) drop_key(sorted[i]);
+  const Key *top = sorted;
   if (np > 1) {
+    sum = joined<T, NT>(row_sum(drop), sum, 1, left, a.c);
     if (threadIdx.x == 0)
       send_float4(&sums[part], make_float4(sum.m, sum.s, sum.u, 0.f), &sent, 0);
     if (part) return;
@@ -579,64 +608,54 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       whole = mbar_wait(&sent, 0, kRowWaitNs);  // none of them comes after the end
     }
     if (!__syncthreads_and(whole)) {
-      write_none(o, t);
+      write_none<NT>(o, t);
       return;
     }
     // A key's place in the row's list: how many are larger in each of the parts' lists.
+    // Behind it, it joins the others, too.
     drop = {kNegInf, F2(0.f), F2(0.f)};
     uint32_t have = 0;  // keys in all lists: the row's list may be shorter than K
-    for (uint32_t i = threadIdx.x; i < np * K; i += kThreads) {
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < np * K; i += NT) {
       const Key key = inbox[i];
       if (!key) continue;
       ++have;
       const uint32_t rank = larger_in_runs(inbox, K, np, 128, key);
       if (rank < K) list[rank] = key;
+      else drop_key(key);
     }
-    have = cta_count(have, counts);
-    for (uint32_t i = have + threadIdx.x; i < K; i += kThreads) list[i] = 0;
+    have = cta_count<NT>(have, counts);
+    if (threadIdx.x < K && threadIdx.x >= have) list[threadIdx.x] = 0;
+    const float4 y = lane < np ? sums[lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+    sum = {y.x, y.y, y.z};
+    top = list;
     __syncthreads();
-    // What of the parts' lists is not of the row's joins the others, too.
-    const Key last = list[K - 1];
-    for (uint32_t i = threadIdx.x; i < np * K; i += kThreads) {
-      const Key key = inbox[i];
-      if (key && key < last) drop_key(key);
-    }
-    const RowSum mine = warp_sum<T, false>(row_sum(drop), a.c);
-    if (lane == 0) left[wid] = mine;
-    __syncthreads();
-    if (wid) return;
-    const float4 y = lane - 16 < np ? sums[lane - 16] : make_float4(kNegInf, 0.f, 0.f, 0.f);
-    sum = warp_sum<T, false>(lane < kWarps ? left[lane] : RowSum{y.x, y.y, y.z}, a.c);
   }
-  if (wid) return;
-  sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0),
-         __shfl_sync(kAllLanes, sum.u, 0)};
-  const Key *top = np > 1 ? list : sorted;
-  const bool any = top[0] != 0;
+  // The list's own sums relative to the row's maximum, and the others'.
+  const Key key = threadIdx.x < K ? top[threadIdx.x] : 0;
+  const bool any = np > 1 ? top[0] != 0 : found != 0;
   const float M = any ? value_of(top[0]) : kNegInf;
+  RowSum in{M, 0.f, 0.f};
+  if (key) {
+    const float y = (value_of(key) - M) * a.c;
+    in.s = ex2(y);
+    if (ENT) in.u = in.s * fmaxf(y, kNoLog);
+  }
+  if (wid * 32 < K) {
+    in.s = warp_add(in.s);
+    if (ENT) in.u = warp_add(in.u);
+    if (lane == 0) red[wid] = in;
+  }
+  sum = joined<T, NT>(row_sum(drop), sum, np, left, a.c);
+  if (wid * 32 >= K && wid) return;
   float S = 0.f, U = 0.f;
-  for (uint32_t k = lane; k < K; k += 32)
-    if (top[k]) {
-      const float y = (value_of(top[k]) - M) * a.c, e = ex2(y);
-      S += e;
-      U = fmaf(e, fmaxf(y, kNoLog), U);
-    }
-#pragma unroll
-  for (int i = 16; i; i >>= 1) {
-    S += __shfl_xor_sync(kAllLanes, S, i);
-    U += __shfl_xor_sync(kAllLanes, U, i);
+  for (uint32_t q = 0; 32 * q < K; ++q) {
+    S += red[q].s;
+    U += red[q].u;
   }
   if (!any && !(sum.s != sum.s)) {  // no token has a probability
-    if (lane == 0) flag(ctrl, DEVERR_ROW, t);
-    for (uint32_t k = lane; k < K; k += 32) {
-      o.ids[t * K + k] = -1;
-      o.top_logp[t * K + k] = kNegInf;
-    }
-    if (lane) return;
-    if (o.logp) o.logp[t] = 0.f;
-    if (o.entropy) o.entropy[t] = 0.f;
-    if (o.rest) o.rest[t] = 0.f;
-    if (o.stats) o.stats[2 * t] = o.stats[2 * t + 1] = 0.f;
+    if (threadIdx.x == 0) flag(ctrl, DEVERR_ROW, t);
+    write_none<NT>(o, t);
     return;
   }
   if (sum.m == kNegInf) {
@@ -648,12 +667,12 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   }
   const float ln = logf(S);
   const bool nan = S != S;
-  for (uint32_t k = lane; k < K; k += 32) {
-    const Key key = top[k];
-    o.ids[t * K + k] = key && !nan ? (int32_t)column_of(key) : -1;
-    o.top_logp[t * K + k] = nan ? S : key ? (value_of(key) - M) * a.inv_t - ln : kNegInf;
+  if (threadIdx.x < K) {
+    o.ids[t * K + threadIdx.x] = key && !nan ? (int32_t)column_of(key) : -1;
+    o.top_logp[t * K + threadIdx.x] =
+        nan ? S : key ? (value_of(key) - M) * a.inv_t - ln : kNegInf;
   }
-  if (lane) return;
+  if (threadIdx.x) return;
   if (o.logp) o.logp[t] = (zt - M) * a.inv_t - ln;
   if (o.entropy) o.entropy[t] = ln - kLn2 * (U / S);
   if (o.rest)
@@ -666,20 +685,59 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
 
 }  // namespace
 
+// The bound for K numbers of a part from `sample` of its `rounds` of vectors, by `warps`
+// warps: `rank`, the place among a warp's lanes' largest, and `among`, that among the warps'
+// numbers of that place, the least first.  The sample's share of the K is Poisson distributed
+// (the vectors are spread evenly), so that three deviations more are hardly ever too few;
+// `rank` of a warp's are below the bound that a mean of `mean` per warp reaches with a
+// probability near one half, which is the warps' number that says most.
+static void first_bound(double K, double sample, double rounds, int warps, uint32_t *rank,
+                        uint32_t *among) {
+  const double share = K * sample / rounds;
+  double mean = (share + 3.0 * std::sqrt(share)) / warps;
+  mean *= 1.0 - mean / 64.0;  // of the lanes: some have two
+  const int r = (int)std::min(std::max(std::ceil(mean), 1.0), 32.0);
+  double below = 0.0, term = std::exp(-mean);
+  for (int i = 0; i < r; term *= mean / ++i) below += term;
+  *rank = (uint32_t)r;
+  *among = (uint32_t)std::min(std::max(std::floor(below * (warps + 1)), 1.0), (double)warps);
+}
+
 cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_t *ids,
                              float *top_logp, float *logp, float *entropy, float *rest,
                              float *stats, cudaStream_t s) {
-  const TopOut o{ids, top_logp, logp, entropy, rest, stats, top};
+  // CTAs per row while there is one per SM at the most and their parts are not small, and
+  // threads by the size of a part.  Measured on bfloat16 rows (us, parts x threads): 1 row of
+  // 152,064: 13.8 as 1 x 256, 9.4 as 8 x 256, 9.9 as 8 x 512; of 32,003: 7.7 as 1 x 256, 8.1
+  // as 8 x 256; 64 rows of 152,064: 19.5 as 1 x 256, 15.1 as 2 x 256, 13.1 as 2 x 512, 16.1
+  // as 4 x 512; 128: 20.0 as 1 x 256, 15.6 as 1 x 512; 2,000 rows of 4,000: 28.3 as 1 x 256,
+  // 16.1 as 1 x 128; 4,096 of 32,003: 82 and 69, but 400 of them 14.7 and 17.9; 2,048 rows of
+  // 152,064: 117 as 1 x 256, 147 as 1 x 512.  With long lists the 4 warps of 128 threads say
+  // too little about a bound (2,000 rows of 4,000 with 128 entries: 92 us, 43 with 256).
+  const uint64_t sms = (uint64_t)ctx->coop_sms;
+  const uint64_t vecs = (uint64_t)z.vocab * (z.dtype == EDP_F32 ? 4 : 2) / 16;
+  uint32_t parts = 1;
+  while (parts < kMostParts && 2 * parts * z.rows <= sms && vecs >= 2ull * parts * 2048) parts *= 2;
+  const uint64_t each = vecs / parts;
+  const bool small = each <= 1024 || (each <= 4096 && z.rows * parts >= 8 * sms);
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    const uint32_t parts = row_parts(ctx, z, 2);
-    auto kern = entropy ? k_token_top<T, true> : k_token_top<T, false>;
-    const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
-    const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + kStages * kUnroll * kThreads);
-    const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
-    if (e != cudaSuccess) return e;
-    return launch_rows(kern, z.rows, parts, true, kThreads, bytes, s, row_args(z), o, ctx->ctrl);
+    auto go = [&](auto threads) {
+      constexpr int NT = decltype(threads)::value;
+      TopOut o{ids, top_logp, logp, entropy, rest, stats, top, 0, 0};
+      first_bound(top, kStages, std::ceil((double)each / (NT * kUnroll)), NT / 32, &o.rank,
+                  &o.among);
+      auto kern = entropy ? k_token_top<T, NT, true> : k_token_top<T, NT, false>;
+      const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
+      const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + kStages * kUnroll * NT);
+      const cudaError_t e = cudaFuncSetAttribute(
+          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+      if (e != cudaSuccess) return e;
+      return launch_rows(kern, z.rows, parts, true, NT, bytes, s, row_args(z), o, ctx->ctrl);
+    };
+    if (small && top <= 64) return go(std::integral_constant<int, 128>{});
+    if (each >= 8192 && z.rows * parts <= sms) return go(std::integral_constant<int, 512>{});
+    return go(std::integral_constant<int, 256>{});
   });
 }
 

@@ -52,12 +52,11 @@ edp_status check_logits(edp_ctx *c, const char *who, const Logits &z, const void
   return EDP_OK;
 }
 
-// The kernels with lists hold a row in the shared memory of 8 CTAs at the most.
+// The kernel of the distillation loss holds a row in the shared memory of 8 CTAs at the most.
 constexpr uint64_t kMostRowBytes = 3ull << 19;
-edp_status check_lists(edp_ctx *c, const char *who, const Logits &z, uint32_t top) {
+
+edp_status check_top(edp_ctx *c, const char *who, uint32_t top) {
   if (top == 0 || top > 128) return fail(c, EDP_ERR_INVALID, "%s: need 0 < top <= 128", who);
-  if (z.vocab * size_of(z.dtype) > kMostRowBytes)
-    return fail(c, EDP_ERR_INVALID, "%s: a row of logits takes more than 1.5 MiB", who);
   return EDP_OK;
 }
 
@@ -184,7 +183,7 @@ edp_status edp_token_top(edp_ctx *ctx, const void *logits, uint32_t dtype, uint6
   if (rows == 0) return EDP_OK;
   const Logits z{logits, dtype, vocab, rows, stride, target, mask, temperature};
   edp_status st = check_logits(ctx, "edp_token_top", z, nullptr, 0, false);
-  if (st == EDP_OK) st = check_lists(ctx, "edp_token_top", z, top);
+  if (st == EDP_OK) st = check_top(ctx, "edp_token_top", top);
   if (st != EDP_OK) return st;
   if (!ids || !top_logp || (logp && !target))
     return fail(ctx, EDP_ERR_INVALID, "edp_token_top: NULL ids or top_logp, or logp without target");
@@ -216,8 +215,10 @@ edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg, const v
                      cfg ? cfg->norm : 0.0};
   edp_status st = check_distill(ctx, "edp_distill_loss", cfg, set, rest != nullptr);
   if (st == EDP_OK) st = check_logits(ctx, "edp_distill_loss", z, dlogits, dstride, false);
-  if (st == EDP_OK) st = check_lists(ctx, "edp_distill_loss", z, top);
+  if (st == EDP_OK) st = check_top(ctx, "edp_distill_loss", top);
   if (st != EDP_OK) return st;
+  if (vocab * size_of(dtype) > kMostRowBytes)
+    return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: a row of logits takes more than 1.5 MiB");
   if (!ids || !value || !loss)
     return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: NULL ids, value or loss");
   if (!device_arrays(ctx, {logits, ids, value, rest, mask, off, loss, row_loss, dlogits}))

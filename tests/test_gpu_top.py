@@ -261,17 +261,58 @@ def test_special_values(edp_lib, dtype, vocab):
     assert status == edp.EDP_ERR_INVALID and "-infinity" in msg and "row 0" in msg
 
 
-@pytest.mark.parametrize("dtype,vocab", [("bf16", 786_432), ("f16", 786_431), ("f32", 393_216)])
-def test_largest_vocabularies(edp_lib, dtype, vocab):
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 786_432), ("f16", 786_431), ("f32", 393_216),
+                                         ("f32", 1_500_001), ("bf16", 3_000_007)])
+def test_large_vocabularies(edp_lib, dtype, vocab):
     edp, ring = edp_lib, ctx_of(edp_lib)
     v, target, zd = make(2, vocab, dtype, 1, shift=3)
     o = outputs(2, 128)
     run(edp, ring, v, target, o)
     edp.edp_sync(ring.ctx)
     check(o, zd, target, 128)
-    _, more = view(1, 786_433 if dtype != "f32" else 393_217, dtype)
-    with pytest.raises(edp.EdpError, match="1.5 MiB"):
-        run(edp, ring, more, target[:1], {k: x[:1] for k, x in o.items()})
+
+
+def skewed(rows, vocab, how, seed):
+    """Rows whose sample says little, or the wrong thing, about the rest."""
+    rng = np.random.default_rng(seed)
+    z = rng.normal(0, 1, (rows, vocab))
+    if how == "rising":
+        z = np.sort(z, 1)
+    elif how == "falling":
+        z = -np.sort(z, 1)
+    elif how == "block":    # all that counts is in one stretch
+        z[:, vocab // 3:vocab // 3 + 400] += 30
+    elif how == "few":      # as many likely tokens as the list has, nothing near them
+        for t in range(rows):
+            z[t] -= 300
+            z[t, rng.permutation(vocab)[:100]] += 300
+    elif how == "comb":     # every 64th token, which are a few threads' alone
+        z[:, 5::64] += 20
+    elif how == "steps":    # a few values, hundreds of each
+        z = np.round(2 * z) / 2
+    return z
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("how", ["rising", "falling", "block", "few", "comb", "steps"])
+@pytest.mark.parametrize("rows,vocab,top", [(3, 3_000, 40), (2, 30_011, 128), (2, 100_003, 100),
+                                            (160, 40_000, 20)])
+def test_skewed_rows(edp_lib, dtype, how, rows, vocab, top):
+    ring = ctx_of(edp_lib)
+    _, v = view(rows, vocab, dtype)
+    few = min(rows, 3)
+    z = skewed(few, vocab, how, vocab)
+    v.copy_(torch.from_numpy(z).repeat((rows + few - 1) // few, 1)[:rows])
+    zd = to_np(v[:few].double())
+    target = np.full(rows, 7, np.int32)
+    o = outputs(rows, top)
+    run(edp_lib, ring, v, target, o)
+    edp_lib.edp_sync(ring.ctx)
+    check({k: x[:few].clone() for k, x in o.items()}, zd, target[:few], top)
+    for x in o.values():
+        for i in range(few, rows, few):
+            n = min(few, rows - i)
+            assert torch.equal(x[i:i + n], x[:n])
 
 
 def test_offsets_beyond_32_bits(edp_lib):
