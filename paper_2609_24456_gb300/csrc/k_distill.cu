@@ -18,15 +18,13 @@
 // are those of the rest, relative to its own maximum; the entries join them afterwards.
 #include <cmath>
 
-#include "edp_rows.cuh"
+#include "edp_stream.cuh"
 
 namespace edp {
 namespace {
 
-constexpr int kThreads = 384;
-// CTAs per SM, which bound the registers: as many as parts of 76 KB allow
-constexpr int kCtas = 3;
-enum class Rest { kGrad, kZero, kCareful };
+// threads per SM, which bound the registers: three CTAs of 384, as parts of 76 KB allow
+constexpr int kLanes = 1152;
 
 struct DistillRule {
   uint32_t kind;
@@ -45,11 +43,6 @@ __device__ __forceinline__ float warp_max(float x) {
   for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kAllLanes, x, o));
   return x;
 }
-__device__ __forceinline__ float warp_add(float x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
-  return x;
-}
 // ln(e^a + e^b)
 __device__ __forceinline__ float log_add(float a, float b) {
   return fmaxf(a, b) + log1pf(expf(-fabsf(a - b)));
@@ -59,91 +52,172 @@ __device__ __forceinline__ float weigh(float weight, float log) {
   return weight == 0.f ? 0.f : weight * log;
 }
 
-// A row's entries over a warp's lanes, E each: entry k = lane + 32 i.  id < 0: none.
-template <int E>
-struct Entries {
-  int32_t id[E];
-  float lp[E], z[E];  // the teacher's log-probability, the student's logit
-};
-
-// What the classes give: the loss, the factor of 2^y of the tokens outside of the list
-// (before `by`), and each entry's gradient (before `by`) in the place of its logit.
-struct Classes {
-  float loss, outside;
-};
-template <int E>
-__device__ __forceinline__ Classes classes(const DistillRule &r, Entries<E> &e, bool has_rest,
-                                           float lpr, const RowSum &rest, float M, float c,
-                                           float inv_t) {
-  const float left = rest.m == kNegInf ? rest.s : rest.s * ex2((rest.m - M) * c);
-  float S = 0.f;
-#pragma unroll
-  for (int i = 0; i < E; ++i) S += e.id[i] >= 0 ? ex2((e.z[i] - M) * c) : 0.f;
-  S = warp_add(S) + left;
-  const float ln = logf(S), inv = 1.f / S;
-  const float qr = left * inv;
-  const float lqr = rest.s == 0.f ? kNegInf : (rest.m - M) * inv_t + logf(rest.s) - ln;
-  const float pr = has_rest ? expf(lpr) : 0.f;
-  Classes o;
-  if (r.kind == EDP_DISTILL_FORWARD) {
-    float l = 0.f, P = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0) {
-        const float p = expf(e.lp[i]);
-        l += weigh(p, e.lp[i] - ((e.z[i] - M) * inv_t - ln));
-        P += p;
-      }
-    o.loss = warp_add(l) + weigh(pr, lpr - lqr);
-    P = warp_add(P) + pr;
-    o.outside = fmaf(P, qr, -pr);
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0) e.z[i] = fmaf(P, ex2((e.z[i] - M) * c) * inv, -expf(e.lp[i]));
-  } else if (r.kind == EDP_DISTILL_REVERSE) {
-    float l = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0) {
-        const float q = ex2((e.z[i] - M) * c) * inv;
-        const float d = (e.z[i] - M) * inv_t - ln - e.lp[i];
-        l += weigh(q, d);
-        e.z[i] = q;
-        e.lp[i] = d;
-      }
-    o.loss = warp_add(l) + weigh(qr, lqr - lpr);
-    o.outside = weigh(qr, lqr - lpr - o.loss);
-#pragma unroll
-    for (int i = 0; i < E; ++i) e.z[i] = weigh(e.z[i], e.lp[i] - o.loss);
-  } else {
-    float l = 0.f, g = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0) {
-        const float lp = e.lp[i], lq = (e.z[i] - M) * inv_t - ln;
-        const float q = ex2((e.z[i] - M) * c) * inv;
-        const float lm = log_add(lp + r.ln_beta, lq + r.ln_alpha);
-        l += weigh(r.beta * expf(lp), lp - lm);
-        g += weigh(r.alpha * q, lq - lm);
-        e.z[i] = q;
-        e.lp[i] = lq - lm;
-      }
-    const float lmr = log_add(lpr + r.ln_beta, lqr + r.ln_alpha);
-    g = warp_add(g) + weigh(r.alpha * qr, lqr - lmr);
-    o.loss = warp_add(l) + weigh(r.beta * pr, lpr - lmr) + g;
-    o.outside = weigh(qr, fmaf(r.alpha, lqr - lmr, -g));
-#pragma unroll
-    for (int i = 0; i < E; ++i) e.z[i] = weigh(e.z[i], fmaf(r.alpha, e.lp[i], -g));
+// Two numbers of each thread with an entry over all of them, in all threads.
+__device__ __forceinline__ float2 list_sums(float x, float y, bool busy, uint32_t warps,
+                                            float2 *room) {
+  if (busy) {
+    x = warp_add(x);
+    y = warp_add(y);
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = make_float2(x, y);
   }
-  o.outside = rest.s == 0.f ? 0.f : o.outside / rest.s;
-  return o;
+  __syncthreads();
+  float2 a = room[0];
+  for (uint32_t i = 1; i < warps; ++i) {
+    a.x += room[i].x;
+    a.y += room[i].y;
+  }
+  return a;
+}
+
+// A thread's entry of a row's list; id < 0: none.
+struct Entry {
+  int32_t id;
+  float lp, p;  // the teacher's log-probability and probability
+  float x, e;   // the student's logarithm relative to the list's maximum, and its power
+};
+// What does not need the row's sums, made while the row is on its way: the list's maximum,
+// the sums of e, of p, and of p (lp - x) with FORWARD or of e (x - lp) with REVERSE.
+struct ListSums {
+  float m, s, p, cross;
+};
+// Of the whole row: its logarithms' normaliser relative to the list's maximum, what takes e
+// to q; the others' q and its logarithm, their maximum and sum.
+struct RowSums {
+  float ln, by, qr, lqr, m, s;
+  bool none;  // no token has a probability
+};
+__device__ __forceinline__ RowSums row_sums(const ListSums &l, const RowSum &o, float c,
+                                            float inv_t) {
+  const float M = fmaxf(l.m, o.m);
+  const float to_row = l.m == kNegInf ? 1.f : ex2((l.m - M) * c);
+  const float left = o.m == kNegInf ? o.s : o.s * ex2((o.m - M) * c);
+  const float S = fmaf(l.s, to_row, left), ln = logf(S), inv = 1.f / S;
+  return {ln + (M - (l.m == kNegInf ? 0.f : l.m)) * inv_t,
+          to_row * inv,
+          left * inv,
+          o.s == 0.f ? kNegInf : (o.m - M) * inv_t + logf(o.s) - ln,
+          o.m,
+          o.s,
+          M == kNegInf && S == S};
+}
+// The row's loss, the others' gradient and `g`, by which an entry's goes, before the weight.
+struct RowLoss {
+  float loss, outside, g;
+};
+// FORWARD and REVERSE.
+__device__ __forceinline__ RowLoss row_loss_of(uint32_t kind, const ListSums &l, const RowSums &r,
+                                               float lpr, float pr) {
+  if (kind == EDP_DISTILL_FORWARD) {
+    const float P = l.p + pr;
+    return {fmaf(l.p, r.ln, l.cross) + weigh(pr, lpr - r.lqr), fmaf(P, r.qr, -pr), P};
+  }
+  const float all = r.by * fmaf(-l.s, r.ln, l.cross) + weigh(r.qr, r.lqr - lpr);
+  return {all, weigh(r.qr, r.lqr - lpr - all), all};
+}
+
+// Shared memory of the list's phase.
+struct ListRoom {
+  float2 sums[4][4];  // of list_sums, of each call its own
+  float weight;
+  int32_t strange;    // an id >= vocab, or -1 (set before)
+};
+// The row's weight by the last warp, the list by a thread per entry (the first 128).  Every
+// logit of it is here when the function returns, and so is the weight.
+template <typename T, int NT>
+__device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights &weights,
+                                              bool by_range, const TeacherLists &lists,
+                                              const DistillRule &rule, const T *row, uint64_t t,
+                                              Entry *entry, ListRoom *s) {
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  if (wid == NT / 32 - 1) {
+    float w;
+    if (by_range) {
+      const Range r = token_range(weights.set);
+      w = 1.f / (float)(r.end - r.first);
+    } else {
+      w = row_weight(weights, t);
+    }
+    if (lane == 0) s->weight = w;
+  }
+  const uint32_t warps = (lists.top + 31) / 32;
+  const bool busy = wid < warps, has_rest = lists.rest != nullptr;
+  Entry e{-1, kNegInf, 0.f, kNegInf, 0.f};
+  ListSums l{kNegInf, 0.f, 0.f, 0.f};
+  if (busy) {
+    float z = kNegInf;
+    if (threadIdx.x < lists.top) {
+      const uint64_t at = t * lists.top + threadIdx.x;
+      e.id = lists.ids[at];
+      e.lp = lists.value[at];
+      if (e.lp == kNegInf) e.id = -1;
+      if (e.id >= 0 && (uint32_t)e.id >= a.vocab) {
+        s->strange = e.id;
+        e.id = -1;
+      }
+      if (e.id >= 0) z = to_f32(row[e.id]);
+    }
+    e.x = z;
+    const float m = warp_max(z), v = warp_max(e.id >= 0 ? e.lp : kNegInf);
+    if (lane == 0) s->sums[0][wid] = make_float2(m, v);
+  }
+  __syncthreads();
+  float top_value = kNegInf;
+  for (uint32_t i = 0; i < warps; ++i) {
+    l.m = fmaxf(l.m, s->sums[0][i].x);
+    top_value = fmaxf(top_value, s->sums[0][i].y);
+  }
+  if (busy) {
+    const float y = e.x - (l.m == kNegInf ? 0.f : l.m);
+    e.e = e.id >= 0 ? ex2(y * a.c) : 0.f;
+    e.x = y * a.inv_t;
+    if (!has_rest) e.lp = (e.lp - top_value) * rule.inv_tt;  // the list's own softmax
+    e.p = e.id >= 0 ? expf(e.lp) : 0.f;
+  }
+  float2 sums = list_sums(e.e, e.p, busy, warps, s->sums[1]);
+  l.s = sums.x;
+  l.p = sums.y;
+  if (!has_rest && busy) {
+    e.lp -= logf(l.p);
+    e.p = e.id >= 0 ? expf(e.lp) : 0.f;
+  }
+  if (rule.kind != EDP_DISTILL_MIX) {
+    const float cross = rule.kind == EDP_DISTILL_FORWARD ? weigh(e.p, e.lp - e.x)
+                                                         : weigh(e.e, e.x - e.lp);
+    sums = list_sums(e.id >= 0 ? cross : 0.f, e.p, busy, warps, s->sums[2]);
+    l.cross = sums.x;
+    l.p = sums.y;
+  }
+  *entry = e;
+  return l;
+}
+// MIX, by all threads; lm: the entry's ln m.
+__device__ __forceinline__ RowLoss mix_loss(const DistillRule &rule, const TeacherLists &lists,
+                                            const Entry &e, const RowSums &r, float lpr, float pr,
+                                            ListRoom *s, float *lm) {
+  const uint32_t warps = (lists.top + 31) / 32;
+  const bool busy = threadIdx.x < 32 * warps;
+  const float lq = e.x - r.ln, q = e.e * r.by;
+  float x = 0.f, y = 0.f;
+  if (busy) {
+    *lm = log_add(e.lp + rule.ln_beta, lq + rule.ln_alpha);
+    if (e.id >= 0) {
+      x = weigh(rule.beta * e.p, e.lp - *lm);
+      y = weigh(rule.alpha * q, lq - *lm);
+    }
+  }
+  const float2 sums = list_sums(x, y, busy, warps, s->sums[3]);
+  const float lmr = log_add(lpr + rule.ln_beta, r.lqr + rule.ln_alpha);
+  const float g = sums.y + weigh(rule.alpha * r.qr, r.lqr - lmr);
+  return {sums.x + weigh(rule.beta * pr, lpr - lmr) + g,
+          weigh(r.qr, fmaf(rule.alpha, r.lqr - lmr, -g)), g};
 }
 
 // The weighted loss of a row, from one CTA of each row; the last of them adds up all
 // rows in a fixed order and leaves the counters at 0.
+template <int NT>
 __device__ __forceinline__ void conclude(float weighted, float *per_row, float *loss,
                                          Ctrl *ctrl) {
-  constexpr int NW = kThreads / 32;
+  constexpr int NW = NT / 32;
   __shared__ Pair sums[NW];
   __shared__ bool last;
   if (threadIdx.x == 0) {
@@ -164,7 +238,7 @@ __device__ __forceinline__ void conclude(float weighted, float *per_row, float *
   if (!last) return;
   __threadfence();
   Pair a{0.f, 0.f};
-  for (uint32_t i = threadIdx.x; i < gridDim.x; i += kThreads) pair_add(a, __ldcg(per_row + i));
+  for (uint32_t i = threadIdx.x; i < gridDim.x; i += NT) pair_add(a, __ldcg(per_row + i));
   a = warp_join(a);
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   if (lane == 0) sums[wid] = a;
@@ -179,19 +253,20 @@ __device__ __forceinline__ void conclude(float weighted, float *per_row, float *
 }
 
 // A cluster of gridDim.y CTAs per row, each with its part in shared memory.
-template <typename T, bool BACK, int E>
-__global__ void __launch_bounds__(kThreads, kCtas)
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, kLanes / NT)
 k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, DistillRule rule,
           float *loss, float *row_loss, float *per_row, void *dz, uint64_t dstride, bool early,
           Ctrl *ctrl) {
-  constexpr int NT = kThreads;
   constexpr bool F = kFused<T>;
   using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>;
   extern __shared__ uint4 resident[];
   __shared__ RowSum red[NT / 32];
-  __shared__ float4 parts[2][8];  // what the cluster's CTAs send: m, S, weight, list's maximum
-  __shared__ RowGrad grad;
-  __shared__ Rest rest;
+  __shared__ float4 parts[2][8];  // what the cluster's CTAs send: m, S, -, a token twice
+  __shared__ ListRoom list;
+  __shared__ RowSums rows;        // what the first warp makes of them
+  __shared__ RowLoss found;
+  __shared__ bool twice, zero, careful;
   __shared__ unsigned long long bar, sent[2];
   const uint64_t t = blockIdx.x;
   const uint32_t part = blockIdx.y, np = gridDim.y;
@@ -203,6 +278,8 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
       mbar_arrive_tx(&sent[k], np * sizeof(float4));
     }
     mbar_init_fence();
+    list.strange = -1;
+    twice = false;
   }
   __syncthreads();
   // early: the kernel before is of this call, waited for all that came before it and
@@ -213,11 +290,11 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
   row_part(a.vocab, part, np, &first, &n);
   T *d = reinterpret_cast<T *>(dz) + t * dstride + first;
   if ((a.mask && !a.mask[t]) || !in_sequences(weights, t)) {
-    if (BACK) part_zero<T, NT>(d, n);
+    part_zero<T, NT>(d, n);
     if (early) pdl_wait();  // so that what waits for this kernel finds the weights
     if (part) return;
     if (row_loss && threadIdx.x == 0) row_loss[t] = 0.f;
-    conclude(0.f, per_row, loss, ctrl);
+    conclude<NT>(0.f, per_row, loss, ctrl);
     return;  // the whole cluster
   }
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride, *p = row + first;
@@ -234,170 +311,282 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
     held[i] = p[i];
   }
   if (np > 1) cluster_started();
-  // The first warp's, beside the copy: the row's weight, the list and its logits (those of
-  // other parts too, before a CTA can have written its gradient there).
-  float w = 0.f, lpr = 0.f;
-  int32_t strange = -1;  // an id >= vocab
-  Entries<E> e;
+  // Beside the copy: the row's weight and its list (its logits in other parts, too: they are
+  // here before this CTA's message leaves, and only then may another write its gradient in
+  // their place, or set back the count behind the weight).
   if (early) pdl_wait();
-  if (wid == 0) {
-    const uint64_t at = t * lists.top;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const uint32_t k = lane + 32 * i;
-      e.id[i] = k < lists.top ? lists.ids[at + k] : -1;
-      e.lp[i] = k < lists.top ? lists.value[at + k] : kNegInf;
-    }
-    if (lists.rest) lpr = lists.rest[t];
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (e.lp[i] == kNegInf) e.id[i] = -1;
-      if (e.id[i] >= 0 && (uint32_t)e.id[i] >= a.vocab) {
-        strange = e.id[i];
-        e.id[i] = -1;
-      }
-      e.z[i] = e.id[i] >= 0 ? to_f32(row[e.id[i]]) : kNegInf;
-    }
-    if (by_range) {
-      const Range r = token_range(weights.set);
-      w = 1.f / (float)(r.end - r.first);
-    } else {
-      w = row_weight(weights, t);
-    }
-    if (!lists.rest) {  // the list's own softmax
-      float m = kNegInf, s = 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (e.id[i] >= 0) m = fmaxf(m, e.lp[i]);
-      m = warp_max(m);
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        e.lp[i] = (e.lp[i] - m) * rule.inv_tt;
-        s += e.id[i] >= 0 ? expf(e.lp[i]) : 0.f;
-      }
-      const float ln = logf(warp_add(s));
-#pragma unroll
-      for (int i = 0; i < E; ++i) e.lp[i] -= ln;
-    }
-  }
+  const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
+  Entry e;
+  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
   if (sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
     if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
     mbar_wait(&bar, 0, kRowWaitNs);  // bounded: the copy lands before the CTA ends
   }
+  // Each entry leaves its number in its place, looks whether it is still there (-infinity is
+  // no entry's number), and takes itself out of the row.
+  const bool here = e.id >= 0 && (uint32_t)e.id - first < n;
+  Bits *place = reinterpret_cast<Bits *>(held) + (here ? (uint32_t)e.id - first : 0);
+  if (here) *place = (Bits)threadIdx.x;
   __syncthreads();
-  bool twice = false;
-  if (wid == 0) {
-    // Each entry leaves its number in its place and looks whether it is still there.
-    Bits *place = reinterpret_cast<Bits *>(held);
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0 && (uint32_t)e.id[i] - first < n)
-        place[(uint32_t)e.id[i] - first] = (Bits)(lane + 32 * i);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0 && (uint32_t)e.id[i] - first < n)
-        twice |= place[(uint32_t)e.id[i] - first] != (Bits)(lane + 32 * i);
-    twice = __any_sync(kAllLanes, twice);
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (e.id[i] >= 0 && (uint32_t)e.id[i] - first < n)
-        held[(uint32_t)e.id[i] - first] = from_f32<T>(kNegInf);
+  if (here) {
+    if (*place != (Bits)threadIdx.x) twice = true;
+    held[(uint32_t)e.id - first] = from_f32<T>(kNegInf);
   }
   __syncthreads();
-  float weighted = 0.f;
-  // The first warp joins the CTA's sums, gives them to the cluster's other CTAs and
-  // takes theirs, and makes of all what the part's gradient needs.
-  auto finish = [&](auto fused, int round) {
+  // The first warp joins the CTA's sums, gives them to the cluster's other CTAs and takes
+  // theirs.
+  auto join = [&](auto fused, int round) {
     constexpr bool FUSED = decltype(fused)::value;
     RowSum sum = warp_sum<T, FUSED, lanes_for(NT / 32)>(
         lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
-    bool whole = true;
-    float M = kNegInf;  // of the list, then of the row
-#pragma unroll
-    for (int i = 0; i < E; ++i) M = fmaxf(M, e.z[i]);
-    M = warp_max(M);
+    bool all = true, again = twice;
     if (np > 1) {
-      // The weight (negative: a token twice) and the list's maximum go along so that the
-      // message leaves after they were read: once it is there, the row's first CTA may set
-      // the count behind the weight back, and others write gradients over the list's logits.
       const float4 mine = make_float4(__shfl_sync(kAllLanes, sum.m, 0),
-                                      __shfl_sync(kAllLanes, sum.s, 0), twice ? -w : w, M);
+                                      __shfl_sync(kAllLanes, sum.s, 0), 0.f, again ? 1.f : 0.f);
       if (lane < np) send_float4(&parts[round][part], mine, &sent[round], lane);
       if (!mbar_wait(&sent[round], 0, kRowWaitNs)) {
         if (lane == 0) flag(ctrl, DEVERR_TIMEOUT, t);
-        whole = mbar_wait(&sent[round], 0, kRowWaitNs);  // none of them comes after the end
+        all = mbar_wait(&sent[round], 0, kRowWaitNs);  // none of them comes after the end
       }
-      whole = __all_sync(kAllLanes, whole);
+      all = __all_sync(kAllLanes, all);
       const float4 x = lane < np ? parts[round][lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
-      twice = __any_sync(kAllLanes, signbit(x.z));
+      again = __any_sync(kAllLanes, x.w != 0.f);
       sum = warp_sum<T, FUSED, 8>(RowSum{x.x, x.y, 0.f}, a.c);
-      sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0), 0.f};
-    } else {
-      sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0), 0.f};
     }
     if (FUSED) sum = exact_sums<T>(sum, a.c);
-    if (FUSED && !sums_hold(sum.m, a.c)) {
-      if (lane == 0) rest = Rest::kCareful;
-      return;
-    }
-    M = fmaxf(M, sum.m);
-    bool nan = sum.s != sum.s;
-#pragma unroll
-    for (int i = 0; i < E; ++i) nan |= e.z[i] != e.z[i];
-    nan = __any_sync(kAllLanes, nan);
-    const bool none = M == kNegInf && !nan;  // no token has a probability
-    const uint32_t wrong = __ballot_sync(kAllLanes, strange >= 0);
-    if (part == 0) {
-      if (strange >= 0 && lane == __ffs(wrong) - 1)
-        flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)strange);
-      if (lane == 0 && twice) flag(ctrl, DEVERR_TWICE, t);
-      if (lane == 0 && none) flag(ctrl, DEVERR_ROW, t);
-    }
-    const bool zero = none || wrong || twice || !whole;
-    const Classes o = classes<E>(rule, e, lists.rest != nullptr, lpr, sum, M, a.c, a.inv_t);
-    const float by = rule.grad_scale * w * a.inv_t;
-#pragma unroll
-    for (int i = 0; i < E; ++i) e.z[i] *= by;
-    weighted = zero ? 0.f : w * o.loss;
+    const RowSums r = row_sums(l, sum, a.c, a.inv_t);
+    const RowLoss f = rule.kind == EDP_DISTILL_MIX ? RowLoss{}
+                                                   : row_loss_of(rule.kind, l, r, lpr, pr);
     if (lane) return;
-    if (part == 0 && row_loss) row_loss[t] = zero ? 0.f : o.loss;
-    rest = zero ? Rest::kZero : Rest::kGrad;
-    // without a finite logit outside of the list there is no maximum to be relative to, and
-    // each 2^y is 0
-    grad.m = sum.m == kNegInf ? 0.f : sum.m;
-    grad.a = by * o.outside;
-    grad.b = grad.at = 0.f;
+    careful = FUSED && !sums_hold(sum.m, a.c);
+    rows = r;
+    found = f;
+    twice = again;
+    zero = r.none || list.strange >= 0 || again || !all;
   };
   RowSum sum = warp_sum<T, F>(part_sum<T, false, F, NT>(held, n, a.c), a.c);
   if (lane == 0) red[wid] = sum;
   if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
   __syncthreads();
-  if (wid == 0) finish(std::integral_constant<bool, F>{}, 0);
+  if (wid == 0) join(std::integral_constant<bool, F>{}, 0);
   __syncthreads();
-  if (F && rest == Rest::kCareful) {  // rare: again, the careful way
+  if (F && careful) {  // rare: again, the careful way
     sum = warp_sum<T, false>(part_sum<T, false, false, NT>(held, n, a.c), a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
-    if (wid == 0) finish(std::false_type{}, 1);
+    if (wid == 0) join(std::false_type{}, 1);
     __syncthreads();
   }
-  if (BACK) {
-    if (rest == Rest::kZero) {
-      part_zero<T, NT>(d, n);
-    } else {
-      part_grad_any<T, false, NT>(held, d, n, n, grad, a.c);
-      __syncthreads();  // before the entries take their places
-      if (wid == 0) {
+  const RowSums r = rows;
+  RowLoss f = found;
+  float mine;  // the entry's gradient before the weight
+  if (rule.kind == EDP_DISTILL_FORWARD) {
+    mine = fmaf(f.g, e.e * r.by, -e.p);
+  } else if (rule.kind == EDP_DISTILL_REVERSE) {
+    mine = weigh(e.e * r.by, e.x - r.ln - e.lp - f.g);
+  } else {
+    float lm = 0.f;
+    f = mix_loss(rule, lists, e, r, lpr, pr, &list, &lm);
+    mine = weigh(e.e * r.by, fmaf(rule.alpha, e.x - r.ln - lm, -f.g));
+  }
+  if (part == 0 && threadIdx.x == 0) {
+    if (list.strange >= 0)
+      flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)list.strange);
+    if (twice) flag(ctrl, DEVERR_TWICE, t);
+    if (r.none) flag(ctrl, DEVERR_ROW, t);
+    if (row_loss) row_loss[t] = zero ? 0.f : f.loss;
+  }
+  if (zero) {
+    part_zero<T, NT>(d, n);
+  } else {
+    const float by = rule.grad_scale * list.weight * a.inv_t;
+    // without a finite logit outside of the list there is no maximum to be relative to,
+    // and each 2^y is 0
+    const RowGrad g{r.m == kNegInf ? 0.f : r.m, r.s == 0.f ? 0.f : by * (f.outside / r.s), 0.f,
+                    0.f};
+    part_grad_any<T, false, NT>(held, d, n, n, g, a.c);
+    __syncthreads();  // before the entries take their places
+    if (here) d[(uint32_t)e.id - first] = from_f32<T>(by * mine);
+  }
+  if (part == 0) conclude<NT>(zero ? 0.f : list.weight * f.loss, per_row, loss, ctrl);
+}
+
+// The loss alone: the row is streamed, and read once too.  A vector with an entry in it is
+// left out of the sums; the first of its entries adds what else there is in it.  All is
+// relative to the list's maximum (no maximum is kept), which is near the row's, most likely:
+// sums that leave fp32 are made again, carefully.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, kStreamLanes / NT)
+k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, DistillRule rule,
+               float *loss, float *row_loss, float *per_row, uint32_t words, bool early,
+               Ctrl *ctrl) {
+  constexpr bool F = kFused<T>;
+  constexpr int N = Vec16<T>::kN;
+  extern __shared__ uint4 shared_words[];
+  __shared__ __align__(16) int32_t ids[128];
+  __shared__ RowSum red[NT / 32];
+  __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S
+  __shared__ ListRoom list;
+  __shared__ uint32_t singles;         // entries before and behind the vectors
+  __shared__ bool twice;
+  __shared__ unsigned long long sent;
+  const uint64_t t = blockIdx.x;
+  const uint32_t part = blockIdx.y, np = gridDim.y;
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  uint4 *ring = shared_words;
+  uint32_t *marks = reinterpret_cast<uint32_t *>(ring + kStages * kUnroll * NT);  // [words]
+  if (threadIdx.x == 0) {
+    if (np > 1) {
+      mbar_init(&sent, 1);
+      if (part == 0) mbar_arrive_tx(&sent, np * sizeof(float4));
+      mbar_init_fence();
+    }
+    list.strange = -1;
+    singles = 0;
+    twice = false;
+  }
+  for (uint32_t i = threadIdx.x; i < words; i += NT) marks[i] = 0;
+  __syncthreads();
+  if (!early) pdl_wait();  // as in k_distill
+  pdl_launch();
+  if ((a.mask && !a.mask[t]) || !in_sequences(weights, t)) {
+    if (early) pdl_wait();
+    if (part) return;
+    if (row_loss && threadIdx.x == 0) row_loss[t] = 0.f;
+    conclude<NT>(0.f, per_row, loss, ctrl);
+    return;  // the whole cluster
+  }
+  uint32_t first, n;
+  row_part(a.vocab, part, np, &first, &n);
+  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+  const Part<T, NT> x(row + first, first, n);
+  x.start(ring);
+  if (np > 1) cluster_started();
+  if (early) pdl_wait();
+  const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
+  Entry e;
+  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
+  // Marks: a bit for each vector with an entry, and for each other number that is one.
+  const uint32_t place = (uint32_t)e.id - first - x.sp.head;  // among the vectors' numbers
+  const bool here = e.id >= 0 && (uint32_t)e.id - first < n, inside = here && place < x.sp.vecs * N;
+  if (threadIdx.x < 128) ids[threadIdx.x] = e.id;
+  if (inside) atomicOr(&marks[place / N / 32], 1u << (place / N & 31));
+  else if (here)
+    atomicOr(&singles, 1u << ((uint32_t)e.id - first < x.sp.head ? (uint32_t)e.id - first
+                                                                  : (uint32_t)e.id - first -
+                                                                        x.sp.vecs * N));
+  __syncthreads();
+  // The vector of an entry without its entries, by the first of them; others have none.
+  bool mine = inside;
+  uint4 rest_of = no_logits<T>();
+  if (e.id >= 0) {
+    const uint32_t begin = (uint32_t)e.id - place % N;
+    uint32_t bits = 0;
+    bool again = false;
+#pragma unroll 2
+    for (uint32_t j = 0; j < lists.top; j += 4) {
+      const int4 four = *reinterpret_cast<const int4 *>(ids + j);
 #pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (e.id[i] >= 0 && (uint32_t)e.id[i] - first < n)
-            d[(uint32_t)e.id[i] - first] = from_f32<T>(e.z[i]);
+      for (uint32_t k = 0; k < 4; ++k) {
+        const int32_t id = k == 0 ? four.x : k == 1 ? four.y : k == 2 ? four.z : four.w;
+        const uint32_t d = (uint32_t)id - begin;
+        if (d < N) {
+          bits |= 1u << d;
+          mine &= j + k >= threadIdx.x;
+        }
+        again |= id == e.id && j + k != threadIdx.x;
       }
     }
+    if (again) twice = true;
+    if (mine) {
+      rest_of = x.vec(place / N);
+      T *z = reinterpret_cast<T *>(&rest_of);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (bits >> i & 1) z[i] = from_f32<T>(kNegInf);
+    }
   }
-  if (part == 0) conclude(weighted, per_row, loss, ctrl);
+  const bool alone = x.single() && !(singles >> threadIdx.x & 1);
+  const float single = alone ? to_f32(x.p[x.single_at()]) : kNegInf;
+  RowSum sum;
+  bool careful = !(fabsf(l.m) < __builtin_huge_valf()) || (F && !sums_hold(l.m, a.c));
+  if (!careful) {
+    const RowLog<T, F> log(l.m, a.c);
+    F2 s(0.f), u(0.f);
+    if (alone) add_one<T, false, F>(s, u, log, single);
+    add_vector<T, false, F>(s, u, rest_of, log);
+    for (uint32_t g = 0; g < x.rounds; ++g) {
+      async_wait<kStages - 1>();
+      uint4 w[kUnroll];
+      x.load(w, ring, g);
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const uint32_t mark = marks[(k * (NT / 32) + wid) * x.rounds + g];
+        if (mark && mark >> lane & 1) w[k] = no_logits<T>();
+        add_vector<T, false, F>(s, u, w[k], log);
+      }
+      x.fetch(ring, g + kStages);
+    }
+    sum = warp_sum<T, false>(RowSum{l.m, s.x() + s.y(), 0.f}, a.c);
+    if (lane == 0) red[wid] = sum;
+    __syncthreads();
+    sum = exact_sums<T>(
+        warp_sum<T, false, lanes_for(NT / 32)>(
+            lane < (NT / 32) ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c), a.c);
+    const float S = __shfl_sync(kAllLanes, sum.s, 0);
+    careful = !(S >= kLeastSum && S < __builtin_huge_valf());
+    if (careful) __syncthreads();
+  }
+  if (careful) {
+    LaneSum b{kNegInf, F2(0.f), F2(0.f)};
+    auto take = [&](const uint4 &w) {
+      const uint4 v[1] = {w};
+      take_vectors<T, false, false>(b, v, a.c);
+    };
+    if (alone) add_one<T, false, false>(b.s, b.u, raise<T, false, false>(b, single, a.c), single);
+    take(rest_of);
+    x.each_vector(ring, [&](const uint4 &w, uint32_t i) {
+      if (!(marks[i / 32] >> (i & 31) & 1)) take(w);
+    });
+    sum = warp_sum<T, false>(row_sum(b), a.c);
+    if (lane == 0) red[wid] = sum;
+    __syncthreads();
+    sum = warp_sum<T, false, lanes_for(NT / 32)>(
+        lane < (NT / 32) ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+  }
+  bool whole = true;
+  if (np > 1) {
+    cluster_wait();  // every CTA has started, so that its shared memory is there
+    if (threadIdx.x == 0)
+      send_float4(&sums[part], make_float4(sum.m, sum.s, 0.f, 0.f), &sent, 0);
+    if (part) return;
+    whole = mbar_wait(&sent, 0, kRowWaitNs);
+    if (!whole) {
+      if (lane == 0) flag(ctrl, DEVERR_TIMEOUT, t);
+      whole = mbar_wait(&sent, 0, kRowWaitNs);  // none of them comes after the end
+    }
+    whole = __syncthreads_and(whole);
+    const float4 y = lane < np ? sums[lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
+    sum = warp_sum<T, false, 8>(RowSum{y.x, y.y, 0.f}, a.c);
+  }
+  sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0), 0.f};
+  const RowSums r = row_sums(l, sum, a.c, a.inv_t);
+  RowLoss f;
+  if (rule.kind == EDP_DISTILL_MIX) {
+    float lm;
+    f = mix_loss(rule, lists, e, r, lpr, pr, &list, &lm);
+  } else {
+    f = row_loss_of(rule.kind, l, r, lpr, pr);
+  }
+  const bool zero = r.none || list.strange >= 0 || twice || !whole;
+  if (threadIdx.x == 0) {
+    if (list.strange >= 0)
+      flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)list.strange);
+    if (twice) flag(ctrl, DEVERR_TWICE, t);
+    if (r.none) flag(ctrl, DEVERR_ROW, t);
+    if (row_loss) row_loss[t] = zero ? 0.f : f.loss;
+  }
+  conclude<NT>(zero ? 0.f : list.weight * f.loss, per_row, loss, ctrl);
 }
 
 }  // namespace
@@ -424,26 +613,44 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
   rule.grad_scale = (float)cfg.grad_scale;
   e = by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
+    if (!dz) {
+      const StreamShape shape = stream_shape(ctx, z, true);
+      return by_threads(shape.threads, [&](auto threads) {
+        constexpr int NT = decltype(threads)::value;
+        constexpr uint64_t round = kUnroll * (NT / 32);  // segments
+        const uint32_t words = (uint32_t)(((shape.vecs + 8) / 32 / round + 1) * round);
+        const size_t bytes = sizeof(uint4) * kStages * kUnroll * NT + 4 * words;
+        auto kern = k_distill_eval<T, NT>;
+        const cudaError_t err = cudaFuncSetAttribute(
+            kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+        if (err != cudaSuccess) return err;
+        return launch_rows(kern, z.rows, shape.parts, true, NT, bytes, s, row_args(z), w,
+                           p.w.by_range, lists, rule, loss, row_loss, p.per_token, words, p.early,
+                           ctx->ctrl);
+      });
+    }
     uint32_t parts = row_parts(ctx, z, 2);
     while (parts < 8 && part_bytes(z, parts) > kResidentPart) parts *= 2;
     // few rows: smaller parts, so that the last of them are a small share
     while (parts < 8 && z.rows * parts < 8ull * ctx->coop_sms && part_bytes(z, parts) > kLeastPart)
       parts *= 2;
-    auto go = [&](auto kern) {
+    const size_t bytes = part_bytes(z, parts);
+    auto go = [&](auto threads) {
+      constexpr int NT = decltype(threads)::value;
+      auto kern = k_distill<T, NT>;
       const cudaError_t err = cudaFuncSetAttribute(
           kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
       if (err != cudaSuccess) return err;
-      return launch_rows(kern, z.rows, parts, true, kThreads, part_bytes(z, parts), s,
-                         row_args(z), w, p.w.by_range, lists, rule, loss, row_loss, p.per_token,
-                         dz, dstride, p.early, ctx->ctrl);
+      return launch_rows(kern, z.rows, parts, true, NT, bytes, s, row_args(z), w, p.w.by_range,
+                         lists, rule, loss, row_loss, p.per_token, dz, dstride, p.early,
+                         ctx->ctrl);
     };
-    auto wide = [&](auto entries) {
-      constexpr int E = decltype(entries)::value;
-      return dz ? go(k_distill<T, true, E>) : go(k_distill<T, false, E>);
-    };
-    if (top <= 32) return wide(std::integral_constant<int, 1>{});
-    if (top <= 64) return wide(std::integral_constant<int, 2>{});
-    return wide(std::integral_constant<int, 4>{});
+    // as many CTAs per SM as its shared memory and kLanes allow alike
+    if (z.rows * parts <= (uint64_t)ctx->coop_sms) return go(std::integral_constant<int, 256>{});
+    if (bytes > 55 * 1024) return go(std::integral_constant<int, 384>{});
+    if (bytes > 36 * 1024) return go(std::integral_constant<int, 256>{});
+    if (bytes > 24 * 1024) return go(std::integral_constant<int, 192>{});
+    return go(std::integral_constant<int, 128>{});
   });
   if (e != cudaSuccess) forget_count(ctx, p, s);
   return e;

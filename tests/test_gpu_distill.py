@@ -205,7 +205,13 @@ def test_parts_of_rows(edp_lib, dtype, kind, rest, vocab, rows, top):
     loss, each = c.run(edp, ring, d)
     edp.edp_sync(ring.ctx)
     c.check(loss, each, d)
-    # the same numbers whatever order the threads ran in, and in the logits' place
+    # the loss alone, twice: the same numbers whatever order the threads ran in
+    alone, one = c.run(edp, ring)
+    edp.edp_sync(ring.ctx)
+    c.check(alone, one)
+    alone2, one2 = c.run(edp, ring)
+    assert torch.equal(alone, alone2) and torch.equal(one, one2)
+    # the same with the gradient, and in the logits' place
     again, each2 = c.run(edp, ring, c.v)
     edp.edp_sync(ring.ctx)
     assert torch.equal(loss, again) and torch.equal(each, each2) and torch.equal(d, c.v)
@@ -288,15 +294,41 @@ def test_excluded_tokens(edp_lib, dtype, vocab, kind, rest):
     c.v.copy_(torch.from_numpy(c.zd))
     _, d = view(3, vocab, dtype)
     loss, each = c.run(edp, ring, d)
+    alone, one = c.run(edp, ring)
     edp.edp_sync(ring.ctx)
     if kind == L.FORWARD:
         assert each[2] == float("inf") and loss[0] == float("inf")
+        assert one[2] == float("inf") and alone[0] == float("inf")
         _, bg = c.bounds()
         _, _, grad = c.expect()
         assert np.all(np.abs(to_np(d.double()) - grad) <=
                       bg + UNIT[dtype] * (np.abs(grad) + bg) + LEAST[dtype])
     else:
         c.check(loss, each, d)
+        c.check(alone, one)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind,rest", KINDS)
+@pytest.mark.parametrize("how", ["list below", "list far below", "list far above", "neighbours"])
+@pytest.mark.parametrize("rows,vocab", [(2, 3_001), (3, 70_000), (160, 9_000)])
+def test_lists_beside_the_row(edp_lib, dtype, kind, rest, how, rows, vocab):
+    """Lists whose tokens are not the likely ones, and lists of tokens side by side (several
+    to a vector, at the row's ends too)."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    keep = np.arange(rows) < 3
+    c = Case(rows, vocab, 90, dtype, kind, rest, 5, absent=False, keep=keep)
+    if how == "neighbours":
+        for t in range(rows):
+            a = [0, vocab - 90, vocab // 2][t % 3]
+            c.ids[t] = np.random.default_rng(t).permutation(np.arange(a, a + 90))
+    else:
+        by = {"list below": -20, "list far below": -150, "list far above": 130}[how]
+        for t in range(rows):
+            c.zd[t, c.ids[t]] = by + np.arange(90) / 30
+    c.v.copy_(torch.from_numpy(c.zd))
+    c.zd = to_np(c.v.double())
+    c.all(edp, ring)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
@@ -326,16 +358,23 @@ def test_special_values(edp_lib, dtype, vocab, kind, rest):
     assert np.isnan(e[:5]).all() and np.isnan(to_np(loss)[0])
     assert np.isnan(g[:5]).all()
     assert not e[5:8].any() and not g[5:8].any()
+    _, alone = c.run(edp, ring)
+    status, msg = edp.edp_sync_status(ring.ctx)
+    assert status == edp.EDP_ERR_INVALID and "out of range" in msg
+    alone = to_np(alone.double())[:10]
+    assert np.isnan(alone[:5]).all() and not alone[5:8].any()
     want, rows_want, grad = c.expect_rows([8, 9])
     be, bg = want
     assert np.all(np.abs(e[8:] - rows_want) <= be + 1e-6 * np.abs(rows_want))
+    assert np.all(np.abs(alone[8:] - rows_want) <= be + 1e-6 * np.abs(rows_want))
     assert np.all(np.abs(g[8:] - grad) <= bg + UNIT[dtype] * (np.abs(grad) + bg) + LEAST[dtype])
     for rows, word in (([5, 9], "twice"), ([7, 9], "-infinity")):
         c.keep = np.isin(np.arange(10), rows)
         c.masked = True
-        c.run(edp, ring, d)
-        status, msg = edp.edp_sync_status(ring.ctx)
-        assert status == edp.EDP_ERR_INVALID and word in msg and "row %d" % rows[0] in msg
+        for out in (d, None):
+            c.run(edp, ring, out)
+            status, msg = edp.edp_sync_status(ring.ctx)
+            assert status == edp.EDP_ERR_INVALID and word in msg and "row %d" % rows[0] in msg
         assert not d[rows[0]].any()
     c.keep = np.arange(10) == 9
     loss, each = c.run(edp, ring, d)
