@@ -792,8 +792,8 @@ typedef struct {
  *   dL/dlogits of the type of the logits, 0 in the rows left out
  * p is taken as it is given, whatever it sums to.  loss (float [1]) = L;
  * row_loss (float [rows], or NULL) = l_t before its weight.  mask, off, n_seq and
- * the tokens outside them as for edp_policy_loss; a list of a row left out is not
- * read.  dlogits may be NULL (the loss alone), or the logits' own array (with
+ * the tokens outside them as for edp_policy_loss; lists of rows left out may hold
+ * anything.  dlogits may be NULL (the loss alone), or the logits' own array (with
  * dstride == stride).
  * A list that holds a token twice, or an id >= vocab, and a row whose logits are
  * all -infinity add 0 to the loss, have gradient 0 and are reported by edp_sync

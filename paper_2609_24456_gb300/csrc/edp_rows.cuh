@@ -242,6 +242,24 @@ __device__ __forceinline__ RowSum part_sum(const T *p, uint32_t n, float c) {
   return {a.m, a.s.x() + a.s.y(), a.u.x() + a.u.y()};
 }
 
+// The sum alone, relative to a number that is known.
+template <typename T, bool FUSED, int NT>
+__device__ __forceinline__ float part_sum_near(const T *p, uint32_t n,
+                                               const RowLog<T, FUSED> &log) {
+  const Span<T> sp(p, n);
+  F2 s(0.f), u;
+  if (threadIdx.x < sp.head + sp.tail) {
+    const uint32_t i =
+        threadIdx.x < sp.head ? threadIdx.x : threadIdx.x + sp.vecs * Vec16<T>::kN;
+    s = F2(ex2(log.of(to_f32(p[i]))), 0.f);
+  }
+  const uint4 *q = reinterpret_cast<const uint4 *>(p + sp.head);
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < sp.vecs; i += NT)
+    add_vector<T, false, FUSED>(s, u, q[i], log);
+  return s.x() + s.y();
+}
+
 // The two halves of a barrier of the cluster (all of whose CTAs are resident, so
 // that each arrives without waiting for another).
 __device__ __forceinline__ void cluster_arrive() {

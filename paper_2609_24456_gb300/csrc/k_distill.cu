@@ -115,6 +115,17 @@ __device__ __forceinline__ RowLoss row_loss_of(uint32_t kind, const ListSums &l,
   return {all, weigh(r.qr, r.lqr - lpr - all), all};
 }
 
+// An entry as the list has it; asked for before anything else of the row is known.
+__device__ __forceinline__ Entry load_entry(const TeacherLists &lists, uint64_t t) {
+  Entry e{-1, kNegInf, 0.f, kNegInf, 0.f};
+  if (threadIdx.x < lists.top) {
+    const uint64_t at = t * lists.top + threadIdx.x;
+    e.id = lists.ids[at];
+    e.lp = lists.value[at];
+  }
+  return e;
+}
+
 // Shared memory of the list's phase.
 struct ListRoom {
   float2 sums[4][4];  // of list_sums, of each call its own
@@ -129,6 +140,21 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
                                               const DistillRule &rule, const T *row, uint64_t t,
                                               Entry *entry, ListRoom *s) {
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const uint32_t warps = (lists.top + 31) / 32;
+  const bool busy = wid < warps, has_rest = lists.rest != nullptr;
+  Entry e = *entry;
+  ListSums l{kNegInf, 0.f, 0.f, 0.f};
+  if (busy) {
+    if (e.lp == kNegInf) e.id = -1;
+    if (e.id >= 0 && (uint32_t)e.id >= a.vocab) {
+      s->strange = e.id;
+      e.id = -1;
+    }
+    const float z = e.id >= 0 ? to_f32(row[e.id]) : kNegInf;
+    e.x = z;
+    const float m = warp_max(z), v = warp_max(e.id >= 0 ? e.lp : kNegInf);
+    if (lane == 0) s->sums[0][wid] = make_float2(m, v);
+  }
   if (wid == NT / 32 - 1) {
     float w;
     if (by_range) {
@@ -138,27 +164,6 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
       w = row_weight(weights, t);
     }
     if (lane == 0) s->weight = w;
-  }
-  const uint32_t warps = (lists.top + 31) / 32;
-  const bool busy = wid < warps, has_rest = lists.rest != nullptr;
-  Entry e{-1, kNegInf, 0.f, kNegInf, 0.f};
-  ListSums l{kNegInf, 0.f, 0.f, 0.f};
-  if (busy) {
-    float z = kNegInf;
-    if (threadIdx.x < lists.top) {
-      const uint64_t at = t * lists.top + threadIdx.x;
-      e.id = lists.ids[at];
-      e.lp = lists.value[at];
-      if (e.lp == kNegInf) e.id = -1;
-      if (e.id >= 0 && (uint32_t)e.id >= a.vocab) {
-        s->strange = e.id;
-        e.id = -1;
-      }
-      if (e.id >= 0) z = to_f32(row[e.id]);
-    }
-    e.x = z;
-    const float m = warp_max(z), v = warp_max(e.id >= 0 ? e.lp : kNegInf);
-    if (lane == 0) s->sums[0][wid] = make_float2(m, v);
   }
   __syncthreads();
   float top_value = kNegInf;
@@ -286,6 +291,7 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
   // writes the weights alone
   if (!early) pdl_wait();
   pdl_launch();
+  Entry e = load_entry(lists, t);
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   T *d = reinterpret_cast<T *>(dz) + t * dstride + first;
@@ -316,7 +322,6 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
   // their place, or set back the count behind the weight).
   if (early) pdl_wait();
   const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
-  Entry e;
   const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
   if (sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
     if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
@@ -335,10 +340,10 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
   __syncthreads();
   // The first warp joins the CTA's sums, gives them to the cluster's other CTAs and takes
   // theirs.
-  auto join = [&](auto fused, int round) {
-    constexpr bool FUSED = decltype(fused)::value;
-    RowSum sum = warp_sum<T, FUSED, lanes_for(NT / 32)>(
-        lane < NT / 32 ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
+  auto join = [&](bool near, int round) {
+    const bool has = lane < NT / 32;
+    RowSum sum = warp_sum<T, false, lanes_for(NT / 32)>(
+        has ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c);
     bool all = true, again = twice;
     if (np > 1) {
       const float4 mine = make_float4(__shfl_sync(kAllLanes, sum.m, 0),
@@ -351,32 +356,35 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
       all = __all_sync(kAllLanes, all);
       const float4 x = lane < np ? parts[round][lane] : make_float4(kNegInf, 0.f, 0.f, 0.f);
       again = __any_sync(kAllLanes, x.w != 0.f);
-      sum = warp_sum<T, FUSED, 8>(RowSum{x.x, x.y, 0.f}, a.c);
+      sum = warp_sum<T, false, 8>(RowSum{x.x, x.y, 0.f}, a.c);
     }
-    if (FUSED) sum = exact_sums<T>(sum, a.c);
+    if (near) sum = exact_sums<T>(sum, a.c);
     const RowSums r = row_sums(l, sum, a.c, a.inv_t);
     const RowLoss f = rule.kind == EDP_DISTILL_MIX ? RowLoss{}
                                                    : row_loss_of(rule.kind, l, r, lpr, pr);
     if (lane) return;
-    careful = FUSED && !sums_hold(sum.m, a.c);
+    careful = near && !(sum.s >= kLeastSum && sum.s < __builtin_huge_valf());
     rows = r;
     found = f;
     twice = again;
     zero = r.none || list.strange >= 0 || again || !all;
   };
-  RowSum sum = warp_sum<T, F>(part_sum<T, false, F, NT>(held, n, a.c), a.c);
-  if (lane == 0) red[wid] = sum;
-  if (np > 1) cluster_wait();  // every CTA has started, so that its shared memory is there
-  __syncthreads();
-  if (wid == 0) join(std::integral_constant<bool, F>{}, 0);
-  __syncthreads();
-  if (F && careful) {  // rare: again, the careful way
-    sum = warp_sum<T, false>(part_sum<T, false, false, NT>(held, n, a.c), a.c);
+  auto whole_row = [&](const RowSum &sum, bool near, int round) {
     if (lane == 0) red[wid] = sum;
+    if (np > 1 && round == 0) cluster_wait();  // every CTA has started: its shared memory is there
     __syncthreads();
-    if (wid == 0) join(std::false_type{}, 1);
+    if (wid == 0) join(near, round);
     __syncthreads();
-  }
+  };
+  // Relative to the list's maximum, which is near the row's, most likely; what leaves fp32
+  // that way is summed again relative to each thread's own.
+  const bool near = fabsf(l.m) < __builtin_huge_valf() && (!F || sums_hold(l.m, a.c));
+  whole_row(near ? warp_sum<T, false>(
+                       RowSum{l.m, part_sum_near<T, F, NT>(held, n, RowLog<T, F>(l.m, a.c)), 0.f},
+                       a.c)
+                 : RowSum{kNegInf, 0.f, 0.f}, near, 0);
+  if (!near || careful)
+    whole_row(warp_sum<T, false>(part_sum<T, false, false, NT>(held, n, a.c), a.c), false, 1);
   const RowSums r = rows;
   RowLoss f = found;
   float mine;  // the entry's gradient before the weight
@@ -449,6 +457,7 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   __syncthreads();
   if (!early) pdl_wait();  // as in k_distill
   pdl_launch();
+  Entry e = load_entry(lists, t);
   if ((a.mask && !a.mask[t]) || !in_sequences(weights, t)) {
     if (early) pdl_wait();
     if (part) return;
@@ -464,7 +473,6 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   if (np > 1) cluster_started();
   if (early) pdl_wait();
   const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
-  Entry e;
   const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
   // Marks: a bit for each vector with an entry, and for each other number that is one.
   const uint32_t place = (uint32_t)e.id - first - x.sp.head;  // among the vectors' numbers
