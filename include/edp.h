@@ -802,8 +802,8 @@ typedef struct {
  * then NaN); NaN or +infinity in a row or its list makes loss and gradient NaN.
  * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, top outside
  * [1, 128], a NULL logits, ids, value or loss, REVERSE or MIX without rest, rows ==
- * 0, a vocabulary whose row takes more than 1.5 MiB (786,432 logits of 16 bits,
- * 393,216 of 32), logits and dlogits as for edp_policy_loss_logits, off and n_seq as
+ * 0, a vocabulary whose row takes more than 16 MiB (8,388,608 logits of 16 bits,
+ * 4,194,304 of 32), logits and dlogits as for edp_policy_loss_logits, off and n_seq as
  * for edp_policy_loss, or arrays outside device memory; EDP_ERR_OOM when the scratch
  * cannot be allocated. */
 EDP_API edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg,

@@ -14,8 +14,24 @@
 // so that every token outside of the list has the same factor of its 2^y.
 //
 // q_r = 1 - sum q_i would lose what it is of when the list holds nearly all: the entries
-// are taken out of the row (set to -infinity in shared memory) before its sums, which then
-// are those of the rest, relative to its own maximum; the entries join them afterwards.
+// are taken out of the row before its sums, which then are those of the rest; the entries
+// join them afterwards.
+//
+// With the gradient a row is read once, into the shared memory of a cluster, and its gradient
+// written once (k_distill); without it the row is streamed (k_distill_stream).  What takes
+// time besides the copies is made beside them, where it can be: a thread per entry reads the
+// list and sums what does not need the row.  The sums are relative to the list's maximum,
+// known by then (with a running maximum: 808 us where it now takes 761).
+//
+// What bounds it, at 6.79 TB/s of measured copy:
+//   8,192 x 152,064 bf16, 64 entries, a tenth masked   761 us   697 us to read and write once
+//   4,096 x 152,064 f16, 32 entries                    395 us   367 us
+//   2,048 x 152,064 bf16, the loss alone               107 us   92 us to read once
+//   515 x 32,003 f32, 100 entries, mixed              32.5 us   17.5 us: 2.3 waves of CTAs, whose
+//                                                               copies and sums hardly overlap
+//   16 x 32,003 bf16, 20 entries                       8.2 us   in a graph: a chain of loads (mask,
+//                                                               entry, its logit), one copy, the
+//                                                               cluster's join
 #include <cmath>
 
 #include "edp_stream.cuh"
@@ -25,6 +41,7 @@ namespace {
 
 // threads per SM, which bound the registers: three CTAs of 384, as parts of 76 KB allow
 constexpr int kLanes = 1152;
+constexpr uint32_t kTwoParts = 112 * 1024;  // bytes of a part, two of which fit an SM
 
 struct DistillRule {
   uint32_t kind;
@@ -217,6 +234,20 @@ __device__ __forceinline__ RowLoss mix_loss(const DistillRule &rule, const Teach
           weigh(r.qr, fmaf(rule.alpha, r.lqr - lmr, -g)), g};
 }
 
+// The gradient of the tokens outside of the list: a factor of their 2^y.  Without a finite
+// logit among them there is no maximum to be relative to, and each 2^y is 0.
+__device__ __forceinline__ RowGrad others_grad(const RowSums &r, const RowLoss &f, float by) {
+  return {r.m == kNegInf ? 0.f : r.m, r.s == 0.f ? 0.f : by * (f.outside / r.s), 0.f, 0.f};
+}
+// An entry's, before the weight.
+__device__ __forceinline__ float entry_grad(const DistillRule &rule, const Entry &e,
+                                            const RowSums &r, const RowLoss &f, float lm) {
+  const float q = e.e * r.by;
+  if (rule.kind == EDP_DISTILL_FORWARD) return fmaf(f.g, q, -e.p);
+  if (rule.kind == EDP_DISTILL_REVERSE) return weigh(q, e.x - r.ln - e.lp - f.g);
+  return weigh(q, fmaf(rule.alpha, e.x - r.ln - lm, -f.g));
+}
+
 // The weighted loss of a row, from one CTA of each row; the last of them adds up all
 // rows in a fixed order and leaves the counters at 0.
 template <int NT>
@@ -387,16 +418,8 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
     whole_row(warp_sum<T, false>(part_sum<T, false, false, NT>(held, n, a.c), a.c), false, 1);
   const RowSums r = rows;
   RowLoss f = found;
-  float mine;  // the entry's gradient before the weight
-  if (rule.kind == EDP_DISTILL_FORWARD) {
-    mine = fmaf(f.g, e.e * r.by, -e.p);
-  } else if (rule.kind == EDP_DISTILL_REVERSE) {
-    mine = weigh(e.e * r.by, e.x - r.ln - e.lp - f.g);
-  } else {
-    float lm = 0.f;
-    f = mix_loss(rule, lists, e, r, lpr, pr, &list, &lm);
-    mine = weigh(e.e * r.by, fmaf(rule.alpha, e.x - r.ln - lm, -f.g));
-  }
+  float lm = 0.f;
+  if (rule.kind == EDP_DISTILL_MIX) f = mix_loss(rule, lists, e, r, lpr, pr, &list, &lm);
   if (part == 0 && threadIdx.x == 0) {
     if (list.strange >= 0)
       flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)list.strange);
@@ -408,26 +431,23 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
     part_zero<T, NT>(d, n);
   } else {
     const float by = rule.grad_scale * list.weight * a.inv_t;
-    // without a finite logit outside of the list there is no maximum to be relative to,
-    // and each 2^y is 0
-    const RowGrad g{r.m == kNegInf ? 0.f : r.m, r.s == 0.f ? 0.f : by * (f.outside / r.s), 0.f,
-                    0.f};
-    part_grad_any<T, false, NT>(held, d, n, n, g, a.c);
+    part_grad_any<T, false, NT>(held, d, n, n, others_grad(r, f, by), a.c);
     __syncthreads();  // before the entries take their places
-    if (here) d[(uint32_t)e.id - first] = from_f32<T>(by * mine);
+    if (here) d[(uint32_t)e.id - first] = from_f32<T>(by * entry_grad(rule, e, r, f, lm));
   }
   if (part == 0) conclude<NT>(zero ? 0.f : list.weight * f.loss, per_row, loss, ctrl);
 }
 
-// The loss alone: the row is streamed, and read once too.  A vector with an entry in it is
+// The loss alone: the row is streamed, and read once too.  BACK: its gradient, with the
+// logits read a second time, for rows of which too little fits shared memory.  A vector with an entry in it is
 // left out of the sums; the first of its entries adds what else there is in it.  All is
 // relative to the list's maximum (no maximum is kept), which is near the row's, most likely:
 // sums that leave fp32 are made again, carefully.
-template <typename T, int NT>
+template <typename T, int NT, bool BACK>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
-k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, DistillRule rule,
-               float *loss, float *row_loss, float *per_row, uint32_t words, bool early,
-               Ctrl *ctrl) {
+k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
+                 DistillRule rule, float *loss, float *row_loss, float *per_row, void *dz, uint64_t dstride,
+                 uint32_t words, bool early, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   constexpr int N = Vec16<T>::kN;
   extern __shared__ uint4 shared_words[];
@@ -446,7 +466,7 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   if (threadIdx.x == 0) {
     if (np > 1) {
       mbar_init(&sent, 1);
-      if (part == 0) mbar_arrive_tx(&sent, np * sizeof(float4));
+      if (BACK || part == 0) mbar_arrive_tx(&sent, np * sizeof(float4));
       mbar_init_fence();
     }
     list.strange = -1;
@@ -458,15 +478,17 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   if (!early) pdl_wait();  // as in k_distill
   pdl_launch();
   Entry e = load_entry(lists, t);
+  uint32_t first, n;
+  row_part(a.vocab, part, np, &first, &n);
+  T *d = reinterpret_cast<T *>(dz) + t * dstride + first;
   if ((a.mask && !a.mask[t]) || !in_sequences(weights, t)) {
+    if (BACK) part_zero<T, NT>(d, n);
     if (early) pdl_wait();
     if (part) return;
     if (row_loss && threadIdx.x == 0) row_loss[t] = 0.f;
     conclude<NT>(0.f, per_row, loss, ctrl);
     return;  // the whole cluster
   }
-  uint32_t first, n;
-  row_part(a.vocab, part, np, &first, &n);
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
   const Part<T, NT> x(row + first, first, n);
   x.start(ring);
@@ -565,9 +587,12 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   bool whole = true;
   if (np > 1) {
     cluster_wait();  // every CTA has started, so that its shared memory is there
-    if (threadIdx.x == 0)
-      send_float4(&sums[part], make_float4(sum.m, sum.s, 0.f, 0.f), &sent, 0);
-    if (part) return;
+    if (wid == 0) {
+      const float4 own = make_float4(__shfl_sync(kAllLanes, sum.m, 0),
+                                     __shfl_sync(kAllLanes, sum.s, 0), 0.f, 0.f);
+      if (lane < (BACK ? np : 1)) send_float4(&sums[part], own, &sent, lane);
+    }
+    if (!BACK && part) return;
     whole = mbar_wait(&sent, 0, kRowWaitNs);
     if (!whole) {
       if (lane == 0) flag(ctrl, DEVERR_TIMEOUT, t);
@@ -580,21 +605,32 @@ k_distill_eval(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
   sum = {__shfl_sync(kAllLanes, sum.m, 0), __shfl_sync(kAllLanes, sum.s, 0), 0.f};
   const RowSums r = row_sums(l, sum, a.c, a.inv_t);
   RowLoss f;
+  float lm = 0.f;
   if (rule.kind == EDP_DISTILL_MIX) {
-    float lm;
     f = mix_loss(rule, lists, e, r, lpr, pr, &list, &lm);
   } else {
     f = row_loss_of(rule.kind, l, r, lpr, pr);
   }
   const bool zero = r.none || list.strange >= 0 || twice || !whole;
-  if (threadIdx.x == 0) {
+  if (part == 0 && threadIdx.x == 0) {
     if (list.strange >= 0)
       flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)list.strange);
     if (twice) flag(ctrl, DEVERR_TWICE, t);
     if (r.none) flag(ctrl, DEVERR_ROW, t);
     if (row_loss) row_loss[t] = zero ? 0.f : f.loss;
   }
-  conclude<NT>(zero ? 0.f : list.weight * f.loss, per_row, loss, ctrl);
+  if (BACK) {
+    if (zero) {
+      part_zero<T, NT>(d, n);
+    } else {
+      const float by = rule.grad_scale * list.weight * a.inv_t;
+      part_grad_any<T, false, NT>(row + first, d, n, n, others_grad(r, f, by), a.c);
+      __syncthreads();  // before the entries take their places
+      if (here) d[(uint32_t)e.id - first] = from_f32<T>(by * entry_grad(rule, e, r, f, lm));
+    }
+  }
+  if (part == 0)
+    conclude<NT>(zero ? 0.f : list.weight * f.loss, per_row, loss, ctrl);
 }
 
 }  // namespace
@@ -621,22 +657,27 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
   rule.grad_scale = (float)cfg.grad_scale;
   e = by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    if (!dz) {
+    auto stream = [&](auto back) {
+      constexpr bool BACK = decltype(back)::value;
       const StreamShape shape = stream_shape(ctx, z, true);
       return by_threads(shape.threads, [&](auto threads) {
         constexpr int NT = decltype(threads)::value;
         constexpr uint64_t round = kUnroll * (NT / 32);  // segments
         const uint32_t words = (uint32_t)(((shape.vecs + 8) / 32 / round + 1) * round);
         const size_t bytes = sizeof(uint4) * kStages * kUnroll * NT + 4 * words;
-        auto kern = k_distill_eval<T, NT>;
+        auto kern = k_distill_stream<T, NT, BACK>;
         const cudaError_t err = cudaFuncSetAttribute(
-            kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+            kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
         if (err != cudaSuccess) return err;
         return launch_rows(kern, z.rows, shape.parts, true, NT, bytes, s, row_args(z), w,
-                           p.w.by_range, lists, rule, loss, row_loss, p.per_token, words, p.early,
-                           ctx->ctrl);
+                           p.w.by_range, lists, rule, loss, row_loss, p.per_token, dz, dstride,
+                           words, p.early, ctx->ctrl);
       });
-    }
+    };
+    if (!dz) return stream(std::false_type{});
+    // Parts of which not two fit an SM are read twice.  1,000 rows of 262,144 fp32 logits
+    // (128 KB): 498 us so, 544 resident; 500 of 400,000 bfloat16 ones (98 KB): 215 and 156.
+    if (part_bytes(z, 8) > kTwoParts) return stream(std::true_type{});
     uint32_t parts = row_parts(ctx, z, 2);
     while (parts < 8 && part_bytes(z, parts) > kResidentPart) parts *= 2;
     // few rows: smaller parts, so that the last of them are a small share
@@ -653,7 +694,10 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
                          lists, rule, loss, row_loss, p.per_token, dz, dstride, p.early,
                          ctx->ctrl);
     };
-    // as many CTAs per SM as its shared memory and kLanes allow alike
+    // As many CTAs per SM as its shared memory and kLanes allow alike; few CTAs: more threads.
+    // Measured (us, parts x threads): 515 rows of 32,003 fp32: 37.4 as 4 x 192, 46.7 as 4 x 384,
+    // 42.6 as 4 x 256; of bfloat16 20.8 as 2 x 192, 26.6 as 2 x 384; 2,000 of 4,000: 17.6 as
+    // 1 x 128, 31.0 as 1 x 384; 64 of 152,064: 12.6 as 8 x 256, 17.5 as 8 x 384.
     if (z.rows * parts <= (uint64_t)ctx->coop_sms) return go(std::integral_constant<int, 256>{});
     if (bytes > 55 * 1024) return go(std::integral_constant<int, 384>{});
     if (bytes > 36 * 1024) return go(std::integral_constant<int, 256>{});

@@ -52,8 +52,8 @@ edp_status check_logits(edp_ctx *c, const char *who, const Logits &z, const void
   return EDP_OK;
 }
 
-// The kernel of the distillation loss holds a row in the shared memory of 8 CTAs at the most.
-constexpr uint64_t kMostRowBytes = 3ull << 19;
+// The distillation loss holds a bit for each 16 bytes of a row in a CTA's shared memory.
+constexpr uint64_t kMostRowBytes = 16ull << 20;
 
 edp_status check_top(edp_ctx *c, const char *who, uint32_t top) {
   if (top == 0 || top > 128) return fail(c, EDP_ERR_INVALID, "%s: need 0 < top <= 128", who);
@@ -218,7 +218,7 @@ edp_status edp_distill_loss(edp_ctx *ctx, const edp_distill_config *cfg, const v
   if (st == EDP_OK) st = check_top(ctx, "edp_distill_loss", top);
   if (st != EDP_OK) return st;
   if (vocab * size_of(dtype) > kMostRowBytes)
-    return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: a row of logits takes more than 1.5 MiB");
+    return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: a row of logits takes more than 16 MiB");
   if (!ids || !value || !loss)
     return fail(ctx, EDP_ERR_INVALID, "edp_distill_loss: NULL ids, value or loss");
   if (!device_arrays(ctx, {logits, ids, value, rest, mask, off, loss, row_loss, dlogits}))

@@ -412,12 +412,53 @@ def test_range_of_temperatures(edp_lib, dtype, kind, rest, T, vocab):
     c.all(edp, ring)
 
 
-@pytest.mark.parametrize("dtype,vocab", [("bf16", 786_432), ("f16", 786_431), ("f32", 393_216)])
-def test_largest_vocabularies(edp_lib, dtype, vocab):
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 327_600), ("f16", 500_001), ("f32", 163_900),
+                                         ("f32", 393_216)])
+@pytest.mark.parametrize("kind,rest", KINDS)
+def test_large_vocabularies(edp_lib, dtype, vocab, kind, rest):
     edp, ring = edp_lib, ctx_of(edp_lib)
-    Case(2, vocab, 128, dtype, L.MIX, True, 1, shift=3).all(edp, ring)
-    with pytest.raises(edp.EdpError, match="1.5 MiB"):
-        Case(1, vocab + 2, 8, dtype, L.MIX, True, 1).run(edp, ring)
+    c = Case(4, vocab, 128, dtype, kind, rest, 1, shift=3, keep=np.array([1, 0, 1, 1], bool))
+    c.v[1] = float("nan")
+    c.all(edp, ring)
+    _, d = view(4, vocab, dtype, shift=1)  # at other alignments, and in place
+    loss, each = c.run(edp, ring, d)
+    again, each2 = c.run(edp, ring, c.v)
+    edp.edp_sync(ring.ctx)
+    assert torch.equal(loss, again) and torch.equal(each, each2) and torch.equal(d, c.v)
+
+
+@pytest.mark.parametrize("dtype,vocab,rows", [("bf16", 8_388_608, 1), ("f32", 4_194_303, 1),
+                                              ("f32", 4_194_304, 160)])
+def test_largest_vocabularies(edp_lib, dtype, vocab, rows):
+    """One row that counts, of one and of many (a CTA then has the whole of it)."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    c = Case(1, vocab, 128, dtype, L.REVERSE, True, 1)
+    if rows == 1:
+        c.all(edp, ring)
+        _, more = view(1, vocab + 8, dtype)
+        c.v = more
+        with pytest.raises(edp.EdpError, match="16 MiB"):
+            c.run(edp, ring)
+        return
+    want, _, grad = c.expect()
+    be, bg = c.bounds()
+    at = rows - 2
+    ids = torch.zeros(rows, 128, dtype=torch.int32, device="cuda")
+    value = torch.zeros(rows, 128, device="cuda")
+    rest, mask = torch.zeros(rows, device="cuda"), torch.zeros(rows, dtype=torch.uint8,
+                                                               device="cuda")
+    ids[at], value[at], rest[at], mask[at] = cuda(c.ids)[0], cuda(c.value)[0], cuda(c.rest)[0], 1
+    z = torch.empty(rows, vocab, dtype=TYPES[dtype], device="cuda")
+    z[at] = c.v[0]
+    loss, d = torch.zeros(1, device="cuda"), torch.full_like(z, 7.0)
+    for out in (None, d):
+        edp.edp_distill_loss(ring.ctx, c.config(edp), z, ids, value, loss, rest=rest, mask=mask,
+                             dlogits=out)
+        edp.edp_sync(ring.ctx)
+        assert abs(float(loss) - want) <= be[0] + 1e-6 * abs(want)
+    assert np.all(np.abs(to_np(d[at].double()) - grad[0]) <=
+                  bg[0] + UNIT[dtype] * (np.abs(grad[0]) + bg[0]) + LEAST[dtype])
+    assert not d[:at].any() and not d[at + 1:].any()
 
 
 def test_offsets_beyond_32_bits(edp_lib):
