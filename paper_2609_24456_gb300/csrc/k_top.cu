@@ -62,6 +62,10 @@ struct Bound {
 struct Candidates {
   Key *list;
   uint32_t *count;
+  // too many already: the pass will be made again, whatever else it finds
+  __device__ __forceinline__ bool full() const {
+    return *const_cast<const volatile uint32_t *>(count) > kRoom;
+  }
   __device__ __forceinline__ void add(float v, uint32_t column) const {
     const uint32_t at = atomicAdd(count, 1u);
     if (at < kRoom) list[at] = key_of(v, column);
@@ -158,6 +162,7 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, B
     x.fetch(ring, g + kStages);
     if (__any_sync(kAllLanes, n > (g + 1 < x.rounds ? kNoted - kUnroll : 0))) {
       each_note(noted, n, [&](uint32_t note, uint32_t owner) {
+        if (to.full()) return;
         const uint32_t at = x.vec_at(note / kUnroll, note % kUnroll, owner);
         add_but<T, ENT, FUSED>(s, u, log, x.vec(at), x.column(at), b, to);
       });
@@ -194,52 +199,80 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
   return n;
 }
 
-// A bound that K to kRoom numbers hold, by halving from `lo` on (which K or more reach,
-// unless it is the lowest): or, where numbers are equal by the hundred, exactly K, with an end
-// among those equal to it, found by halving too.  Rare, so that it only has to end: 64 counts
-// at the most.
+// A bound that K to kRoom numbers hold, searched from `lo` on (which more reach, unless it is
+// the lowest) by counts: whether it is the K-th largest number itself (equal by the hundred, as
+// masked ones are), else the number by halving; and of those equal to it an end, by steps that
+// grow and by halving.  Rare, so that it only has to end: 64 counts at the most.
 template <typename T, int NT>
 __device__ __forceinline__ Bound search_bound(const Part<T, NT> &x, uint4 *ring, uint32_t n,
                                               uint32_t lo, uint32_t K, uint32_t *red) {
   constexpr uint32_t kAll = 0xffffffffu;
-  enum { kLowest, kValue, kColumn } look = lo == kLeastOrder ? kLowest : kValue;
-  uint32_t hi = 0xff800001u, some = kRoom + 1;  // nothing is above +infinity
-  uint32_t a = x.first, b = x.first + n;        // too few with the end a, enough with b
+  enum { kLowest, kAbove, kValue, kColumn } look = lo == kLeastOrder ? kLowest : kAbove;
+  uint32_t hi = 0xff800001u;              // nothing is above +infinity
+  uint32_t a = x.first, b = x.first + n;  // too few with the end a, enough with b
+  uint32_t step = 4 * K;
   for (;;) {
-    if (look == kValue && some <= kRoom) return {of_order(lo), kAll};
     if (look == kValue && hi - lo <= 1) look = kColumn;
     if (look == kColumn && b - a <= 1) return {of_order(lo), b};
     const uint32_t mid = look == kValue ? lo + (hi - lo) / 2 : lo;
-    const uint32_t column = look == kColumn ? a + (b - a) / 2 : kAll;
+    const uint32_t column = look == kAbove    ? 0
+                            : look == kColumn ? a + min(step, (b - a) / 2)
+                                              : kAll;
     const Bound probe{of_order(mid), column};
     uint32_t c = 0;
     x.each(ring, [&](float v, uint32_t at) { c += probe.holds(v, at); });
     c = cta_count<NT>(c, red);
-    if (look == kColumn) {
-      (c >= K ? b : a) = column;
-    } else if (c >= K) {
-      lo = mid;
-      some = c;
+    if (look != kAbove && c >= K && c <= kRoom) return probe;
+    if (look == kLowest) {
+      if (c < K) return probe;
+      look = kAbove;
+    } else if (look == kAbove) {
+      if (c < K) hi = lo + 1;
       look = kValue;
-    } else if (look == kLowest) {
-      return probe;
+    } else if (look == kValue) {
+      (c >= K ? lo : hi) = mid;
     } else {
-      hi = mid;
+      (c >= K ? b : a) = column;
+      step = c >= K ? kAll : 8 * min(step, n);
     }
   }
 }
 
-// The r-th largest (MAX) or smallest of a warp's numbers, r <= 32; ties by lane.
-template <bool MAX>
-__device__ __forceinline__ uint32_t warp_nth(uint32_t x, uint32_t r) {
-  const uint32_t lane = threadIdx.x & 31;
-  uint32_t best = 0;
+// The place of x among the numbers of all threads, the largest first, equal ones in any order
+// of their own.  runs: NT numbers, which then hold each warp's in order.
+template <int NT>
+__device__ __forceinline__ uint32_t place_of(uint32_t *x, uint32_t *runs) {
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+#pragma unroll
+  for (uint32_t size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (uint32_t by = size / 2; by; by /= 2) {
+      const uint32_t y = __shfl_xor_sync(kAllLanes, *x, by);
+      const bool large = ((lane & by) == 0) == ((lane & size) == 0 || size == 32);
+      *x = large ? max(*x, y) : min(*x, y);
+    }
+  runs[threadIdx.x] = *x;
+  __syncthreads();
+  constexpr uint32_t kSide = NT / 32 < 8 ? NT / 32 : 8;  // runs side by side
+  uint32_t place = lane;
 #pragma unroll 1
-  for (uint32_t k = 0; k < r; ++k) {
-    best = MAX ? __reduce_max_sync(kAllLanes, x) : __reduce_min_sync(kAllLanes, x);
-    if (lane == __ffs(__ballot_sync(kAllLanes, x == best)) - 1) x = MAX ? 0u : 0xffffffffu;
+  for (uint32_t q = 0; q < NT / 32; q += kSide) {
+    uint32_t at[kSide];
+#pragma unroll
+    for (uint32_t j = 0; j < kSide; ++j) at[j] = 0;
+#pragma unroll
+    for (uint32_t step = 32; step; step >>= 1) {
+#pragma unroll
+      for (uint32_t j = 0; j < kSide; ++j) {
+        const uint32_t to = min(at[j] + step, 32u), y = runs[32 * (q + j) + to - 1];
+        // larger, or as large in a run before
+        at[j] = y + (q + j < wid) > *x ? to : at[j];
+      }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kSide; ++j) place += q + j != wid ? at[j] : 0;
   }
-  return best;
+  return place;
 }
 
 // A warp's keys, the largest first.
@@ -282,7 +315,7 @@ struct TopOut {
   int32_t *ids;
   float *top_logp, *logp, *entropy, *rest, *stats;
   uint32_t top;
-  uint32_t rank, among;  // the bound of a sample: see first_bound
+  uint32_t sampled;  // the place of the bound in a sample: see first_bound
 };
 
 template <int NT>
@@ -306,7 +339,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   extern __shared__ uint4 shared_words[];
   __shared__ RowSum red[(NT / 32)], left[(NT / 32)];
-  __shared__ uint32_t bound[(NT / 32)], counts[(NT / 32)], noted[(NT / 32)][kNoted * 32];
+  __shared__ uint32_t bound[NT], counts[(NT / 32)], noted[(NT / 32)][kNoted * 32];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S, U
   __shared__ uint32_t count;
   __shared__ unsigned long long sent;
@@ -344,13 +377,12 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   const Part<T, NT> x(row + first, first, n);
   x.start(ring);
   const float zt = a.target && part == 0 ? to_f32(row[target]) : 0.f;
-  // The first rounds' numbers, each lane's largest, give a bound that K of the part reach:
-  // where they are all, the least of the warps' r-th largest; else see first_bound.
+  // The first rounds' numbers, each thread's largest, in order: the K-th is a bound that K of
+  // the part reach, where these are all; else see first_bound.
   const uint32_t sample = min(x.rounds, (uint32_t)kStages);
-  const uint32_t full = x.rounds > 1 ? NT / 32 : min(NT / 32u, x.sp.vecs / 32);
-  const uint32_t r = x.rounds > sample ? o.rank : full ? (K + full - 1) / full : 33;
-  uint32_t nth = x.rounds > sample ? o.among : 1;
-  if (r <= 32) {
+  const uint32_t full = min((uint32_t)NT, x.sp.vecs);  // threads that have any
+  uint32_t nth = x.rounds > sample ? o.sampled : K;
+  if (nth <= full) {
     float m = kNegInf;
     async_wait<0>();
 #pragma unroll 1
@@ -360,15 +392,15 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) m = fmaxf(m, Vec16<T>::max(w[k]));
     }
-    const uint32_t best = warp_nth<true>(order_of(m + 0.f), r);
-    if (lane == 0) bound[wid] = best;
+    uint32_t mine = order_of(m + 0.f);
+    const uint32_t place = place_of<NT>(&mine, noted[0]);
+    bound[place] = mine;
   }
+  const bool sorted_sample = nth <= full;
   if (np > 1) cluster_started();
   __syncthreads();
   auto bound_at = [&](uint32_t i) {
-    return r > 32 || i - 1 >= full
-               ? kLeastOrder
-               : max(kLeastOrder, warp_nth<false>(lane < full ? bound[lane] : 0xffffffffu, i));
+    return sorted_sample && i - 1 < full ? max(kLeastOrder, bound[i - 1]) : kLeastOrder;
   };
   uint32_t lo = bound_at(nth);
   const Candidates to{list, &count};
@@ -409,12 +441,15 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
     }
     __syncthreads();
     if (enough) continue;
-    // the next of the warps' numbers, unless there is none or that leads back
+    // another of the sample's numbers, unless there is none or that leads back
     const bool over = found > kRoom;
     if (over) reached = lo;
     (over ? many : few) = true;
     uint32_t next = lo;
-    while (next == lo && nth - 1 < full) next = bound_at(nth += over ? 1 : -1);
+    while (next == lo && nth - 1 < full) {
+      nth = over ? nth / 2 : nth < full ? min(2 * nth, full) : full + 1;
+      next = bound_at(nth);
+    }
     if (nth - 1 < full && !(many && few)) {
       lo = next;
       b.least = of_order(lo);
@@ -544,22 +579,14 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
 
 }  // namespace
 
-// The bound for K numbers of a part from `sample` of its `rounds` of vectors, by `warps`
-// warps: `rank`, the place among a warp's lanes' largest, and `among`, that among the warps'
-// numbers of that place, the least first.  The sample's share of the K is Poisson distributed
-// (the vectors are spread evenly), so that three deviations more are hardly ever too few;
-// `rank` of a warp's are below the bound that a mean of `mean` per warp reaches with a
-// probability near one half, which is the warps' number that says most.
-static void first_bound(double K, double sample, double rounds, int warps, uint32_t *rank,
-                        uint32_t *among) {
-  const double share = K * sample / rounds;
-  double mean = (share + 3.0 * std::sqrt(share)) / warps;
-  mean *= 1.0 - mean / 64.0;  // of the lanes: some have two
-  const int r = (int)std::min(std::max(std::ceil(mean), 1.0), 32.0);
-  double below = 0.0, term = std::exp(-mean);
-  for (int i = 0; i < r; term *= mean / ++i) below += term;
-  *rank = (uint32_t)r;
-  *among = (uint32_t)std::min(std::max(std::floor(below * (warps + 1)), 1.0), (double)warps);
+// The bound for K numbers of a part from `sample` of its `rounds` of vectors: its place among
+// the threads' largest.  The sample's share of the K is Poisson distributed (the vectors are
+// spread evenly), so that three deviations more are hardly ever too few; so many numbers are
+// the largest of fewer threads, some of which have several.
+static uint32_t first_bound(double K, double sample, double rounds, double threads) {
+  const double share = K * sample / std::max(rounds, sample);
+  const double some = share + 3.0 * std::sqrt(share);
+  return (uint32_t)std::max(std::ceil(threads * (1.0 - std::exp(-some / threads))), 1.0);
 }
 
 cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_t *ids,
@@ -571,9 +598,9 @@ cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_
     using T = decltype(x);
     auto go = [&](auto threads) {
       constexpr int NT = decltype(threads)::value;
-      TopOut o{ids, top_logp, logp, entropy, rest, stats, top, 0, 0};
-      first_bound(top, kStages, std::ceil((double)shape.vecs / (NT * kUnroll)), NT / 32,
-                  &o.rank, &o.among);
+      const uint32_t sampled =
+          first_bound(top, kStages, std::ceil((double)shape.vecs / (NT * kUnroll)), NT);
+      const TopOut o{ids, top_logp, logp, entropy, rest, stats, top, sampled};
       auto kern = entropy ? k_token_top<T, NT, true> : k_token_top<T, NT, false>;
       const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
       const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + kStages * kUnroll * NT);
