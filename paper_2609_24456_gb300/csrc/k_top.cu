@@ -7,11 +7,19 @@
 // logits reach, most likely (first_bound).  Then it passes over all: numbers that reach the
 // bound are collected as candidates, the others go into the sums of exponentials, so that
 // `rest` comes without cancellation.  Fewer than K candidates (a row in some hundred) ask for
-// another pass with the next lower bound of the sample, more than there is room for with the
-// next higher one; where that leads nowhere (logits that are equal by the hundred) the bound
-// is searched by halving.  The candidates are ordered by value, then index (all different, so
-// that nothing depends on the order in which they came), and those behind the list join the
-// sums.  A row's first CTA merges its parts' lists.
+// another pass with a lower bound of the sample, more than there is room for with a higher one;
+// where that leads nowhere (logits that are equal by the hundred) the bound is searched by
+// counts.  The candidates are ordered by value, then index (all different, so that nothing
+// depends on the order in which they came), and those behind the list join the sums.  A row's
+// first CTA merges its parts' lists.
+//
+// What bounds it, at 6.79 TB/s of measured copy:
+//   8,192 x 152,064 bf16, 64 entries, entropy, a tenth masked   388 us   331 us to read them; issue:
+//                                                 11 instructions an element at 2.9 of 4 a cycle
+//   777 x 32,003 f32, 128 entries   30 us   14.8 us; 608 CTAs at a time, so a second wave
+//   256 x 32,003 f16, 8 entries     10.3 us in a graph, 2.4 us to read them: four rounds a row
+//   one row of 152,064, 20 entries  9.4 us  in a graph: a chain of loads, sample, pass, order
+//                                           and join of 8 lists
 #include <algorithm>
 #include <cmath>
 
