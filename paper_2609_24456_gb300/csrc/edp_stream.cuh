@@ -8,7 +8,6 @@
 namespace edp {
 
 constexpr int kStreamLanes = 1024;  // threads per SM, which bounds the registers
-constexpr int kStages = 2;  // rounds in shared memory or on their way there
 constexpr uint32_t kMostParts = 8;
 // Sums below lose bits of numbers whose power of 2 leaves fp32.
 constexpr float kLeastSum = 0x1p-64f;
@@ -41,7 +40,8 @@ __device__ __forceinline__ void async_wait() {
 // kUnroll segments per warp and round, and the numbers before and behind the vectors by the
 // first threads.  Round g takes segments g, g + rounds, g + 2 rounds, ..., so that the
 // first round's are spread evenly over the part.
-template <typename T, int NT>
+// S: rounds in shared memory or on their way there.
+template <typename T, int NT, int S>
 struct Part {
   const T *p;
   uint32_t first;  // its first column
@@ -70,7 +70,7 @@ struct Part {
   }
   // Round g of this thread's vectors to its own places, -infinity where there are none.
   __device__ __forceinline__ void fetch(uint4 *ring, uint32_t g) const {
-    uint4 *to = ring + g % kStages * (kUnroll * NT) + threadIdx.x;
+    uint4 *to = ring + g % S * (kUnroll * NT) + threadIdx.x;
     const uint4 *from = mine + 32 * g;
     if (g < whole) {
 #pragma unroll
@@ -86,12 +86,19 @@ struct Part {
   }
   __device__ __forceinline__ void start(uint4 *ring) const {
 #pragma unroll
-    for (int g = 0; g < kStages; ++g) fetch(ring, g);
+    for (int g = 0; g < S; ++g) fetch(ring, g);
   }
   __device__ __forceinline__ void load(uint4 (&w)[kUnroll], const uint4 *ring, uint32_t g) const {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k)
-      w[k] = ring[(g % kStages * kUnroll + k) * NT + threadIdx.x];
+      w[k] = ring[(g % S * kUnroll + k) * NT + threadIdx.x];
+  }
+  // A lane's vector of round g, from the ring while it is there (after a __syncwarp).
+  __device__ __forceinline__ uint4 vec_of(const uint4 *ring, uint32_t g, uint32_t k,
+                                          uint32_t lane) const {
+    if (g + S >= rounds)
+      return ring[(g % S * kUnroll + k) * NT + (threadIdx.x & ~31u) + lane];
+    return vec(vec_at(g, k, lane));
   }
   __device__ __forceinline__ bool single() const { return threadIdx.x < sp.head + sp.tail; }
   __device__ __forceinline__ uint32_t single_at() const {
@@ -104,13 +111,13 @@ struct Part {
     start(ring);
 #pragma unroll 1
     for (uint32_t g = 0; g < rounds; ++g) {
-      async_wait<kStages - 1>();
+      async_wait<S - 1>();
 #pragma unroll 1
       for (uint32_t k = 0; k < kUnroll; ++k) {
-        const uint4 w = ring[(g % kStages * kUnroll + k) * NT + threadIdx.x];
+        const uint4 w = ring[(g % S * kUnroll + k) * NT + threadIdx.x];
         f(w, vec_at(g, k, threadIdx.x & 31));
       }
-      fetch(ring, g + kStages);
+      fetch(ring, g + S);
     }
   }
   // f(number, column) of all of this thread's numbers.
@@ -167,7 +174,7 @@ __device__ __forceinline__ RowSum joined(const RowSum &mine, const RowSum &more,
 // 128 threads say too little about a bound (2,000 rows of 4,000 with 128 entries: 92 us, 43
 // with 256).
 struct StreamShape {
-  uint32_t parts, threads;
+  uint32_t parts, threads, stages;
   uint64_t vecs;  // of a part
 };
 inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, bool few_entries) {
@@ -177,15 +184,19 @@ inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, bool few_en
   while (parts < kMostParts && 2 * parts * z.rows <= sms && vecs >= 2ull * parts * 2048) parts *= 2;
   const uint64_t each = vecs / parts;
   const bool small = each <= 1024 || (each <= 4096 && z.rows * parts >= 8 * sms);
-  if (small && few_entries) return {parts, 128, each};
-  return {parts, each >= 8192 && z.rows * parts <= sms ? 512u : 256u, each};
+  if (small && few_entries) return {parts, 128, 2, each};
+  if (each >= 8192 && z.rows * parts <= sms) return {parts, 512, 4, each};
+  return {parts, 256, z.rows * parts <= 2 * sms ? 4u : 2u, each};
 }
-// f of a whole number that is a constant: 128, 256 or 512.
+// f of two whole numbers that are constants: threads and stages.
 template <typename F>
-cudaError_t by_threads(uint32_t threads, F f) {
-  if (threads == 128) return f(std::integral_constant<int, 128>{});
-  if (threads == 512) return f(std::integral_constant<int, 512>{});
-  return f(std::integral_constant<int, 256>{});
+cudaError_t by_shape(const StreamShape &s, F f) {
+  using Two = std::integral_constant<int, 2>;
+  using Four = std::integral_constant<int, 4>;
+  if (s.threads == 128) return f(std::integral_constant<int, 128>{}, Two{});
+  if (s.threads == 512) return f(std::integral_constant<int, 512>{}, Four{});
+  return s.stages == 4 ? f(std::integral_constant<int, 256>{}, Four{})
+                       : f(std::integral_constant<int, 256>{}, Two{});
 }
 
 }  // namespace edp

@@ -443,7 +443,7 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
 // left out of the sums; the first of its entries adds what else there is in it.  All is
 // relative to the list's maximum (no maximum is kept), which is near the row's, most likely:
 // sums that leave fp32 are made again, carefully.
-template <typename T, int NT, bool BACK>
+template <typename T, int NT, int ST, bool BACK>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
                  DistillRule rule, float *loss, float *row_loss, float *per_row, void *dz, uint64_t dstride,
@@ -462,7 +462,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
   const uint32_t part = blockIdx.y, np = gridDim.y;
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   uint4 *ring = shared_words;
-  uint32_t *marks = reinterpret_cast<uint32_t *>(ring + kStages * kUnroll * NT);  // [words]
+  uint32_t *marks = reinterpret_cast<uint32_t *>(ring + ST * kUnroll * NT);  // [words]
   if (threadIdx.x == 0) {
     if (np > 1) {
       mbar_init(&sent, 1);
@@ -490,7 +490,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
     return;  // the whole cluster
   }
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
-  const Part<T, NT> x(row + first, first, n);
+  const Part<T, NT, ST> x(row + first, first, n);
   x.start(ring);
   if (np > 1) cluster_started();
   if (early) pdl_wait();
@@ -546,7 +546,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
     if (alone) add_one<T, false, F>(s, u, log, single);
     add_vector<T, false, F>(s, u, rest_of, log);
     for (uint32_t g = 0; g < x.rounds; ++g) {
-      async_wait<kStages - 1>();
+      async_wait<ST - 1>();
       uint4 w[kUnroll];
       x.load(w, ring, g);
 #pragma unroll
@@ -555,7 +555,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
         if (mark && mark >> lane & 1) w[k] = no_logits<T>();
         add_vector<T, false, F>(s, u, w[k], log);
       }
-      x.fetch(ring, g + kStages);
+      x.fetch(ring, g + ST);
     }
     sum = warp_sum<T, false>(RowSum{l.m, s.x() + s.y(), 0.f}, a.c);
     if (lane == 0) red[wid] = sum;
@@ -659,13 +659,14 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
     using T = decltype(x);
     auto stream = [&](auto back) {
       constexpr bool BACK = decltype(back)::value;
-      const StreamShape shape = stream_shape(ctx, z, true);
-      return by_threads(shape.threads, [&](auto threads) {
-        constexpr int NT = decltype(threads)::value;
+      StreamShape shape = stream_shape(ctx, z, true);
+      if (shape.vecs > 8 * 64 * 1024) shape.threads = 256, shape.stages = 2;  // room for marks
+      return by_shape(shape, [&](auto threads, auto stages) {
+        constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;
         constexpr uint64_t round = kUnroll * (NT / 32);  // segments
         const uint32_t words = (uint32_t)(((shape.vecs + 8) / 32 / round + 1) * round);
-        const size_t bytes = sizeof(uint4) * kStages * kUnroll * NT + 4 * words;
-        auto kern = k_distill_stream<T, NT, BACK>;
+        const size_t bytes = sizeof(uint4) * ST * kUnroll * NT + 4 * words;
+        auto kern = k_distill_stream<T, NT, ST, BACK>;
         const cudaError_t err = cudaFuncSetAttribute(
             kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
         if (err != cudaSuccess) return err;

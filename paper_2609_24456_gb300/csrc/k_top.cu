@@ -137,8 +137,8 @@ __device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f
 // rows of 152,064 bfloat16 logits took 470 us, without 433).  A vector that has a candidate is
 // taken out whole and noted; the warp looks at those at the end, or when a lane may have no
 // room for another round's.
-template <typename T, int NT, bool ENT, bool FUSED>
-__device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, Bound b, float ref,
+template <typename T, int NT, int ST, bool ENT, bool FUSED>
+__device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *ring, Bound b, float ref,
                                             const Candidates &to, uint32_t *noted, float c) {
   const RowLog<T, FUSED> log(ref, c);
   F2 s(0.f), u(0.f);
@@ -151,7 +151,7 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, B
   const uint32_t lane = threadIdx.x & 31;
   uint32_t n = 0;
   for (uint32_t g = 0; g < x.rounds; ++g) {
-    async_wait<kStages - 1>();
+    async_wait<ST - 1>();
     uint4 w[kUnroll];
     x.load(w, ring, g);
     float m[kUnroll];
@@ -167,12 +167,13 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, B
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) add_vector<T, ENT, FUSED>(s, u, w[k], log);
-    x.fetch(ring, g + kStages);
+    x.fetch(ring, g + ST);
     if (__any_sync(kAllLanes, n > (g + 1 < x.rounds ? kNoted - kUnroll : 0))) {
       each_note(noted, n, [&](uint32_t note, uint32_t owner) {
         if (to.full()) return;
-        const uint32_t at = x.vec_at(note / kUnroll, note % kUnroll, owner);
-        add_but<T, ENT, FUSED>(s, u, log, x.vec(at), x.column(at), b, to);
+        const uint32_t round = note / kUnroll, k = note % kUnroll;
+        add_but<T, ENT, FUSED>(s, u, log, x.vec_of(ring, round, k, owner),
+                               x.column(x.vec_at(round, k, owner)), b, to);
       });
       n = 0;
     }
@@ -180,8 +181,8 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT> &x, uint4 *ring, B
   return {ref, s.x() + s.y(), u.x() + u.y()};
 }
 // The same relative to each thread's maximum, where the sums ask for that: rare.
-template <typename T, int NT, bool ENT>
-__device__ __forceinline__ RowSum take_carefully(const Part<T, NT> &x, uint4 *ring, Bound b,
+template <typename T, int NT, int ST, bool ENT>
+__device__ __forceinline__ RowSum take_carefully(const Part<T, NT, ST> &x, uint4 *ring, Bound b,
                                                  const Candidates &to, float c) {
   LaneSum a{kNegInf, F2(0.f), F2(0.f)};
   auto one = [&](float v, uint32_t column) {
@@ -211,8 +212,8 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
 // the lowest) by counts: whether it is the K-th largest number itself (equal by the hundred, as
 // masked ones are), else the number by halving; and of those equal to it an end, by steps that
 // grow and by halving.  Rare, so that it only has to end: 64 counts at the most.
-template <typename T, int NT>
-__device__ __forceinline__ Bound search_bound(const Part<T, NT> &x, uint4 *ring, uint32_t n,
+template <typename T, int NT, int ST>
+__device__ __forceinline__ Bound search_bound(const Part<T, NT, ST> &x, uint4 *ring, uint32_t n,
                                               uint32_t lo, uint32_t K, uint32_t *red) {
   constexpr uint32_t kAll = 0xffffffffu;
   enum { kLowest, kAbove, kValue, kColumn } look = lo == kLeastOrder ? kLowest : kAbove;
@@ -341,7 +342,7 @@ __device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
 }
 
 // A cluster of gridDim.y CTAs per row, each a part of it.
-template <typename T, int NT, bool ENT>
+template <typename T, int NT, int ST, bool ENT>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
@@ -358,7 +359,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   Key *inbox = list + kRoom;                          // [np][K], the lists of the parts
   uint4 *ring = shared_words + (kRoom + (np > 1 ? np * K : 0) + 1) / 2;
   Key *sorted = reinterpret_cast<Key *>(ring);        // [kRoom], in order, after the passes
-  static_assert(kRoom * sizeof(Key) <= sizeof(uint4) * kStages * kUnroll * NT, "in the ring");
+  static_assert(kRoom * sizeof(Key) <= sizeof(uint4) * ST * kUnroll * NT, "in the ring");
   if (threadIdx.x == 0) {
     if (np > 1) {
       mbar_init(&sent, 1);
@@ -382,12 +383,12 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   uint32_t first, n;
   row_part(a.vocab, part, np, &first, &n);
   const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
-  const Part<T, NT> x(row + first, first, n);
+  const Part<T, NT, ST> x(row + first, first, n);
   x.start(ring);
   const float zt = a.target && part == 0 ? to_f32(row[target]) : 0.f;
   // The first rounds' numbers, each thread's largest, in order: the K-th is a bound that K of
   // the part reach, where these are all; else see first_bound.
-  const uint32_t sample = min(x.rounds, (uint32_t)kStages);
+  const uint32_t sample = min(x.rounds, (uint32_t)ST);
   const uint32_t full = min((uint32_t)NT, x.sp.vecs);  // threads that have any
   uint32_t nth = x.rounds > sample ? o.sampled : K;
   if (nth <= full) {
@@ -428,8 +429,8 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       __syncthreads();
     }
     again = true;
-    sum = careful ? take_carefully<T, NT, ENT>(x, ring, b, to, a.c)
-                  : take_part<T, NT, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
+    sum = careful ? take_carefully<T, NT, ST, ENT>(x, ring, b, to, a.c)
+                  : take_part<T, NT, ST, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
     sum = warp_sum<T, false>(sum, a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
@@ -462,7 +463,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       lo = next;
       b.least = of_order(lo);
     } else {
-      b = search_bound<T, NT>(x, ring, n, reached, K, counts);
+      b = search_bound<T, NT, ST>(x, ring, n, reached, K, counts);
       lo = order_of(b.least);
       searched = true;
     }
@@ -604,20 +605,19 @@ cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_
   const uint32_t parts = shape.parts;
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    auto go = [&](auto threads) {
-      constexpr int NT = decltype(threads)::value;
+    return by_shape(shape, [&](auto threads, auto stages) {
+      constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;
       const uint32_t sampled =
-          first_bound(top, kStages, std::ceil((double)shape.vecs / (NT * kUnroll)), NT);
+          first_bound(top, ST, std::ceil((double)shape.vecs / (NT * kUnroll)), NT);
       const TopOut o{ids, top_logp, logp, entropy, rest, stats, top, sampled};
-      auto kern = entropy ? k_token_top<T, NT, true> : k_token_top<T, NT, false>;
+      auto kern = entropy ? k_token_top<T, NT, ST, true> : k_token_top<T, NT, ST, false>;
       const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
-      const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + kStages * kUnroll * NT);
+      const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + ST * kUnroll * NT);
       const cudaError_t e = cudaFuncSetAttribute(
-          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
       if (e != cudaSuccess) return e;
       return launch_rows(kern, z.rows, parts, true, NT, bytes, s, row_args(z), o, ctx->ctrl);
-    };
-    return by_threads(shape.threads, go);
+    });
   });
 }
 

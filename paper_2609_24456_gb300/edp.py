@@ -717,10 +717,12 @@ def _other_array(x, kind, n, who):
 def _rows(t):
     """(address, dtype, rows, columns, stride) of a 2-D tensor whose rows are
     contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("logits: a 2-D tensor with contiguous rows")
-    rows, cols = t.shape
-    return t.data_ptr(), _dtype(t), rows, cols, t.stride(0) if rows > 1 else max(cols, 1)
+    shape = t.shape
+    if len(shape) == 2:
+        (rows, cols), (stride, step) = shape, t.stride()
+        if step == 1 or cols <= 1:
+            return t.data_ptr(), _dtype(t), rows, cols, stride if rows > 1 else max(cols, 1)
+    raise ValueError("logits: a 2-D tensor with contiguous rows")
 
 
 def _grad_rows(t, z):
@@ -809,11 +811,15 @@ def edp_balance_loss(ctx, logits, sel, coef, loss, counts, mask=None, prob=None,
         stream_handle(stream)), who)
 
 
-def _lists(x, rows, who):
-    """Entries per row of the lists x."""
-    if x.dim() != 2 or x.shape[0] != rows:
+def _lists(ids, rows, who):
+    """(address, entries per row) of lists of tokens."""
+    shape = ids.shape
+    if len(shape) != 2 or shape[0] != rows:
         raise ValueError("%s: lists are 2-D tensors with a row for each of the logits'" % who)
-    return x.shape[1]
+    top = shape[1]
+    if ids.dtype in _i32 and ids.is_contiguous():
+        return ids.data_ptr(), top
+    return _other_array(ids, _i32, rows * top, who), top
 
 
 def edp_token_top(ctx, logits, ids, top_logp, target=None, logp=None, mask=None,
@@ -821,10 +827,10 @@ def edp_token_top(ctx, logits, ids, top_logp, target=None, logp=None, mask=None,
     """The likeliest tokens of each row: ids and top_logp [rows][top]."""
     who = "edp_token_top"
     p, dt, rows, vocab, stride = _rows(logits)
-    top = _lists(ids, rows, who)
+    tokens, top = _lists(ids, rows, who)
     return _check(ctx, lib().edp_token_top(
         ctx, p, dt, rows, vocab, stride, _arr(target, _i32, rows, who),
-        _arr(mask, _mask, rows, who), temperature, top, _arr(ids, _i32, rows * top, who),
+        _arr(mask, _mask, rows, who), temperature, top, tokens,
         _arr(top_logp, _f32, rows * top, who), _vec(logp, who), _vec(entropy, who),
         _vec(rest, who), _vec(stats, who), stream_handle(stream)), who)
 
@@ -837,12 +843,12 @@ def edp_distill_loss(ctx, cfg: edp_distill_config, logits, ids, value, loss, res
     who = "edp_distill_loss"
     p, dt, rows, vocab, stride = _rows(logits)
     d, dstride = _grad_rows(dlogits, logits)
-    top = _lists(ids, rows, who)
+    tokens, top = _lists(ids, rows, who)
     return _check(ctx, lib().edp_distill_loss(
-        ctx, C.byref(cfg), p, dt, rows, vocab, stride, temperature,
-        _arr(ids, _i32, rows * top, who), _arr(value, _f32, rows * top, who), top,
-        _vec(rest, who), _arr(mask, _mask, rows, who), _arr(off, _u64, n_seq + 1, who), n_seq,
-        _vec(loss, who), _vec(row_loss, who), d, dstride, stream_handle(stream)), who)
+        ctx, C.byref(cfg), p, dt, rows, vocab, stride, temperature, tokens,
+        _arr(value, _f32, rows * top, who), top, _vec(rest, who), _arr(mask, _mask, rows, who),
+        _arr(off, _u64, n_seq + 1, who), n_seq, _vec(loss, who), _vec(row_loss, who), d, dstride,
+        stream_handle(stream)), who)
 
 
 def edp_save(ctx, path, stream=None):

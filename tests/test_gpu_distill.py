@@ -428,7 +428,8 @@ def test_large_vocabularies(edp_lib, dtype, vocab, kind, rest):
 
 
 @pytest.mark.parametrize("dtype,vocab,rows", [("bf16", 8_388_608, 1), ("f32", 4_194_303, 1),
-                                              ("f32", 4_194_304, 160)])
+                                              ("f32", 4_194_304, 100),
+                                              ("bf16", 8_388_608, 160)])
 def test_largest_vocabularies(edp_lib, dtype, vocab, rows):
     """One row that counts, of one and of many (a CTA then has the whole of it)."""
     edp, ring = edp_lib, ctx_of(edp_lib)
