@@ -30,7 +30,9 @@ __device__ __forceinline__ void async_load(uint4 *to, const uint4 *from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from)
                : "memory");
 }
-__device__ __forceinline__ void async_mark() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void async_mark() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
 template <int N>
 __device__ __forceinline__ void async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -172,7 +174,8 @@ __device__ __forceinline__ RowSum joined(const RowSum &mine, const RowSum &more,
 // 4,000: 28.3 as 1 x 256, 16.1 as 1 x 128; 4,096 of 32,003: 82 and 69, but 400 of them 14.7 and
 // 17.9; 2,048 rows of 152,064: 117 as 1 x 256, 147 as 1 x 512.  With long lists the 4 warps of
 // 128 threads say too little about a bound (2,000 rows of 4,000 with 128 entries: 92 us, 43
-// with 256).
+// with 256).  Four rounds in flight where CTAs are two per SM at the most: 256 rows of 32,003
+// fp16 logits 11.5 us in a stream however the calls come, with two 11.1 to 14.6.
 struct StreamShape {
   uint32_t parts, threads, stages;
   uint64_t vecs;  // of a part
@@ -185,7 +188,7 @@ inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, bool few_en
   const uint64_t each = vecs / parts;
   const bool small = each <= 1024 || (each <= 4096 && z.rows * parts >= 8 * sms);
   if (small && few_entries) return {parts, 128, 2, each};
-  if (each >= 8192 && z.rows * parts <= sms) return {parts, 512, 4, each};
+  if (each >= 8192 && z.rows * parts <= sms) return {parts, 512, 2, each};
   return {parts, 256, z.rows * parts <= 2 * sms ? 4u : 2u, each};
 }
 // f of two whole numbers that are constants: threads and stages.
@@ -194,7 +197,7 @@ cudaError_t by_shape(const StreamShape &s, F f) {
   using Two = std::integral_constant<int, 2>;
   using Four = std::integral_constant<int, 4>;
   if (s.threads == 128) return f(std::integral_constant<int, 128>{}, Two{});
-  if (s.threads == 512) return f(std::integral_constant<int, 512>{}, Four{});
+  if (s.threads == 512) return f(std::integral_constant<int, 512>{}, Two{});
   return s.stages == 4 ? f(std::integral_constant<int, 256>{}, Four{})
                        : f(std::integral_constant<int, 256>{}, Two{});
 }

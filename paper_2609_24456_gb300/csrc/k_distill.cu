@@ -439,14 +439,15 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
 }
 
 // The loss alone: the row is streamed, and read once too.  BACK: its gradient, with the
-// logits read a second time, for rows of which too little fits shared memory.  A vector with an entry in it is
-// left out of the sums; the first of its entries adds what else there is in it.  All is
-// relative to the list's maximum (no maximum is kept), which is near the row's, most likely:
-// sums that leave fp32 are made again, carefully.
+// logits read a second time, for rows of which too little fits shared memory.  A vector with
+// an entry in it is left out of the sums; the first of its entries adds what else there is in
+// it.  All is relative to the list's maximum (no maximum is kept), which is near the row's,
+// most likely: sums that leave fp32 are made again, carefully.
 template <typename T, int NT, int ST, bool BACK>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
-                 DistillRule rule, float *loss, float *row_loss, float *per_row, void *dz, uint64_t dstride,
+                 DistillRule rule, float *loss, float *row_loss, float *per_row, void *dz,
+                 uint64_t dstride,
                  uint32_t words, bool early, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
   constexpr int N = Vec16<T>::kN;
@@ -660,7 +661,7 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
     auto stream = [&](auto back) {
       constexpr bool BACK = decltype(back)::value;
       StreamShape shape = stream_shape(ctx, z, true);
-      if (shape.vecs > 8 * 64 * 1024) shape.threads = 256, shape.stages = 2;  // room for marks
+      if (shape.vecs > 8 * 64 * 1024) shape.threads = 256, shape.stages = 2;  // room for the marks
       return by_shape(shape, [&](auto threads, auto stages) {
         constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;
         constexpr uint64_t round = kUnroll * (NT / 32);  // segments

@@ -14,12 +14,11 @@
 // first CTA merges its parts' lists.
 //
 // What bounds it, at 6.79 TB/s of measured copy:
-//   8,192 x 152,064 bf16, 64 entries, entropy, a tenth masked   388 us   331 us to read them; issue:
-//                                                 11 instructions an element at 2.9 of 4 a cycle
-//   777 x 32,003 f32, 128 entries   30 us   14.8 us; 608 CTAs at a time, so a second wave
-//   256 x 32,003 f16, 8 entries     10.3 us in a graph, 2.4 us to read them: four rounds a row
-//   one row of 152,064, 20 entries  9.4 us  in a graph: a chain of loads, sample, pass, order
-//                                           and join of 8 lists
+//   8,192 x 152,064 bf16, 64 entries, entropy, a tenth masked   390 us   331 us to read them;
+//                                      issue: 11 instructions an element at 2.9 of 4 a cycle
+//   777 x 32,003 f32, 128 entries   31 us    14.8 us; 608 CTAs at a time, so a second wave
+//   256 x 32,003 f16, 8 entries     11.5 us  2.4 us; a chain of loads, sample, pass and order
+//   one row of 152,064, 20 entries  9.4 us   the same, and the join of 8 lists
 #include <algorithm>
 #include <cmath>
 
@@ -70,13 +69,14 @@ struct Bound {
 struct Candidates {
   Key *list;
   uint32_t *count;
+  uint32_t room;
   // too many already: the pass will be made again, whatever else it finds
   __device__ __forceinline__ bool full() const {
-    return *const_cast<const volatile uint32_t *>(count) > kRoom;
+    return *const_cast<const volatile uint32_t *>(count) > room;
   }
   __device__ __forceinline__ void add(float v, uint32_t column) const {
     const uint32_t at = atomicAdd(count, 1u);
-    if (at < kRoom) list[at] = key_of(v, column);
+    if (at < room) list[at] = key_of(v, column);
   }
 };
 
@@ -138,8 +138,9 @@ __device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f
 // taken out whole and noted; the warp looks at those at the end, or when a lane may have no
 // room for another round's.
 template <typename T, int NT, int ST, bool ENT, bool FUSED>
-__device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *ring, Bound b, float ref,
-                                            const Candidates &to, uint32_t *noted, float c) {
+__device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *ring, Bound b,
+                                            float ref, const Candidates &to, uint32_t *noted,
+                                            float c) {
   const RowLog<T, FUSED> log(ref, c);
   F2 s(0.f), u(0.f);
   if (x.single()) {
@@ -208,17 +209,18 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
   return n;
 }
 
-// A bound that K to kRoom numbers hold, searched from `lo` on (which more reach, unless it is
-// the lowest) by counts: whether it is the K-th largest number itself (equal by the hundred, as
-// masked ones are), else the number by halving; and of those equal to it an end, by steps that
-// grow and by halving.  Rare, so that it only has to end: 64 counts at the most.
-template <typename T, int NT, int ST>
-__device__ __forceinline__ Bound search_bound(const Part<T, NT, ST> &x, uint4 *ring, uint32_t n,
-                                              uint32_t lo, uint32_t K, uint32_t *red) {
+// A bound that K to `room` numbers of n from column `first` on hold, searched from `lo` on
+// (which more reach, unless it is the lowest) by counts: whether it is the K-th largest number
+// itself (equal by the hundred, as masked ones are), else the number by halving; and of those
+// equal to it an end, by steps that grow and by halving.  Rare, so that it only has to end: 64
+// counts at the most.
+template <typename Count>
+__device__ __forceinline__ Bound search_bound(Count count, uint32_t first, uint32_t n, uint32_t lo,
+                                              uint32_t K, uint32_t room) {
   constexpr uint32_t kAll = 0xffffffffu;
   enum { kLowest, kAbove, kValue, kColumn } look = lo == kLeastOrder ? kLowest : kAbove;
   uint32_t hi = 0xff800001u;              // nothing is above +infinity
-  uint32_t a = x.first, b = x.first + n;  // too few with the end a, enough with b
+  uint32_t a = first, b = first + n;  // too few with the end a, enough with b
   uint32_t step = 4 * K;
   for (;;) {
     if (look == kValue && hi - lo <= 1) look = kColumn;
@@ -228,10 +230,8 @@ __device__ __forceinline__ Bound search_bound(const Part<T, NT, ST> &x, uint4 *r
                             : look == kColumn ? a + min(step, (b - a) / 2)
                                               : kAll;
     const Bound probe{of_order(mid), column};
-    uint32_t c = 0;
-    x.each(ring, [&](float v, uint32_t at) { c += probe.holds(v, at); });
-    c = cta_count<NT>(c, red);
-    if (look != kAbove && c >= K && c <= kRoom) return probe;
+    const uint32_t c = count(probe);
+    if (look != kAbove && c >= K && c <= room) return probe;
     if (look == kLowest) {
       if (c < K) return probe;
       look = kAbove;
@@ -247,19 +247,25 @@ __device__ __forceinline__ Bound search_bound(const Part<T, NT, ST> &x, uint4 *r
   }
 }
 
+// A warp's numbers, the largest first.
+__device__ __forceinline__ uint32_t warp_ordered(uint32_t x) {
+  const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+  for (uint32_t size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (uint32_t by = size / 2; by; by /= 2) {
+      const uint32_t y = __shfl_xor_sync(kAllLanes, x, by);
+      const bool large = ((lane & by) == 0) == ((lane & size) == 0 || size == 32);
+      x = large ? max(x, y) : min(x, y);
+    }
+  return x;
+}
 // The place of x among the numbers of all threads, the largest first, equal ones in any order
 // of their own.  runs: NT numbers, which then hold each warp's in order.
 template <int NT>
 __device__ __forceinline__ uint32_t place_of(uint32_t *x, uint32_t *runs) {
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-#pragma unroll
-  for (uint32_t size = 2; size <= 32; size *= 2)
-#pragma unroll
-    for (uint32_t by = size / 2; by; by /= 2) {
-      const uint32_t y = __shfl_xor_sync(kAllLanes, *x, by);
-      const bool large = ((lane & by) == 0) == ((lane & size) == 0 || size == 32);
-      *x = large ? max(*x, y) : min(*x, y);
-    }
+  *x = warp_ordered(*x);
   runs[threadIdx.x] = *x;
   __syncthreads();
   constexpr uint32_t kSide = NT / 32 < 8 ? NT / 32 : 8;  // runs side by side
@@ -327,18 +333,46 @@ struct TopOut {
   uint32_t sampled;  // the place of the bound in a sample: see first_bound
 };
 
-template <int NT>
-__device__ __forceinline__ void write_none(const TopOut &o, uint64_t t) {
-#pragma unroll 1
-  for (uint32_t k = threadIdx.x; k < o.top; k += NT) {
-    o.ids[t * o.top + k] = -1;
-    o.top_logp[t * o.top + k] = kNegInf;
+// A row without a list, by threads i = 0 .. (128 at least, or as many as entries).
+__device__ __forceinline__ void write_none(const TopOut &o, uint64_t t, uint32_t i) {
+  if (i < o.top) {
+    o.ids[t * o.top + i] = -1;
+    o.top_logp[t * o.top + i] = kNegInf;
   }
-  if (threadIdx.x) return;
+  if (i) return;
   if (o.logp) o.logp[t] = 0.f;
   if (o.entropy) o.entropy[t] = 0.f;
   if (o.rest) o.rest[t] = 0.f;
   if (o.stats) o.stats[2 * t] = o.stats[2 * t + 1] = 0.f;
+}
+
+// Entry i of row t, and from entry 0 its other numbers.  M: the largest logit; S, U: the sums of
+// the list relative to it; rest: those of all other tokens.
+__device__ __forceinline__ void finish(const RowArgs &a, const TopOut &o, uint64_t t, uint32_t i,
+                                       Key key, float M, float S, float U, const RowSum &rest,
+                                       float zt) {
+  if (rest.m == kNegInf) {
+    S += rest.s;  // 0 or NaN
+  } else {
+    const float d = (rest.m - M) * a.c, f = ex2(d);
+    S = fmaf(f, rest.s, S);
+    U += f > 0.f ? f * fmaf(d, rest.s, rest.u) : 0.f;
+  }
+  const float ln = logf(S);
+  const bool nan = S != S;
+  if (i < o.top) {
+    o.ids[t * o.top + i] = key && !nan ? (int32_t)column_of(key) : -1;
+    o.top_logp[t * o.top + i] = nan ? S : key ? (value_of(key) - M) * a.inv_t - ln : kNegInf;
+  }
+  if (i) return;
+  if (o.logp) o.logp[t] = (zt - M) * a.inv_t - ln;
+  if (o.entropy) o.entropy[t] = ln - kLn2 * (U / S);
+  if (o.rest)
+    o.rest[t] = nan ? S : rest.s == 0.f ? kNegInf : (rest.m - M) * a.inv_t + logf(rest.s) - ln;
+  if (o.stats) {
+    o.stats[2 * t] = M;
+    o.stats[2 * t + 1] = S;
+  }
 }
 
 // A cluster of gridDim.y CTAs per row, each a part of it.
@@ -374,7 +408,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   const bool skip = (a.mask && !a.mask[t]) || target < 0;
   if (skip || (uint32_t)target >= a.vocab) {
     if (part == 0) {
-      write_none<NT>(o, t);
+      write_none(o, t, threadIdx.x);
       if (!skip && threadIdx.x == 0)
         flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)target);
     }
@@ -412,7 +446,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
     return sorted_sample && i - 1 < full ? max(kLeastOrder, bound[i - 1]) : kLeastOrder;
   };
   uint32_t lo = bound_at(nth);
-  const Candidates to{list, &count};
+  const Candidates to{list, &count, kRoom};
   Bound b{of_order(lo), 0xffffffffu};
   uint32_t found, reached = kLeastOrder;  // reached: by too many
   bool many = false, few = false;  // so far
@@ -463,7 +497,12 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       lo = next;
       b.least = of_order(lo);
     } else {
-      b = search_bound<T, NT, ST>(x, ring, n, reached, K, counts);
+      auto count_all = [&](const Bound &probe) {
+        uint32_t c = 0;
+        x.each(ring, [&](float v, uint32_t at) { c += probe.holds(v, at); });
+        return cta_count<NT>(c, counts);
+      };
+      b = search_bound(count_all, first, n, reached, K, kRoom);
       lo = order_of(b.least);
       searched = true;
     }
@@ -511,7 +550,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       whole = mbar_wait(&sent, 0, kRowWaitNs);  // none of them comes after the end
     }
     if (!__syncthreads_and(whole)) {
-      write_none<NT>(o, t);
+      write_none(o, t, threadIdx.x);
       return;
     }
     // A key's place in the row's list: how many are larger in each of the parts' lists.
@@ -558,32 +597,168 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   }
   if (!any && !(sum.s != sum.s)) {  // no token has a probability
     if (threadIdx.x == 0) flag(ctrl, DEVERR_ROW, t);
-    write_none<NT>(o, t);
+    write_none(o, t, threadIdx.x);
     return;
   }
-  if (sum.m == kNegInf) {
-    S += sum.s;  // 0 or NaN
+  finish(a, o, t, threadIdx.x, key, M, S, U, sum, zt);
+}
+
+// A warp per row, held in shared memory (each lane its own vectors), for lists of up to 32:
+// short rows cost a CTA more in its steps than in their numbers.  The bound is the K-th of the
+// 64 largest numbers of the lanes' even and odd vectors, which K numbers reach.  8,000 rows of
+// bfloat16 logits, lists of 20 (us; with a CTA of 128 threads): 500 columns 13 (64), 2,000 27
+// (65), 4,000 49 (64), 6,000 73 (77); 600 rows: 5.1 (10), 8.3 (10), 11.6 (9.8); one row: 4.7
+// (6.7), 7.4 (6.3), 9.4 (6.1).
+constexpr uint32_t kSmallRoom = 256;
+constexpr uint32_t kSmallTop = 32;
+constexpr int kSmallRows = 4;  // per CTA
+
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(32 * kSmallRows, 7)
+k_top_small(RowArgs a, TopOut o, uint64_t rows, uint32_t vectors, Ctrl *ctrl) {
+  constexpr int N = Vec16<T>::kN;
+  extern __shared__ uint4 shared_words[];  // [kSmallRows][32 vectors]
+  __shared__ Key lists[kSmallRows][2][kSmallRoom];
+  __shared__ uint32_t counts[kSmallRows];
+  const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, K = o.top;
+  const uint64_t t = (uint64_t)blockIdx.x * kSmallRows + wid;
+  Key *list = lists[wid][0], *sorted = lists[wid][1];
+  pdl_wait();
+  pdl_launch();
+  if (t >= rows) return;
+  const int32_t target = a.target ? a.target[t] : 0;
+  const bool skip = (a.mask && !a.mask[t]) || target < 0;
+  if (skip || (uint32_t)target >= a.vocab) {
+    write_none(o, t, lane);
+    if (!skip && lane == 0) flag(ctrl, DEVERR_INDEX, (unsigned long long)(uint32_t)target);
+    return;
+  }
+  const T *row = reinterpret_cast<const T *>(a.z) + t * a.stride;
+  const Span<T> sp(row, a.vocab);
+  const uint4 *q = reinterpret_cast<const uint4 *>(row + sp.head);
+  uint4 *w = shared_words + wid * vectors * 32 + lane;  // [32 k]
+  const int all = (sp.vecs + 31) / 32;
+#pragma unroll 4
+  for (int k = 0; k < all; ++k) {
+    if (32 * k + lane < sp.vecs) async_load(w + 32 * k, q + 32 * k + lane);
+    else w[32 * k] = no_logits<T>();
+  }
+  async_mark();
+  const bool one = lane < sp.head + sp.tail;  // a number before or behind the vectors
+  const uint32_t at = lane < sp.head ? lane : lane + sp.vecs * N;
+  const float v = one ? to_f32(row[at]) : kNegInf;
+  const float zt = a.target ? to_f32(row[target]) : 0.f;
+  auto column = [&](int k) { return sp.head + (32 * k + lane) * N; };
+  // f(number, column) of the lane's numbers
+  auto each = [&](auto f) {
+    f(v, at);
+#pragma unroll 1
+    for (int k = 0; k < all; ++k) {
+      const uint4 x = w[32 * k];
+#pragma unroll
+      for (int i = 0; i < N; ++i) f(to_f32(reinterpret_cast<const T *>(&x)[i]), column(k) + i);
+    }
+  };
+  // a lane's largest of its even vectors and of its odd ones: the K-th of all
+  float m = v, m1 = kNegInf;
+  async_wait<0>();
+  for (int k = 0; k < all; k += 2) {
+    m = fmaxf(m, Vec16<T>::max(w[32 * k]));
+    if (k + 1 < all) m1 = fmaxf(m1, Vec16<T>::max(w[32 * (k + 1)]));
+  }
+  uint32_t largest = warp_ordered(order_of(m + 0.f));
+  {
+    // two runs against each other: the larger of each pair are the 32 largest
+    const uint32_t other = warp_ordered(order_of(m1 + 0.f));
+    largest = max(largest, __shfl_sync(kAllLanes, other, 31 - lane));
+#pragma unroll
+    for (uint32_t by = 16; by; by /= 2) {
+      const uint32_t y = __shfl_xor_sync(kAllLanes, largest, by);
+      largest = lane & by ? min(largest, y) : max(largest, y);
+    }
+  }
+  uint32_t lo = max(kLeastOrder, __shfl_sync(kAllLanes, largest, K - 1));
+  const Candidates to{list, &counts[wid], kSmallRoom};
+  Bound b{of_order(lo), 0xffffffffu};
+  LaneSum sum;
+  uint32_t found;
+  for (bool own = false;;) {
+    // nothing but -infinity and NaN is left out by the lowest bound
+    const bool others = lo != kLeastOrder || b.end != 0xffffffffu;
+    const float ref = own ? m : others ? b.least : 0.f;
+    const RowLog<T, false> log(ref, a.c);
+    F2 s(0.f), u(0.f);
+    if (lane == 0) counts[wid] = 0;
+    __syncwarp();
+    if (b.holds(v, at)) to.add(v, at);
+    else add_one<T, ENT, false>(s, u, log, v);
+#pragma unroll 1
+    for (int k = 0; k < all; ++k)
+      if (const uint4 x = w[32 * k]; __any_sync(kAllLanes, Vec16<T>::max(x) >= b.least))
+        add_but<T, ENT, false>(s, u, log, x, column(k), b, to);
+      else
+        add_vector<T, ENT, false>(s, u, x, log);
+    __syncwarp();
+    found = counts[wid];
+    sum = {others ? ref : kNegInf, s, u};
+    if (found > kSmallRoom) {  // equal ones, by the hundred
+      auto count = [&](const Bound &probe) {
+        uint32_t c = 0;
+        each([&](float z, uint32_t i) { c += probe.holds(z, i); });
+        return __reduce_add_sync(kAllLanes, c);
+      };
+      b = search_bound(count, 0, a.vocab, lo, K, kSmallRoom);
+      lo = order_of(b.least);
+      __syncwarp();
+      continue;
+    }
+    if (own || !others || !(warp_add(s.x() + s.y()) < kLeastSum)) break;
+    // so low that the numbers lose bits: relative to their own maximum
+    m = kNegInf;
+    each([&](float z, uint32_t i) { m = b.holds(z, i) ? m : fmaxf(m, z); });
+#pragma unroll
+    for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(kAllLanes, m, i));
+    own = true;
+    __syncwarp();
+  }
+  const uint32_t runs = (found + 31) / 32;
+#pragma unroll 1
+  for (uint32_t r = 0; r < runs; ++r)
+    list[32 * r + lane] = warp_sorted(32 * r + lane < found ? list[32 * r + lane] : 0);
+  __syncwarp();
+  if (runs > 1) {
+#pragma unroll 1
+    for (uint32_t i = lane; i < found; i += 32) {
+      const Key key = list[i];
+      sorted[larger_in_runs(list, 32, runs, 32, key)] = key;
+    }
+    __syncwarp();
   } else {
-    const float d = (sum.m - M) * a.c, f = ex2(d);
-    S = fmaf(f, sum.s, S);
-    U += f > 0.f ? f * fmaf(d, sum.s, sum.u) : 0.f;
+    sorted = list;
   }
-  const float ln = logf(S);
-  const bool nan = S != S;
-  if (threadIdx.x < K) {
-    o.ids[t * K + threadIdx.x] = key && !nan ? (int32_t)column_of(key) : -1;
-    o.top_logp[t * K + threadIdx.x] =
-        nan ? S : key ? (value_of(key) - M) * a.inv_t - ln : kNegInf;
+  const Key key = lane < K && lane < found ? sorted[lane] : 0;
+  // candidates behind the list join the others
+#pragma unroll 1
+  for (uint32_t i = K + lane; i < found; i += 32) {
+    const float z = value_of(sorted[i]);
+    add_one<T, ENT, false>(sum.s, sum.u, raise<T, ENT, false>(sum, z, a.c), z);
   }
-  if (threadIdx.x) return;
-  if (o.logp) o.logp[t] = (zt - M) * a.inv_t - ln;
-  if (o.entropy) o.entropy[t] = ln - kLn2 * (U / S);
-  if (o.rest)
-    o.rest[t] = nan ? S : sum.s == 0.f ? kNegInf : (sum.m - M) * a.inv_t + logf(sum.s) - ln;
-  if (o.stats) {
-    o.stats[2 * t] = M;
-    o.stats[2 * t + 1] = S;
+  const RowSum rest = warp_sum<T, false>(row_sum(sum), a.c);
+  if (!found && !(rest.s != rest.s)) {  // no token has a probability
+    if (lane == 0) flag(ctrl, DEVERR_ROW, t);
+    write_none(o, t, lane);
+    return;
   }
+  const float M = found ? value_of(__shfl_sync(kAllLanes, key, 0)) : kNegInf;
+  float S = 0.f, U = 0.f;
+  if (key) {
+    const float y = (value_of(key) - M) * a.c;
+    S = ex2(y);
+    if (ENT) U = S * fmaxf(y, kNoLog);
+  }
+  S = warp_add(S);
+  if (ENT) U = warp_add(U);
+  finish(a, o, t, lane, key, M, S, U, rest, zt);
 }
 
 }  // namespace
@@ -601,6 +776,25 @@ static uint32_t first_bound(double K, double sample, double rounds, double threa
 cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_t *ids,
                              float *top_logp, float *logp, float *entropy, float *rest,
                              float *stats, cudaStream_t s) {
+  const uint64_t row_bytes = (uint64_t)z.vocab * (z.dtype == EDP_F32 ? 4 : 2);
+  const uint64_t sms = (uint64_t)ctx->coop_sms;
+  const uint64_t small = z.rows >= 8 * sms   ? top <= 8 ? 12288 : 8192
+                         : z.rows >= 2 * sms ? 4096
+                                             : 2048;
+  if (top <= kSmallTop && row_bytes <= small) {
+    return by_type(z.dtype, [&](auto x) {
+      using T = decltype(x);
+      const TopOut o{ids, top_logp, logp, entropy, rest, stats, top, 0};
+      auto kern = entropy ? k_top_small<T, true> : k_top_small<T, false>;
+      const uint32_t vectors = (uint32_t)(row_bytes / 16 + 31) / 32;  // per lane
+      const cudaError_t e = cudaFuncSetAttribute(
+          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 48 * 1024);
+      if (e != cudaSuccess) return e;
+      return launch_rows(kern, (z.rows + kSmallRows - 1) / kSmallRows, 1, false, 32 * kSmallRows,
+                         (size_t)kSmallRows * vectors * 512, s, row_args(z), o, z.rows, vectors,
+                         ctx->ctrl);
+    });
+  }
   const StreamShape shape = stream_shape(ctx, z, top <= 64);
   const uint32_t parts = shape.parts;
   return by_type(z.dtype, [&](auto x) {
@@ -614,7 +808,7 @@ cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_
       const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
       const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + ST * kUnroll * NT);
       const cudaError_t e = cudaFuncSetAttribute(
-          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+          kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
       if (e != cudaSuccess) return e;
       return launch_rows(kern, z.rows, parts, true, NT, bytes, s, row_args(z), o, ctx->ctrl);
     });
