@@ -171,23 +171,24 @@ __device__ __forceinline__ RowSum joined(const RowSum &mine, const RowSum &more,
 // (us, parts x threads): 1 row of 152,064: 13.8 as 1 x 256, 9.4 as 8 x 256, 9.9 as 8 x 512; of
 // 32,003: 7.7 as 1 x 256, 8.1 as 8 x 256; 64 rows of 152,064: 19.5 as 1 x 256, 15.1 as 2 x
 // 256, 13.1 as 2 x 512, 16.1 as 4 x 512; 128: 20.0 as 1 x 256, 15.6 as 1 x 512; 2,000 rows of
-// 4,000: 28.3 as 1 x 256, 16.1 as 1 x 128; 4,096 of 32,003: 82 and 69, but 400 of them 14.7 and
-// 17.9; 2,048 rows of 152,064: 117 as 1 x 256, 147 as 1 x 512.  With long lists the 4 warps of
-// 128 threads say too little about a bound (2,000 rows of 4,000 with 128 entries: 92 us, 43
-// with 256).  Four rounds in flight where CTAs are two per SM at the most: 256 rows of 32,003
-// fp16 logits 11.5 us in a stream however the calls come, with two 11.1 to 14.6.
+// 4,000: 28.3 as 1 x 256, 16.1 as 1 x 128; 5,400 of 16,000: 109 and 86; 4,000 of 32,003: 94 and
+// 75; 2,000 of 100,000: 97 and 86, but of 152,064 116 and 126, and 700 of 61,882 30 and 41; 2,048
+// of 152,064: 117 as 1 x 256, 147 as 1 x 512.  Of a part that is all sampled 128 threads give no
+// bound for more entries than they are (2,000 rows of 4,000 with 128 entries: 92 us, 43 with 256).
+// Four rounds in flight where CTAs are two per SM at the most: 256 rows of 32,003 fp16 logits
+// 11.5 us in a stream however the calls come, with two 11.1 to 14.6.
 struct StreamShape {
   uint32_t parts, threads, stages;
   uint64_t vecs;  // of a part
 };
-inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, bool few_entries) {
+inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, uint32_t entries) {
   const uint64_t sms = (uint64_t)ctx->coop_sms;
   const uint64_t vecs = (uint64_t)z.vocab * (z.dtype == EDP_F32 ? 4 : 2) / 16;
   uint32_t parts = 1;
   while (parts < kMostParts && 2 * parts * z.rows <= sms && vecs >= 2ull * parts * 2048) parts *= 2;
   const uint64_t each = vecs / parts;
-  const bool small = each <= 1024 || (each <= 4096 && z.rows * parts >= 8 * sms);
-  if (small && few_entries) return {parts, 128, 2, each};
+  const bool small = each <= 1024 ? entries <= 96 : each <= 12800 && z.rows * parts >= 8 * sms;
+  if (small) return {parts, 128, 2, each};
   if (each >= 8192 && z.rows * parts <= sms) return {parts, 512, 2, each};
   return {parts, 256, z.rows * parts <= 2 * sms ? 4u : 2u, each};
 }

@@ -660,7 +660,7 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
     using T = decltype(x);
     auto stream = [&](auto back) {
       constexpr bool BACK = decltype(back)::value;
-      StreamShape shape = stream_shape(ctx, z, true);
+      StreamShape shape = stream_shape(ctx, z, 1);
       if (shape.vecs > 8 * 64 * 1024) shape.threads = 256, shape.stages = 2;  // room for the marks
       return by_shape(shape, [&](auto threads, auto stages) {
         constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;

@@ -450,6 +450,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   Bound b{of_order(lo), 0xffffffffu};
   uint32_t found, reached = kLeastOrder;  // reached: by too many
   bool many = false, few = false;  // so far
+  uint32_t tries = 0;
   RowSum sum;
 #pragma unroll 1
   for (bool again = false, searched = false, careful = false;;) {
@@ -484,15 +485,18 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
     }
     __syncthreads();
     if (enough) continue;
-    // another of the sample's numbers, unless there is none or that leads back
+    // another of the sample's numbers, first a quarter of the way further (most lack little),
+    // then more, unless there is none or that leads back
     const bool over = found > kRoom;
     if (over) reached = lo;
     (over ? many : few) = true;
     uint32_t next = lo;
     while (next == lo && nth - 1 < full) {
-      nth = over ? nth / 2 : nth < full ? min(2 * nth, full) : full + 1;
+      const uint32_t by = max(1u, nth >> (tries < 2 ? 2 - tries : 0));
+      nth = over ? (nth > by ? nth - by : nth / 2) : nth < full ? min(nth + by, full) : full + 1;
       next = bound_at(nth);
     }
+    ++tries;
     if (nth - 1 < full && !(many && few)) {
       lo = next;
       b.least = of_order(lo);
@@ -795,7 +799,7 @@ cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_
                          ctx->ctrl);
     });
   }
-  const StreamShape shape = stream_shape(ctx, z, top <= 64);
+  const StreamShape shape = stream_shape(ctx, z, top);
   const uint32_t parts = shape.parts;
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
