@@ -78,7 +78,8 @@ class Batch:
 @pytest.mark.parametrize("teacher,student", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f16")])
 @pytest.mark.parametrize("kind,beta,with_rest", [(L.FORWARD, 0.0, True), (L.FORWARD, 0.0, False),
                                                  (L.REVERSE, 0.0, True), (L.MIX, 0.6, True)])
-@pytest.mark.parametrize("rows,vocab,top", [(9, 97, 100), (24, 4_001, 20), (60, 33_003, 64)])
+@pytest.mark.parametrize("rows,vocab,top", [(9, 97, 100), (24, 4_001, 20), (60, 33_003, 64),
+                                            (1_500, 301, 12), (1_200, 2_600, 40)])
 def test_lists_to_loss(edp_lib, teacher, student, kind, beta, with_rest, rows, vocab, top):
     edp, ring = edp_lib, ctx_of(edp_lib)
     b = Batch(rows, vocab, top, teacher, student, rows + top)
@@ -170,3 +171,32 @@ def test_sampled_token_among_the_list(edp_lib):
     edp.edp_sync(ring.ctx)
     want = L.token_logprob_grad(to_np(b.t.double()), to_np(target), np.ones(30))
     assert np.all(np.abs(to_np(d.double()) - want) <= UNIT["bf16"] * np.abs(want) + 4e-5)
+
+
+@pytest.mark.parametrize("reduce", [L.TOKEN_MEAN, L.SEQ_MEAN])
+def test_lists_right_before_the_loss(edp_lib, reduce):
+    """Teacher after teacher without a pause: each loss is of the lists written just before it
+    (the loss's kernels start while the ones before them end)."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    batches = [Batch(2_000, 1_001, 16, "bf16", "bf16", s) for s in range(4)]
+    cfg = edp.make_distill_config(edp.EDP_DISTILL_FORWARD, reduce)
+    d = [torch.zeros_like(b.s) for b in batches]
+    alone = []
+    for b, g in zip(batches, d):
+        b.teach(edp, ring)
+        torch.cuda.synchronize()
+        b.learn(edp, ring, cfg, g)
+        torch.cuda.synchronize()
+        alone.append((b.loss.clone(), b.each.clone(), g.clone()))
+        b.ids.fill_(-1)
+        b.lp.fill_(float("nan"))
+        g.fill_(7.0)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, g in zip(batches, d):
+            b.teach(edp, ring)
+            b.learn(edp, ring, cfg, g)
+    edp.edp_sync(ring.ctx)
+    for b, g, want in zip(batches, d, alone):
+        for x, y in zip((b.loss, b.each, g), want):
+            assert torch.equal(x, y)
