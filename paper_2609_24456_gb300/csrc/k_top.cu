@@ -212,7 +212,7 @@ __device__ __forceinline__ uint32_t cta_count(uint32_t n, uint32_t *red) {
 // A bound that K to `room` numbers of n from column `first` on hold, searched from `lo` on
 // (which more reach, unless it is the lowest) by counts: whether it is the K-th largest number
 // itself (equal by the hundred, as masked ones are), else the number by halving; and of those
-// equal to it an end, by steps that grow and by halving.  Rare, so that it only has to end: 64
+// equal to it an end, by steps that grow and by halving.  Rare, so that it only has to end: 80
 // counts at the most.
 template <typename Count>
 __device__ __forceinline__ Bound search_bound(Count count, uint32_t first, uint32_t n, uint32_t lo,
@@ -242,7 +242,7 @@ __device__ __forceinline__ Bound search_bound(Count count, uint32_t first, uint3
       (c >= K ? lo : hi) = mid;
     } else {
       (c >= K ? b : a) = column;
-      step = c >= K ? kAll : 8 * min(step, n);
+      step = c >= K ? kAll : step > n / 8 ? n : 8 * step;  // (8 n may pass 32 bits)
     }
   }
 }

@@ -336,6 +336,32 @@ def test_offsets_beyond_32_bits(edp_lib):
     check(o, to_np(v.double()), target, 10)
 
 
+@pytest.mark.parametrize("top", [1, 64])
+def test_equal_at_the_end_of_the_longest_rows(edp_lib, top):
+    """Equal numbers, more than a row's candidates may be, at the end of 2^29 columns and more:
+    the search for the last of them passes sizes whose eighth part fits 29 bits.  One row of 77
+    is in use (with fewer the row would be split)."""
+    ring = ctx_of(edp_lib)
+    rows, vocab, n = 77, (1 << 29) + 3, 1_500
+    if torch.cuda.mem_get_info()[0] < 2 * rows * vocab + (4 << 30):
+        pytest.skip("too little memory is free")
+    z = torch.empty(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    z[-2].fill_(float("-inf"))
+    z[-2, -n:] = 1.0
+    mask = np.zeros(rows, np.uint8)
+    mask[-2] = 1
+    o = {k: x for k, x in outputs(rows, top).items() if k in ("ids", "top_logp", "rest")}
+    run(edp_lib, ring, z, None, o, mask=mask)
+    edp_lib.edp_sync(ring.ctx)
+    del z
+    torch.cuda.empty_cache()
+    live = mask != 0
+    ids, logp, rest = (to_np(o[k]) for k in ("ids", "top_logp", "rest"))
+    assert np.array_equal(ids[live][0], vocab - n + np.arange(top))
+    assert near(logp[live], np.full((1, top), -np.log(n))) and near(rest[live], np.log1p(-top / n))
+    assert (ids[~live] == -1).all() and np.isneginf(logp[~live]).all() and not rest[~live].any()
+
+
 def test_stream_and_graph(edp_lib):
     """On a stream of its own, and captured: replays read what the arrays then hold."""
     edp, ring = edp_lib, ctx_of(edp_lib)
