@@ -9,8 +9,10 @@ namespace edp {
 
 constexpr int kStreamLanes = 1024;  // threads per SM, which bounds the registers
 constexpr uint32_t kMostParts = 8;
-// Sums below lose bits of numbers whose power of 2 leaves fp32.
+// Sums below lose bits of numbers whose power of 2 leaves fp32.  Of those above, eight parts'
+// sums may add up to infinity, and what is divided by them leaves fp32 below.
 constexpr float kLeastSum = 0x1p-64f;
+constexpr float kMostSum = 0x1p64f;
 
 // A vector of logits at -infinity.
 template <typename T>

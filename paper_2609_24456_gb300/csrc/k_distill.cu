@@ -442,7 +442,7 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
 // logits read a second time, for rows of which too little fits shared memory.  A vector with
 // an entry in it is left out of the sums; the first of its entries adds what else there is in
 // it.  All is relative to the list's maximum (no maximum is kept), which is near the row's,
-// most likely: sums that leave fp32 are made again, carefully.
+// most likely: a part whose sum is far from 1 is summed again relative to its own.
 template <typename T, int NT, int ST, bool BACK>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
@@ -565,7 +565,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
         warp_sum<T, false, lanes_for(NT / 32)>(
             lane < (NT / 32) ? red[lane] : RowSum{kNegInf, 0.f, 0.f}, a.c), a.c);
     const float S = __shfl_sync(kAllLanes, sum.s, 0);
-    careful = !(S >= kLeastSum && S < __builtin_huge_valf());
+    careful = !(S >= kLeastSum && S <= kMostSum);
     if (careful) __syncthreads();
   }
   if (careful) {
