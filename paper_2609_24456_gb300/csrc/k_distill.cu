@@ -394,7 +394,7 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
     const RowLoss f = rule.kind == EDP_DISTILL_MIX ? RowLoss{}
                                                    : row_loss_of(rule.kind, l, r, lpr, pr);
     if (lane) return;
-    careful = near && !(sum.s >= kLeastSum && sum.s < __builtin_huge_valf());
+    careful = near && !(sum.s >= kLeastSum && sum.s <= kMostSum);
     rows = r;
     found = f;
     twice = again;
@@ -407,8 +407,10 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
     if (wid == 0) join(near, round);
     __syncthreads();
   };
-  // Relative to the list's maximum, which is near the row's, most likely; what leaves fp32
-  // that way is summed again relative to each thread's own.
+  // Relative to the list's maximum, which is near the row's, most likely; a sum that is far
+  // from 1 that way is made again relative to each thread's own.  (The gradient's factor of
+  // 2^y is divided by it: in a mean over 8,192 rows it would be below fp32's least normal
+  // number from 2^113 on.)
   const bool near = fabsf(l.m) < __builtin_huge_valf() && (!F || sums_hold(l.m, a.c));
   whole_row(near ? warp_sum<T, false>(
                        RowSum{l.m, part_sum_near<T, F, NT>(held, n, RowLog<T, F>(l.m, a.c)), 0.f},

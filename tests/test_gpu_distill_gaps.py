@@ -43,3 +43,30 @@ def test_loss_alone(edp_lib, dtype, vocab, rows, first, kind, rest):
     edp.edp_sync(ring.ctx)
     assert torch.isfinite(each).all()
     c.check(loss, each)
+
+
+@pytest.mark.parametrize("vocab", [3_001, 66_000, 240_000])
+@pytest.mark.parametrize("first", [60, 78])
+@pytest.mark.parametrize("kind,rest", KINDS)
+@pytest.mark.parametrize("scale,norm,T", [(1.0, 8_192.0, 1.0), (1e-3, 1_000.0, 1.0),
+                                          (1.0, 1e6, 0.1)])
+def test_small_gradients(edp_lib, vocab, first, kind, rest, scale, norm, T):
+    """In fp32, whose bits the other tokens' factor has to have: held in shared memory, and
+    (240,000 columns) from a second reading."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    c = below(18, vocab, "f32", kind, rest, first, T=T, scale=scale, norm=norm)
+    _, d = view(18, vocab, "f32")
+    loss, each = c.run(edp, ring, d)
+    edp.edp_sync(ring.ctx)
+    c.check(loss, each, d)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 3_001), ("f16", 70_001), ("bf16", 470_000)])
+@pytest.mark.parametrize("first", [60, 78])
+def test_gradients_of_16_bits(edp_lib, dtype, vocab, first):
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    c = below(18, vocab, dtype, L.MIX, True, first)
+    _, d = view(18, vocab, dtype)
+    loss, each = c.run(edp, ring, d)
+    edp.edp_sync(ring.ctx)
+    c.check(loss, each, d)
