@@ -799,7 +799,8 @@ typedef struct {
  * all -infinity add 0 to the loss, have gradient 0 and are reported by edp_sync
  * (EDP_ERR_INVALID).  A class with p > 0 and q = 0 makes FORWARD infinite (its
  * gradient stays finite), one with q > 0 and p = 0 REVERSE (its row's gradient is
- * then NaN); NaN or +infinity in a row or its list makes loss and gradient NaN.
+ * then NaN); NaN or +infinity in a row, its list or its rest makes its loss and
+ * gradient NaN, whatever the student's probabilities are.
  * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, top outside
  * [1, 128], a NULL logits, ids, value or loss, REVERSE or MIX without rest, rows ==
  * 0, a vocabulary whose row takes more than 16 MiB (8,388,608 logits of 16 bits,

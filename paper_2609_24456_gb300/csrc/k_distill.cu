@@ -94,9 +94,14 @@ struct Entry {
 };
 // What does not need the row's sums, made while the row is on its way: the list's maximum,
 // the sums of e, of p, and of p (lp - x) with FORWARD or of e (x - lp) with REVERSE.
+// bad: NaN where the teacher has NaN or +infinity, which a student's q of 0 would hide, else 0.
 struct ListSums {
-  float m, s, p, cross;
+  float m, s, p, cross, bad;
 };
+// NaN in the place of +infinity, which is no logarithm of a probability either.
+__device__ __forceinline__ float teacher_log(float x) {
+  return x < __builtin_huge_valf() ? x : __int_as_float(0x7fffffff);
+}
 // Of the whole row: its logarithms' normaliser relative to the list's maximum, what takes e
 // to q; the others' q and its logarithm, their maximum and sum.
 struct RowSums {
@@ -108,14 +113,14 @@ __device__ __forceinline__ RowSums row_sums(const ListSums &l, const RowSum &o, 
   const float M = fmaxf(l.m, o.m);
   const float to_row = l.m == kNegInf ? 1.f : ex2((l.m - M) * c);
   const float left = o.m == kNegInf ? o.s : o.s * ex2((o.m - M) * c);
-  const float S = fmaf(l.s, to_row, left), ln = logf(S), inv = 1.f / S;
+  const float sum = fmaf(l.s, to_row, left), S = sum + l.bad, ln = logf(S), inv = 1.f / S;
   return {ln + (M - (l.m == kNegInf ? 0.f : l.m)) * inv_t,
           to_row * inv,
           left * inv,
           o.s == 0.f ? kNegInf : (o.m - M) * inv_t + logf(o.s) - ln,
           o.m,
           o.s,
-          M == kNegInf && S == S};
+          M == kNegInf && sum == sum};
 }
 // The row's loss, the others' gradient and `g`, by which an entry's goes, before the weight.
 struct RowLoss {
@@ -155,14 +160,15 @@ template <typename T, int NT>
 __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights &weights,
                                               bool by_range, const TeacherLists &lists,
                                               const DistillRule &rule, const T *row, uint64_t t,
-                                              Entry *entry, ListRoom *s) {
+                                              float pr, Entry *entry, ListRoom *s) {
   const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const uint32_t warps = (lists.top + 31) / 32;
   const bool busy = wid < warps, has_rest = lists.rest != nullptr;
   Entry e = *entry;
-  ListSums l{kNegInf, 0.f, 0.f, 0.f};
+  ListSums l{kNegInf, 0.f, 0.f, 0.f, 0.f};
   if (busy) {
     if (e.lp == kNegInf) e.id = -1;
+    e.lp = teacher_log(e.lp);
     if (e.id >= 0 && (uint32_t)e.id >= a.vocab) {
       s->strange = e.id;
       e.id = -1;
@@ -209,6 +215,8 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
     l.cross = sums.x;
     l.p = sums.y;
   }
+  const float all = l.p + pr;
+  if (all != all) l.bad = all;
   *entry = e;
   return l;
 }
@@ -235,9 +243,11 @@ __device__ __forceinline__ RowLoss mix_loss(const DistillRule &rule, const Teach
 }
 
 // The gradient of the tokens outside of the list: a factor of their 2^y.  Without a finite
-// logit among them there is no maximum to be relative to, and each 2^y is 0.
+// logit among them there is no maximum to be relative to, and each 2^y is 0 (whose product
+// with NaN is NaN).
 __device__ __forceinline__ RowGrad others_grad(const RowSums &r, const RowLoss &f, float by) {
-  return {r.m == kNegInf ? 0.f : r.m, r.s == 0.f ? 0.f : by * (f.outside / r.s), 0.f, 0.f};
+  return {r.m == kNegInf ? 0.f : r.m,
+          r.s == 0.f && f.outside == f.outside ? 0.f : by * (f.outside / r.s), 0.f, 0.f};
 }
 // An entry's, before the weight.
 __device__ __forceinline__ float entry_grad(const DistillRule &rule, const Entry &e,
@@ -352,8 +362,9 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
   // here before this CTA's message leaves, and only then may another write its gradient in
   // their place, or set back the count behind the weight).
   if (early) pdl_wait();
-  const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
-  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
+  const float lpr = lists.rest ? teacher_log(lists.rest[t]) : kNegInf,
+              pr = lists.rest ? expf(lpr) : 0.f;
+  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, pr, &e, &list);
   if (sp.vecs && !mbar_wait(&bar, 0, kRowWaitNs)) {
     if (threadIdx.x == 0) flag(ctrl, DEVERR_TIMEOUT, t);
     mbar_wait(&bar, 0, kRowWaitNs);  // bounded: the copy lands before the CTA ends
@@ -497,8 +508,9 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
   x.start(ring);
   if (np > 1) cluster_started();
   if (early) pdl_wait();
-  const float lpr = lists.rest ? lists.rest[t] : kNegInf, pr = lists.rest ? expf(lpr) : 0.f;
-  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, &e, &list);
+  const float lpr = lists.rest ? teacher_log(lists.rest[t]) : kNegInf,
+              pr = lists.rest ? expf(lpr) : 0.f;
+  const ListSums l = read_list<T, NT>(a, weights, by_range, lists, rule, row, t, pr, &e, &list);
   // Marks: a bit for each vector with an entry, and for each other number that is one.
   const uint32_t place = (uint32_t)e.id - first - x.sp.head;  // among the vectors' numbers
   const bool here = e.id >= 0 && (uint32_t)e.id - first < n, inside = here && place < x.sp.vecs * N;
