@@ -134,7 +134,9 @@ __device__ __forceinline__ RowLoss row_loss_of(uint32_t kind, const ListSums &l,
     return {fmaf(l.p, r.ln, l.cross) + weigh(pr, lpr - r.lqr), fmaf(P, r.qr, -pr), P};
   }
   const float all = r.by * fmaf(-l.s, r.ln, l.cross) + weigh(r.qr, r.lqr - lpr);
-  return {all, weigh(r.qr, r.lqr - lpr - all), all};
+  // where the teacher excludes what the student does not, an infinite loss has no gradient
+  const float g = fmaf(0.f, all, all);
+  return {all, weigh(r.qr, r.lqr - lpr - g), g};
 }
 
 // An entry as the list has it; asked for before anything else of the row is known.
@@ -253,6 +255,7 @@ __device__ __forceinline__ RowGrad others_grad(const RowSums &r, const RowLoss &
 __device__ __forceinline__ float entry_grad(const DistillRule &rule, const Entry &e,
                                             const RowSums &r, const RowLoss &f, float lm) {
   const float q = e.e * r.by;
+  if (f.g != f.g) return f.g;  // (a weight of 0 would hide it)
   if (rule.kind == EDP_DISTILL_FORWARD) return fmaf(f.g, q, -e.p);
   if (rule.kind == EDP_DISTILL_REVERSE) return weigh(q, e.x - r.ln - e.lp - f.g);
   return weigh(q, fmaf(rule.alpha, e.x - r.ln - lm, -f.g));

@@ -81,3 +81,24 @@ def test_nan_and_infinity_in_lists_without_rest(edp_lib, dtype, vocab, top):
         assert torch.isnan(loss[0]) and torch.isnan(each[:4]).all()
         near_rows(c, [4, 5], each, out)
     assert torch.isnan(d[:4]).all()
+
+
+@pytest.mark.parametrize("dtype,vocab", SIZES)
+def test_reverse_where_the_teacher_excludes_the_rest(edp_lib, dtype, vocab):
+    """The loss is infinite, and the row's gradient NaN throughout: at the entries, at those
+    that the student gives nothing, and at all others."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    c = Case(4, vocab, 12, dtype, L.REVERSE, True, 4, absent=False)
+    c.rest[:2] = -np.inf
+    c.zd[1, c.ids[1, 2]], c.zd[1, c.ids[1, 3]] = -300, -np.inf
+    exclude(c, 2, np.setdiff1d(np.arange(vocab), c.ids[2]))  # nothing is left to exclude
+    c.rest[2] = -np.inf
+    c.v.copy_(torch.from_numpy(c.zd))
+    c.zd = to_np(c.v.double())
+    _, d = view(4, vocab, dtype)
+    for out in (d, None):
+        loss, each = c.run(edp, ring, out)
+        edp.edp_sync(ring.ctx)
+        assert loss[0] == float("inf") and (each[:2] == float("inf")).all()
+        near_rows(c, [2, 3], each, out)
+    assert torch.isnan(d[:2]).all()
