@@ -800,7 +800,9 @@ typedef struct {
  * (EDP_ERR_INVALID).  A class with p > 0 and q = 0 makes FORWARD infinite (its
  * gradient stays finite), one with q > 0 and p = 0 REVERSE (its row's gradient is
  * then NaN); NaN or +infinity in a row, its list or its rest makes its loss and
- * gradient NaN, whatever the student's probabilities are.
+ * gradient NaN, whatever the student's probabilities are.  So does a list without
+ * an entry whose values are all NaN, as edp_token_top writes it for a teacher's row
+ * with NaN or +infinity; other values beside negative ids may be anything.
  * Errors: EDP_ERR_INVALID for a configuration outside the ranges above, top outside
  * [1, 128], a NULL logits, ids, value or loss, REVERSE or MIX without rest, rows ==
  * 0, a vocabulary whose row takes more than 16 MiB (8,388,608 logits of 16 bits,

@@ -55,6 +55,9 @@ struct TeacherLists {
   uint32_t top;
 };
 
+constexpr float kNaN = __builtin_nanf("");
+
+// NaN apart, which it is of NaN alone
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kAllLanes, x, o));
@@ -100,7 +103,7 @@ struct ListSums {
 };
 // NaN in the place of +infinity, which is no logarithm of a probability either.
 __device__ __forceinline__ float teacher_log(float x) {
-  return x < __builtin_huge_valf() ? x : __int_as_float(0x7fffffff);
+  return x < __builtin_huge_valf() ? x : kNaN;
 }
 // Of the whole row: its logarithms' normaliser relative to the list's maximum, what takes e
 // to q; the others' q and its logarithm, their maximum and sum.
@@ -141,7 +144,7 @@ __device__ __forceinline__ RowLoss row_loss_of(uint32_t kind, const ListSums &l,
 
 // An entry as the list has it; asked for before anything else of the row is known.
 __device__ __forceinline__ Entry load_entry(const TeacherLists &lists, uint64_t t) {
-  Entry e{-1, kNegInf, 0.f, kNegInf, 0.f};
+  Entry e{-1, kNaN, 0.f, kNegInf, 0.f};
   if (threadIdx.x < lists.top) {
     const uint64_t at = t * lists.top + threadIdx.x;
     e.id = lists.ids[at];
@@ -170,14 +173,16 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
   ListSums l{kNegInf, 0.f, 0.f, 0.f, 0.f};
   if (busy) {
     if (e.lp == kNegInf) e.id = -1;
-    e.lp = teacher_log(e.lp);
+    if (e.id >= 0) e.lp = teacher_log(e.lp);
     if (e.id >= 0 && (uint32_t)e.id >= a.vocab) {
       s->strange = e.id;
       e.id = -1;
     }
     const float z = e.id >= 0 ? to_f32(row[e.id]) : kNegInf;
     e.x = z;
-    const float m = warp_max(z), v = warp_max(e.id >= 0 ? e.lp : kNegInf);
+    // v: NaN where there are no entries and NaN is all that the list has, which is how
+    // edp_token_top marks the row of a teacher that went wrong
+    const float m = warp_max(z), v = warp_max(e.id >= 0 || e.lp != e.lp ? e.lp : kNegInf);
     if (lane == 0) s->sums[0][wid] = make_float2(m, v);
   }
   if (wid == NT / 32 - 1) {
@@ -191,7 +196,7 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
     if (lane == 0) s->weight = w;
   }
   __syncthreads();
-  float top_value = kNegInf;
+  float top_value = kNaN;
   for (uint32_t i = 0; i < warps; ++i) {
     l.m = fmaxf(l.m, s->sums[0][i].x);
     top_value = fmaxf(top_value, s->sums[0][i].y);
@@ -218,7 +223,7 @@ __device__ __forceinline__ ListSums read_list(const RowArgs &a, const RowWeights
     l.p = sums.y;
   }
   const float all = l.p + pr;
-  if (all != all) l.bad = all;
+  if (all != all || top_value != top_value) l.bad = kNaN;
   *entry = e;
   return l;
 }

@@ -102,3 +102,35 @@ def test_reverse_where_the_teacher_excludes_the_rest(edp_lib, dtype, vocab):
         assert loss[0] == float("inf") and (each[:2] == float("inf")).all()
         near_rows(c, [2, 3], each, out)
     assert torch.isnan(d[:2]).all()
+
+
+@pytest.mark.parametrize("top", [1, 20, 33, 128])
+@pytest.mark.parametrize("vocab", [130, 33_001])
+@pytest.mark.parametrize("with_rest", [True, False])
+def test_a_broken_teacher(edp_lib, top, vocab, with_rest):
+    """A teacher's row with NaN or +infinity is the student's, too: edp_token_top marks it by
+    ids of -1 and NaN, and the loss does not pass over it as over a row without a list."""
+    edp, ring = edp_lib, ctx_of(edp_lib)
+    t = torch.randn(6, vocab, device="cuda")
+    t[0, 5], t[1, vocab - 1] = float("nan"), float("inf")
+    s = torch.randn(6, vocab, device="cuda")
+    mask = torch.tensor([1, 1, 0, 1, 1, 1], dtype=torch.uint8, device="cuda")
+    ids = torch.zeros(6, top, dtype=torch.int32, device="cuda")
+    lp, rest = torch.zeros(6, top, device="cuda"), torch.zeros(6, device="cuda")
+    edp.edp_token_top(ring.ctx, t, ids, lp, mask=mask, rest=rest)
+    ids[4], lp[4], rest[4] = -1, -float("inf"), -float("inf")  # a row without a list
+    # places without a token hold anything, unless it is NaN alone
+    ids[3, 1:], lp[3, 1:] = -1, float("nan")
+    ids[5], lp[5], rest[5] = -1, float("nan"), -float("inf")
+    lp[5, top // 2] = 3.0
+    loss, each = torch.zeros(1, device="cuda"), torch.zeros(6, device="cuda")
+    d = torch.full_like(s, 7.0)
+    for out in (d, None):
+        edp.edp_distill_loss(ring.ctx, edp.make_distill_config(), s, ids, lp, loss,
+                             rest=rest if with_rest else None, mask=mask, row_loss=each,
+                             dlogits=out)
+        edp.edp_sync(ring.ctx)
+        assert torch.isnan(loss).all() and torch.isnan(each[:2]).all()
+        assert not each[[2, 4, 5]].any() and torch.isfinite(each[3])
+    assert torch.isnan(d[:2]).all()
+    assert not d[[2, 4, 5]].any() and torch.isfinite(d[3]).all()
