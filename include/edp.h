@@ -531,8 +531,9 @@ EDP_API edp_status edp_grpo_pack_deliver(edp_ctx *ctx, const float *r,
  * logits may hold anything, their outputs and gradients are 0.  Outputs overlap
  * no input, but for a gradient in its logits' place.  Arithmetic is fp32, and
  * outputs are rounded to their type.  Sums: a row's exponentials in fp32, by up
- * to thousands of lanes; the policy loss's terms in fp32 for 32 tokens of a lane
- * and in pairs of fp32 numbers beyond, the preference loss's log ratios in such
+ * to thousands of lanes (of rows that edp_token_top and edp_distill_loss stream, in
+ * pairs of fp32 numbers beyond 1,024 of a lane); the policy loss's terms in fp32 for
+ * 32 tokens of a lane and in such pairs beyond, the preference loss's log ratios in
  * pairs; the router's probabilities in fp32 for a few hundred rows of a lane
  * (2^-15 of the sum at the worst) and as whole numbers beyond, as counts and the
  * gradients of shared sequences.  No result depends on the order in which threads

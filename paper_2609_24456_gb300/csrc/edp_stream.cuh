@@ -136,17 +136,93 @@ struct Part {
   }
 };
 
+__device__ __forceinline__ float warp_add(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
+  return x;
+}
+
+// Numbers that are alike round the same way: n of them, added one after another, lose up to
+// n 2^-25 of their sum.  So a lane adds up 512 in each of its two sums (2^-16 at the worst) in the
+// rounds between two carries, where its warp takes them over in pairs.  Parts with more rounds
+// (LONG) have kernels of their own: with the carry in all of them 8,192 lists of 152,064
+// columns took 406 us, without 384.  (8,388,001 fp16 numbers of one CTA: the logarithm of their
+// sum was off by 6.6e-5 without the carry.)
+template <typename T>
+constexpr uint32_t kAloneRounds = 512 / (kUnroll * Vec16<T>::kPairs);
+struct Carried {
+  Pair s, u;
+};
+// take(g) of all rounds, which adds to s and u.  c: the warp's own.
+template <typename T, bool LONG, bool ENT, typename F>
+__device__ __forceinline__ void each_round(uint32_t rounds, Carried *c, F2 &s, F2 &u, F take) {
+  if constexpr (!LONG) {
+    for (uint32_t g = 0; g < rounds; ++g) take(g);
+  } else {
+    if ((threadIdx.x & 31) == 0) *c = Carried{};
+    for (uint32_t g = 0; g < rounds;) {
+      const uint32_t stop = min(rounds, g + kAloneRounds<T>);
+      for (; g < stop; ++g) take(g);
+      const float a = warp_add(s.x() + s.y()), b = ENT ? warp_add(u.x() + u.y()) : 0.f;
+      if ((threadIdx.x & 31) == 0) {
+        pair_add(c->s, a);
+        if (ENT) pair_add(c->u, b);
+      }
+      s = u = F2(0.f);
+    }
+  }
+}
+// A thread's sums relative to ref; what its warp carried is its first lane's.
+template <bool LONG>
+__device__ __forceinline__ RowSum sums_of(const Carried *c, float ref, F2 s, F2 u) {
+  if constexpr (!LONG) return {ref, s.x() + s.y(), u.x() + u.y()};
+  if (threadIdx.x & 31) return {ref, 0.f, 0.f};
+  return {ref, as_df(c->s).hi, as_df(c->u).hi};
+}
+// Two sums beside each other with their rounding errors, for the passes that are rare.
+struct F2Pair {
+  F2 hi = F2(0.f), lo = F2(0.f);
+  __device__ __forceinline__ void add(F2 x) {
+    const F2 less(-1.f), s = hi + x, b = fma2(hi, less, s);
+    lo = lo + (fma2(fma2(b, less, s), less, hi) + fma2(b, less, x));
+    hi = s;
+  }
+  // of both; the errors of infinities are NaN
+  __device__ __forceinline__ float sum() const {
+    const float s = hi.x() + hi.y();
+    return isfinite(s) ? s + (lo.x() + lo.y()) : s;
+  }
+};
+// A lane's sums relative to a number that it raises only where another is 32 powers of 2 above:
+// a sum that is scaled then is 2^-32 of what comes, and its roundings are nothing.
+struct FarSum {
+  float m = kNegInf;
+  F2Pair s, u;
+  template <typename T, bool ENT>
+  __device__ __forceinline__ RowLog<T, false> raise(float to, float c) {
+    if (to > m + 32.f / c) {
+      if (m != kNegInf) {
+        const float d = (m - to) * c, f = ex2(d);
+        if (ENT) {
+          u.hi = f > 0.f ? F2(f) * fma2(F2(d), s.hi, u.hi) : F2(0.f);
+          u.lo = f > 0.f ? F2(f) * fma2(F2(d), s.lo, u.lo) : F2(0.f);
+        }
+        s.hi = F2(f) * s.hi;
+        s.lo = F2(f) * s.lo;
+      }
+      m = to;
+    }
+    return RowLog<T, false>(m, c);
+  }
+  __device__ __forceinline__ RowSum sum() const { return {m, s.sum(), u.sum()}; }
+};
+
 // A number's share of the sums relative to `log`.
 template <typename T, bool ENT, bool FUSED>
 __device__ __forceinline__ void add_one(F2 &s, F2 &u, const RowLog<T, FUSED> &log, float v) {
   const float y = log.of(v), e = ex2(y);
   s = s + F2(e, 0.f);
   if (ENT) u = fma2(F2(e, 0.f), F2(fmaxf(y, kNoLog), 0.f), u);
-}
-__device__ __forceinline__ float warp_add(float x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(kAllLanes, x, o);
-  return x;
 }
 
 // The threads' sums and those that lanes 0 .. n - 1 of each warp have in `more`, in all.
@@ -194,15 +270,20 @@ inline StreamShape stream_shape(const edp_ctx *ctx, const Logits &z, uint32_t en
   if (each >= 8192 && z.rows * parts <= sms) return {parts, 512, 2, each};
   return {parts, 256, z.rows * parts <= 2 * sms ? 4u : 2u, each};
 }
-// f of two whole numbers that are constants: threads and stages.
-template <typename F>
+// f of constants: threads, stages, and whether lanes have so many numbers that warps carry
+// their sums (no parts of 128 threads are so large).
+template <typename T, typename F>
 cudaError_t by_shape(const StreamShape &s, F f) {
   using Two = std::integral_constant<int, 2>;
   using Four = std::integral_constant<int, 4>;
-  if (s.threads == 128) return f(std::integral_constant<int, 128>{}, Two{});
-  if (s.threads == 512) return f(std::integral_constant<int, 512>{}, Two{});
-  return s.stages == 4 ? f(std::integral_constant<int, 256>{}, Four{})
-                       : f(std::integral_constant<int, 256>{}, Two{});
+  if (s.threads == 128) return f(std::integral_constant<int, 128>{}, Two{}, std::false_type{});
+  auto by_threads = [&](auto is_long) {
+    if (s.threads == 512) return f(std::integral_constant<int, 512>{}, Two{}, is_long);
+    return s.stages == 4 ? f(std::integral_constant<int, 256>{}, Four{}, is_long)
+                         : f(std::integral_constant<int, 256>{}, Two{}, is_long);
+  };
+  return s.vecs > (uint64_t)kAloneRounds<T> * kUnroll * s.threads ? by_threads(std::true_type{})
+                                                                  : by_threads(std::false_type{});
 }
 
 }  // namespace edp

@@ -464,7 +464,7 @@ k_distill(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists, Dist
 // an entry in it is left out of the sums; the first of its entries adds what else there is in
 // it.  All is relative to the list's maximum (no maximum is kept), which is near the row's,
 // most likely: a part whose sum is far from 1 is summed again relative to its own.
-template <typename T, int NT, int ST, bool BACK>
+template <typename T, int NT, int ST, bool BACK, bool LONG>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists lists,
                  DistillRule rule, float *loss, float *row_loss, float *per_row, void *dz,
@@ -476,6 +476,7 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
   __shared__ __align__(16) int32_t ids[128];
   __shared__ RowSum red[NT / 32];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S
+  __shared__ Carried carried[LONG ? NT / 32 : 1];
   __shared__ ListRoom list;
   __shared__ uint32_t singles;         // entries before and behind the vectors
   __shared__ bool twice;
@@ -568,7 +569,8 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
     F2 s(0.f), u(0.f);
     if (alone) add_one<T, false, F>(s, u, log, single);
     add_vector<T, false, F>(s, u, rest_of, log);
-    for (uint32_t g = 0; g < x.rounds; ++g) {
+    Carried *own = &carried[LONG ? wid : 0];
+    each_round<T, LONG, false>(x.rounds, own, s, u, [&](uint32_t g) {
       async_wait<ST - 1>();
       uint4 w[kUnroll];
       x.load(w, ring, g);
@@ -579,8 +581,8 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
         add_vector<T, false, F>(s, u, w[k], log);
       }
       x.fetch(ring, g + ST);
-    }
-    sum = warp_sum<T, false>(RowSum{l.m, s.x() + s.y(), 0.f}, a.c);
+    });
+    sum = warp_sum<T, false>(sums_of<LONG>(own, l.m, s, F2(0.f)), a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
     sum = exact_sums<T>(
@@ -591,17 +593,33 @@ k_distill_stream(RowArgs a, RowWeights weights, bool by_range, TeacherLists list
     if (careful) __syncthreads();
   }
   if (careful) {
-    LaneSum b{kNegInf, F2(0.f), F2(0.f)};
+    std::conditional_t<LONG, FarSum, LaneSum> b;
+    if constexpr (!LONG) b = {kNegInf, F2(0.f), F2(0.f)};
     auto take = [&](const uint4 &w) {
-      const uint4 v[1] = {w};
-      take_vectors<T, false, false>(b, v, a.c);
+      if constexpr (LONG) {
+        F2 s(0.f), u;
+        add_vector<T, false, false>(s, u, w, b.template raise<T, false>(Vec16<T>::max(w), a.c));
+        b.s.add(s);
+      } else {
+        const uint4 v[1] = {w};
+        take_vectors<T, false, false>(b, v, a.c);
+      }
     };
-    if (alone) add_one<T, false, false>(b.s, b.u, raise<T, false, false>(b, single, a.c), single);
+    if (alone) {
+      if constexpr (LONG) {
+        F2 s(0.f), u;
+        add_one<T, false, false>(s, u, b.template raise<T, false>(single, a.c), single);
+        b.s.add(s);
+      } else {
+        add_one<T, false, false>(b.s, b.u, raise<T, false, false>(b, single, a.c), single);
+      }
+    }
     take(rest_of);
     x.each_vector(ring, [&](const uint4 &w, uint32_t i) {
       if (!(marks[i / 32] >> (i & 31) & 1)) take(w);
     });
-    sum = warp_sum<T, false>(row_sum(b), a.c);
+    if constexpr (LONG) sum = warp_sum<T, false>(b.sum(), a.c);
+    else sum = warp_sum<T, false>(row_sum(b), a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
     sum = warp_sum<T, false, lanes_for(NT / 32)>(
@@ -684,12 +702,13 @@ cudaError_t launch_distill_loss(edp_ctx *ctx, const edp_distill_config &cfg, con
       constexpr bool BACK = decltype(back)::value;
       StreamShape shape = stream_shape(ctx, z, 1);
       if (shape.vecs > 8 * 64 * 1024) shape.threads = 256, shape.stages = 2;  // room for the marks
-      return by_shape(shape, [&](auto threads, auto stages) {
+      return by_shape<T>(shape, [&](auto threads, auto stages, auto is_long) {
         constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;
+        constexpr bool LONG = decltype(is_long)::value;
         constexpr uint64_t round = kUnroll * (NT / 32);  // segments
         const uint32_t words = (uint32_t)(((shape.vecs + 8) / 32 / round + 1) * round);
         const size_t bytes = sizeof(uint4) * ST * kUnroll * NT + 4 * words;
-        auto kern = k_distill_stream<T, NT, ST, BACK>;
+        auto kern = k_distill_stream<T, NT, ST, BACK, LONG>;
         const cudaError_t err = cudaFuncSetAttribute(
             kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kResidentMost);
         if (err != cudaSuccess) return err;

@@ -137,10 +137,10 @@ __device__ __forceinline__ void each_note(const uint32_t *notes, uint32_t n, F f
 // rows of 152,064 bfloat16 logits took 470 us, without 433).  A vector that has a candidate is
 // taken out whole and noted; the warp looks at those at the end, or when a lane may have no
 // room for another round's.
-template <typename T, int NT, int ST, bool ENT, bool FUSED>
+template <typename T, int NT, int ST, bool ENT, bool FUSED, bool LONG>
 __device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *ring, Bound b,
                                             float ref, const Candidates &to, uint32_t *noted,
-                                            float c) {
+                                            Carried *carried, float c) {
   const RowLog<T, FUSED> log(ref, c);
   F2 s(0.f), u(0.f);
   if (x.single()) {
@@ -151,7 +151,7 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *rin
   }
   const uint32_t lane = threadIdx.x & 31;
   uint32_t n = 0;
-  for (uint32_t g = 0; g < x.rounds; ++g) {
+  auto take = [&](uint32_t g) {
     async_wait<ST - 1>();
     uint4 w[kUnroll];
     x.load(w, ring, g);
@@ -178,13 +178,39 @@ __device__ __forceinline__ RowSum take_part(const Part<T, NT, ST> &x, uint4 *rin
       });
       n = 0;
     }
-  }
-  return {ref, s.x() + s.y(), u.x() + u.y()};
+  };
+  each_round<T, LONG, ENT>(x.rounds, carried, s, u, take);
+  return sums_of<LONG>(carried, ref, s, u);
 }
 // The same relative to each thread's maximum, where the sums ask for that: rare.
-template <typename T, int NT, int ST, bool ENT>
+template <typename T, int NT, int ST, bool ENT, bool LONG>
 __device__ __forceinline__ RowSum take_carefully(const Part<T, NT, ST> &x, uint4 *ring, Bound b,
                                                  const Candidates &to, float c) {
+  if constexpr (LONG) {
+    FarSum a;
+    x.each_vector(ring, [&](const uint4 &w, uint32_t i) {
+      float m = kNegInf;
+#pragma unroll
+      for (int e = 0; e < Vec16<T>::kN; ++e) {
+        const float v = to_f32(reinterpret_cast<const T *>(&w)[e]);
+        m = b.holds(v, x.column(i) + e) ? m : fmaxf(m, v);
+      }
+      F2 s(0.f), u(0.f);
+      add_but<T, ENT, false>(s, u, a.template raise<T, ENT>(m, c), w, x.column(i), b, to);
+      a.s.add(s);
+      if (ENT) a.u.add(u);
+    });
+    if (x.single()) {
+      const uint32_t at = x.single_at();
+      const float v = to_f32(x.p[at]);
+      F2 s(0.f), u(0.f);
+      if (b.holds(v, x.first + at)) to.add(v, x.first + at);
+      else add_one<T, ENT, false>(s, u, a.template raise<T, ENT>(v, c), v);
+      a.s.add(s);
+      if (ENT) a.u.add(u);
+    }
+    return a.sum();
+  }
   LaneSum a{kNegInf, F2(0.f), F2(0.f)};
   auto one = [&](float v, uint32_t column) {
     if (b.holds(v, column)) {
@@ -376,7 +402,7 @@ __device__ __forceinline__ void finish(const RowArgs &a, const TopOut &o, uint64
 }
 
 // A cluster of gridDim.y CTAs per row, each a part of it.
-template <typename T, int NT, int ST, bool ENT>
+template <typename T, int NT, int ST, bool ENT, bool LONG>
 __global__ void __launch_bounds__(NT, kStreamLanes / NT)
 k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   constexpr bool F = kFused<T>;
@@ -384,6 +410,7 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
   __shared__ RowSum red[(NT / 32)], left[(NT / 32)];
   __shared__ uint32_t bound[NT], counts[(NT / 32)], noted[(NT / 32)][kNoted * 32];
   __shared__ float4 sums[kMostParts];  // what the cluster's CTAs send: m, S, U
+  __shared__ Carried carried[LONG ? (NT / 32) : 1];
   __shared__ uint32_t count;
   __shared__ unsigned long long sent;
   const uint64_t t = blockIdx.x;
@@ -464,8 +491,9 @@ k_token_top(RowArgs a, TopOut o, Ctrl *ctrl) {
       __syncthreads();
     }
     again = true;
-    sum = careful ? take_carefully<T, NT, ST, ENT>(x, ring, b, to, a.c)
-                  : take_part<T, NT, ST, ENT, F>(x, ring, b, ref, to, noted[wid], a.c);
+    sum = careful ? take_carefully<T, NT, ST, ENT, LONG>(x, ring, b, to, a.c)
+                  : take_part<T, NT, ST, ENT, F, LONG>(x, ring, b, ref, to, noted[wid],
+                                                       &carried[LONG ? wid : 0], a.c);
     sum = warp_sum<T, false>(sum, a.c);
     if (lane == 0) red[wid] = sum;
     __syncthreads();
@@ -803,12 +831,14 @@ cudaError_t launch_token_top(edp_ctx *ctx, const Logits &z, uint32_t top, int32_
   const uint32_t parts = shape.parts;
   return by_type(z.dtype, [&](auto x) {
     using T = decltype(x);
-    return by_shape(shape, [&](auto threads, auto stages) {
+    return by_shape<T>(shape, [&](auto threads, auto stages, auto is_long) {
       constexpr int NT = decltype(threads)::value, ST = decltype(stages)::value;
+      constexpr bool LONG = decltype(is_long)::value;
       const uint32_t sampled =
           first_bound(top, ST, std::ceil((double)shape.vecs / (NT * kUnroll)), NT);
       const TopOut o{ids, top_logp, logp, entropy, rest, stats, top, sampled};
-      auto kern = entropy ? k_token_top<T, NT, ST, true> : k_token_top<T, NT, ST, false>;
+      auto kern = entropy ? k_token_top<T, NT, ST, true, LONG>
+                          : k_token_top<T, NT, ST, false, LONG>;
       const uint32_t keys = kRoom + (parts > 1 ? parts * top : 0);
       const size_t bytes = sizeof(uint4) * ((keys + 1) / 2 + ST * kUnroll * NT);
       const cudaError_t e = cudaFuncSetAttribute(

@@ -22,69 +22,83 @@ def ctx_of(edp):
     return edp.Ring(cfg, action=False, reward=False, done=False)
 
 
-def long_row(vocab, dtype, high):
-    """(logits with one row in use, its index, mask, columns of the likely tokens, the
-    others' logit): more rows than half of the SMs, so that none is split."""
+def long_row(vocab, dtype, shape):
+    """(logits with one row in use, its index, mask, columns of the likely tokens): more rows
+    than half of the SMs, so that none is split.  flat: all but the likely tokens are alike;
+    rising: each is a little above the one before."""
     rows = torch.cuda.get_device_properties(0).multi_processor_count // 2 + 1
     z = torch.empty(rows, vocab, dtype=TYPES[dtype], device="cuda")
     at = rows - 2
-    z[at] = -0.3
-    low = float(z[at, 0])
+    z[at] = -0.3 if shape == "flat" else torch.linspace(-6.3, -0.3, vocab, device="cuda")
     columns = torch.arange(LIKELY, device="cuda") * (vocab // LIKELY) + 3
-    z[at, columns] = high
+    z[at, columns] = 0.0
     mask = torch.zeros(rows, dtype=torch.uint8, device="cuda")
     mask[at] = 1
-    return z, at, mask, columns, low
+    return z, at, mask, columns
+
+
+def sums(z, inside):
+    """(logarithm of the list's sum, of the others', entropy) in 64 bits."""
+    x = z.double()
+    ln = torch.logsumexp(x, 0)
+    rest = x.clone()
+    rest[inside] = -math.inf
+    return float(torch.logsumexp(x[inside], 0)), float(torch.logsumexp(rest, 0)), \
+        float(ln - ((x - ln).exp() * x).sum())
 
 
 @pytest.mark.parametrize("dtype,vocab", SIZES)
+@pytest.mark.parametrize("shape", ["flat", "rising"])
 @pytest.mark.parametrize("high", [0.0, 100.0])
 @pytest.mark.parametrize("top", [64, 128])
-def test_lists_of_long_rows(edp_lib, dtype, vocab, high, top):
+def test_lists_of_long_rows(edp_lib, dtype, vocab, shape, high, top):
     """high 100: the list lies so far above all others that these are summed relative to
     their own maximum."""
     edp, ring = edp_lib, ctx_of(edp_lib)
-    z, at, mask, columns, low = long_row(vocab, dtype, 0.0)
-    z[at, columns[:top]] = high
+    z, at, mask, columns = long_row(vocab, dtype, shape)
+    inside = columns[:top]
+    z[at, inside] = high
     rows = len(z)
     ids = torch.zeros(rows, top, dtype=torch.int32, device="cuda")
     lp = torch.zeros(rows, top, device="cuda")
     rest, H = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
     edp.edp_token_top(ring.ctx, z, ids, lp, mask=mask, rest=rest, entropy=H)
     edp.edp_sync(ring.ctx)
-    assert torch.equal(ids[at].long(), columns[:top])
-    few, many = LIKELY - top, vocab - LIKELY
-    outside = few + many * math.exp(low)
-    S = top + outside * math.exp(-high)                 # relative to the largest
-    ln_s = math.log(S)
-    U = few * -high + many * math.exp(low) * (low - high)
-    for got, want, most in ((lp[at], -ln_s, 0), (rest[at], math.log(outside) - high - ln_s, high),
-                            (H[at], ln_s - U * math.exp(-high) / S, 0)):
+    assert torch.equal(ids[at].long(), inside)
+    of_list, of_rest, entropy = sums(z[at], inside)
+    ln = float(np.logaddexp(of_list, of_rest))
+    far = (high > 0) * 3 * 128 * 2.0**-24
+    for got, want, more in ((lp[at], high - ln, 0), (rest[at], of_rest - ln, far),
+                            (H[at], entropy, 0)):
         got = to_np(got.double())
-        assert np.all(np.abs(got - want) <= 1e-5 + 1e-6 * min(abs(want), 40) +
-                      (most > 0) * 3 * 128 * 2.0**-24), (got.reshape(-1)[0], want)
+        assert np.all(np.abs(got - want) <= 1e-5 + 1e-6 * min(abs(want), 40) + more), \
+            (got.reshape(-1)[0], want)
 
 
 @pytest.mark.parametrize("dtype,vocab", SIZES)
-@pytest.mark.parametrize("high", [0.0, 100.0])
-def test_distillation_of_long_rows(edp_lib, dtype, vocab, high):
+@pytest.mark.parametrize("shape", ["flat", "rising"])
+@pytest.mark.parametrize("high", [0.0, 100.0, -60.0])
+def test_distillation_of_long_rows(edp_lib, dtype, vocab, shape, high):
     """sum p ln(p/q) with p = 1/20 at entries and 1/2 in all for the others, so that the
-    loss has ln q of the list and of the others, and the gradient their sum."""
+    loss has ln q of the list and of the others, and the gradient their sum.  The list lies
+    at the others' likely tokens, far above and far below."""
     edp, ring = edp_lib, ctx_of(edp_lib)
-    z, at, mask, columns, low = long_row(vocab, dtype, 0.0)
+    z, at, mask, columns = long_row(vocab, dtype, shape)
     n = 10
-    z[at, columns[-n:]] = high
+    inside = columns[-n:]
+    z[at, inside] = high
     rows = len(z)
-    ids = columns[-n:].to(torch.int32).repeat(rows, 1)
+    ids = inside.to(torch.int32).repeat(rows, 1)
     value = torch.full((rows, n), -math.log(20.0), device="cuda")
     rest = torch.full((rows,), -math.log(2.0), device="cuda")
     loss = torch.zeros(1, device="cuda")
-    outside = LIKELY - n + (vocab - LIKELY) * math.exp(low)
-    S = n + outside * math.exp(-high)
-    lq, lqr = -math.log(S), math.log(outside) - high - math.log(S)
+    of_list, of_rest, _ = sums(z[at], inside)
+    ln = float(np.logaddexp(of_list, of_rest))
+    lq, lqr = high - ln, of_rest - ln
     want = .5 * (-math.log(20) - lq) + .5 * (-math.log(2) - lqr)
     # both logarithms' bounds, and roundings of the logarithms of p and of the loss
-    bound = 1e-5 + .5e-6 * (abs(lq) + min(abs(lqr), 40)) + (high > 0) * 3 * 128 * 2.0**-24
+    far = (high != 0) * 3 * 128 * 2.0**-24
+    bound = 1e-5 + .5e-6 * (min(abs(lq), 40) + min(abs(lqr), 40)) + far
     d = torch.full_like(z, 7.0)
     for out in (None, d):
         edp.edp_distill_loss(ring.ctx, edp.make_distill_config(), z, ids, value, loss, rest=rest,
@@ -92,12 +106,12 @@ def test_distillation_of_long_rows(edp_lib, dtype, vocab, high):
         edp.edp_sync(ring.ctx)
         assert abs(float(loss) - want) <= bound, (float(loss), want)
     eps = torch.finfo(TYPES[dtype]).eps / 2
-    free = torch.ones(vocab, dtype=torch.bool, device="cuda")
-    free[columns] = False
-    for got, y, tol in ((d[at, free], low, 1.2e-5), (d[at, columns[:-n]], 0.0, 1.2e-5)):
-        q = math.exp(y - high) / S
-        grad = q - .5 * math.exp(y) / outside
-        # q and a token's share of its class, each to 1.2e-5 of itself (and e^-100 of nothing)
-        err = tol * (q + .5 * math.exp(y) / outside) + eps * abs(grad) + \
-            (2.0**-24 if dtype == "f16" else 1e-37)
-        assert (got.double() - grad).abs().max() <= err, (float(got[0]), grad)
+    x = z[at].double()
+    q, share = (x - ln).exp(), (x - of_rest).exp()
+    q[inside] = share[inside] = 0
+    # q and a token's share of its class, each to 1.2e-5 of itself, rounded to the type
+    grad = q - .5 * share
+    err = 1.2e-5 * (q + .5 * share) + eps * grad.abs() + (2.0**-24 if dtype == "f16" else 1e-37)
+    off = (d[at].double() - grad).abs() - err
+    off[inside] = 0
+    assert off.max() <= 0, (float(off.max()), int(off.argmax()))
