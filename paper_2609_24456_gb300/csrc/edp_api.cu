@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdarg>
+#include <cstddef>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -1418,10 +1419,11 @@ edp_status edp_sync(edp_ctx *ctx, edp_stream stream) {
   e = cudaMemcpy(&h, ctx->ctrl, sizeof h, cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return cuda_fail(ctx, e, "edp_sync(read flags)");
   if (h.err == 0) return EDP_OK;
-  const uint32_t zero[2] = {0, 0};
+  const uint64_t zero[4] = {0, 0, 0, 0};
   cudaMemcpy(&ctx->ctrl->err, zero, 4, cudaMemcpyHostToDevice);
-  cudaMemcpy(&ctx->ctrl->bad_index, zero, 8, cudaMemcpyHostToDevice);
-  const unsigned long long bi = h.bad_index ? h.bad_index - 1 : 0;
+  cudaMemcpy(&ctx->ctrl->bad_index, zero, sizeof zero, cudaMemcpyHostToDevice);
+  static_assert(offsetof(Ctrl, row_twice) - offsetof(Ctrl, bad_index) == 3 * sizeof zero[0],
+                "side by side");
   if (h.err & DEVERR_TIMEOUT)
     return fail(ctx, EDP_ERR_TIMEOUT, "device: a bounded wait expired (flags 0x%x)", h.err);
   if (h.err & DEVERR_EMPTY)
@@ -1431,17 +1433,18 @@ edp_status edp_sync(edp_ctx *ctx, edp_stream stream) {
   if (h.err & DEVERR_OVERFLOW)
     return fail(ctx, EDP_ERR_INVALID,
                 "device: a packed output or a sum of shard totals exceeds its capacity "
-                "(%llu, flags 0x%x)", bi, h.err);
+                "(%llu, flags 0x%x)", h.over - 1, h.err);
   if (!(h.err & DEVERR_INDEX) && (h.err & DEVERR_TWICE))
     return fail(ctx, EDP_ERR_INVALID,
                 "device: a teacher's list that holds a token twice (first row %llu, flags 0x%x)",
-                bi, h.err);
+                ~h.row_twice, h.err);
   if (!(h.err & DEVERR_INDEX))
     return fail(ctx, EDP_ERR_INVALID,
                 "device: a row of logits that are all -infinity (first row %llu, flags 0x%x)",
-                bi, h.err);
+                ~h.row_none, h.err);
   return fail(ctx, EDP_ERR_INVALID,
-              "device: index out of range (first offender %llu, flags 0x%x)", bi, h.err);
+              "device: index out of range (first offender %llu, flags 0x%x)",
+              h.bad_index - 1, h.err);
 }
 
 edp_status edp_probe_host_read(const void *host_src, uint64_t bytes,

@@ -35,7 +35,10 @@ struct Ctrl {
   // long sequences listed, gather CTAs done with the list
   uint32_t pack_ticket, pack_long, pack_left;
   uint32_t pad[2];
-  unsigned long long bad_index;  // first offending index (diagnostics)
+  // what the flags are about, each kind's own (diagnostics): an index out of range and a length
+  // beyond a capacity, one more than the first that was met; the lowest rows without a
+  // distribution and with a token twice, as all bits but theirs
+  unsigned long long bad_index, over, row_none, row_twice;
   unsigned long long host_bytes;  // two-tier deliveries: bytes read from the host tier
   // losses (calls are ordered), each 0 between calls: tokens counted, CTAs done
   unsigned long long loss_tokens;
@@ -391,8 +394,12 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t n
 
 __device__ __forceinline__ void flag(Ctrl *c, uint32_t bits,
                                      unsigned long long detail) {
-  if ((atomicOr(&c->err, bits) & bits) == 0)
-    atomicCAS(&c->bad_index, 0ull, detail + 1);
+  if (bits == DEVERR_INDEX || bits == DEVERR_OVERFLOW)
+    atomicCAS(bits == DEVERR_INDEX ? &c->bad_index : &c->over, 0ull, detail + 1);
+  else if (bits == DEVERR_ROW || bits == DEVERR_TWICE)
+    atomicMax(bits == DEVERR_ROW ? &c->row_none : &c->row_twice, ~detail);
+  __threadfence();  // whoever sees the flag sees what it is about
+  atomicOr(&c->err, bits);
 }
 
 // Programmatic dependent launch (sm_90+): a kernel launched with
