@@ -831,8 +831,9 @@ def edp_token_top(ctx, logits, ids, top_logp, target=None, logp=None, mask=None,
     return _check(ctx, lib().edp_token_top(
         ctx, p, dt, rows, vocab, stride, _arr(target, _i32, rows, who),
         _arr(mask, _mask, rows, who), temperature, top, tokens,
-        _arr(top_logp, _f32, rows * top, who), _vec(logp, who), _vec(entropy, who),
-        _vec(rest, who), _vec(stats, who), stream_handle(stream)), who)
+        _arr(top_logp, _f32, rows * top, who), _arr(logp, _f32, rows, who),
+        _arr(entropy, _f32, rows, who), _arr(rest, _f32, rows, who),
+        _arr(stats, _f32, 2 * rows, who), stream_handle(stream)), who)
 
 
 def edp_distill_loss(ctx, cfg: edp_distill_config, logits, ids, value, loss, rest=None,
@@ -846,8 +847,9 @@ def edp_distill_loss(ctx, cfg: edp_distill_config, logits, ids, value, loss, res
     tokens, top = _lists(ids, rows, who)
     return _check(ctx, lib().edp_distill_loss(
         ctx, C.byref(cfg), p, dt, rows, vocab, stride, temperature, tokens,
-        _arr(value, _f32, rows * top, who), top, _vec(rest, who), _arr(mask, _mask, rows, who),
-        _arr(off, _u64, n_seq + 1, who), n_seq, _vec(loss, who), _vec(row_loss, who), d, dstride,
+        _arr(value, _f32, rows * top, who), top, _arr(rest, _f32, rows, who),
+        _arr(mask, _mask, rows, who), _arr(off, _u64, n_seq + 1, who), n_seq,
+        _arr(loss, _f32, 1, who), _arr(row_loss, _f32, rows, who), d, dstride,
         stream_handle(stream)), who)
 
 
