@@ -556,7 +556,7 @@ typedef enum { EDP_F32 = 0, EDP_BF16 = 1, EDP_F16 = 2 } edp_dtype;
  * -infinity is a token of probability 0.  A row with a negative target is left
  * out like a masked one.  A target >= vocab, and a row whose logits are all
  * -infinity, are written as 0 (S as 0) and reported by edp_sync
- * (EDP_ERR_INVALID).  NaN or +infinity in a row makes its outputs NaN.
+ * (EDP_ERR_INVALID).  NaN or +infinity in a row makes its outputs NaN (of stats, S).
  * Errors: EDP_ERR_INVALID for an unknown dtype, vocab == 0, stride < vocab,
  * rows or vocab >= 2^31, temperature outside [1e-6, 1e6], a NULL logits,
  * target or logp, arrays outside device memory, or logits not aligned to their
@@ -600,7 +600,7 @@ EDP_API edp_status edp_token_logprob_grad(edp_ctx *ctx, const void *logits, uint
  * or by a negative target have an empty list and 0 in the other outputs; so has a
  * row with a target >= vocab, or whose logits are all -infinity, which edp_sync
  * reports (EDP_ERR_INVALID).  NaN or +infinity in a row makes its ids -1 and its
- * numbers NaN.
+ * numbers NaN (of stats, S).
  * Errors: as edp_token_logprob, and EDP_ERR_INVALID for top outside [1, 128], NULL
  * ids or top_logp, or logp without target. */
 EDP_API edp_status edp_token_top(edp_ctx *ctx, const void *logits, uint32_t dtype,

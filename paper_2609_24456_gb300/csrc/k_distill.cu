@@ -29,7 +29,7 @@
 //   2,048 x 152,064 bf16, the loss alone               107 us   92 us to read once
 //   515 x 32,003 f32, 100 entries, mixed              32.5 us   17.5 us: 2.3 waves of CTAs, whose
 //                                                               copies and sums hardly overlap
-//   16 x 32,003 bf16, 20 entries                       8.2 us   in a graph: a chain of loads (mask,
+//   16 x 32,003 bf16, 20 entries                       7.6 us   in a graph: a chain of loads (mask,
 //                                                               entry, its logit), one copy, the
 //                                                               cluster's join
 #include <cmath>

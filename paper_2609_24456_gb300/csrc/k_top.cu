@@ -16,9 +16,15 @@
 // What bounds it, at 6.79 TB/s of measured copy:
 //   8,192 x 152,064 bf16, 64 entries, entropy, a tenth masked   390 us   331 us to read them;
 //                                      issue: 11 instructions an element at 2.9 of 4 a cycle
-//   777 x 32,003 f32, 128 entries   31 us    14.8 us; 608 CTAs at a time, so a second wave
+//   777 x 32,003 f32, 128 entries   31 us    14.8 us; 608 CTAs at a time, 169 in a second wave;
+//                                      1,216 rows (two waves) 48 us, 23.1 to read them
 //   256 x 32,003 f16, 8 entries     11.5 us  2.4 us; a chain of loads, sample, pass and order
 //   one row of 152,064, 20 entries  9.4 us   the same, and the join of 8 lists
+//   5,400 x 8,394 bf16, 128 entries 83 us    14 us; the order of the sample and of the candidates,
+//                                      during which a CTA loads nothing (16,000 columns: 82 us)
+//   8,000 x 2,000 bf16, 20 entries  27 us    4.9 us (k_top_small); issue, 39 instructions an element
+// Four CTAs of 256 threads an SM leave 64 registers a thread: 27 of the 42 forms of k_token_top
+// spill 4 or 8 bytes.
 #include <algorithm>
 #include <cmath>
 

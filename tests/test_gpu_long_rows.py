@@ -115,3 +115,9 @@ def test_distillation_of_long_rows(edp_lib, dtype, vocab, shape, high):
     off = (d[at].double() - grad).abs() - err
     off[inside] = 0
     assert off.max() <= 0, (float(off.max()), int(off.argmax()))
+
+
+def test_rows_that_are_not_split(edp_lib):
+    """77 rows are more than half of the SMs, so that each is one CTA's, as the test of the
+    longest rows' ties (test_gpu_top.py) and those here need it."""
+    assert 2 * 77 > torch.cuda.get_device_properties(0).multi_processor_count
