@@ -22,11 +22,11 @@ def ctx_of(edp):
     return edp.Ring(cfg, action=False, reward=False, done=False)
 
 
-def long_row(vocab, dtype, shape):
-    """(logits with one row in use, its index, mask, columns of the likely tokens): more rows
-    than half of the SMs, so that none is split.  flat: all but the likely tokens are alike;
+def long_row(vocab, dtype, shape, rows):
+    """(logits with one row in use, its index, mask, columns of the likely tokens); of rows
+    that are not given more than half of the SMs, so that none is split.  flat: all but the likely tokens are alike;
     rising: each is a little above the one before."""
-    rows = torch.cuda.get_device_properties(0).multi_processor_count // 2 + 1
+    rows = rows or torch.cuda.get_device_properties(0).multi_processor_count // 2 + 1
     z = torch.empty(rows, vocab, dtype=TYPES[dtype], device="cuda")
     at = rows - 2
     z[at] = -0.3 if shape == "flat" else torch.linspace(-6.3, -0.3, vocab, device="cuda")
@@ -51,11 +51,11 @@ def sums(z, inside):
 @pytest.mark.parametrize("shape", ["flat", "rising"])
 @pytest.mark.parametrize("high", [0.0, 100.0])
 @pytest.mark.parametrize("top", [64, 128])
-def test_lists_of_long_rows(edp_lib, dtype, vocab, shape, high, top):
+def test_lists_of_long_rows(edp_lib, dtype, vocab, shape, high, top, rows=None):
     """high 100: the list lies so far above all others that these are summed relative to
     their own maximum."""
     edp, ring = edp_lib, ctx_of(edp_lib)
-    z, at, mask, columns = long_row(vocab, dtype, shape)
+    z, at, mask, columns = long_row(vocab, dtype, shape, rows)
     inside = columns[:top]
     z[at, inside] = high
     rows = len(z)
@@ -78,12 +78,12 @@ def test_lists_of_long_rows(edp_lib, dtype, vocab, shape, high, top):
 @pytest.mark.parametrize("dtype,vocab", SIZES)
 @pytest.mark.parametrize("shape", ["flat", "rising"])
 @pytest.mark.parametrize("high", [0.0, 100.0, -60.0])
-def test_distillation_of_long_rows(edp_lib, dtype, vocab, shape, high):
+def test_distillation_of_long_rows(edp_lib, dtype, vocab, shape, high, rows=None):
     """sum p ln(p/q) with p = 1/20 at entries and 1/2 in all for the others, so that the
     loss has ln q of the list and of the others, and the gradient their sum.  The list lies
     at the others' likely tokens, far above and far below."""
     edp, ring = edp_lib, ctx_of(edp_lib)
-    z, at, mask, columns = long_row(vocab, dtype, shape)
+    z, at, mask, columns = long_row(vocab, dtype, shape, rows)
     n = 10
     inside = columns[-n:]
     z[at, inside] = high
@@ -115,6 +115,16 @@ def test_distillation_of_long_rows(edp_lib, dtype, vocab, shape, high):
     off = (d[at].double() - grad).abs() - err
     off[inside] = 0
     assert off.max() <= 0, (float(off.max()), int(off.argmax()))
+
+
+@pytest.mark.parametrize("dtype,vocab,rows", [("bf16", 8_388_608, 3), ("f32", 4_194_301, 5),
+                                              ("f16", 700_001, 200), ("f32", 300_007, 160),
+                                              ("bf16", 600_000, 400), ("f32", 270_000, 350)])
+@pytest.mark.parametrize("high", [0.0, 100.0])
+def test_other_shapes(edp_lib, dtype, vocab, rows, high):
+    """Rows in parts, and more rows than SMs (one and two of them to an SM)."""
+    test_lists_of_long_rows(edp_lib, dtype, vocab, "rising", high, 64, rows)
+    test_distillation_of_long_rows(edp_lib, dtype, vocab, "flat", high, rows)
 
 
 def test_rows_that_are_not_split(edp_lib):
